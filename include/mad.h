@@ -229,6 +229,71 @@ int mad_verify_attn_vt(const void *q, int B, int T, int Hq, int Hkv, int d, int 
                        void *out, float *lse, void *ws, size_t ws_bytes, void *stream);
 
 /*
+ * An 8-bit key/value cache: e4m3 codes (the OCP format: 448 the largest value,
+ * no infinities, 0x7f and 0xff NaN) and one fp32 scale for each block of
+ * tokens of a sequence and KV head, K and V apart.  An element's value is its
+ * code's value times its block's scale.  Row i of sequence b, KV head h:
+ *     codes   k + b * seq_stride + h * head_stride + i * head_dim      (bytes)
+ *     scale   k_scale + b * scale_seq_stride + h * scale_head_stride + i / block
+ * and likewise v, v_scale.  seq_stride and scale_seq_stride may be 0 together
+ * (every sequence index aliases the same buffer; not for mad_kv8_append with
+ * B > 1).  head_stride >= cap * head_dim; scale_head_stride >= ceil(cap / block).
+ *   block  16, 32, 64 or 128 tokens
+ *   len    HOST int32[B], number of valid rows, 0 <= len <= cap
+ */
+typedef struct mad_kv8_view {
+    void *k;
+    void *v;
+    float *k_scale;
+    float *v_scale;
+    int64_t seq_stride;
+    int64_t head_stride;
+    int64_t scale_seq_stride;
+    int64_t scale_head_stride;
+    int32_t cap;
+    int32_t block;
+    const int32_t *len;
+} mad_kv8_view;
+
+/*
+ * Append new rows to an 8-bit cache: rows len[b] .. len[b] + n[b] - 1 of every
+ * sequence b from k_new, v_new.  The caller then raises len[b] by n[b]; a
+ * rollback lowers it.  For each block, KV head and tensor that gets a new row:
+ *   need  = the least 2^k, k >= -100, with |x| <= 448 * 2^k for every finite new
+ *           element x of the block
+ *   scale = max(its scale, need) if the block holds rows below len[b], else need
+ *   code  = e4m3(x / scale), round to nearest even; an element that is not
+ *           finite is stored as NaN
+ * Where the scale grows, the block's rows below len[b] are written again with
+ * it, e4m3(code * old scale / scale): the scales are powers of two, so this is
+ * exact but for codes that get below 2^-6.  A block's scale never falls while
+ * it holds rows, also not by a rollback.  Rows and scales of other blocks, and
+ * rows from len[b] + n[b] on, are left as they are.
+ *   k_new, v_new  device [B][n_cap][Hkv][d], dtype; rows from n[b] on are not read
+ *   n             HOST int32[B], 0 <= n[b] <= n_cap, len[b] + n[b] <= cap;
+ *                 NULL = n_cap for every sequence
+ * dtype F32 or BF16; d in {64, 128}.  No workspace.
+ */
+int mad_kv8_append(const void *k_new, const void *v_new, const int32_t *n, int B, int n_cap, int Hkv, int d,
+                   int dtype, const mad_kv8_view *kv, void *stream);
+
+/*
+ * Verify attention (mad_verify_attn) over an 8-bit cache; T = 1 is the decode
+ * step of a single token.  Query t sees rows 0 .. len[b]-T+t; one that sees no
+ * row (len[b] < T - t, a padded sequence with len[b] = 0 among them) gets out =
+ * 0 and lse = -inf.  Rows from len[b] on may hold anything; what a query does not see has no
+ * effect on it, NaN and infinite scores included.
+ *   q    device [B][T][Hq][d], dtype     out  device [B][T][Hq][d], dtype
+ *   lse  device fp32 [B][T][Hq] or NULL
+ *   kv   scales >= 0
+ * T * G <= MAD_MAX_VERIFY_ROWS; d in {64, 128}; dtype BF16 or F32, both on the
+ * matrix cores (F32: q as three bf16 terms, the probabilities as two fp16
+ * terms, so that products keep fp32's precision).  Workspace MAD_OP_VERIFY.
+ */
+int mad_verify_attn_kv8(const void *q, int B, int T, int Hq, int Hkv, int d, int dtype, float scale,
+                        const mad_kv8_view *kv, void *out, float *lse, void *ws, size_t ws_bytes, void *stream);
+
+/*
  * Greedy accept/reject (Sec. 2.1; greedy decoding at temperature 0, Sec. 4.1).
  * For each sequence b, with am[t] = argmax_v logits[b][t][v] (ties -> lowest
  * index, a NaN ranks above every number):

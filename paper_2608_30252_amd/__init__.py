@@ -15,6 +15,8 @@ Entry points (same names as the C ABI, without the ``mad_`` prefix):
     memory_update       mirrored K/V projection + RoPE + append of new memory slots
     verify_attn         target (gamma+1)-query verify attention over the full KV
                         (verify_attn_vt: the same over a transposed V cache)
+    kv8_append          new K/V rows into an 8-bit cache (e4m3, a scale per block of tokens and KV head)
+    verify_attn_kv8     verify attention over an 8-bit cache
     accept_greedy       greedy accept/reject
 """
 import ctypes
@@ -43,6 +45,13 @@ class _KVView(ctypes.Structure):
                 ("cap", ctypes.c_int32), ("start", _i32p), ("len", _i32p)]
 
 
+class _KV8View(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("seq_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("scale_seq_stride", ctypes.c_int64), ("scale_head_stride", ctypes.c_int64),
+                ("cap", ctypes.c_int32), ("block", ctypes.c_int32), ("len", _i32p)]
+
+
 _LIB = None
 
 
@@ -61,6 +70,9 @@ def _load_library():
     lib.mad_verify_attn.argtypes = [vp, i, i, i, i, i, i, f, kvp, vp, vp, vp, sz, vp]
     lib.mad_verify_attn_vt.argtypes = [vp, i, i, i, i, i, i, f, vp, vp, ctypes.c_int64, ctypes.c_int64,
                                        ctypes.c_int32, _i32p, vp, vp, vp, sz, vp]
+    kv8p = ctypes.POINTER(_KV8View)
+    lib.mad_kv8_append.argtypes = [vp, vp, _i32p, i, i, i, i, i, kv8p, vp]
+    lib.mad_verify_attn_kv8.argtypes = [vp, i, i, i, i, i, i, f, kv8p, vp, vp, vp, sz, vp]
     lib.mad_accept_greedy.argtypes = [vp, i, vp, i, i, i, vp, vp, vp, sz, vp]
     lib.mad_accept_stochastic.argtypes = [vp, vp, vp, vp, i, i, i, vp, vp, vp, sz, vp]
     lib.mad_draft_step_attn.argtypes = [vp, i, i, i, i, i, f, kvp, kvp, vp, vp, _u8p, vp, vp, vp, sz, vp]
@@ -79,6 +91,7 @@ def _load_library():
     lib.mad_last_error.restype = ctypes.c_char_p
     lib.mad_version.restype = ctypes.c_char_p
     for fn in ("mad_draft_decode_attn", "mad_memory_update", "mad_verify_attn", "mad_verify_attn_vt", "mad_accept_greedy",
+               "mad_kv8_append", "mad_verify_attn_kv8",
                "mad_accept_stochastic", "mad_draft_step_attn", "mad_draft_decode_attn_noalloc",
                "mad_memory_prefill_attn",
                "mad_rmsnorm_qkv_rope", "mad_linear_residual", "mad_rmsnorm_swiglu", "mad_probe_stream_read",
@@ -91,7 +104,8 @@ def _load_library():
 _FAST = None
 _FAST_ENTRIES = ("mad_draft_decode_attn", "mad_draft_step_attn", "mad_memory_update", "mad_verify_attn",
                  "mad_verify_attn_vt", "mad_accept_greedy", "mad_accept_stochastic", "mad_rmsnorm_qkv_rope",
-                 "mad_linear_residual", "mad_rmsnorm_swiglu", "mad_workspace_bytes")
+                 "mad_linear_residual", "mad_rmsnorm_swiglu", "mad_workspace_bytes", "mad_kv8_append",
+                 "mad_verify_attn_kv8")
 
 
 class _CtypesOnly:
@@ -116,6 +130,7 @@ def _fast():
             return _FAST
         _fastcall.bind(tuple(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in _FAST_ENTRIES), KV,
                        _default_ws, torch._C._cuda_getCurrentRawStream)
+        _fastcall.bind_kv8(KV8)
         _FAST = _fastcall
     return _FAST
 
@@ -192,6 +207,60 @@ class KV:
         self._start = _host_i32(self.start, B) if self.start is not None else None
         return _KVView(k.data_ptr(), v.data_ptr(), k.stride(0) if k.shape[0] > 1 else 0, k.stride(1),
                        k.shape[2], self._start, self._len)
+
+
+@dataclass
+class KV8:
+    """An 8-bit cache: K and V codes [B, Hkv, cap, d] in torch.float8_e4m3fn (any strides with contiguous rows, the
+    same for both), their float32 scales [B, Hkv, ceil(cap / block)], one for each `block` tokens, and per-sequence
+    host lengths."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+    length: Sequence[int]
+    block: int
+
+    @staticmethod
+    def empty(B, Hkv, cap, d, block, device="cuda"):
+        """A cache without rows.  Neither codes nor scales need a value before their rows are appended."""
+        nb = -(-cap // block)
+        mk = lambda: torch.zeros((B, Hkv, cap, d), dtype=torch.uint8, device=device).view(torch.float8_e4m3fn)   # noqa: E731
+        return KV8(mk(), mk(), torch.ones((B, Hkv, nb), device=device), torch.ones((B, Hkv, nb), device=device),
+                   [0] * B, block)
+
+    def view(self, B, Hkv=None, d=None, device=None, name="kv"):
+        """The C view of this cache for a call over B rows.  The batch dimension must be B, or 1 (every row then
+        aliases sequence 0); the KV heads, head_dim and device must match the call's."""
+        k, v, ks, vs = self.k, self.v, self.k_scale, self.v_scale
+        if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride():
+            raise ValueError(f"{name}: K and V must be [B, Hkv, cap, d] tensors with identical strides")
+        if k.dtype != torch.float8_e4m3fn or v.dtype != torch.float8_e4m3fn:
+            raise ValueError(f"{name}: K and V must be torch.float8_e4m3fn")
+        if k.stride(3) != 1 or k.stride(2) != k.shape[3]:
+            raise ValueError(f"{name}: K/V rows must be contiguous")
+        if k.shape[0] not in (1, B):
+            raise ValueError(f"{name}: batch dimension {k.shape[0]} must be 1 or B={B}")
+        if Hkv is not None and k.shape[1] != Hkv:
+            raise ValueError(f"{name}: {k.shape[1]} KV heads, the call has {Hkv}")
+        if d is not None and k.shape[3] != d:
+            raise ValueError(f"{name}: head_dim {k.shape[3]}, the call has {d}")
+        if self.block not in (16, 32, 64, 128):
+            raise ValueError(f"{name}: block {self.block} must be 16, 32, 64 or 128")
+        want = (k.shape[0], k.shape[1], -(-k.shape[2] // self.block))
+        if ks.shape != want or vs.shape != want or ks.stride() != vs.stride() or ks.stride(2) != 1:
+            raise ValueError(f"{name}: scales must be [B, Hkv, ceil(cap / block)] = {want}, contiguous along the blocks")
+        if ks.dtype != torch.float32 or vs.dtype != torch.float32:
+            raise ValueError(f"{name}: scales must be float32")
+        for t in (k, v, ks, vs):
+            if device is not None and t.device != device:
+                raise ValueError(f"{name}: tensors on {t.device}, the call is on {device}")
+        if len(self.length) < B:
+            raise ValueError(f"{name}: lengths need one entry per row ({B})")
+        self._len = _host_i32(self.length, B)
+        many = k.shape[0] > 1
+        return _KV8View(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), k.stride(0) if many else 0, k.stride(1),
+                        ks.stride(0) if many else 0, ks.stride(1), k.shape[2], self.block, self._len)
 
 
 def _need(cond, msg):
@@ -443,6 +512,48 @@ def verify_attn_vt(q: torch.Tensor, k: torch.Tensor, vt: torch.Tensor, length, o
                                             _ptr(vt), k.stride(0) if B > 1 else 0, k.stride(1), cap,
                                             _host_i32(length, B), _ptr(out), _ptr(lse), _ptr(w), w.numel(),
                                             _stream(q.device))
+    _check(rc)
+    return out, lse
+
+
+def kv8_append(k_new: torch.Tensor, v_new: torch.Tensor, kv: KV8, n: Optional[Sequence[int]] = None):
+    """Appends rows 0 .. n[b]-1 of k_new, v_new [B, n_cap, Hkv, d] (all of them without n) to an 8-bit cache, at
+    rows kv.length[b] .. of every sequence.  A block's scale is a power of two and grows with its rows; rows that it
+    already holds are then written again.  The caller then raises its lengths."""
+    rc = (_FAST or _fast()).kv8_append(k_new, v_new, kv, n)
+    if rc is not None:
+        _check(rc)
+        return
+    _need(k_new.dim() == 4 and v_new.shape == k_new.shape and v_new.dtype == k_new.dtype,
+          "k_new and v_new must be [B, n_cap, Hkv, d] of one type")
+    B, n_cap, Hkv, d = k_new.shape
+    _need(n is None or len(n) == B, "n needs one entry per sequence")
+    _contiguous(k_new=k_new, v_new=v_new)
+    _same_device(k_new.device, v_new=v_new)
+    view = kv.view(B, Hkv, d, k_new.device, "kv")
+    _check(_load_library().mad_kv8_append(_ptr(k_new), _ptr(v_new), None if n is None else _host_i32(n, B), B, n_cap,
+                                          Hkv, d, _dtype_code(k_new), ctypes.byref(view), _stream(k_new.device)))
+
+
+def verify_attn_kv8(q: torch.Tensor, kv: KV8, out=None, lse=None, scale: Optional[float] = None,
+                    ws: Optional[torch.Tensor] = None):
+    """verify_attn over an 8-bit cache: q [B, T, Hq, d] (bf16 or fp32), query t sees rows 0 .. kv.length[b]-T+t
+    (T = 1: a single token's attention).  Returns (out [B, T, Hq, d], lse [B, T, Hq]); a query that sees no row has
+    out 0 and lse -inf."""
+    if out is not None and lse is not None:
+        rc = (_FAST or _fast()).verify8(q, kv, out, lse, scale, ws)
+        if rc is not None:
+            _check(rc)
+            return out, lse
+    out, lse, scale = _verify_out(q, out, lse, scale)
+    B, T, Hq, d = q.shape
+    Hkv = kv.k.shape[1]
+    _need(Hkv >= 1 and Hq % Hkv == 0, f"Hq={Hq} must be a multiple of the KV heads {Hkv}")
+    view = kv.view(B, Hkv, d, q.device, "kv")
+    nbytes = workspace_bytes(MAD_OP_VERIFY, B, Hq, Hkv, d, T)
+    w = _ws_for(q.device, nbytes, ws)
+    rc = _load_library().mad_verify_attn_kv8(_ptr(q), B, T, Hq, Hkv, d, _dtype_code(q), float(scale), ctypes.byref(view),
+                                             _ptr(out), _ptr(lse), _ptr(w), w.numel(), _stream(q.device))
     _check(rc)
     return out, lse
 

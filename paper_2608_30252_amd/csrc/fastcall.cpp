@@ -35,9 +35,11 @@ struct Entry {
     decltype(&mad_linear_residual) linear;
     decltype(&mad_rmsnorm_swiglu) swiglu;
     decltype(&mad_workspace_bytes) ws_bytes;
+    decltype(&mad_kv8_append) kv8_append;
+    decltype(&mad_verify_attn_kv8) verify8;
 } g;
-PyObject *g_kv, *g_ws, *g_stream;   // class KV, the default workspaces' dict, the raw-stream getter
-PyObject *s_k, *s_v, *s_length, *s_start, *s_buf;
+PyObject *g_kv, *g_kv8, *g_ws, *g_stream;   // classes KV and KV8, the default workspaces' dict, the raw-stream getter
+PyObject *s_k, *s_v, *s_length, *s_start, *s_buf, *s_k_scale, *s_v_scale, *s_block;
 
 struct Unhandled {};   // thrown for every call the Python path has to take
 void need(bool ok) {
@@ -126,6 +128,7 @@ bool plain_attr(PyObject *o, PyObject *name, bool none) {
 bool plain_kv(PyObject *o) {
     return Py_TYPE(o) == (PyTypeObject *)g_kv && plain_attr(o, s_length, false) && plain_attr(o, s_start, true);
 }
+bool plain_kv8(PyObject *o) { return Py_TYPE(o) == (PyTypeObject *)g_kv8 && plain_attr(o, s_length, false); }
 bool plain_tensors(PyObject *const *a, std::initializer_list<int> at) {
     for (int i : at)
         if (!THPVariable_CheckExact(a[i])) return false;
@@ -158,6 +161,42 @@ struct View {
         c.head_stride = k.stride(1);
         c.cap = small(k.size(2));
         c.start = so.p != Py_None ? start : nullptr;
+        c.len = len;
+        return &c;
+    }
+};
+
+struct View8 {
+    mad_kv8_view c;
+    int32_t len[MAD_MAX_BATCH];
+    // KV8 `o` for B rows of [Hkv, cap, d] (Hkv < 0: any, returned in Hkv)
+    mad_kv8_view *read(PyObject *o, int B, int64_t *Hkv, int64_t d, const at::Device &dev) {
+        need(Py_TYPE(o) == (PyTypeObject *)g_kv8 && B >= 1 && B <= MAD_MAX_BATCH);
+        Ref ko(PyObject_GetAttr(o, s_k)), vo(PyObject_GetAttr(o, s_v)), kso(PyObject_GetAttr(o, s_k_scale)),
+            vso(PyObject_GetAttr(o, s_v_scale)), lo(PyObject_GetAttr(o, s_length)), bo(PyObject_GetAttr(o, s_block));
+        const at::Tensor &k = tensor(ko.p), &v = tensor(vo.p), &ks = tensor(kso.p), &vs = tensor(vso.p);
+        need(k.dim() == 4 && k.sizes() == v.sizes() && k.strides() == v.strides());
+        need(k.scalar_type() == at::kFloat8_e4m3fn && v.scalar_type() == at::kFloat8_e4m3fn);
+        need(k.stride(3) == 1 && k.stride(2) == k.size(3));
+        need(k.size(0) == 1 || k.size(0) == B);
+        if (*Hkv < 0) *Hkv = k.size(1);
+        need(k.size(1) == *Hkv && k.size(3) == d);
+        c.block = as_int(bo.p);
+        need(c.block == 16 || c.block == 32 || c.block == 64 || c.block == 128);
+        c.cap = small(k.size(2));
+        need(ks.dim() == 3 && shape(ks, {k.size(0), *Hkv, ((int64_t)c.cap + c.block - 1) / c.block}) && vs.sizes() == ks.sizes());
+        need(ks.strides() == vs.strides() && ks.stride(2) == 1 && ks.scalar_type() == at::kFloat && vs.scalar_type() == at::kFloat);
+        need(k.device() == dev && v.device() == dev && ks.device() == dev && vs.device() == dev);
+        ints(lo.p, B, len);
+        const bool many = k.size(0) > 1;
+        c.k = k.data_ptr();
+        c.v = v.data_ptr();
+        c.k_scale = (float *)ks.data_ptr();
+        c.v_scale = (float *)vs.data_ptr();
+        c.seq_stride = many ? k.stride(0) : 0;
+        c.head_stride = k.stride(1);
+        c.scale_seq_stride = many ? ks.stride(0) : 0;
+        c.scale_head_stride = ks.stride(1);
         c.len = len;
         return &c;
     }
@@ -349,6 +388,52 @@ PyObject *verify_vt(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+// kv8_append(k_new, v_new, kv, n | None)
+PyObject *kv8_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    ORDINARY(4, plain_tensors(a, {0, 1}) && plain_kv8(a[2]) && (a[3] == Py_None || plain_ints(a[3])));
+    return guarded([&]() -> int {
+        const at::Tensor &k = first(a[0]);
+        const at::Device dev = k.device();
+        const at::Tensor &v = dense(a[1], dev);
+        need(k.dim() == 4 && v.sizes() == k.sizes() && v.scalar_type() == k.scalar_type());
+        const int B = small(k.size(0)), n_cap = small(k.size(1)), d = small(k.size(3));
+        int64_t Hkv = small(k.size(2));
+        View8 kv;
+        mad_kv8_view *c = kv.read(a[2], B, &Hkv, d, dev);
+        int32_t rows[MAD_MAX_BATCH];
+        if (a[3] != Py_None) ints(a[3], B, rows);
+        const int32_t *np = a[3] != Py_None ? rows : nullptr;
+        const int dt = dtype_code(k);
+        void *st = stream_of(dev), *kp = k.data_ptr(), *vp = v.data_ptr();
+        RELEASED(g.kv8_append(kp, vp, np, B, n_cap, (int)Hkv, d, dt, c, st));
+    });
+}
+
+// verify8(q, kv, out, lse, scale, ws)
+PyObject *verify8(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    ORDINARY(6, plain_tensors(a, {0, 2, 3}) && plain_kv8(a[1]) && (a[4] == Py_None || plain_real(a[4])));
+    return guarded([&]() -> int {
+        const at::Tensor &q = first(a[0]);
+        const at::Device dev = q.device();
+        need(q.dim() == 4);
+        const int B = small(q.size(0)), T = small(q.size(1)), Hq = small(q.size(2)), d = small(q.size(3));
+        int64_t Hkv = -1;
+        View8 kv;
+        mad_kv8_view *v = kv.read(a[1], B, &Hkv, d, dev);
+        need(Hkv >= 1 && Hq % Hkv == 0);
+        const at::Tensor &out = dense(a[2], dev), &lse = dense(a[3], dev);
+        need(out.sizes() == q.sizes() && out.scalar_type() == q.scalar_type());
+        need(shape(lse, {B, T, Hq}) && lse.scalar_type() == at::kFloat);
+        const float scale = scale_of(a[4], d);
+        void *st = stream_of(dev);
+        const Scratch ws(a[5], dev, st, g.ws_bytes(MAD_OP_VERIFY, B, Hq, (int)Hkv, d, T, 0));
+        const int dt = dtype_code(q);
+        void *qp = q.data_ptr(), *op = out.data_ptr();
+        float *lp = (float *)lse.data_ptr();
+        RELEASED(g.verify8(qp, B, T, Hq, (int)Hkv, d, dt, scale, v, op, lp, ws.p, ws.n, st));
+    });
+}
+
 const at::Tensor &i32(PyObject *o, const at::Device &dev, std::initializer_list<int64_t> want) {
     const at::Tensor &t = dense(o, dev);
     need(t.scalar_type() == at::kInt && shape(t, want));
@@ -480,9 +565,17 @@ PyObject *bind(PyObject *, PyObject *args) {
     Py_RETURN_NONE;
 }
 
+// bind_kv8(KV8)
+PyObject *bind_kv8(PyObject *, PyObject *kv8) {
+    Py_INCREF(kv8);
+    Py_XSETREF(g_kv8, kv8);
+    Py_RETURN_NONE;
+}
+
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, nullptr}, FAST(attn), FAST(update), FAST(verify), FAST(verify_vt),
-                         FAST(greedy), FAST(stoch), FAST(qkv), FAST(linear), FAST(swiglu), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, nullptr}, {"bind_kv8", bind_kv8, METH_O, nullptr}, FAST(attn), FAST(update), FAST(verify), FAST(verify_vt),
+                         FAST(greedy), FAST(stoch), FAST(qkv), FAST(linear), FAST(swiglu), FAST(kv8_append),
+                         FAST(verify8), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
@@ -493,5 +586,8 @@ PyMODINIT_FUNC PyInit__fastcall(void) {
     s_length = PyUnicode_InternFromString("length");
     s_start = PyUnicode_InternFromString("start");
     s_buf = PyUnicode_InternFromString("buf");
+    s_k_scale = PyUnicode_InternFromString("k_scale");
+    s_v_scale = PyUnicode_InternFromString("v_scale");
+    s_block = PyUnicode_InternFromString("block");
     return PyModule_Create(&module);
 }

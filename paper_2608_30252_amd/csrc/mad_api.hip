@@ -38,6 +38,8 @@ int elem_size(int dtype) { return dtype == MAD_BF16 ? 2 : 4; }
 
 bool pow2_group(int G) { return G == 1 || G == 2 || G == 4 || G == 8 || G == 16; }
 
+int log2_of(int x) { return 31 - __builtin_clz((unsigned)x); }
+
 // Common shape checks for attention entry points.
 int check_heads(int B, int Hq, int Hkv, int d, int dtype) {
     if (B < 1 || B > MAD_MAX_BATCH) return fail(MAD_EINVAL, "B=%d outside [1, %d]", B, MAD_MAX_BATCH);
@@ -73,6 +75,35 @@ int check_view(const mad_kv_view *v, const char *name, int B, int Hkv, int d, in
             if (st < 0 || st >= v->cap) return fail(MAD_EINVAL, "%s: start[%d]=%d outside [0, cap)", name, b, st);
         }
     }
+    return MAD_OK;
+}
+
+// Validate an 8-bit view for B sequences.
+int check_view8(const mad_kv8_view *v, int B, int Hkv, int d) {
+    if (!v) return fail(MAD_EINVAL, "null kv");
+    if (!v->k || !v->v || !v->k_scale || !v->v_scale) return fail(MAD_EINVAL, "kv: null k, v, k_scale or v_scale");
+    if (!aligned16(v->k) || !aligned16(v->v)) return fail(MAD_EINVAL, "kv: k/v not 16-byte aligned");
+    if (((uintptr_t)v->k_scale & 3u) || ((uintptr_t)v->v_scale & 3u)) return fail(MAD_EINVAL, "kv: scales not 4-byte aligned");
+    if (v->cap < 1) return fail(MAD_EINVAL, "kv: cap=%d", v->cap);
+    if (v->block != 16 && v->block != 32 && v->block != 64 && v->block != 128)
+        return fail(MAD_ENOTSUP, "kv: block %d not supported (16, 32, 64 or 128 tokens)", v->block);
+    if (!v->len) return fail(MAD_EINVAL, "kv: null len");
+    if (v->seq_stride < 0 || v->head_stride < (int64_t)v->cap * d || v->seq_stride % 16 || v->head_stride % 16)
+        return fail(MAD_EINVAL, "kv: bad strides (seq %lld, head %lld) for cap %d, d %d", (long long)v->seq_stride,
+                    (long long)v->head_stride, v->cap, d);
+    const int64_t nb = ((int64_t)v->cap + v->block - 1) / v->block;
+    if (v->scale_seq_stride < 0 || v->scale_head_stride < nb)
+        return fail(MAD_EINVAL, "kv: bad scale strides (seq %lld, head %lld) for %lld blocks",
+                    (long long)v->scale_seq_stride, (long long)v->scale_head_stride, (long long)nb);
+    if ((v->seq_stride == 0) != (v->scale_seq_stride == 0) && B > 1)
+        return fail(MAD_EINVAL, "kv: codes and scales are shared by all sequences, or neither");
+    if (B > 1 && v->seq_stride != 0 && (v->seq_stride < (int64_t)Hkv * v->head_stride ||
+                                        v->scale_seq_stride < (int64_t)Hkv * v->scale_head_stride))
+        return fail(MAD_EINVAL, "kv: seq_stride %lld (scales %lld) overlaps heads", (long long)v->seq_stride,
+                    (long long)v->scale_seq_stride);
+    for (int b = 0; b < B; ++b)
+        if (v->len[b] < 0 || v->len[b] > v->cap)
+            return fail(MAD_EINVAL, "kv: len[%d]=%d outside [0, cap=%d]", b, v->len[b], v->cap);
     return MAD_OK;
 }
 
@@ -457,6 +488,94 @@ int mad_verify_attn_vt(const void *q, int B, int T, int Hq, int Hkv, int d, int 
                        void *out, float *lse, void *ws, size_t ws_bytes, void *stream) {
     return verify_impl(q, B, T, Hq, Hkv, d, dtype, scale, k, vt, false, seq_stride, head_stride, cap, len, out, lse,
                        ws, ws_bytes, stream);
+}
+
+int mad_kv8_append(const void *k_new, const void *v_new, const int32_t *n, int B, int n_cap, int Hkv, int d,
+                   int dtype, const mad_kv8_view *kv, void *stream) {
+    if (B < 1 || B > MAD_MAX_BATCH) return fail(MAD_EINVAL, "B=%d outside [1, %d]", B, MAD_MAX_BATCH);
+    if (n_cap < 1) return fail(MAD_EINVAL, "n_cap=%d", n_cap);
+    if (Hkv < 1) return fail(MAD_EINVAL, "Hkv=%d", Hkv);
+    if (dtype != MAD_F32 && dtype != MAD_BF16) return fail(MAD_ENOTSUP, "dtype %d not supported", dtype);
+    if (d != 64 && d != 128) return fail(MAD_ENOTSUP, "head_dim %d not supported (64 or 128)", d);
+    if (!k_new || !v_new) return fail(MAD_EINVAL, "null k_new or v_new");
+    if (!aligned16(k_new) || !aligned16(v_new)) return fail(MAD_EINVAL, "k_new/v_new not 16-byte aligned");
+    const int rc = check_view8(kv, B, Hkv, d);
+    if (rc) return rc;
+    if (B > 1 && (kv->seq_stride == 0 || kv->scale_seq_stride == 0))
+        return fail(MAD_EINVAL, "kv: sequences that share one buffer cannot all append to it");
+    mad::Kv8AppendArgs a;
+    memset(&a, 0, sizeof(a));
+    int64_t blocks = 0;
+    for (int b = 0; b < B; ++b) {
+        const int nb = n ? n[b] : n_cap, len = kv->len[b];
+        if (nb < 0 || nb > n_cap) return fail(MAD_EINVAL, "n[%d]=%d outside [0, n_cap=%d]", b, nb, n_cap);
+        if ((int64_t)len + nb > kv->cap)
+            return fail(MAD_EINVAL, "kv: len[%d]=%d + n=%d exceeds cap %d", b, len, nb, kv->cap);
+        a.row[b].x = (int)blocks;
+        a.row[b].y = len;
+        a.row[b].z = nb;
+        if (nb > 0) blocks += (len + nb - 1) / kv->block - len / kv->block + 1;
+        if (blocks * 2 * Hkv > 0x7fffffff) return fail(MAD_EINVAL, "too many blocks in one call");
+    }
+    for (int b = B; b < MAD_MAX_BATCH; ++b) a.row[b].x = (int)blocks;
+    if (blocks == 0) return ok();
+    a.k_new = k_new;
+    a.v_new = v_new;
+    a.k = kv->k;
+    a.v = kv->v;
+    a.k_scale = kv->k_scale;
+    a.v_scale = kv->v_scale;
+    a.seq = kv->seq_stride;
+    a.head = kv->head_stride;
+    a.s_seq = kv->scale_seq_stride;
+    a.s_head = kv->scale_head_stride;
+    a.n_cap = n_cap;
+    a.Hkv = Hkv;
+    a.d = d;
+    a.log2_block = log2_of(kv->block);
+    a.blocks = (int)blocks;
+    return hip_status(mad::launch_kv8_append(a, dtype, (hipStream_t)stream), "kv8 append launch");
+}
+
+int mad_verify_attn_kv8(const void *q, int B, int T, int Hq, int Hkv, int d, int dtype, float scale,
+                        const mad_kv8_view *kv, void *out, float *lse, void *ws, size_t ws_bytes, void *stream) {
+    int rc = check_heads(B, Hq, Hkv, d, dtype);
+    if (rc) return rc;
+    const int G = Hq / Hkv;
+    if (T < 1 || T * G > MAD_MAX_VERIFY_ROWS)
+        return fail(MAD_EINVAL, "T=%d: T*G=%d must be in [1, %d]", T, T * G, MAD_MAX_VERIFY_ROWS);
+    if (!q || !out) return fail(MAD_EINVAL, "null q or out");
+    if (!aligned16(q) || !aligned16(out)) return fail(MAD_EINVAL, "q/out not 16-byte aligned");
+    if (!(scale > 0.f) || scale != scale) return fail(MAD_EINVAL, "scale must be positive");
+    if ((rc = check_view8(kv, B, Hkv, d))) return rc;
+    const size_t need = mad::verify_ws_bytes(B, Hq, Hkv, d, T);
+    if (!ws) return fail(MAD_EWS, "workspace required (%zu bytes)", need);
+    if (ws_bytes < need) return fail(MAD_EWS, "workspace %zu bytes < %zu", ws_bytes, need);
+    if (!aligned16(ws)) return fail(MAD_EINVAL, "workspace not 16-byte aligned");
+    mad::Stream8Args a;
+    memset(&a, 0, sizeof(a));
+    a.q = q;
+    a.k = kv->k;
+    a.v = kv->v;
+    a.k_scale = kv->k_scale;
+    a.v_scale = kv->v_scale;
+    a.kind = mad::kStream8;
+    a.out = out;
+    a.lse = lse;
+    a.seq = kv->seq_stride;
+    a.head = kv->head_stride;
+    a.s_seq = kv->scale_seq_stride;
+    a.s_head = kv->scale_head_stride;
+    a.log2_block = log2_of(kv->block);
+    a.part = (float *)((char *)ws + mad::kCounterRegionBytes);
+    a.counters = (unsigned *)ws;
+    a.scale_log2 = scale * 1.4426950408889634f;
+    a.cap = kv->cap;
+    a.Hq = Hq;
+    a.G = G;
+    a.T = T;
+    mad::plan_stream(a, B, Hkv, d, kv->len);
+    return hip_status(mad::launch_stream8(a, dtype, d, (hipStream_t)stream), "8-bit verify launch");
 }
 
 int mad_memory_prefill_attn(const void *q_raw, const void *q_slot, int B, int Hq, int Hkv, int d, int dtype,

@@ -84,8 +84,8 @@ constexpr int kMergeBytes = 128 << 10;      // LDS for the pieces of a unit that
 constexpr int kMergeInLaunch = 48 << 10;    // such pieces where the units are few (plan_stream)
 
 // verify over a cache of K and V rows; over K rows and V^T (one run of cap keys per feature);
-// the draft's decode: memory rows, window ring, new token (T = 1)
-enum { kStreamRows = 0, kStreamVT = 1, kStreamDraft = 2 };
+// the draft's decode: memory rows, window ring, new token (T = 1); verify over an 8-bit cache
+enum { kStreamRows = 0, kStreamVT = 1, kStreamDraft = 2, kStream8 = 3 };
 
 struct StreamArgs {
     const void *q, *k, *v;    // draft: k and v are the memory rows
@@ -122,6 +122,28 @@ void plan_stream(StreamArgs &a, int B, int Hkv, int d, const int *n_keys);
 hipError_t launch_stream(const StreamArgs &a, int d, hipStream_t st);
 size_t verify_ws_bytes(int B, int Hq, int Hkv, int d, int T);
 size_t stream_part_bytes(int units, int rows, int d);
+
+// ------------------------------------------------------------------- kv8 ----
+// new rows into the 8-bit cache (kv8.hip)
+struct Kv8AppendArgs {
+    const void *k_new, *v_new;   // [B][n_cap][Hkv][d]
+    void *k, *v;                 // codes
+    float *k_scale, *v_scale;
+    int64_t seq, head, s_seq, s_head;
+    int n_cap, Hkv, d, log2_block;
+    int blocks;                  // touched blocks of one head over all rows
+    // per row: touched blocks of the rows before it, length, new rows; past the last row: the end
+    int4 row[kMaxB];
+};
+hipError_t launch_kv8_append(const Kv8AppendArgs &a, int dtype, hipStream_t st);
+
+// attention over the 8-bit cache (stream8.hip)
+struct Stream8Args : StreamArgs {
+    const float *k_scale, *v_scale;
+    int64_t s_seq, s_head;
+    int log2_block;
+};
+hipError_t launch_stream8(const Stream8Args &a, int dtype, int d, hipStream_t st);
 
 // ----------------------------------------------------------------- layer ----
 constexpr int kMaxLinRows = MAD_MAX_LAYER_ROWS;
