@@ -80,6 +80,8 @@ bool update_uses_gemv(int R, int D, int dtype);
 constexpr int kStreamWGs = 256;   // workgroups of a launch: one per CU
 __host__ __device__ constexpr int stream_slab(int d) { return d == 128 ? 64 : 128; }   // keys per slab (32 KB of K + V)
 
+__host__ __device__ constexpr int stream8_slab(int d) { return stream_slab(d); }   // ... of an 8-bit cache (16 KB)
+
 constexpr int kMergeBytes = 128 << 10;      // LDS for the pieces of a unit that a workgroup merges in the launch
 constexpr int kMergeInLaunch = 48 << 10;    // such pieces where the units are few (plan_stream)
 

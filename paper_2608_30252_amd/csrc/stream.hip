@@ -584,7 +584,8 @@ __global__ __launch_bounds__(512, 1) void stream_kernel(const StreamArgs args) {
 // splits of one length).  By unit also serves launches with more units than workgroups can
 // count (a unit each: no pieces, no counters).
 void plan_stream(StreamArgs &a, int B, int Hkv, int d, const int *n_keys) {
-    const int slab = stream_slab(d) * (a.kind == kStream8 ? 2 : 1);   // 32 KB of K + V
+    const int slab = a.kind == kStream8 ? stream8_slab(d) : stream_slab(d);
+    const int least = a.kind == kStream8 ? 4 : 1;   // slabs that a workgroup takes at least (8 bits: a chunk for each of its waves)
     int64_t rows = 0;
     int nt[kMaxB], nt_max = 1;
     for (int b = 0; b < B; ++b) {
@@ -601,7 +602,7 @@ void plan_stream(StreamArgs &a, int B, int Hkv, int d, const int *n_keys) {
     a.Hkv = Hkv;
     a.merge2 = 0;
     const bool whole = (int64_t)B * Hkv > kCounterLines || total > 0x3fffffff;   // a unit each
-    a.n_wg = total < kStreamWGs ? (int)total : kStreamWGs;
+    a.n_wg = total < (int64_t)kStreamWGs * least ? (int)((total + least - 1) / least) : kStreamWGs;
     a.base = whole ? 1 : (int)(total / a.n_wg);
     a.rem = whole ? 0 : (int)(total % a.n_wg);
     int np_max = 1;

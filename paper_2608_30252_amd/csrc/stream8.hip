@@ -1,7 +1,6 @@
 // stream8.hip -- the target's verify attention (Sec. 2.1, Sec. 3.3; T = 1: a
 // single token's) over an 8-bit cache: e4m3 codes with one scale per block of
-// tokens and KV head.  Decomposition, ring and merge are stream.hip's; a slab is
-// again 32 KB of K + V, here of twice the keys.
+// tokens and KV head.
 //
 // Mathematics.  With key j's code row kc_j, its block's scales ks_j, vs_j and
 // row r's query q (cs = softmax scale * log2 e):
@@ -15,17 +14,33 @@
 //                 (24 bits), three products to the same accumulator.
 //   O^T = V^T P^T fp16 x fp16.  fp16 keeps 3 bits more of a probability than
 //                 bf16 (2^-12 against 2^-9 relative, which against the output's own
-//                 2^-9 is nothing); its range is made up for by p' = 2^15 p vs / vref,
-//                 vref the largest V scale the wave has met in the unit: p' <= 2^15, and
-//                 its precision holds down to p vs / vref = 2^-29.  fp32: a second
-//                 fp16 term holds what the first leaves (22 bits).
-// A K row's 16-byte chunk holds features 16 c .. 16 c + 15: the first 8 are one
+//                 2^-9 is nothing); its range is made up for by p' = 2^11 p vs / vref,
+//                 vref the largest V scale the wave has met in the unit.  m is the
+//                 running maximum to within 2^4: it is raised, and o scaled, only
+//                 where a score exceeds it by more (with 16 rows to a wave some
+//                 row's maximum grows in most steps, by little), so p' <= 2^15,
+//                 and fp16's precision holds down to p vs / vref = 2^-25.  fp32: a
+//                 second fp16 term holds what the first leaves (22 bits).
+//
+// Work decomposition.  As in stream.hip a unit is one (sequence, KV head) with
+// its T * G query rows, its keys are cut into slabs (16 KB of codes), and the
+// slabs of all units are dealt to one workgroup per CU (plan_stream).  Inside a
+// workgroup the eight waves take chunks of 8 KB (32 keys at d 128, 64 at d 64)
+// in turn, each on its own: a wave loads its chunks into its own two LDS stages,
+// reads a chunk's operands into registers, issues the chunk after next into the
+// place and computes, for every query row.  A code is converted once per chunk,
+// no wave waits for another inside a unit, and 64 - 128 KB per CU are in flight.
+// With slabs that eight waves shared, row block by row block (stream.hip's
+// way), every row block's wave converted the codes again and the vector ALU was the
+// bound: 16 sequences of 600 .. 12000 keys, 64/8 heads, 6 queries 86 us.  At a
+// unit's end the waves' results are merged through the stages.
+//   A K row's 16-byte chunk holds features 16 c .. 16 c + 15: the first 8 are one
 // 32-feature step's, the rest the next one's; the query fragments are read in
 // the same order.  V^T fragments (8 keys of one feature) come from transposing
 // byte reads (ds_read_b64_tr_b8).
 //
 // What a row does not see is left out whatever it holds: scores by selection,
-// and where a slab with hidden keys has NaN codes in V (0 * NaN is NaN) those are
+// and where a step with hidden keys has NaN codes in V (0 * NaN is NaN) those are
 // taken out and given back to the rows that see them.
 #include "stream_device.h"
 
@@ -37,35 +52,37 @@ typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_v;
 typedef __attribute__((ext_vector_type(2))) float f32x2_v;
 typedef int v2i_t __attribute__((ext_vector_type(2)));
 
-constexpr float kPShift = 15.f;   // p' = 2^15 p
+constexpr float kPShift = 11.f;   // p' = 2^11 p
+constexpr float kLazy = 4.f;      // the maximum is raised where a score exceeds it by more (log2 units)
 
 // T: bf16_t or float (queries and output)
 template <int D, int NB, typename T>
 struct Stream8Cfg {
     static constexpr bool F32 = std::is_same<T, float>::value;
-    static constexpr int SLAB = 2 * stream_slab(D);        // keys per slab
-    static constexpr int RB = D;                           // bytes per K (and V) row
-    static constexpr int CPR = D / 16;                     // 16-byte chunks per row
-    static constexpr int KBYTES = SLAB * RB;               // K bytes per slab (= V bytes)
-    static constexpr int STAGE = 2 * KBYTES;
-    static constexpr int NST = 4;                          // ring stages
     static constexpr int NWV = 8;                          // waves
-    static constexpr int IPW = STAGE / 1024 / NWV + 1;     // direct loads per wave per slab: codes, and 8 scales
+    static constexpr int RB = D;                           // bytes per K (and V) row
+    static constexpr int CPR = D / 16;                     // 16-byte pieces per row
+    static constexpr int KPC = 4096 / D;                   // keys per chunk
+    static constexpr int CHUNK = 8192;                     // K, then V
+    static constexpr int LOADS = 9;                        // direct loads per chunk: 4 + 4 of 1 KB, and the scales
+    static constexpr int KST = D / 32, DB = D / 16, NQ = F32 ? 3 : 1;
     static constexpr int RP = NB * 16;                     // padded query rows
-    static constexpr int KS = NB == 1 ? (SLAB / 32 < 8 ? SLAB / 32 : 8) : NB == 2 ? 4 : 2;   // key groups of a slab
-    static constexpr int KPG = SLAB / KS;                  // keys per group, in steps of 32
-    static constexpr int QRB = D * (F32 ? 4 : 2);          // bytes per query row
-    static constexpr int QBYTES = RP * QRB;
-    // query areas: 2 where they are small, none (queries straight from memory) where LDS has no room
-    static constexpr int QSLOTS = QBYTES <= 12288 ? 2 : QBYTES <= 24576 ? 1 : 0;
-    static constexpr int OFF_S = NST * STAGE;              // scales: 64 floats per stage
-    static constexpr int OFF_Q = OFF_S + NST * 256;
-    static constexpr int OFF_ML = OFF_Q + QSLOTS * QBYTES;
-    static constexpr int SMEM = OFF_ML + KS * RP * 8;
-    static constexpr int XPASS = KS * RP * D * 4 > STAGE ? 2 : 1;   // passes of the key groups' exchange through one stage
-    static_assert(STAGE == 32768 && IPW == 5 && KS * NB <= NWV && KPG % 32 == 0 && SLAB / 4 <= 64, "waves");
-    static_assert(KS * RP * D * 4 <= XPASS * STAGE, "the key groups' exchange fits one stage");
+    // query fragments (1 KB each), in registers where they and the accumulators leave room for the rest
+    static constexpr int QBYTES = NB * KST * NQ * 1024;
+    static constexpr bool QREG = NB * (KST * NQ + DB) * 4 < 120;
+    static constexpr bool LATE_V = NB * DB * 4 > 96;       // V's codes are read behind the softmax, for the same reason
+    static constexpr int REST = NWV * 2 * 64 + NWV * RP * 8 + QBYTES;
+    static constexpr int NST = NWV * 2 * CHUNK + REST + 1536 <= 160 * 1024 ? 2 : 1;   // stages per wave
+    static constexpr int RING = NWV * NST * CHUNK;
+    static constexpr int OFF_S = RING;                     // scales: 16 floats per wave and stage
+    static constexpr int OFF_ML = OFF_S + NWV * 2 * 64;    // the waves' (maximum, sum) per row
+    static constexpr int OFF_Q = OFF_ML + NWV * RP * 8;
+    static constexpr int USED = OFF_Q + QBYTES;
+    static constexpr int SMEM = USED > kMergeBytes ? USED : kMergeBytes;
+    // passes of the waves' exchange through the stages
+    static constexpr int XPASS = NWV * RP * D * 4 <= RING ? 1 : NWV * RP * D * 4 <= 2 * RING ? 2 : 4;
     static_assert(SMEM + 2 * MAD_MAX_VERIFY_ROWS * 4 + 64 <= 160 * 1024, "LDS, with the kernel's static arrays");
+    static_assert(NWV * RP * D * 4 <= XPASS * RING && D / XPASS >= 16, "exchange");
 };
 
 // Swizzles: 16-byte chunk c of key row k sits at chunk c ^ swz(k).
@@ -102,6 +119,13 @@ __device__ __forceinline__ f16x8_v codes_f16(uint32_t lo, uint32_t hi) {
 // 0x80 in every byte that is a NaN code
 __device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 
+// The same value, computed from here on: keeps the addresses that a rare part of the kernel derives from it out of
+// registers in the loop (the compiler would form them once, ahead of it).
+__device__ __forceinline__ int here(int v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
 struct KvScales {
     uint64_t k, v;
     int64_t seq, head;
@@ -111,14 +135,14 @@ struct KvScales {
 template <int D, int NB, typename T>
 __global__ __launch_bounds__(512, 1) void stream8_kernel(const Stream8Args args) {
     using C = Stream8Cfg<D, NB, T>;
-    constexpr int KST = D / 32, DB = D / 16, NQ = C::F32 ? 3 : 1;
+    constexpr int KST = C::KST, DB = C::DB, NQ = C::NQ, SLAB = stream8_slab(D);
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ int s_last[2];
     const StreamCtx a = load_ctx(args);
     KvScales sc = {ptr_bits(args.k_scale), ptr_bits(args.v_scale), args.s_seq, args.s_head, args.log2_block};
     asm volatile("" : "+s"(sc.k), "+s"(sc.v), "+s"(sc.seq), "+s"(sc.head), "+s"(sc.shift));
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lr = lane & 15, lg = lane >> 4;
     const int w = blockIdx.x;
     const int TT = a.T, G = a.G, R = TT * G, Hkv = a.Hkv;
@@ -145,280 +169,306 @@ __global__ __launch_bounds__(512, 1) void stream8_kernel(const Stream8Args args)
         t = rel - c * n0;
     }
 
-    // ---- issue side: the next slab to load is slab i_t of unit (i_b, i_c) ----
-    const int wv = __builtin_amdgcn_readfirstlane(wave);
-    int i_b = b, i_c = c, i_t = t, i_left = left, i_nt = 0;
-    int issued = 0, q_issued = 0, q_done = 0;   // slabs; query areas filled, and copied to registers
-    int i_stage = 0;                            // stage of the slab
-    int64_t i_keys = 0;                         // the unit's keys from the slab on
-    const uint8_t *i_k = nullptr, *i_v = nullptr;   // the slab's K and V rows
-    const float *i_s = nullptr;                     // lane < 8: the unit's K or V scales, as this lane loads them
-    // scale entry e = 8 wave + lane of a stage: K's of keys 8 e .., then V's (NG each)
-    constexpr int NG = C::SLAB / 8;
-    const int s_e = (wave * 8 + (lane & 7)) & (2 * NG - 1), s_key = (s_e & (NG - 1)) * 8;
-    auto i_unit = [&]() {
-        i_nt = a.slabs(i_b);
-        i_keys = a.len(i_b) - (int64_t)i_t * C::SLAB;
-        i_k = bits_ptr<const uint8_t>(a.k) + i_b * a.seq + i_c * a.head + (int64_t)i_t * C::SLAB * D;
-        i_v = bits_ptr<const uint8_t>(a.v) + i_b * a.seq + i_c * a.head + (int64_t)i_t * C::SLAB * D;
-        i_s = bits_ptr<const float>(s_e < NG ? sc.k : sc.v) + i_b * sc.seq + i_c * sc.head;
+    // ---- loads: lane l of load j (j = 0 .. 3 for K, and for V) fetches LDS slot cidx % CPR of the chunk's row
+    // cidx / CPR (cidx = 64 j + l), which holds the row's piece slot ^ swizzle(row).  The second load of a pair adds
+    // 1024 to both of its addresses (an instruction offset). ----
+    struct Offsets {
+        uint32_t k[4], v[4];
     };
-    i_unit();
-    // lane l of wave load inst fetches row cidx / CPR (cidx = 64 inst + l) of the slab; LDS slot cidx % CPR of
-    // the row holds its chunk slot ^ swizzle(row).  A wave's load j adds 1024 j to both of its addresses.
-    constexpr int LPW = (C::IPW - 1) / 2;   // K (and V) loads per wave
-    static_assert(LPW == 2, "lds_stream16_x2");
-    uint32_t k_off[LPW], v_off[LPW];
-    #pragma unroll
-    for (int j = 0; j < LPW; ++j) {
-        const int cidx = (wave * LPW + j) * 64 + lane, kr = cidx / C::CPR, slot = cidx % C::CPR;
-        k_off[j] = kr * C::RB + ((slot ^ k8_swz<D>(kr)) << 4) - 1024 * j;
-        v_off[j] = kr * C::RB + ((slot ^ v8_swz<D>(kr)) << 4) - 1024 * j;
-    }
-    const uint32_t lds_base = __builtin_amdgcn_readfirstlane(lds_addr(smem));
-    const uint32_t lds0 = lds_base + wv * LPW * 1024;
-    // the first slab of a unit (or of the run) needs a free query area
-    auto can_issue = [&]() {
-        return i_left > 0 && (C::QSLOTS == 0 || (i_t > 0 && issued > 0) || q_issued - q_done < C::QSLOTS);
-    };
-    auto issue = [&]() {
-        if (C::QSLOTS > 0 && (i_t == 0 || issued == 0)) {
-            // the unit's query rows, 1 KB per wave load; lanes past them fetch the last chunk again
-            constexpr int QC = C::QRB / 16;
-            unsigned char *qa = smem + C::OFF_Q + (C::QSLOTS == 2 ? (q_issued & 1) * C::QBYTES : 0);
-            const T *qb = bits_ptr<const T>(a.q) + ((size_t)i_b * TT * a.Hq + (size_t)i_c * G) * D;
-            for (int p = wv; p * 1024 < R * C::QRB; p += C::NWV) {
-                const int ch = min(p * 64 + lane, R * QC - 1), r = ch / QC, tt = r / G;
-                lds_stream16(reinterpret_cast<const unsigned char *>(qb + ((size_t)tt * a.Hq + (r - tt * G)) * D) + (ch % QC) * 16,
-                             qa + p * 1024);
-            }
-            ++q_issued;
-        }
-        if (lane < 8) {   // every wave 8 of the stage's scales (the block of a key past the last: the last one's)
-            const int64_t key = (int64_t)i_t * C::SLAB + min((int64_t)s_key, max(i_keys - 1, (int64_t)0));
-            lds_stream4(i_s + (key >> sc.shift), lds_base + C::OFF_S + i_stage * 256 + wv * 32);
-        }
-        const uint32_t st = i_stage * C::STAGE;
-        if (i_keys >= C::SLAB) {
-            lds_stream16_x2<true>(i_k, k_off[0], k_off[1], lds0 + st);
-            lds_stream16_x2<true>(i_v, v_off[0], v_off[1], lds0 + st + C::KBYTES);
-        } else {
-            const int last = max((int)i_keys - 1, 0);   // an empty row reads the cache's first, hidden
-            #pragma unroll
-            for (int j = 0; j < LPW; ++j) {
-                const int inst = wv * LPW + j;
-                const int cidx = inst * 64 + lane, kr = cidx / C::CPR, slot = cidx % C::CPR;
-                const int key = min(kr, last);   // rows past len: the last one again, hidden
-                lds_stream16_nt(i_k + key * D + (slot ^ k8_swz<D>(kr)) * 16, smem + st + inst * 1024);
-                lds_stream16_nt(i_v + key * D + (slot ^ v8_swz<D>(kr)) * 16, smem + st + C::KBYTES + inst * 1024);
-            }
-        }
-        ++issued;
-        --i_left;
-        i_stage = (i_stage + 1) & (C::NST - 1);
-        i_keys -= C::SLAB;
-        i_k += C::SLAB * D;
-        i_v += C::SLAB * D;
-        if (++i_t == i_nt && i_left > 0) {
-            i_t = 0;
-            if (++i_c == Hkv) {
-                i_c = 0;
-                ++i_b;
-            }
-            i_unit();
-        }
-    };
-
-    // ---- compute side: row block rbw, key group kg of every slab ----
-    const int rbw = wave % NB, kg = wave / NB, row = rbw * 16 + lr;
-    const bool active = kg < C::KS;
-    const int row_q = min(row, R - 1), row_t = row_q / G;   // this row's query index t
-    bf16x8_v qf[NQ][KST];
-    int len = 0, lim = 0, nt = 0;
-    f32x4_v o[DB];
-    float m_run = -INFINITY, l_run = 0.f;   // in log2 units; sum of p'
-    float vref = 0.f, inv_vref = 0.f;       // the largest V scale so far (the same in every lane)
-    const float cs = a.cs;
-
-    auto start_unit = [&]() {
-        nt = a.slabs(b);
-        len = a.len(b);
-        lim = len - TT + row_t;
-        const unsigned char *qa;
-        if constexpr (C::QSLOTS > 0)
-            qa = smem + C::OFF_Q + (C::QSLOTS == 2 ? (q_done & 1) * C::QBYTES : 0) + row_q * C::QRB;
-        else
-            qa = reinterpret_cast<const unsigned char *>(bits_ptr<const T>(a.q) + (((size_t)b * TT + row_t) * a.Hq + (size_t)c * G + (row_q - row_t * G)) * D);
+    auto offsets = [](int ln) {
+        Offsets x;
         #pragma unroll
-        for (int ks = 0; ks < KST; ++ks) {
-            const int f0 = 16 * lg + 64 * (ks >> 1) + 8 * (ks & 1);   // chunk lg + 4 (ks / 2) of the row, its half ks % 2
-            if constexpr (!C::F32) {
-                qf[0][ks] = *reinterpret_cast<const bf16x8_v *>(qa + f0 * 2);
+        for (int j = 0; j < 4; ++j) {
+            const int cidx = 64 * j + ln, kr = cidx / C::CPR, slot = cidx % C::CPR;
+            x.k[j] = kr * C::RB + ((slot ^ k8_swz<D>(kr)) << 4) - 1024 * (j & 1);
+            x.v[j] = kr * C::RB + ((slot ^ v8_swz<D>(kr)) << 4) - 1024 * (j & 1);
+        }
+        return x;
+    };
+    const Offsets kept = offsets(lane);
+    constexpr int NG = C::KPC / 8;   // scales of a chunk: K's of keys 8 e .., then V's (NG each), a lane each
+    unsigned char *ring = smem + wave * (C::NST * C::CHUNK);
+    float *ring_s = reinterpret_cast<float *>(smem + C::OFF_S) + wave * 32;
+    const uint32_t lds_k = lds_addr(ring), lds_s = lds_addr(ring_s);
+    const float cs = a.cs;
+    float *lse = bits_ptr<float>(a.lse);
+    int pu0 = -1, pu1 = -1;   // units of which this run holds a piece: begun by an earlier workgroup, begun here
+
+    for (bool first = true; left > 0; first = false) {
+        // ---- a segment: slabs t .. t1 - 1 of unit (b, c), keys [key0, key1) ----
+        const int u = b * Hkv + c, nt = a.slabs(b), len = a.len(b), t1 = min(nt, t + left);
+        const int64_t key0 = (int64_t)t * SLAB, key1 = min((int64_t)len, (int64_t)t1 * SLAB);
+        const uint8_t *kp = bits_ptr<const uint8_t>(a.k) + b * a.seq + c * a.head;
+        const uint8_t *vp = bits_ptr<const uint8_t>(a.v) + b * a.seq + c * a.head;
+        const float *sp = bits_ptr<const float>(lane < NG ? sc.k : sc.v) + b * sc.seq + c * sc.head;
+        auto issue = [&](int64_t key, int stage) {
+            const uint32_t at = lds_k + stage * C::CHUNK;
+            const uint8_t *k0 = kp + key * D, *v0 = vp + key * D;
+            const int last = (int)min(key1 - key, (int64_t)C::KPC) - 1;   // the chunk's last key
+            const int in_block = (int)(key & ((1 << sc.shift) - 1));
+            if (lane < 2 * NG)   // (the block of a key past the last: the last one's)
+                lds_stream4(sp + (key >> sc.shift) + ((in_block + min((lane & (NG - 1)) * 8, last)) >> sc.shift), lds_s + stage * 64);
+            if (last == C::KPC - 1) {
+                const Offsets x = C::LATE_V ? offsets(here(lane)) : kept;   // (no registers to keep them in)
+                lds_stream16_x2<true>(k0, x.k[0], x.k[1], at);
+                lds_stream16_x2<true>(k0, x.k[2], x.k[3], at + 2048);
+                lds_stream16_x2<true>(v0, x.v[0], x.v[1], at + 4096);
+                lds_stream16_x2<true>(v0, x.v[2], x.v[3], at + 6144);
             } else {
-                // three bf16 terms: each what the ones before leave, to nearest
-                float x[8];
-                *reinterpret_cast<f32x4_v *>(x) = *reinterpret_cast<const f32x4_v *>(qa + f0 * 4);
-                *reinterpret_cast<f32x4_v *>(x + 4) = *reinterpret_cast<const f32x4_v *>(qa + f0 * 4 + 16);
+                const int ln = here(lane);
                 #pragma unroll
-                for (int i = 0; i < NQ; ++i)
+                for (int j = 0; j < 4; ++j) {
+                    const int cidx = 64 * j + ln, kr = cidx / C::CPR, slot = cidx % C::CPR;
+                    const int row = min(kr, last);   // rows past the last: the last one again, hidden
+                    lds_stream16_nt(k0 + row * D + (slot ^ k8_swz<D>(kr)) * 16, ring + stage * C::CHUNK + j * 1024);
+                    lds_stream16_nt(v0 + row * D + (slot ^ v8_swz<D>(kr)) * 16, ring + stage * C::CHUNK + 4096 + j * 1024);
+                }
+            }
+        };
+        int64_t key = key0 + wave * C::KPC;   // this wave's next chunk
+        constexpr int STEP = C::NWV * C::KPC;
+        #pragma unroll
+        for (int s = 0; s < C::NST; ++s)
+            if (key + s * STEP < key1) issue(key + s * STEP, s);
+
+        // ---- the unit's queries: fragment (ks, nb) holds feature 16 lg + 64 (ks / 2) + 8 (ks % 2) + e of row
+        // 16 nb + lr (fp32: as three bf16 terms, each what the ones before leave); rows past R repeat the last ----
+        const int q_lane = here(lane), q_lr = q_lane & 15, q_lg = q_lane >> 4;
+        for (int f = wave; f < KST * NB; f += C::NWV) {
+            const int ks = f % KST, row = min(f / KST * 16 + q_lr, R - 1), rt = row / G;
+            const T *src = bits_ptr<const T>(a.q) + (((size_t)b * TT + rt) * a.Hq + (size_t)c * G + (row - rt * G)) * D +
+                           16 * q_lg + 64 * (ks >> 1) + 8 * (ks & 1);
+            u32x4_v *dst = reinterpret_cast<u32x4_v *>(smem + C::OFF_Q) + f * NQ * 64 + q_lane;
+            if constexpr (!C::F32) {
+                *dst = *reinterpret_cast<const u32x4_v *>(src);
+            } else {
+                float x[8];
+                *reinterpret_cast<f32x4_v *>(x) = *reinterpret_cast<const f32x4_v *>(src);
+                *reinterpret_cast<f32x4_v *>(x + 4) = *reinterpret_cast<const f32x4_v *>(src + 4);
+                #pragma unroll
+                for (int i = 0; i < NQ; ++i) {
+                    bf16x8_v h;
                     #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        const __bf16 h = (__bf16)x[e];
-                        qf[i][ks][e] = h;
-                        x[e] -= (float)h;
+                        h[e] = (__bf16)x[e];
+                        x[e] -= (float)h[e];
                     }
-            }
-        }
-        m_run = -INFINITY;
-        l_run = 0.f;
-        vref = inv_vref = 0.f;
-        #pragma unroll
-        for (int db = 0; db < DB; ++db) o[db] = f32x4_v{0.f, 0.f, 0.f, 0.f};
-    };
-
-    // 32 keys of the slab, from key 32 kh of it
-    auto compute = [&](const unsigned char *st, const float *ss, int kb, int kh) {
-        // A row m of block blk is key 32 kh + 8(m/4) + 4 blk + m%4 of the slab, so
-        // accumulator element e&3 of block e>>2 is key 32 kh + 8 lg + e
-        u32x4_v kc[2][KST / 2];
-        v2i_t vc[DB];
-        #pragma unroll
-        for (int blk = 0; blk < 2; ++blk) {
-            const int kr = 32 * kh + 8 * (lr >> 2) + 4 * blk + (lr & 3);
-            #pragma unroll
-            for (int j = 0; j < KST / 2; ++j)
-                kc[blk][j] = *reinterpret_cast<const u32x4_v *>(st + kr * C::RB + (((4 * j + lg) ^ k8_swz<D>(kr)) << 4));
-        }
-        const float ksc = ss[4 * kh + lg], vsc = ss[NG + 4 * kh + lg];
-        const int vr = 32 * kh + 8 * lg + (lr >> 1);
-        #pragma unroll
-        for (int db = 0; db < DB; ++db)   // features db*16 + lr, keys 32 kh + 8 lg .. +7
-            vc[db] = lds_read_tr8(st + C::KBYTES + vr * C::RB + ((db ^ v8_swz<D>(vr)) << 4) + 8 * (lr & 1));
-        f32x4_v sacc[2];
-        #pragma unroll
-        for (int blk = 0; blk < 2; ++blk) {
-            sacc[blk] = f32x4_v{0.f, 0.f, 0.f, 0.f};
-            #pragma unroll
-            for (int ks = 0; ks < KST; ++ks) {
-                const bf16x8_v kf = codes_bf16(kc[blk][ks >> 1][2 * (ks & 1)], kc[blk][ks >> 1][2 * (ks & 1) + 1]);
-                #pragma unroll
-                for (int i = 0; i < NQ; ++i)
-                    sacc[blk] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[i][ks], sacc[blk], 0, 0, 0);
-            }
-        }
-        float x[8];
-        float mt = -INFINITY;
-        const float csk = cs * ksc;
-        const int kg0 = kb + 32 * kh + 8 * lg;
-        const bool open = __all(kb + C::SLAB - 1 <= lim);   // every row sees the whole slab
-        #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = sacc[j >> 2][j & 3] * csk;
-        if (!open) {
-            #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = kg0 + j <= lim ? x[j] : -INFINITY;
-        }
-        #pragma unroll
-        for (int j = 0; j < 8; ++j) mt = fmaxf(mt, x[j]);
-        mt = max_over_row_lanes(mt);
-        const float vm = max_over_row_lanes(vsc);
-        const float mn = fmaxf(m_run, mt);
-        const bool same = mn == m_run;
-        const float ms = (mn == -INFINITY) ? 0.f : mn - kPShift;
-        float alpha = same ? 1.f : __builtin_amdgcn_exp2f(m_run - mn);
-        m_run = mn;
-        const float l_alpha = alpha;
-        const bool vgrew = vm > vref;   // the same in every lane
-        if (vgrew) {
-            inv_vref = 1.f / vm;
-            alpha *= vref * inv_vref;
-            vref = vm;
-        }
-        const float rv = vsc * inv_vref;
-        float ps = 0.f;
-        uint32_t pk[4], pl[4];
-        #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            float p0 = __builtin_amdgcn_exp2f(x[2 * e] - ms), p1 = __builtin_amdgcn_exp2f(x[2 * e + 1] - ms);
-            ps += p0 + p1;
-            p0 *= rv;
-            p1 *= rv;
-            const f16x2_v h = __builtin_convertvector((f32x2_v{p0, p1}), f16x2_v);
-            pk[e] = __builtin_bit_cast(uint32_t, h);
-            if constexpr (C::F32)
-                pl[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_v{p0 - (float)h[0], p1 - (float)h[1]}), f16x2_v));
-        }
-        const f16x8_v pf = __builtin_bit_cast(f16x8_v, u32x4_v{pk[0], pk[1], pk[2], pk[3]});
-        l_run = fmaf(l_run, l_alpha, ps);
-        if (!__all(same && !vgrew)) {
-            #pragma unroll
-            for (int db = 0; db < DB; ++db) o[db] *= alpha;
-        }
-        if (!open) {
-            // NaN codes that some row does not see: out of the product, and into the rows that see them
-            uint32_t any = 0;
-            #pragma unroll
-            for (int db = 0; db < DB; ++db) any |= nan_codes(vc[db][0]) | nan_codes(vc[db][1]);
-            if (__any(any != 0)) {
-                f16x8_v seen;
-                #pragma unroll
-                for (int j = 0; j < 8; ++j) seen[j] = kg0 + j <= lim ? (_Float16)1.f : (_Float16)0.f;
-                #pragma unroll
-                for (int db = 0; db < DB; ++db) {
-                    const uint32_t n0 = nan_codes(vc[db][0]) >> 7, n1 = nan_codes(vc[db][1]) >> 7;   // 1 in each such byte
-                    const f32x4_v hit = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_f16(n0 * 0x38u, n1 * 0x38u), seen, f32x4_v{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);   // 0x38: 1.0
-                    #pragma unroll
-                    for (int e = 0; e < 4; ++e) o[db][e] = hit[e] > 0.f ? __builtin_nanf("") : o[db][e];
-                    vc[db][0] &= ~(n0 * 0xffu);
-                    vc[db][1] &= ~(n1 * 0xffu);
+                    dst[i * 64] = __builtin_bit_cast(u32x4_v, h);
                 }
             }
         }
-        #pragma unroll
-        for (int db = 0; db < DB; ++db) {
-            const f16x8_v vf = codes_f16(vc[db][0], vc[db][1]);
-            o[db] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf, o[db], 0, 0, 0);
-            if constexpr (C::F32)
-                o[db] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, __builtin_bit_cast(f16x8_v, u32x4_v{pl[0], pl[1], pl[2], pl[3]}), o[db], 0, 0, 0);
+        __syncthreads();
+        auto q_frag = [&](int nb, int ks, int i) {
+            return *reinterpret_cast<const bf16x8_v *>(smem + C::OFF_Q + (((nb * KST + ks) * NQ + i) * 64 + lane) * 16);
+        };
+        bf16x8_v qf[C::QREG ? NB : 1][KST][NQ];
+        if constexpr (C::QREG) {
+            #pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+                #pragma unroll
+                for (int ks = 0; ks < KST; ++ks)
+                    #pragma unroll
+                    for (int i = 0; i < NQ; ++i) qf[nb][ks][i] = q_frag(nb, ks, i);
         }
-    };
 
-    // ---- end of a unit's run in this workgroup: the key groups' results are exchanged through the stage just
-    // read and every thread merges whole 16-byte chunks, the unit's result or its piece (stream.hip) ----
-    int pu0 = -1, pu1 = -1;   // units of which this run holds a piece: begun by an earlier workgroup, begun here
-    float *lse = bits_ptr<float>(a.lse);
-    auto flush = [&](unsigned char *st, bool from0) {
-        const bool whole = from0 && t == nt;   // every slab of the unit ran here
-        const int u = b * Hkv + c;
-        if (!from0) pu0 = u;
-        else if (!whole) pu1 = u;
-        constexpr int DP = D / C::XPASS, QP = DP / 4;                 // features, chunks of a row per pass
-        float2 *xml = reinterpret_cast<float2 *>(smem + C::OFF_ML);   // [KS][RP]
-        const float lt = sum_over_row_lanes(l_run);
+        f32x4_v o[NB][DB];
+        float m_run[NB], l_run[NB];           // in log2 units; sum of p'
+        int lim[NB];                          // the last key that row 16 nb + lr sees
+        float vref = 0.f, inv_vref = 0.f;     // the largest V scale so far (the same in every lane)
+        #pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            m_run[nb] = -INFINITY;
+            l_run[nb] = 0.f;
+            lim[nb] = len - TT + min(16 * nb + lr, R - 1) / G;
+            #pragma unroll
+            for (int db = 0; db < DB; ++db) o[nb][db] = f32x4_v{0.f, 0.f, 0.f, 0.f};
+        }
+        const int open_to = len - TT;   // keys up to here are seen by every row
+
+        for (int stage = 0; key < key1; key += STEP, stage ^= C::NST - 1) {
+            if (C::NST == 2 && key + STEP < key1) asm volatile("s_waitcnt vmcnt(9)" : : : "memory");   // LOADS: the next chunk's
+            else asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+            const unsigned char *st = ring + stage * C::CHUNK;
+            const float *ss = ring_s + stage * 16;
+            #pragma unroll
+            for (int kh = 0; kh < C::KPC / 32; ++kh) {
+                // A row m of block blk is key 32 kh + 8(m/4) + 4 blk + m%4 of the chunk, so
+                // accumulator element e&3 of block e>>2 is key 32 kh + 8 lg + e
+                u32x4_v kc[2][KST / 2];
+                v2i_t vc[DB];
+                #pragma unroll
+                for (int blk = 0; blk < 2; ++blk) {
+                    const int kr = 32 * kh + 8 * (lr >> 2) + 4 * blk + (lr & 3);
+                    #pragma unroll
+                    for (int j = 0; j < KST / 2; ++j)
+                        kc[blk][j] = *reinterpret_cast<const u32x4_v *>(st + kr * C::RB + (((4 * j + lg) ^ k8_swz<D>(kr)) << 4));
+                }
+                const float ksc = ss[4 * kh + lg], vsc = ss[NG + 4 * kh + lg];
+                auto read_v = [&]() {
+                    const int vr = 32 * kh + 8 * lg + (lr >> 1);
+                    #pragma unroll
+                    for (int db = 0; db < DB; ++db)   // features db*16 + lr, keys 32 kh + 8 lg .. +7
+                        vc[db] = lds_read_tr8(st + 4096 + vr * C::RB + ((db ^ v8_swz<D>(vr)) << 4) + 8 * (lr & 1));
+                    if (kh == C::KPC / 32 - 1) {
+                        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");   // the stage is read
+                        if (key + C::NST * STEP < key1) issue(key + C::NST * STEP, stage);
+                    }
+                };
+                if constexpr (!C::LATE_V) read_v();
+
+                // (The scheduling fences keep one row block's, one fragment's temporaries from living beside the next's:
+                // without them the kernel spills from 32 rows on.)
+                f32x4_v sacc[NB][2];
+                #pragma unroll
+                for (int blk = 0; blk < 2; ++blk)
+                    #pragma unroll
+                    for (int ks = 0; ks < KST; ++ks) {
+                        if (ks % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+                        const bf16x8_v kf = codes_bf16(kc[blk][ks >> 1][2 * (ks & 1)], kc[blk][ks >> 1][2 * (ks & 1) + 1]);
+                        #pragma unroll
+                        for (int nb = 0; nb < NB; ++nb)
+                            #pragma unroll
+                            for (int i = 0; i < NQ; ++i) {
+                                bf16x8_v q;
+                                if constexpr (C::QREG) q = qf[nb][ks][i];
+                                else q = q_frag(nb, ks, i);
+                                sacc[nb][blk] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q, ks == 0 && i == 0 ? f32x4_v{0.f, 0.f, 0.f, 0.f} : sacc[nb][blk], 0, 0, 0);
+                            }
+                    }
+
+                __builtin_amdgcn_sched_barrier(0);
+                const float vm = max_over_row_lanes(vsc);
+                if (vm > vref) {   // the same in every lane
+                    inv_vref = 1.f / vm;
+                    const float down = vref * inv_vref;
+                    #pragma unroll
+                    for (int nb = 0; nb < NB; ++nb)
+                        #pragma unroll
+                        for (int db = 0; db < DB; ++db) o[nb][db] *= down;
+                    vref = vm;
+                }
+                const float rv = vsc * inv_vref, csk = cs * ksc;
+                const int kg0 = 32 * kh + 8 * lg;   // this lane's first key of the chunk
+                const bool open = key + C::KPC - 1 <= open_to;   // every row sees the whole chunk
+                u32x4_v pk[NB], pl[C::F32 ? NB : 1];
+                #pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    float x[8], mt = -INFINITY;
+                    #pragma unroll
+                    for (int j = 0; j < 8; ++j) x[j] = sacc[nb][j >> 2][j & 3] * csk;
+                    if (!open) {
+                        const int seen = lim[nb] - (int)key - kg0;   // (from -63 on: a key of the unit is in the chunk)
+                        #pragma unroll
+                        for (int j = 0; j < 8; ++j) x[j] = j <= seen ? x[j] : -INFINITY;
+                    }
+                    #pragma unroll
+                    for (int j = 0; j < 8; ++j) mt = fmaxf(mt, x[j]);
+                    mt = max_over_row_lanes(mt);
+                    if (!__all(mt <= m_run[nb] + kLazy)) {
+                        const float mn = mt > m_run[nb] + kLazy ? mt : m_run[nb];
+                        const float alpha = mn == m_run[nb] ? 1.f : __builtin_amdgcn_exp2f(m_run[nb] - mn);
+                        m_run[nb] = mn;
+                        l_run[nb] *= alpha;
+                        #pragma unroll
+                        for (int db = 0; db < DB; ++db) o[nb][db] *= alpha;
+                    }
+                    const float ms = m_run[nb] == -INFINITY ? 0.f : m_run[nb] - kPShift;
+                    float ps = 0.f;
+                    #pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float p0 = __builtin_amdgcn_exp2f(x[2 * e] - ms), p1 = __builtin_amdgcn_exp2f(x[2 * e + 1] - ms);
+                        ps += p0 + p1;
+                        p0 *= rv;
+                        p1 *= rv;
+                        const f16x2_v h = __builtin_convertvector((f32x2_v{p0, p1}), f16x2_v);
+                        pk[nb][e] = __builtin_bit_cast(uint32_t, h);
+                        if constexpr (C::F32)
+                            pl[nb][e] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_v{p0 - (float)h[0], p1 - (float)h[1]}), f16x2_v));
+                    }
+                    l_run[nb] += ps;
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if constexpr (C::LATE_V) read_v();
+                if (!open) {
+                    // NaN codes that some row does not see: out of the product, and into the rows that see them
+                    uint32_t any = 0;
+                    #pragma unroll
+                    for (int db = 0; db < DB; ++db) any |= nan_codes(vc[db][0]) | nan_codes(vc[db][1]);
+                    if (__any(any != 0)) {
+                        #pragma unroll
+                        for (int db = 0; db < DB; ++db) {
+                            const uint32_t n0 = nan_codes(vc[db][0]) >> 7, n1 = nan_codes(vc[db][1]) >> 7;   // 1 in each such byte
+                            const f16x8_v is_nan = codes_f16(n0 * 0x38u, n1 * 0x38u);                        // 0x38: 1.0
+                            #pragma unroll
+                            for (int nb = 0; nb < NB; ++nb) {
+                                f16x8_v seen;
+                                #pragma unroll
+                                for (int j = 0; j < 8; ++j) seen[j] = kg0 + j <= lim[nb] - (int)key ? (_Float16)1.f : (_Float16)0.f;
+                                const f32x4_v hit = __builtin_amdgcn_mfma_f32_16x16x32_f16(is_nan, seen, f32x4_v{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+                                #pragma unroll
+                                for (int e = 0; e < 4; ++e) o[nb][db][e] = hit[e] > 0.f ? __builtin_nanf("") : o[nb][db][e];
+                            }
+                            vc[db][0] &= ~(n0 * 0xffu);
+                            vc[db][1] &= ~(n1 * 0xffu);
+                        }
+                    }
+                }
+                #pragma unroll
+                for (int db = 0; db < DB; ++db) {
+                    const f16x8_v vf = codes_f16(vc[db][0], vc[db][1]);
+                    #pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) {
+                        o[nb][db] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, __builtin_bit_cast(f16x8_v, pk[nb]), o[nb][db], 0, 0, 0);
+                        if constexpr (C::F32)
+                            o[nb][db] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, __builtin_bit_cast(f16x8_v, pl[nb]), o[nb][db], 0, 0, 0);
+                    }
+                    if (db & 1) __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        }
+
+        // ---- the segment's end: the waves' results are exchanged through the stages (16-byte pieces swizzled by
+        // row) and every thread merges whole pieces, the unit's result or its part of it for the merge ----
+        left -= t1 - t;
+        const bool from0 = t == 0, whole = from0 && t1 == nt;   // every slab of the unit ran here
+        if (!whole) {
+            if (first) pu0 = u;   // the run's first unit; another one that does not end here is its last
+            else pu1 = u;
+        }
+        constexpr int DP = D / C::XPASS, QP = DP / 4;                 // features, pieces of a row per pass
+        constexpr int SW = QP < 16 ? QP - 1 : 15;
+        float2 *xml = reinterpret_cast<float2 *>(smem + C::OFF_ML);   // [8][RP]
+        const int x_lane = here(lane), x_lg = x_lane >> 4, x_tid = here(tid);
         #pragma unroll
         for (int ps = 0; ps < C::XPASS; ++ps) {
-            __syncthreads();   // every wave is done with the stage
-            if (active) {
+            __syncthreads();   // every wave is done with the stages, or with the pass before
+            #pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                const int row = 16 * nb + (x_lane & 15);
                 #pragma unroll
                 for (int db = 0; db < DP / 16; ++db)
-                    *reinterpret_cast<f32x4_v *>(st + ((kg * C::RP + row) * QP + ((db * 4 + lg) ^ (row & (QP - 1) & 15))) * 16) =
-                        o[ps * (DP / 16) + db] * vref;
-                // (max, sum of p) in log2 units: the sum is of p' = 2^15 p
-                if (ps == 0 && lg == 0) xml[kg * C::RP + row] = make_float2(m_run - kPShift, lt);
+                    *reinterpret_cast<f32x4_v *>(smem + ((wave * C::RP + row) * QP + ((db * 4 + x_lg) ^ (row & SW))) * 16) =
+                        o[nb][ps * (DP / 16) + db] * vref;
+                // (max, sum of p) in log2 units: the sum is of p' = 2^11 p
+                if (ps == 0) {
+                    const float lt = sum_over_row_lanes(l_run[nb]);
+                    if (x_lg == 0) xml[wave * C::RP + row] = make_float2(m_run[nb] - kPShift, lt);
+                }
             }
             __syncthreads();
-            for (int x = tid; x < R * QP; x += 512) {
+            for (int x = x_tid; x < R * QP; x += 512) {
                 const int r = x / QP, ch = x % QP;
-                float m[C::KS], M = -INFINITY, L = 0.f;
+                float m[C::NWV], M = -INFINITY, L = 0.f;
                 f32x4_v y = f32x4_v{0.f, 0.f, 0.f, 0.f};
                 #pragma unroll
-                for (int k = 0; k < C::KS; ++k) {
+                for (int k = 0; k < C::NWV; ++k) {
                     m[k] = xml[k * C::RP + r].x;
                     M = fmaxf(M, m[k]);
                 }
                 #pragma unroll
-                for (int k = 0; k < C::KS; ++k) {
+                for (int k = 0; k < C::NWV; ++k) {
                     const float wt = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[k] - M);
-                    const f32x4_v v = *reinterpret_cast<const f32x4_v *>(st + ((k * C::RP + r) * QP + (ch ^ (r & (QP - 1) & 15))) * 16);
+                    const f32x4_v v = *reinterpret_cast<const f32x4_v *>(smem + ((k * C::RP + r) * QP + (ch ^ (r & SW))) * 16);
                     L = fmaf(wt, xml[k * C::RP + r].y, L);
                     #pragma unroll
                     for (int e = 0; e < 4; ++e) y[e] = fmaf(wt, v[e], y[e]);
@@ -436,42 +486,12 @@ __global__ __launch_bounds__(512, 1) void stream8_kernel(const Stream8Args args)
                 }
             }
         }
-    };
-
-    while (issued < C::NST - 1 && can_issue()) issue();
-    bool first = true;   // the run's first unit
-    int c_stage = 0;
-    for (int i = 0; i < left; ++i) {
-        if (issued <= i) {   // the slab waited for a query area, which every wave has read by now
-            __syncthreads();
-            issue();
+        t = 0;
+        if (++c == Hkv) {
+            c = 0;
+            ++b;
         }
-        wait_vm(C::IPW * (issued - 1 - i));   // slab i has landed (this wave's part; newer query loads only make it stricter)
-        __syncthreads();                      // ... every wave's part; stage (i-1) % NST is free
-        while (issued < i + C::NST && can_issue()) issue();
-        if (t == 0 || i == 0) {
-            start_unit();
-            ++q_done;
-        }
-        unsigned char *st = smem + c_stage * C::STAGE;
-        const float *ss = reinterpret_cast<const float *>(smem + C::OFF_S + c_stage * 256);
-        c_stage = (c_stage + 1) & (C::NST - 1);
-        if (active) {
-            #pragma unroll
-            for (int h = 0; h < C::KPG / 32; ++h) compute(st, ss, t * C::SLAB, kg * (C::KPG / 32) + h);
-        }
-        ++t;
-        if (t == nt || i == left - 1) {
-            flush(st, !first || i + 1 == t);
-            first = false;
-            if (t == nt) {
-                t = 0;
-                if (++c == Hkv) {
-                    c = 0;
-                    ++b;
-                }
-            }
-        }
+        __syncthreads();   // the stages are free
     }
     if ((pu0 < 0 && pu1 < 0) || a.merge2) return;
 
@@ -496,7 +516,6 @@ __global__ __launch_bounds__(512, 1) void stream8_kernel(const Stream8Args args)
     if (last == 0) return;
     const int bytes0 = (last & 1) ? up0.np * pf * 4 : 0, bytes1 = (last & 2) ? up1.np * pf * 4 : 0;
     const int at1 = (bytes0 + 1023) & ~1023;
-    static_assert(kMergeBytes <= C::OFF_S, "the pieces lie in the ring");
     __shared__ float sinv[2 * MAD_MAX_VERIFY_ROWS];
     auto merge = [&](bool first_unit, bool second_unit, int at) {
         if (first_unit) load_pieces(part + (size_t)up0.p0 * pf, bytes0, smem);

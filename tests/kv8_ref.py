@@ -98,11 +98,11 @@ def out_tolerance(out, mean, A, n, d, vmax, bf16):
     probabilities' (fp16: 2^-11 of each, in two terms 2^-22); a score's error E = 2^-24 (2 sqrt(d) A + 8 A + 8),
     the rounding of a d-term fp32 sum with a factor 2 of margin, of its scaling and of the exponential's argument
     and result, which moves each weight by E and their sum too; fp32 sums over n keys, 2^-24 * 2 sqrt(n); and fp16's
-    smallest step, 2^-25 of p' = 2^15 p, on every key."""
+    smallest step, 2^-25 of p' = 2^11 p (p the weight against a maximum that is no larger than the row's), on every key."""
     u = 2.0 ** -24
     E = u * (2 * math.sqrt(d) * A + 8 * A + 8)
     rel = (2.0 ** -11 if bf16 else 2.0 ** -22) + 2 * E + u * (4 + 2 * np.sqrt(n))
-    return (2.0 ** -8 if bf16 else u) * np.abs(out) + rel[..., None] * mean + (n * 2.0 ** -40 * vmax)[..., None] + 1e-30
+    return (2.0 ** -8 if bf16 else u) * np.abs(out) + rel[..., None] * mean + (n * 2.0 ** -36 * vmax)[..., None] + 1e-30
 
 
 def check_out(got, out, tol, what=""):
