@@ -73,16 +73,17 @@ struct Stream8Cfg {
     static constexpr bool LATE_V = NB * DB * 4 > 96;       // V's codes are read behind the softmax, for the same reason
     static constexpr int REST = NWV * 2 * 64 + NWV * RP * 8 + QBYTES;
     static constexpr int NST = NWV * 2 * CHUNK + REST + 1536 <= 160 * 1024 ? 2 : 1;   // stages per wave
-    static constexpr int RING = NWV * NST * CHUNK;
+    static constexpr int RING = NWV * NST * CHUNK;         // stage 0 of every wave, then stage 1
     static constexpr int OFF_S = RING;                     // scales: 16 floats per wave and stage
     static constexpr int OFF_ML = OFF_S + NWV * 2 * 64;    // the waves' (maximum, sum) per row
     static constexpr int OFF_Q = OFF_ML + NWV * RP * 8;
     static constexpr int USED = OFF_Q + QBYTES;
     static constexpr int SMEM = USED > kMergeBytes ? USED : kMergeBytes;
-    // passes of the waves' exchange through the stages
-    static constexpr int XPASS = NWV * RP * D * 4 <= RING ? 1 : NWV * RP * D * 4 <= 2 * RING ? 2 : 4;
+    // the waves' exchange goes through the last stage of all of them, XD feature blocks at a time
+    static constexpr int OFF_X = RING - NWV * CHUNK;
+    static constexpr int XD = NB * DB <= 8 ? DB : NB == 2 ? 4 : NB == 1 ? 8 : 2;
     static_assert(SMEM + 2 * MAD_MAX_VERIFY_ROWS * 4 + 64 <= 160 * 1024, "LDS, with the kernel's static arrays");
-    static_assert(NWV * RP * D * 4 <= XPASS * RING && D / XPASS >= 16, "exchange");
+    static_assert(NWV * NB * XD * 1024 <= NWV * CHUNK && NB * XD <= NWV && DB % XD == 0, "exchange");
 };
 
 // Swizzles: 16-byte chunk c of key row k sits at chunk c ^ swz(k).
@@ -187,80 +188,109 @@ __global__ __launch_bounds__(512, 1) void stream8_kernel(const Stream8Args args)
     };
     const Offsets kept = offsets(lane);
     constexpr int NG = C::KPC / 8;   // scales of a chunk: K's of keys 8 e .., then V's (NG each), a lane each
-    unsigned char *ring = smem + wave * (C::NST * C::CHUNK);
+    constexpr int STAGE = C::NWV * C::CHUNK;   // from a wave's stage to its next
+    unsigned char *ring = smem + wave * C::CHUNK;
     float *ring_s = reinterpret_cast<float *>(smem + C::OFF_S) + wave * 32;
     const uint32_t lds_k = lds_addr(ring), lds_s = lds_addr(ring_s);
     const float cs = a.cs;
     float *lse = bits_ptr<float>(a.lse);
     int pu0 = -1, pu1 = -1;   // units of which this run holds a piece: begun by an earlier workgroup, begun here
 
-    for (bool first = true; left > 0; first = false) {
-        // ---- a segment: slabs t .. t1 - 1 of unit (b, c), keys [key0, key1) ----
-        const int u = b * Hkv + c, nt = a.slabs(b), len = a.len(b), t1 = min(nt, t + left);
-        const int64_t key0 = (int64_t)t * SLAB, key1 = min((int64_t)len, (int64_t)t1 * SLAB);
-        const uint8_t *kp = bits_ptr<const uint8_t>(a.k) + b * a.seq + c * a.head;
-        const uint8_t *vp = bits_ptr<const uint8_t>(a.v) + b * a.seq + c * a.head;
-        const float *sp = bits_ptr<const float>(lane < NG ? sc.k : sc.v) + b * sc.seq + c * sc.head;
-        auto issue = [&](int64_t key, int stage) {
-            const uint32_t at = lds_k + stage * C::CHUNK;
-            const uint8_t *k0 = kp + key * D, *v0 = vp + key * D;
-            const int last = (int)min(key1 - key, (int64_t)C::KPC) - 1;   // the chunk's last key
-            const int in_block = (int)(key & ((1 << sc.shift) - 1));
-            if (lane < 2 * NG)   // (the block of a key past the last: the last one's)
-                lds_stream4(sp + (key >> sc.shift) + ((in_block + min((lane & (NG - 1)) * 8, last)) >> sc.shift), lds_s + stage * 64);
-            if (last == C::KPC - 1) {
-                const Offsets x = C::LATE_V ? offsets(here(lane)) : kept;   // (no registers to keep them in)
-                lds_stream16_x2<true>(k0, x.k[0], x.k[1], at);
-                lds_stream16_x2<true>(k0, x.k[2], x.k[3], at + 2048);
-                lds_stream16_x2<true>(v0, x.v[0], x.v[1], at + 4096);
-                lds_stream16_x2<true>(v0, x.v[2], x.v[3], at + 6144);
-            } else {
-                const int ln = here(lane);
-                #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int cidx = 64 * j + ln, kr = cidx / C::CPR, slot = cidx % C::CPR;
-                    const int row = min(kr, last);   // rows past the last: the last one again, hidden
-                    lds_stream16_nt(k0 + row * D + (slot ^ k8_swz<D>(kr)) * 16, ring + stage * C::CHUNK + j * 1024);
-                    lds_stream16_nt(v0 + row * D + (slot ^ v8_swz<D>(kr)) * 16, ring + stage * C::CHUNK + 4096 + j * 1024);
-                }
-            }
-        };
-        int64_t key = key0 + wave * C::KPC;   // this wave's next chunk
-        constexpr int STEP = C::NWV * C::KPC;
-        #pragma unroll
-        for (int s = 0; s < C::NST; ++s)
-            if (key + s * STEP < key1) issue(key + s * STEP, s);
-
-        // ---- the unit's queries: fragment (ks, nb) holds feature 16 lg + 64 (ks / 2) + 8 (ks % 2) + e of row
-        // 16 nb + lr (fp32: as three bf16 terms, each what the ones before leave); rows past R repeat the last ----
-        const int q_lane = here(lane), q_lr = q_lane & 15, q_lg = q_lane >> 4;
-        for (int f = wave; f < KST * NB; f += C::NWV) {
-            const int ks = f % KST, row = min(f / KST * 16 + q_lr, R - 1), rt = row / G;
-            const T *src = bits_ptr<const T>(a.q) + (((size_t)b * TT + rt) * a.Hq + (size_t)c * G + (row - rt * G)) * D +
-                           16 * q_lg + 64 * (ks >> 1) + 8 * (ks & 1);
-            u32x4_v *dst = reinterpret_cast<u32x4_v *>(smem + C::OFF_Q) + f * NQ * 64 + q_lane;
-            if constexpr (!C::F32) {
-                *dst = *reinterpret_cast<const u32x4_v *>(src);
-            } else {
-                float x[8];
-                *reinterpret_cast<f32x4_v *>(x) = *reinterpret_cast<const f32x4_v *>(src);
-                *reinterpret_cast<f32x4_v *>(x + 4) = *reinterpret_cast<const f32x4_v *>(src + 4);
-                #pragma unroll
-                for (int i = 0; i < NQ; ++i) {
-                    bf16x8_v h;
-                    #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        h[e] = (__bf16)x[e];
-                        x[e] -= (float)h[e];
-                    }
-                    dst[i * 64] = __builtin_bit_cast(u32x4_v, h);
-                }
+    // ---- a segment of the run: slabs t .. t1 - 1 of unit (b, c), keys [key0, key1) ----
+    struct Segment {
+        int b, c, t, t1, nt, len;
+        int64_t key0, key1;
+        const uint8_t *k, *v;
+        const float *s;   // lane < NG: the K scales, else the V scales
+    };
+    auto segment = [&](int b, int c, int t, int left) {
+        Segment x;
+        x.b = b; x.c = c; x.t = t;
+        x.nt = a.slabs(b);
+        x.len = a.len(b);
+        x.t1 = min(x.nt, t + left);
+        x.key0 = (int64_t)t * SLAB;
+        x.key1 = min((int64_t)x.len, (int64_t)x.t1 * SLAB);
+        x.k = bits_ptr<const uint8_t>(a.k) + b * a.seq + c * a.head;
+        x.v = bits_ptr<const uint8_t>(a.v) + b * a.seq + c * a.head;
+        x.s = bits_ptr<const float>(lane < NG ? sc.k : sc.v) + b * sc.seq + c * sc.head;
+        return x;
+    };
+    auto issue = [&](const Segment &g, int64_t key, int stage) {
+        const uint32_t at = lds_k + stage * STAGE;
+        const uint8_t *k0 = g.k + key * D, *v0 = g.v + key * D;
+        const int last = (int)min(g.key1 - key, (int64_t)C::KPC) - 1;   // the chunk's last key
+        const int in_block = (int)(key & ((1 << sc.shift) - 1));
+        if (lane < 2 * NG)   // (the block of a key past the last: the last one's)
+            lds_stream4(g.s + (key >> sc.shift) + ((in_block + min((lane & (NG - 1)) * 8, last)) >> sc.shift), lds_s + stage * 64);
+        if (last == C::KPC - 1) {
+            const Offsets x = C::LATE_V ? offsets(here(lane)) : kept;   // (no registers to keep them in)
+            lds_stream16_x2<true>(k0, x.k[0], x.k[1], at);
+            lds_stream16_x2<true>(k0, x.k[2], x.k[3], at + 2048);
+            lds_stream16_x2<true>(v0, x.v[0], x.v[1], at + 4096);
+            lds_stream16_x2<true>(v0, x.v[2], x.v[3], at + 6144);
+        } else {
+            const int ln = here(lane);
+            #pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int cidx = 64 * j + ln, kr = cidx / C::CPR, slot = cidx % C::CPR;
+                const int row = min(kr, last);   // rows past the last: the last one again, hidden
+                lds_stream16_nt(k0 + row * D + (slot ^ k8_swz<D>(kr)) * 16, ring + stage * STAGE + j * 1024);
+                lds_stream16_nt(v0 + row * D + (slot ^ v8_swz<D>(kr)) * 16, ring + stage * STAGE + 4096 + j * 1024);
             }
         }
+    };
+    // ---- a unit's queries: fragment (nb, ks) holds feature 16 lg + 64 (ks / 2) + 8 (ks % 2) + e of row 16 nb + lr;
+    // rows past R repeat the last.  Wave w loads fragments w, w + 8, .. into LDS, 1 KB each as they are used (bf16);
+    // fp32 ones as 2 KB that split_q turns into their three bf16 terms, each what the ones before leave. ----
+    auto fetch_q = [&](const Segment &g) {
+        const int ln = here(lane), q_lr = ln & 15, q_lg = ln >> 4;
+        for (int f = wave; f < KST * NB; f += C::NWV) {
+            const int ks = f % KST, row = min(f / KST * 16 + q_lr, R - 1), rt = row / G;
+            const T *src = bits_ptr<const T>(a.q) + (((size_t)g.b * TT + rt) * a.Hq + (size_t)g.c * G + (row - rt * G)) * D +
+                           16 * q_lg + 64 * (ks >> 1) + 8 * (ks & 1);
+            unsigned char *dst = smem + C::OFF_Q + f * NQ * 1024;
+            lds_stream16(src, dst);
+            if constexpr (C::F32) lds_stream16(src + 4, dst + 1024);
+        }
+    };
+    auto split_q = [&]() {   // (a lane reads its own 32 bytes and writes over them)
+        for (int f = wave; f < KST * NB; f += C::NWV) {
+            u32x4_v *p = reinterpret_cast<u32x4_v *>(smem + C::OFF_Q + f * NQ * 1024) + here(lane);
+            f32x4_v x[2] = {__builtin_bit_cast(f32x4_v, p[0]), __builtin_bit_cast(f32x4_v, p[64])};
+            #pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+                bf16x8_v h;
+                #pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    h[e] = (__bf16)x[e >> 2][e & 3];
+                    x[e >> 2][e & 3] -= (float)h[e];
+                }
+                p[n * 64] = __builtin_bit_cast(u32x4_v, h);
+            }
+        }
+    };
+    auto q_frag = [&](int nb, int ks, int i) {
+        return *reinterpret_cast<const bf16x8_v *>(smem + C::OFF_Q + (((nb * KST + ks) * NQ + i) * 64 + lane) * 16);
+    };
+
+    constexpr int STEP = C::NWV * C::KPC;
+    Segment g = segment(b, c, t, left);
+    int64_t key = g.key0 + wave * C::KPC;   // this wave's next chunk
+    fetch_q(g);
+    if (key < g.key1) issue(g, key, 0);
+    // the wave's oldest chunk and queries have landed, the next chunk's loads (LOADS of them) may be on their way
+    auto landed = [&]() {
+        static_assert(C::LOADS == 9, "");
+        if (C::NST == 2 && key + STEP < g.key1) asm volatile("s_waitcnt vmcnt(9)" : : : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+    };
+    for (bool first = true;; first = false) {
+        const int u = g.b * Hkv + g.c;
+        if (C::NST == 2 && key + STEP < g.key1) issue(g, key + STEP, 1);
+        landed();
+        if constexpr (C::F32) split_q();
         __syncthreads();
-        auto q_frag = [&](int nb, int ks, int i) {
-            return *reinterpret_cast<const bf16x8_v *>(smem + C::OFF_Q + (((nb * KST + ks) * NQ + i) * 64 + lane) * 16);
-        };
         bf16x8_v qf[C::QREG ? NB : 1][KST][NQ];
         if constexpr (C::QREG) {
             #pragma unroll
@@ -279,16 +309,15 @@ __global__ __launch_bounds__(512, 1) void stream8_kernel(const Stream8Args args)
         for (int nb = 0; nb < NB; ++nb) {
             m_run[nb] = -INFINITY;
             l_run[nb] = 0.f;
-            lim[nb] = len - TT + min(16 * nb + lr, R - 1) / G;
+            lim[nb] = g.len - TT + min(16 * nb + lr, R - 1) / G;
             #pragma unroll
             for (int db = 0; db < DB; ++db) o[nb][db] = f32x4_v{0.f, 0.f, 0.f, 0.f};
         }
-        const int open_to = len - TT;   // keys up to here are seen by every row
+        const int open_to = g.len - TT;   // keys up to here are seen by every row
 
-        for (int stage = 0; key < key1; key += STEP, stage ^= C::NST - 1) {
-            if (C::NST == 2 && key + STEP < key1) asm volatile("s_waitcnt vmcnt(9)" : : : "memory");   // LOADS: the next chunk's
-            else asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
-            const unsigned char *st = ring + stage * C::CHUNK;
+        for (int stage = 0; key < g.key1; key += STEP, stage ^= C::NST - 1) {
+            landed();
+            const unsigned char *st = ring + stage * STAGE;
             const float *ss = ring_s + stage * 16;
             #pragma unroll
             for (int kh = 0; kh < C::KPC / 32; ++kh) {
@@ -303,15 +332,20 @@ __global__ __launch_bounds__(512, 1) void stream8_kernel(const Stream8Args args)
                     for (int j = 0; j < KST / 2; ++j)
                         kc[blk][j] = *reinterpret_cast<const u32x4_v *>(st + kr * C::RB + (((4 * j + lg) ^ k8_swz<D>(kr)) << 4));
                 }
+                bf16x8_v qc[NB];
+                if constexpr (!C::QREG) {
+                    #pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) qc[nb] = q_frag(nb, 0, 0);
+                }
                 const float ksc = ss[4 * kh + lg], vsc = ss[NG + 4 * kh + lg];
                 auto read_v = [&]() {
-                    const int vr = 32 * kh + 8 * lg + (lr >> 1);
+                    const int ln = here(lane), vr = 32 * kh + 8 * (ln >> 4) + ((ln & 15) >> 1);
                     #pragma unroll
                     for (int db = 0; db < DB; ++db)   // features db*16 + lr, keys 32 kh + 8 lg .. +7
-                        vc[db] = lds_read_tr8(st + 4096 + vr * C::RB + ((db ^ v8_swz<D>(vr)) << 4) + 8 * (lr & 1));
+                        vc[db] = lds_read_tr8(st + 4096 + vr * C::RB + ((db ^ v8_swz<D>(vr)) << 4) + 8 * (ln & 1));
                     if (kh == C::KPC / 32 - 1) {
                         asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");   // the stage is read
-                        if (key + C::NST * STEP < key1) issue(key + C::NST * STEP, stage);
+                        if (key + C::NST * STEP < g.key1) issue(g, key + C::NST * STEP, stage);
                     }
                 };
                 if constexpr (!C::LATE_V) read_v();
@@ -319,23 +353,36 @@ __global__ __launch_bounds__(512, 1) void stream8_kernel(const Stream8Args args)
                 // (The scheduling fences keep one row block's, one fragment's temporaries from living beside the next's:
                 // without them the kernel spills from 32 rows on.)
                 f32x4_v sacc[NB][2];
+                bf16x8_v kf[2];
                 #pragma unroll
-                for (int blk = 0; blk < 2; ++blk)
-                    #pragma unroll
-                    for (int ks = 0; ks < KST; ++ks) {
-                        if (ks % 2 == 0) __builtin_amdgcn_sched_barrier(0);
-                        const bf16x8_v kf = codes_bf16(kc[blk][ks >> 1][2 * (ks & 1)], kc[blk][ks >> 1][2 * (ks & 1) + 1]);
-                        #pragma unroll
-                        for (int nb = 0; nb < NB; ++nb)
+                for (int n = 0; n < KST * NQ; ++n) {   // step ks = n / NQ, query term n % NQ
+                    const int ks = n / NQ;
+                    bf16x8_v qn[NB];   // the next term's, on their way from LDS
+                    if constexpr (!C::QREG) {
+                        if (n + 1 < KST * NQ) {
                             #pragma unroll
-                            for (int i = 0; i < NQ; ++i) {
-                                bf16x8_v q;
-                                if constexpr (C::QREG) q = qf[nb][ks][i];
-                                else q = q_frag(nb, ks, i);
-                                sacc[nb][blk] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q, ks == 0 && i == 0 ? f32x4_v{0.f, 0.f, 0.f, 0.f} : sacc[nb][blk], 0, 0, 0);
-                            }
+                            for (int nb = 0; nb < NB; ++nb) qn[nb] = q_frag(nb, (n + 1) / NQ, (n + 1) % NQ);
+                        }
                     }
-
+                    if (n % NQ == 0) {
+                        #pragma unroll
+                        for (int blk = 0; blk < 2; ++blk)
+                            kf[blk] = codes_bf16(kc[blk][ks >> 1][2 * (ks & 1)], kc[blk][ks >> 1][2 * (ks & 1) + 1]);
+                    }
+                    #pragma unroll
+                    for (int nb = 0; nb < NB; ++nb)
+                        #pragma unroll
+                        for (int blk = 0; blk < 2; ++blk) {
+                            const f32x4_v acc = n == 0 ? f32x4_v{0.f, 0.f, 0.f, 0.f} : sacc[nb][blk];
+                            if constexpr (C::QREG) sacc[nb][blk] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[blk], qf[nb][ks][n % NQ], acc, 0, 0, 0);
+                            else sacc[nb][blk] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[blk], qc[nb], acc, 0, 0, 0);
+                        }
+                    if constexpr (!C::QREG) {
+                        #pragma unroll
+                        for (int nb = 0; nb < NB; ++nb) qc[nb] = qn[nb];
+                    }
+                    if (n % 2 == 1 || !C::QREG) __builtin_amdgcn_sched_barrier(0);
+                }
                 __builtin_amdgcn_sched_barrier(0);
                 const float vm = max_over_row_lanes(vsc);
                 if (vm > vref) {   // the same in every lane
@@ -427,71 +474,90 @@ __global__ __launch_bounds__(512, 1) void stream8_kernel(const Stream8Args args)
             }
         }
 
-        // ---- the segment's end: the waves' results are exchanged through the stages (16-byte pieces swizzled by
-        // row) and every thread merges whole pieces, the unit's result or its part of it for the merge ----
-        left -= t1 - t;
-        const bool from0 = t == 0, whole = from0 && t1 == nt;   // every slab of the unit ran here
+        // ---- the segment's end.  The next one's first chunks (into stage 0, which this wave has read) and queries
+        // are on their way while the waves' results are added up ----
+        left -= g.t1 - g.t;
+        const bool whole = g.t == 0 && g.t1 == g.nt;   // every slab of the unit ran here
         if (!whole) {
             if (first) pu0 = u;   // the run's first unit; another one that does not end here is its last
             else pu1 = u;
         }
-        constexpr int DP = D / C::XPASS, QP = DP / 4;                 // features, pieces of a row per pass
-        constexpr int SW = QP < 16 ? QP - 1 : 15;
+        const bool more = left > 0;
+        if (more) {
+            const bool wrap = g.c + 1 == Hkv;
+            g = segment(wrap ? g.b + 1 : g.b, wrap ? 0 : g.c + 1, 0, left);
+            key = g.key0 + wave * C::KPC;
+            if (C::NST == 2 && key < g.key1) issue(g, key, 0);
+        }
+        // each wave's (max, sum of p) per row, in log2 units (the sum is of p' = 2^11 p), and from all of them its factor
+        const int x_lane = here(lane), x_lr = x_lane & 15, x_lg = x_lane >> 4;
         float2 *xml = reinterpret_cast<float2 *>(smem + C::OFF_ML);   // [8][RP]
-        const int x_lane = here(lane), x_lg = x_lane >> 4, x_tid = here(tid);
         #pragma unroll
-        for (int ps = 0; ps < C::XPASS; ++ps) {
-            __syncthreads();   // every wave is done with the stages, or with the pass before
+        for (int nb = 0; nb < NB; ++nb) {
+            const float lt = sum_over_row_lanes(l_run[nb]);
+            if (x_lg == 0) xml[wave * C::RP + 16 * nb + x_lr] = make_float2(m_run[nb] - kPShift, lt);
+        }
+        __syncthreads();   // (also: every wave is done with its stages and the queries)
+        if (more) fetch_q(g);
+        float M[NB], L[NB];
+        #pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            float2 ml[C::NWV];
+            M[nb] = -INFINITY;
+            L[nb] = 0.f;
             #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {
-                const int row = 16 * nb + (x_lane & 15);
-                #pragma unroll
-                for (int db = 0; db < DP / 16; ++db)
-                    *reinterpret_cast<f32x4_v *>(smem + ((wave * C::RP + row) * QP + ((db * 4 + x_lg) ^ (row & SW))) * 16) =
-                        o[nb][ps * (DP / 16) + db] * vref;
-                // (max, sum of p) in log2 units: the sum is of p' = 2^11 p
-                if (ps == 0) {
-                    const float lt = sum_over_row_lanes(l_run[nb]);
-                    if (x_lg == 0) xml[wave * C::RP + row] = make_float2(m_run[nb] - kPShift, lt);
-                }
+            for (int k = 0; k < C::NWV; ++k) {
+                ml[k] = xml[k * C::RP + 16 * nb + x_lr];
+                M[nb] = fmaxf(M[nb], ml[k].x);
             }
+            const float mr = M[nb] == -INFINITY ? 0.f : M[nb];
+            #pragma unroll
+            for (int k = 0; k < C::NWV; ++k) L[nb] = fmaf(__builtin_amdgcn_exp2f(ml[k].x - mr), ml[k].y, L[nb]);
+            const float wt = __builtin_amdgcn_exp2f(m_run[nb] - kPShift - mr) * vref;
+            #pragma unroll
+            for (int db = 0; db < DB; ++db) o[nb][db] *= wt;
+        }
+        // the sums, XD feature blocks at a time: every wave's fragments to LDS as they are (1 KB each), wave w adds up
+        // the w-th of them
+        f32x4_v *xo = reinterpret_cast<f32x4_v *>(smem + C::OFF_X) + x_lane;
+        #pragma unroll
+        for (int d0 = 0; d0 < DB; d0 += C::XD) {
+            if (d0 > 0) __syncthreads();
+            #pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+                #pragma unroll
+                for (int db = 0; db < C::XD; ++db) xo[((nb * C::XD + db) * C::NWV + wave) * 64] = o[nb][d0 + db];
             __syncthreads();
-            for (int x = x_tid; x < R * QP; x += 512) {
-                const int r = x / QP, ch = x % QP;
-                float m[C::NWV], M = -INFINITY, L = 0.f;
-                f32x4_v y = f32x4_v{0.f, 0.f, 0.f, 0.f};
+            if (wave < NB * C::XD) {
+                const int nb = wave / C::XD, db = d0 + wave % C::XD, r = 16 * nb + x_lr;
+                f32x4_v y = xo[wave * C::NWV * 64];
                 #pragma unroll
-                for (int k = 0; k < C::NWV; ++k) {
-                    m[k] = xml[k * C::RP + r].x;
-                    M = fmaxf(M, m[k]);
-                }
+                for (int k = 1; k < C::NWV; ++k) y += xo[(wave * C::NWV + k) * 64];
+                float mr = M[0], lr_ = L[0];
                 #pragma unroll
-                for (int k = 0; k < C::NWV; ++k) {
-                    const float wt = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[k] - M);
-                    const f32x4_v v = *reinterpret_cast<const f32x4_v *>(smem + ((k * C::RP + r) * QP + (ch ^ (r & SW))) * 16);
-                    L = fmaf(wt, xml[k * C::RP + r].y, L);
-                    #pragma unroll
-                    for (int e = 0; e < 4; ++e) y[e] = fmaf(wt, v[e], y[e]);
+                for (int n = 1; n < NB; ++n) {
+                    mr = nb == n ? M[n] : mr;
+                    lr_ = nb == n ? L[n] : lr_;
                 }
-                if (whole) {
-                    const size_t head = out_head(a, u, r);
-                    const float inv = L == 0.f ? 0.f : 1.f / L;
-                    store_quad(bits_ptr<T>(a.out) + head * D + ps * DP + ch * 4, y * inv);
-                    if (lse && ps == 0 && ch == 0) lse[head] = L == 0.f ? -INFINITY : (M + log2f(L)) * kLn2;
-                } else {
-                    // runs and units both advance in slab order, so piece + u numbers the pieces one after the other
-                    float *pp = bits_ptr<float>(a.part) + (size_t)(piece + u) * piece_floats(R, D);
-                    store_agent4(pp + r * D + ps * DP + ch * 4, y);
-                    if (ps == 0 && ch == 0) store_agent2(pp + R * D + 2 * r, M, L);
+                const int f = db * 16 + 4 * x_lg;   // this lane's four features
+                if (r < R) {
+                    if (whole) {
+                        const size_t head = out_head(a, u, r);
+                        const float inv = lr_ == 0.f ? 0.f : 1.f / lr_;
+                        store_quad(bits_ptr<T>(a.out) + head * D + f, y * inv);
+                        if (lse && f == 0) lse[head] = lr_ == 0.f ? -INFINITY : (mr + log2f(lr_)) * kLn2;
+                    } else {
+                        // runs and units both advance in slab order, so piece + u numbers the pieces one after the other
+                        float *pp = bits_ptr<float>(a.part) + (size_t)(piece + u) * piece_floats(R, D);
+                        store_agent4(pp + r * D + f, y);
+                        if (f == 0) store_agent2(pp + R * D + 2 * r, mr, lr_);
+                    }
                 }
             }
         }
-        t = 0;
-        if (++c == Hkv) {
-            c = 0;
-            ++b;
-        }
-        __syncthreads();   // the stages are free
+        if (!more) break;
+        __syncthreads();   // the exchange area is stage NST - 1
+        if (C::NST == 1 && key < g.key1) issue(g, key, 0);
     }
     if ((pu0 < 0 && pu1 < 0) || a.merge2) return;
 
