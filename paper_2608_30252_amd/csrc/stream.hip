@@ -608,7 +608,8 @@ void plan_stream(StreamArgs &a, int B, int Hkv, int d, const int *n_keys) {
     int np_max = 1;
     const int even = a.base + (a.rem > 0 ? 1 : 0);
     a.by_unit = 0;
-    for (int share = whole ? nt_max : even; whole || share <= even + 2 + even / 16; share += 1 + even / 64) {
+    const int slack = a.kind == kStream8 ? 12 + even / 8 : 2 + even / 16;
+    for (int share = whole ? nt_max : even; whole || share <= even + slack; share += 1 + even / 64) {
         int wgs = 0;
         np_max = 1;
         for (int b = 0; b < B; ++b) {

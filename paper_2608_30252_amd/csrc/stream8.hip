@@ -400,18 +400,19 @@ __global__ __launch_bounds__(512, 1) void stream8_kernel(const Stream8Args args)
                 u32x4_v pk[NB], pl[C::F32 ? NB : 1];
                 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
-                    float x[8], mt = -INFINITY;
-                    #pragma unroll
-                    for (int j = 0; j < 8; ++j) x[j] = sacc[nb][j >> 2][j & 3] * csk;
+                    // the lane's largest score (hidden ones -inf from here on)
                     if (!open) {
                         const int seen = lim[nb] - (int)key - kg0;   // (from -63 on: a key of the unit is in the chunk)
                         #pragma unroll
-                        for (int j = 0; j < 8; ++j) x[j] = j <= seen ? x[j] : -INFINITY;
+                        for (int j = 0; j < 8; ++j) sacc[nb][j >> 2][j & 3] = j <= seen ? sacc[nb][j >> 2][j & 3] : -INFINITY;
                     }
+                    float mt = sacc[nb][0][0];
                     #pragma unroll
-                    for (int j = 0; j < 8; ++j) mt = fmaxf(mt, x[j]);
-                    mt = max_over_row_lanes(mt);
-                    if (!__all(mt <= m_run[nb] + kLazy)) {
+                    for (int j = 1; j < 8; ++j) mt = fmaxf(mt, sacc[nb][j >> 2][j & 3]);
+                    mt = mt == -INFINITY ? mt : mt * csk;   // (csk may be 0)
+                    if (__any(mt > m_run[nb] + kLazy)) {
+                        // the four lanes of a row agree on its maximum; rows that stay have alpha 1
+                        mt = max_over_row_lanes(mt);
                         const float mn = mt > m_run[nb] + kLazy ? mt : m_run[nb];
                         const float alpha = mn == m_run[nb] ? 1.f : __builtin_amdgcn_exp2f(m_run[nb] - mn);
                         m_run[nb] = mn;
@@ -419,11 +420,18 @@ __global__ __launch_bounds__(512, 1) void stream8_kernel(const Stream8Args args)
                         #pragma unroll
                         for (int db = 0; db < DB; ++db) o[nb][db] *= alpha;
                     }
-                    const float ms = m_run[nb] == -INFINITY ? 0.f : m_run[nb] - kPShift;
+                    const float ms = m_run[nb] == -INFINITY ? -kPShift : m_run[nb] - kPShift;
+                    float x[8];
+                    #pragma unroll
+                    for (int j = 0; j < 8; ++j) x[j] = fmaf(sacc[nb][j >> 2][j & 3], csk, -ms);
+                    if (!open) {   // (-inf * 0 is NaN)
+                        #pragma unroll
+                        for (int j = 0; j < 8; ++j) x[j] = sacc[nb][j >> 2][j & 3] == -INFINITY ? -INFINITY : x[j];
+                    }
                     float ps = 0.f;
                     #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        float p0 = __builtin_amdgcn_exp2f(x[2 * e] - ms), p1 = __builtin_amdgcn_exp2f(x[2 * e + 1] - ms);
+                        float p0 = __builtin_amdgcn_exp2f(x[2 * e]), p1 = __builtin_amdgcn_exp2f(x[2 * e + 1]);
                         ps += p0 + p1;
                         p0 *= rv;
                         p1 *= rv;
