@@ -64,6 +64,7 @@ extern "C" {
 #define MAD_OP_ACCEPT 3
 #define MAD_OP_ACCEPT_STOCH 4
 #define MAD_OP_DECODE_LEAST 5
+#define MAD_OP_SAMPLE 6
 
 /*
  * A per-sequence, per-KV-head run of key/value rows in device memory.
@@ -339,6 +340,39 @@ int mad_accept_stochastic(const float *p, const float *q, const int32_t *draft_t
                           int V, int32_t *n_accept, int32_t *next_tok, void *ws, size_t ws_bytes, void *stream);
 
 /*
+ * Sampling from logits, with uniforms supplied by the caller: tokens and the
+ * distributions they are drawn from, for the draft's own tokens (its q) and the
+ * target's p that mad_accept_stochastic reads.  For each row (b, t) with logits
+ * x, settings of sequence b:
+ *   order   entries by value, ties by the lower index first
+ *   w_v     = exp((x_v - max x) / temperature[b]), in double precision
+ *   top-k   the first top_k of the order stay (0, or V and above: all)
+ *   top-p   of these, the ones before which less than top_p of their mass lies
+ *           (1: all)
+ *   min-p   of these, the ones with w_v >= min_p, i.e. at least min_p times the
+ *           most probable entry's probability (0: all)
+ *   probs_v = w_v / (mass of what stays), 0 for the rest (rounded to fp32 once)
+ *   tok     = the smallest v, in index order, whose running mass exceeds u times
+ *           the whole (the last that stays where rounding leaves none)
+ * temperature 0 is greedy: the whole mass on the row's largest entry (the lower
+ * index of equal ones), the filters have no effect.  -inf is an entry of
+ * weight 0; +inf takes the whole mass (shared by equal ones).  A row with a NaN,
+ * or with nothing but -inf, has no distribution: tok = -1 (no token: the accept
+ * rules reject it), probs all 0.
+ *   logits  device [B][T][V], dtype F32 or BF16
+ *   u       device float32 [B][T] uniforms in [0, 1); NULL if tok is
+ *   temperature, top_k, top_p, min_p   HOST arrays [B] (double, top_k int32);
+ *           NULL: 1, 0, 1 and 0
+ *   tok     device int32 [B][T] or NULL;  probs  device float32 [B][T][V] or NULL (not both)
+ * temperature >= 0 and finite, top_k >= 0, 0 < top_p <= 1, 0 <= min_p <= 1;
+ * T <= 64, V <= 2^20.  probs must not overlap logits.  Rows may start at any address that suits their
+ * type.  Workspace MAD_OP_SAMPLE.
+ */
+int mad_sample(const void *logits, int dtype, const float *u, const double *temperature, const int32_t *top_k,
+               const double *top_p, const double *min_p, int B, int T, int V, int32_t *tok, float *probs, void *ws,
+               size_t ws_bytes, void *stream);
+
+/*
  * Memory-prefill attention (Sec. 3.3, prefill; the appendix on memory
  * prefill): the draft's single masked pass over a prefix, which builds its
  * initial compact memory.  The mask applies the write policy of decoding, so
@@ -450,6 +484,7 @@ int mad_probe_handoff_latency(void *buf, size_t buf_bytes, unsigned long long *c
  *   ACCEPT: B, T, max_keys = V                  (Hq, Hkv, d ignored)
  *   ACCEPT_STOCH: B, max_keys = V               (Hq, Hkv, d, T ignored)
  *   DECODE_LEAST: B, Hq, Hkv, d
+ *   SAMPLE: B, T, max_keys = V                  (Hq, Hkv, d ignored)
  * A decode call is accepted from DECODE_LEAST on, what its split partials take
  * (at most 68 KB for each of the B * Hkv units).  With less than DECODE a call
  * may run another kernel: the same sums in another order.

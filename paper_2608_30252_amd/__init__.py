@@ -17,6 +17,7 @@ Entry points (same names as the C ABI, without the ``mad_`` prefix):
                         (verify_attn_vt: the same over a transposed V cache)
     kv8_append          new K/V rows into an 8-bit cache (e4m3, a scale per block of tokens and KV head)
     verify_attn_kv8     verify attention over an 8-bit cache
+    sample              temperature, top-k, top-p and min-p: tokens and their distributions
     accept_greedy       greedy accept/reject
 """
 import ctypes
@@ -33,10 +34,12 @@ LIB_PATH = os.path.join(_HERE, "libmad.so")
 MAD_OK, MAD_EINVAL, MAD_ENOTSUP, MAD_EHIP, MAD_EWS = 0, -1, -2, -3, -4
 MAD_F32, MAD_BF16 = 0, 1
 MAD_OP_DECODE, MAD_OP_UPDATE, MAD_OP_VERIFY, MAD_OP_ACCEPT, MAD_OP_ACCEPT_STOCH, MAD_OP_DECODE_LEAST = 0, 1, 2, 3, 4, 5
+MAD_OP_SAMPLE = 6
 MAX_BATCH = 64
 
 _i32p = ctypes.POINTER(ctypes.c_int32)
 _u8p = ctypes.POINTER(ctypes.c_uint8)
+_f64p = ctypes.POINTER(ctypes.c_double)
 
 
 class _KVView(ctypes.Structure):
@@ -73,6 +76,7 @@ def _load_library():
     kv8p = ctypes.POINTER(_KV8View)
     lib.mad_kv8_append.argtypes = [vp, vp, _i32p, i, i, i, i, i, kv8p, vp]
     lib.mad_verify_attn_kv8.argtypes = [vp, i, i, i, i, i, i, f, kv8p, vp, vp, vp, sz, vp]
+    lib.mad_sample.argtypes = [vp, i, vp, _f64p, _i32p, _f64p, _f64p, i, i, i, vp, vp, vp, sz, vp]
     lib.mad_accept_greedy.argtypes = [vp, i, vp, i, i, i, vp, vp, vp, sz, vp]
     lib.mad_accept_stochastic.argtypes = [vp, vp, vp, vp, i, i, i, vp, vp, vp, sz, vp]
     lib.mad_draft_step_attn.argtypes = [vp, i, i, i, i, i, f, kvp, kvp, vp, vp, _u8p, vp, vp, vp, sz, vp]
@@ -91,7 +95,7 @@ def _load_library():
     lib.mad_last_error.restype = ctypes.c_char_p
     lib.mad_version.restype = ctypes.c_char_p
     for fn in ("mad_draft_decode_attn", "mad_memory_update", "mad_verify_attn", "mad_verify_attn_vt", "mad_accept_greedy",
-               "mad_kv8_append", "mad_verify_attn_kv8",
+               "mad_kv8_append", "mad_verify_attn_kv8", "mad_sample",
                "mad_accept_stochastic", "mad_draft_step_attn", "mad_draft_decode_attn_noalloc",
                "mad_memory_prefill_attn",
                "mad_rmsnorm_qkv_rope", "mad_linear_residual", "mad_rmsnorm_swiglu", "mad_probe_stream_read",
@@ -105,7 +109,7 @@ _FAST = None
 _FAST_ENTRIES = ("mad_draft_decode_attn", "mad_draft_step_attn", "mad_memory_update", "mad_verify_attn",
                  "mad_verify_attn_vt", "mad_accept_greedy", "mad_accept_stochastic", "mad_rmsnorm_qkv_rope",
                  "mad_linear_residual", "mad_rmsnorm_swiglu", "mad_workspace_bytes", "mad_kv8_append",
-                 "mad_verify_attn_kv8")
+                 "mad_verify_attn_kv8", "mad_sample")
 
 
 class _CtypesOnly:
@@ -556,6 +560,48 @@ def verify_attn_kv8(q: torch.Tensor, kv: KV8, out=None, lse=None, scale: Optiona
                                              _ptr(out), _ptr(lse), _ptr(w), w.numel(), _stream(q.device))
     _check(rc)
     return out, lse
+
+
+def _host_f64(vals, n) -> ctypes.Array:
+    return (ctypes.c_double * n)(*[float(x) for x in vals])
+
+
+def sample(logits: torch.Tensor, u: Optional[torch.Tensor] = None, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
+           tok: Optional[torch.Tensor] = None, probs: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+    """logits [B, T, V] (fp32 or bf16) -> (tok int32 [B, T], probs float32 [B, T, V]).
+
+    Temperature (0: greedy), then top-k (0: off), top-p (1: off) and min-p (0: off), each a number or one per
+    sequence; tok is drawn with the uniforms u float32 [B, T] (without u there are none, and probs is made), probs is
+    the distribution drawn from, written where a tensor is given.  A row without a distribution (a NaN, nothing but
+    -inf) has tok -1 and probs 0."""
+    if (tok is not None or u is None) and (tok is not None or probs is not None):
+        rc = (_FAST or _fast()).sample(logits, u, temperature, top_k, top_p, min_p, tok, probs, ws)
+        if rc is not None:
+            _check(rc)
+            return tok, probs
+    _need(logits.dim() == 3, "logits must be [B, T, V]")
+    B, T, V = logits.shape
+    dev = logits.device
+    _need(u is not None or tok is None, "tok needs the uniforms u")
+    if u is not None and tok is None:
+        tok = torch.empty((B, T), dtype=torch.int32, device=dev)
+    if u is None and probs is None:
+        probs = torch.empty((B, T, V), dtype=torch.float32, device=dev)
+    _need(u is None or (u.shape == (B, T) and u.dtype == torch.float32), "u must be float32 [B, T]")
+    _need(tok is None or (tok.shape == (B, T) and tok.dtype == torch.int32), "tok must be int32 [B, T]")
+    _need(probs is None or (probs.shape == (B, T, V) and probs.dtype == torch.float32), "probs must be float32 [B, T, V]")
+    settings = []
+    for name, v in (("temperature", temperature), ("top_k", top_k), ("top_p", top_p), ("min_p", min_p)):
+        v = [v] * B if not hasattr(v, "__len__") else v
+        _need(len(v) == B, f"{name} needs one entry per sequence")
+        settings.append((_host_i32 if name == "top_k" else _host_f64)(v, B))
+    _contiguous(logits=logits, u=u, tok=tok, probs=probs)
+    _same_device(dev, u=u, tok=tok, probs=probs)
+    dt = _dtype_code(logits)
+    w = _ws_for(dev, workspace_bytes(MAD_OP_SAMPLE, B, 1, 1, 64, T, V), ws)
+    _check(_load_library().mad_sample(_ptr(logits), dt, _ptr(u), *settings, B, T, V, _ptr(tok), _ptr(probs), _ptr(w),
+                                      w.numel(), _stream(dev)))
+    return tok, probs
 
 
 def accept_greedy(logits: torch.Tensor, draft_tok: Optional[torch.Tensor], n_accept=None, next_tok=None,

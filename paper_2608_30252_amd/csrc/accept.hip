@@ -32,58 +32,7 @@
 
 namespace mad {
 
-__device__ __forceinline__ uint64_t argmax_key(float x, int idx) {
-    uint32_t u = __float_as_uint(x);
-    uint32_t ord;
-    if ((u & 0x7fffffffu) > 0x7f800000u) ord = 0xffffffffu;      // NaN: above everything
-    else if ((u & 0x7fffffffu) == 0u) ord = 0x80000000u;         // +0 and -0 compare equal
-    else ord = (u & 0x80000000u) ? ~u : (u | 0x80000000u);
-    return ((uint64_t)ord << 32) | (uint64_t)(0xffffffffu - (uint32_t)idx);
-}
-__device__ __forceinline__ int key_index(uint64_t k) { return (int)(0xffffffffu - (uint32_t)k); }
 
-// Cross-lane exchanges of 64-bit values (two 32-bit halves) on the vector ALU,
-// without an LDS round trip: DPP within rows of 16 lanes, then the gfx950
-// lane swaps between rows.  dpp_u64<CTRL, ROWS>: the DPP move CTRL into the
-// rows of ROWS; lanes without a source, and rows outside ROWS, read 0.
-template <int CTRL, int ROWS = 0xF>
-__device__ __forceinline__ uint64_t dpp_u64(uint64_t v) {
-    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)v, CTRL, ROWS, 0xF, false);
-    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(v >> 32), CTRL, ROWS, 0xF, false);
-    return ((uint64_t)hi << 32) | lo;
-}
-// the values of lanes l & ~W and l | W (W = 16 or 32), in that order
-template <int W>
-__device__ __forceinline__ void lane_pair_u64(uint64_t v, uint64_t &a, uint64_t &b) {
-    const uint32_t lo = (uint32_t)v, hi = (uint32_t)(v >> 32);
-    if constexpr (W == 16) {
-        const auto l = __builtin_amdgcn_permlane16_swap(lo, lo, false, false);
-        const auto h = __builtin_amdgcn_permlane16_swap(hi, hi, false, false);
-        a = ((uint64_t)h[0] << 32) | l[0];
-        b = ((uint64_t)h[1] << 32) | l[1];
-    } else {
-        const auto l = __builtin_amdgcn_permlane32_swap(lo, lo, false, false);
-        const auto h = __builtin_amdgcn_permlane32_swap(hi, hi, false, false);
-        a = ((uint64_t)h[0] << 32) | l[0];
-        b = ((uint64_t)h[1] << 32) | l[1];
-    }
-}
-// f folded over the 64 lanes, the same value in every lane: pairs within a
-// quad, then the two quads of 8 lanes (half mirror), the two 8s of a row
-// (mirror), the two 16s of 32 lanes, the two 32s.  Every lane combines the same
-// operands in the same order, so a floating-point sum is bitwise uniform.
-template <typename F>
-__device__ __forceinline__ uint64_t wave_fold_u64(uint64_t v, F f) {
-    v = f(v, dpp_u64<0xB1>(v));    // quad_perm [1, 0, 3, 2]
-    v = f(v, dpp_u64<0x4E>(v));    // quad_perm [2, 3, 0, 1]
-    v = f(v, dpp_u64<0x141>(v));   // row_half_mirror
-    v = f(v, dpp_u64<0x140>(v));   // row_mirror
-    uint64_t a, b;
-    lane_pair_u64<16>(v, a, b);
-    v = f(a, b);
-    lane_pair_u64<32>(v, a, b);
-    return f(a, b);
-}
 __device__ __forceinline__ uint64_t wave_max_u64(uint64_t v) {
     return wave_fold_u64(v, [](uint64_t x, uint64_t y) { return x > y ? x : y; });
 }
@@ -246,31 +195,6 @@ size_t accept_ws_bytes(int B, int T, int V) {
 
 // ---------------------------------------------------------- stochastic ----
 
-__device__ __forceinline__ uint64_t add_f64_bits(uint64_t x, uint64_t y) {
-    return (uint64_t)__double_as_longlong(__longlong_as_double((long long)x) + __longlong_as_double((long long)y));
-}
-// inclusive prefix sum over the 64 lanes of a wave (lane order): shifts by 1,
-// 2, 4, 8 within each row of 16, then row 0's total into row 1 and row 2's
-// into row 3 (row_bcast:15), then rows 0-1's total into rows 2-3 (row_bcast:31)
-__device__ __forceinline__ double wave_scan_f64(double v) {
-    uint64_t u = (uint64_t)__double_as_longlong(v);
-    u = add_f64_bits(u, dpp_u64<0x111>(u));
-    u = add_f64_bits(u, dpp_u64<0x112>(u));
-    u = add_f64_bits(u, dpp_u64<0x114>(u));
-    u = add_f64_bits(u, dpp_u64<0x118>(u));
-    u = add_f64_bits(u, dpp_u64<0x142, 0xA>(u));
-    u = add_f64_bits(u, dpp_u64<0x143, 0xC>(u));
-    return __longlong_as_double((long long)u);
-}
-__device__ __forceinline__ double read_lane_f64(double v, int l) {
-    const uint64_t u = __double_as_longlong(v);
-    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)u, l);
-    const uint32_t hi = __builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), l);
-    return __longlong_as_double((long long)(((uint64_t)hi << 32) | lo));
-}
-__device__ __forceinline__ double wave_sum_f64(double v) {
-    return __longlong_as_double((long long)wave_fold_u64((uint64_t)__double_as_longlong(v), add_f64_bits));
-}
 // weight of entry v in the draw: max(0, p - q) (q given) or max(0, p)
 __device__ __forceinline__ double draw_weight(float p, float q, bool resid) {
     const double r = resid ? (double)p - (double)q : (double)p;

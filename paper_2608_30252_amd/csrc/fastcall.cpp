@@ -37,6 +37,7 @@ struct Entry {
     decltype(&mad_workspace_bytes) ws_bytes;
     decltype(&mad_kv8_append) kv8_append;
     decltype(&mad_verify_attn_kv8) verify8;
+    decltype(&mad_sample) sample;
 } g;
 PyObject *g_kv, *g_kv8, *g_ws, *g_stream;   // classes KV and KV8, the default workspaces' dict, the raw-stream getter
 PyObject *s_k, *s_v, *s_length, *s_start, *s_buf, *s_k_scale, *s_v_scale, *s_block;
@@ -459,6 +460,71 @@ PyObject *greedy(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+// a number for all of n sequences, or a list or tuple of them
+bool plain_reals(PyObject *o) {
+    if (plain_real(o)) return true;
+    const Py_ssize_t n = PyList_CheckExact(o) || PyTuple_CheckExact(o) ? PySequence_Fast_GET_SIZE(o) : 0;
+    return n > 0 && plain_real(PySequence_Fast_GET_ITEM(o, 0)) && plain_real(PySequence_Fast_GET_ITEM(o, n - 1));
+}
+void reals(PyObject *o, int n, double *out) {
+    if (plain_real(o)) {
+        const double v = as_double(o);
+        for (int i = 0; i < n; ++i) out[i] = v;
+        return;
+    }
+    need(PySequence_Fast_GET_SIZE(o) == n);
+    for (int i = 0; i < n; ++i) {
+        PyObject *x = PySequence_Fast_ITEMS(o)[i];
+        need(plain_real(x));
+        out[i] = as_double(x);
+    }
+}
+
+// sample(logits, u | None, temperature, top_k, top_p, min_p, tok | None, probs | None, ws)
+PyObject *sample(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    auto maybe = [&](int i) { return a[i] == Py_None || THPVariable_CheckExact(a[i]); };
+    ORDINARY(9, plain_tensors(a, {0}) && maybe(1) && maybe(6) && maybe(7) && plain_reals(a[2]) &&
+                    (PyLong_CheckExact(a[3]) || plain_ints(a[3])) && plain_reals(a[4]) && plain_reals(a[5]));
+    return guarded([&]() -> int {
+        const at::Tensor &x = first(a[0]);
+        const at::Device dev = x.device();
+        need(x.dim() == 3);
+        const int B = small(x.size(0)), T = small(x.size(1)), V = small(x.size(2));
+        need(B >= 1 && B <= MAD_MAX_BATCH);
+        double t[MAD_MAX_BATCH], p[MAD_MAX_BATCH], mp[MAD_MAX_BATCH];
+        int32_t k[MAD_MAX_BATCH];
+        reals(a[2], B, t);
+        reals(a[4], B, p);
+        reals(a[5], B, mp);
+        if (PyLong_CheckExact(a[3])) {
+            const int v = as_int(a[3]);
+            for (int b = 0; b < B; ++b) k[b] = v;
+        } else {
+            ints(a[3], B, k);
+        }
+        const float *u = nullptr;
+        int32_t *tok = nullptr;
+        float *probs = nullptr;
+        if (a[1] != Py_None) {
+            const at::Tensor &w = dense(a[1], dev);
+            need(shape(w, {B, T}) && w.scalar_type() == at::kFloat);
+            u = (const float *)w.data_ptr();
+        }
+        if (a[6] != Py_None) tok = (int32_t *)i32(a[6], dev, {B, T}).data_ptr();
+        if (a[7] != Py_None) {
+            const at::Tensor &w = dense(a[7], dev);
+            need(shape(w, {B, T, V}) && w.scalar_type() == at::kFloat);
+            probs = (float *)w.data_ptr();
+        }
+        need((tok || probs) && (u || !tok) && (tok || !u));
+        void *st = stream_of(dev);
+        const Scratch ws(a[8], dev, st, g.ws_bytes(MAD_OP_SAMPLE, B, 1, 1, 64, T, V));
+        const int dt = dtype_code(x);
+        void *xp = x.data_ptr();
+        RELEASED(g.sample(xp, dt, u, t, k, p, mp, B, T, V, tok, probs, ws.p, ws.n, st));
+    });
+}
+
 // stoch(p, q, draft, u, n_accept, next_tok, ws)
 PyObject *stoch(PyObject *, PyObject *const *a, Py_ssize_t n) {
     ORDINARY(7, plain_tensors(a, {0, 1, 2, 3, 4, 5}));
@@ -575,7 +641,7 @@ PyObject *bind_kv8(PyObject *, PyObject *kv8) {
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, nullptr}, {"bind_kv8", bind_kv8, METH_O, nullptr}, FAST(attn), FAST(update), FAST(verify), FAST(verify_vt),
                          FAST(greedy), FAST(stoch), FAST(qkv), FAST(linear), FAST(swiglu), FAST(kv8_append),
-                         FAST(verify8), {nullptr, nullptr, 0, nullptr}};
+                         FAST(verify8), FAST(sample), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

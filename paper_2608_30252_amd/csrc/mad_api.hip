@@ -130,6 +130,9 @@ size_t mad_workspace_bytes(int op, int B, int Hq, int Hkv, int d, int T, int max
         case MAD_OP_ACCEPT_STOCH:   // B, max_keys = V
             if (B < 1 || B > MAD_MAX_BATCH || max_keys < 1) return 0;
             return mad::stoch_ws_bytes(B, max_keys);
+        case MAD_OP_SAMPLE:   // B, T, max_keys = V
+            if (B < 1 || B > MAD_MAX_BATCH || T < 1 || T > 64 || max_keys < 1 || max_keys > mad::kSampleMaxV) return 0;
+            return mad::sample_ws_bytes(B, T, max_keys);
         case MAD_OP_ACCEPT:   // B, T, max_keys = V
             if (B < 1 || B > MAD_MAX_BATCH || T < 1 || T > mad::kAcceptMaxT || max_keys < 1) return 0;
             return mad::accept_ws_bytes(B, T, max_keys);
@@ -753,6 +756,54 @@ int mad_accept_greedy(const void *logits, int dtype, const int32_t *draft_tok, i
     const size_t esz = dtype == MAD_BF16 ? 2 : 4;
     a.vec16 = aligned16(logits) && ((size_t)V * esz) % 16 == 0;
     return hip_status(mad::launch_accept(a, dtype, (hipStream_t)stream), "accept launch");
+}
+
+int mad_sample(const void *logits, int dtype, const float *u, const double *temperature, const int32_t *top_k,
+               const double *top_p, const double *min_p, int B, int T, int V, int32_t *tok, float *probs, void *ws,
+               size_t ws_bytes, void *stream) {
+    if (B < 1 || B > MAD_MAX_BATCH) return fail(MAD_EINVAL, "B=%d outside [1, %d]", B, MAD_MAX_BATCH);
+    if (T < 1 || T > 64) return fail(MAD_EINVAL, "T=%d outside [1, 64]", T);
+    if (V < 1 || V > mad::kSampleMaxV) return fail(MAD_EINVAL, "V=%d outside [1, %d]", V, mad::kSampleMaxV);
+    if (dtype != MAD_F32 && dtype != MAD_BF16) return fail(MAD_ENOTSUP, "dtype %d not supported", dtype);
+    if (!logits) return fail(MAD_EINVAL, "null logits");
+    if (!tok && !probs) return fail(MAD_EINVAL, "neither tok nor probs is given");
+    if (tok && !u) return fail(MAD_EINVAL, "u required with tok");
+    const size_t esz = dtype == MAD_BF16 ? 2 : 4, n = (size_t)B * T * V;
+    if (((uintptr_t)logits & (esz - 1)) || ((uintptr_t)u & 3) || ((uintptr_t)tok & 3) || ((uintptr_t)probs & 3))
+        return fail(MAD_EINVAL, "logits, u, tok or probs not aligned to their type");
+    if (probs && (const char *)probs < (const char *)logits + n * esz && (const char *)logits < (const char *)(probs + n))
+        return fail(MAD_EINVAL, "probs overlaps logits");
+    mad::SampleArgs a;
+    memset(&a, 0, sizeof(a));
+    for (int b = 0; b < B; ++b) {
+        const double t = temperature ? temperature[b] : 1.0, p = top_p ? top_p[b] : 1.0, mp = min_p ? min_p[b] : 0.0;
+        const int k = top_k ? top_k[b] : 0;
+        if (!(t >= 0.0) || isinf(t)) return fail(MAD_EINVAL, "temperature[%d]=%g must be finite and >= 0", b, t);
+        if (k < 0) return fail(MAD_EINVAL, "top_k[%d]=%d", b, k);
+        if (!(p > 0.0) || p > 1.0) return fail(MAD_EINVAL, "top_p[%d]=%g outside (0, 1]", b, p);
+        if (!(mp >= 0.0) || mp > 1.0) return fail(MAD_EINVAL, "min_p[%d]=%g outside [0, 1]", b, mp);
+        const bool greedy = t == 0.0;   // the first entry of the order, whatever the filters
+        a.c[b] = 1.4426950408889634 / (greedy ? 1.0 : t);
+        a.top_k[b] = greedy ? 1 : k < V ? k : 0;
+        a.top_p[b] = greedy ? 1.0 : p;
+        a.min_p[b] = greedy ? 0.0 : mp;
+    }
+    const size_t need = mad::sample_ws_bytes(B, T, V);
+    if (!ws) return fail(MAD_EWS, "workspace required (%zu bytes)", need);
+    if (ws_bytes < need) return fail(MAD_EWS, "workspace %zu bytes < %zu", ws_bytes, need);
+    if (((uintptr_t)ws & 255u) != 0) return fail(MAD_EINVAL, "workspace not 256-byte aligned");
+    a.logits = logits;
+    a.u = u;
+    a.tok = tok;
+    a.probs = probs;
+    a.counters = (unsigned *)ws;
+    a.rows = (mad::RowResult *)((char *)ws + mad::kCounterRegionBytes);
+    a.records = (char *)a.rows + mad::align256((size_t)B * T * sizeof(mad::RowResult));
+    a.B = B;
+    a.T = T;
+    a.V = V;
+    a.n_chunks = (V + mad::kSampleChunk - 1) / mad::kSampleChunk;
+    return hip_status(mad::launch_sample(a, dtype, (hipStream_t)stream), "sample launch");
 }
 
 int mad_accept_stochastic(const float *p, const float *q, const int32_t *draft_tok, const float *u, int B, int T,

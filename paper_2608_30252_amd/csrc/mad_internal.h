@@ -211,6 +211,35 @@ struct StochArgs {
 size_t stoch_ws_bytes(int B, int V);
 hipError_t launch_stoch(const StochArgs &a, hipStream_t st);
 
+// ---------------------------------------------------------------- sample ----
+constexpr int kSampleChunk = 8192;                            // entries per workgroup
+constexpr int kSampleMaxV = 1 << 20, kSampleMaxChunks = kSampleMaxV / kSampleChunk;
+constexpr int kListK = 128;                                   // the largest top-k whose candidates go through the workspace
+constexpr int kEmit = 512;                                    // candidates of a chunk
+constexpr size_t kSampleRecord = 4352;                        // a chunk's record in the workspace
+
+struct RowResult {         // a row's threshold key, the mass at and above it, its maximum
+    uint64_t t;
+    double mass;
+    float m;
+    int valid;
+};
+struct SampleArgs {
+    const void *logits;    // [B][T][V]
+    const float *u;        // [B][T]
+    int32_t *tok;          // [B][T] or null
+    float *probs;          // [B][T][V] or null
+    RowResult *rows;
+    char *records;         // [B * T][n_chunks] of kSampleRecord bytes
+    unsigned *counters;    // line r: arrivals of row r's workgroups
+    int B, T, V, n_chunks;
+    double c[kMaxB];       // log2 e / temperature
+    double top_p[kMaxB], min_p[kMaxB];
+    int top_k[kMaxB];      // 0: off
+};
+size_t sample_ws_bytes(int B, int T, int V);
+hipError_t launch_sample(const SampleArgs &a, int dtype, hipStream_t st);
+
 // ws layout helpers: counters first (256-byte aligned), then partials.
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
