@@ -218,11 +218,14 @@ constexpr int kListK = 128;                                   // the largest top
 constexpr int kEmit = 512;                                    // candidates of a chunk
 constexpr size_t kSampleRecord = 4352;                        // a chunk's record in the workspace
 
-struct RowResult {         // a row's threshold key, the mass at and above it, its maximum
-    uint64_t t;
-    double mass;
-    float m;
-    int valid;
+// What a row's launches hand on.  kRowDone: t and mass are final (or the row is finished); kRowNone: no distribution;
+// kRowCut: `target` is reached among the values in [lo, hi), and nothing below t stays; kRowSlow: by passes over the row.
+enum { kRowDone = 0, kRowNone = 1, kRowCut = 2, kRowSlow = 3 };
+struct RowResult {
+    uint64_t t;            // the least key that stays
+    double mass, target;   // mass of what stays
+    float lo, hi, m;       // m: the row's maximum
+    int mode;
 };
 struct SampleArgs {
     const void *logits;    // [B][T][V]

@@ -18,21 +18,23 @@
 // on the order.
 //
 // Work.  Workgroup (chunk, row) of 1024 threads reads 8192 entries, 8 a thread.
-//   * Rows with a small top-k (kListK): it counts its entries into 256 bins of
-//     1/8 below its maximum, finds the bin that holds its k-th largest and
-//     writes the entries down to it, some 1/8 more than k, to the workspace, as
-//     keys.  The row's last workgroup has every candidate: it finds the k-th by
-//     radix steps in LDS, sorts the k, and applies the other filters, the draw
-//     and the probabilities to them.  The row is read once and nothing else of
-//     V entries is touched but the zeros of the distribution.
-//   * Other rows: it sums its weights, and where a filter is on, also by bin.
-//     The row's last workgroup finds the bin where top-p (or a large top-k)
-//     ends, gathers that bin's entries from the row (out of L2), and narrows it
-//     down in LDS to the one entry where the count or mass is reached.  Where
-//     distributions are asked for, a second launch writes them (and draws).
-//   Whatever the bins do not resolve (values further apart than 32, thousands of
-//   equal ones, huge magnitudes) is narrowed down by passes over the row, with
-//   2048 buckets of the key range each.
+//   * Rows with a small top-k (kListK): it finds a value that at least top_k of
+//     its entries reach (from its threads' maxima, counted into bins of 1/8) and
+//     writes the entries down to there, somewhat more than top_k, to the
+//     workspace.  The row's last workgroup then has every candidate: it sorts
+//     the best and applies the filters, the draw and the probabilities to them.
+//     The row is read once and nothing else of V entries is touched but the
+//     zeros of the distribution.
+//   * Other rows: it sums its weights, and where a filter is on, also by bins of
+//     1/8 below its maximum.  The row's last workgroup finds the bin in which
+//     top-p (or a large top-k) ends.  A second launch, over all chunks again,
+//     collects that bin's entries and the mass above it; its last workgroup finds
+//     the entry where the count or mass is reached, and draws.  Where distributions
+//     are asked for, a third launch writes them.
+//   What the bins do not resolve (values further apart than 32, thousands of
+//   equal ones, huge magnitudes, a large top-k with top-p) is narrowed down by
+//   one workgroup in passes over the row, with 2048 buckets of the key range
+//   each.
 #include "mad_device.h"
 #include "mad_internal.h"
 
@@ -117,34 +119,37 @@ __device__ __forceinline__ void put64(void *p, uint64_t v) {
     __hip_atomic_store(reinterpret_cast<uint64_t *>(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 __device__ __forceinline__ uint64_t get64(const void *p) { return load_agent64(reinterpret_cast<const uint64_t *>(p)); }
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+    return (uint32_t)wave_fold_u64(v, [](uint64_t x, uint64_t y) { return x > y ? x : y; });
+}
 __device__ __forceinline__ uint64_t f64_bits(double v) { return (uint64_t)__double_as_longlong(v); }
 __device__ __forceinline__ double bits_f64(uint64_t v) { return __longlong_as_double((long long)v); }
 
-// A chunk's record in the workspace: 32 bytes of header, then the candidates' keys, or the bins' masses and counts.
-//   header: maximum and flags | first value that is certainly a candidate, candidates | mass of the chunk | -
-struct ChunkHead {
-    float max;
-    uint32_t flags;   // 1: a NaN; 2: no bins; 4: candidates left out below `edge`
-    float edge;
-    uint32_t n;
-    double mass;
-};
-constexpr int kHead = 32, kRecord = kHead + kBins * 12;
-static_assert(kRecord <= kSampleRecord && kHead + kEmit * 8 <= kSampleRecord, "chunk record");
+// A chunk's record in the workspace: a header of 32 bytes, then keys, or the bins' masses and counts.
+//   first launch:  maximum, flags | edge, keys | mass          second: count and keys | mass above the range
+constexpr int kHead = 32;
+static_assert(kHead + kBins * 12 <= (int)kSampleRecord && kHead + kEmit * 8 <= (int)kSampleRecord, "chunk record");
+constexpr uint32_t kNaN = 1, kNoBins = 2, kLeft = 4;   // flags: a NaN; magnitudes beyond the bins; candidates left out below `edge`
 
 struct SampleLds {
     uint64_t list[kList];       // gathered keys
     uint64_t mass[kBuckets];    // histogram: masses (integers), or doubles' bits
     uint32_t cnt[kBuckets];
-    double c_mass[kSampleMaxChunks];    // per chunk: mass against the row's maximum, kept mass
-    float c_max[kSampleMaxChunks], c_edge[kSampleMaxChunks];
-    uint32_t c_flags[kSampleMaxChunks], c_n[kSampleMaxChunks];
+    double c_mass[kSampleMaxChunks];    // per chunk: kept mass; against the row's maximum
+    uint64_t c_fix[kSampleMaxChunks];   // the same of listed entries, in units of 2^-50
+    float c_max[kSampleMaxChunks];
     double part[16], part2[16];   // one per wave
     double res[4];
     uint64_t key[4];
+    float fmx[16];
+    uint32_t flag[16];
     int num[4];
 };
 static_assert(sizeof(SampleLds) <= 64 * 1024, "static LDS");
+__device__ __forceinline__ SampleLds &lds() {
+    __shared__ SampleLds s;
+    return s;
+}
 
 // sum over the workgroup, the same in every thread (fixed order); `part`: 16 doubles of LDS, free again behind the
 // next barrier
@@ -173,7 +178,6 @@ template <typename T> struct Row {
     int V, n_chunks;
     float m;       // maximum
     double c;      // log2 e / temperature
-    SampleLds *s;
 
     // f(value, index) for every entry; four chunks in flight
     template <typename F> __device__ __forceinline__ void each(F f) const {
@@ -235,14 +239,16 @@ __device__ __forceinline__ int crossing(SampleLds &s, int nb, bool by_count, dou
     return b;
 }
 
-// The entry at which `target` is reached, among the keys of r (n of them in the list if in_list): its key; r.mass and
-// r.count become what lies at and above it.  The row has at least one entry in the range.
-template <typename T>
-__device__ uint64_t select(const Row<T> &row, Range &r, bool by_count, double target, int n, bool in_list) {
-    SampleLds &s = *row.s;
+// The entry at which `target` is reached, among the keys of r: its key (or the end of r, where rounding leaves
+// nothing in it); r.mass and r.count become what lies at and above it.  STREAM: out of the row; else out of the list,
+// which holds n keys of r.
+template <bool STREAM, typename T>
+__device__ __forceinline__ uint64_t select(const Row<T> &row, Range &r, bool by_count, double target, int n) {
+    SampleLds &s = lds();
     const int tid = threadIdx.x;
+    bool in_list = !STREAM;
     for (;;) {
-        if (!in_list) {   // into the list, if it takes them
+        if constexpr (STREAM) if (!in_list) {   // into the list, if it takes them
             if (tid == 0) s.num[3] = 0;
             __syncthreads();
             row.each([&](float x, int i) {
@@ -274,7 +280,7 @@ __device__ uint64_t select(const Row<T> &row, Range &r, bool by_count, double ta
         if (in_list) {
             const int all = s.num[3];
             for (int i = tid; i < all; i += kThreads) count(s.list[i], key_value(s.list[i]));
-        } else {
+        } else if constexpr (STREAM) {
             row.each([&](float x, int i) { count(argmax_key(x, i), x); });
         }
         __syncthreads();
@@ -326,73 +332,102 @@ __device__ uint64_t select(const Row<T> &row, Range &r, bool by_count, double ta
     return t;
 }
 
-// The row's bins (against its maximum, 1/8 apart) from its chunks' records, into s.mass / s.cnt: bin 0, the one of the
-// maximum, last.
-__device__ __forceinline__ void merge_bins(SampleLds &s, const char *rec, int n_chunks, float m, double c) {
-    const int tid = threadIdx.x, j = tid & (kBins - 1), part = tid / kBins;   // four parts of the chunks a bin
-    const float mb = floorf(m * 8.f);
-    double w = 0.0;
-    uint32_t n = 0;
-    #pragma unroll 4
-    for (int k = part; k < n_chunks; k += kThreads / kBins) {
-        const float cm = s.c_max[k];
-        const float d = mb - floorf(cm * 8.f);   // the chunk's bin of the row's bin j is j - d
-        if (cm == -INFINITY || (float)j < d) continue;
-        const char *p = rec + (size_t)k * kSampleRecord + kHead;
-        const int jc = j - (int)d;
-        w += (double)get64(p + 8 * jc) * kBinUnit * weight(cm, m, c);
-        n += __hip_atomic_load(reinterpret_cast<uint32_t *>(const_cast<char *>(p) + 8 * kBins + 4 * jc), __ATOMIC_RELAXED,
-                               __HIP_MEMORY_SCOPE_AGENT);
+// The first of the 256 values v(0), v(1), .. with which `target` is reached, by one wave (four a lane): its index (the
+// last that is not 0 where none is), and the sum before it.
+template <typename F>
+__device__ __forceinline__ int first_reaching(F v, double target, double *before) {
+    const int lane = threadIdx.x & 63;
+    double x[kBins / 64], sum = 0.0;
+    #pragma unroll
+    for (int i = 0; i < kBins / 64; ++i) {
+        x[i] = v(lane * (kBins / 64) + i);
+        sum += x[i];
     }
-    s.list[tid] = f64_bits(w);
-    s.cnt[kBins + tid] = n;
-    __syncthreads();
-    if (tid < kBins) {
-        double sum = 0.0;
-        uint32_t num = 0;
+    const double run = wave_scan_f64(sum) - sum;
+    int at = -1;
+    double pre = 0.0;
+    #pragma unroll
+    for (int i = kBins / 64 - 1; i >= 0; --i) {
+        double upto = run;
         #pragma unroll
-        for (int k = 0; k < kThreads / kBins; ++k) {
-            sum += bits_f64(s.list[j + k * kBins]);
-            num += s.cnt[kBins + j + k * kBins];
-        }
-        s.mass[kBins - 1 - j] = f64_bits(sum);
-        s.cnt[kBins - 1 - j] = num;
+        for (int k = 0; k < i; ++k) upto += x[k];
+        if (x[i] > 0.0 && upto + x[i] >= target) at = i, pre = upto;
     }
-    __syncthreads();
+    const unsigned long long hit = __ballot(at >= 0), some = __ballot(sum > 0.0);
+    const int l = hit ? __ffsll((long long)hit) - 1 : some ? 63 - __clzll((long long)some) : 0;
+    if (!hit) {
+        #pragma unroll
+        for (int i = 0; i < kBins / 64; ++i) {
+            if (x[i] > 0.0) at = i;
+        }
+        at = max(at, 0);
+        pre = run;
+        for (int k = 0; k < at; ++k) pre += x[k];
+    }
+    *before = read_lane_f64(pre, l);
+    return l * (kBins / 64) + __builtin_amdgcn_readlane(at, l);
 }
 
-// The range of keys that holds the place where `target` is reached, by the row's bins; whole: by none.
-__device__ __forceinline__ Range by_bins(SampleLds &s, float m, bool by_count, double target) {
-    Range r = {0, ~(uint64_t)0, 0.0, 0.0};
-    int n;
-    const double mb = (double)floorf(m * 8.f);
-    // total of the bins: below them the range is open
-    double tm = 0.0, tn = 0.0;
-    if (threadIdx.x < kBins) {
-        tm = bits_f64(s.mass[threadIdx.x]);
-        tn = (double)s.cnt[threadIdx.x];
+// The row's last workgroup: every chunk's header, lane c of each wave has chunks c and c + 64.
+struct Heads {
+    float max[2], edge[2];
+    uint32_t flags[2], n[2];
+    double mass[2];
+    // over the row
+    float m, worst;    // maximum; the highest edge below which candidates were left out
+    bool nan, no_bins, left;
+    int total;
+};
+__device__ __forceinline__ Heads load_heads(const char *rec0, int n_chunks) {
+    Heads h;
+    const int lane = threadIdx.x & 63;
+    uint64_t w[2][3];
+    #pragma unroll
+    for (int i = 0; i < 2; ++i)
+        #pragma unroll
+        for (int k = 0; k < 3; ++k) w[i][k] = lane + 64 * i < n_chunks ? get64(rec0 + (size_t)(lane + 64 * i) * kSampleRecord + 8 * k) : 0;
+    float m = -INFINITY, worst = -INFINITY, total = 0.f;
+    uint32_t all = 0;
+    #pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const bool in = lane + 64 * i < n_chunks;
+        h.max[i] = in ? __uint_as_float((uint32_t)w[i][0]) : -INFINITY;
+        h.flags[i] = (uint32_t)(w[i][0] >> 32);
+        h.edge[i] = __uint_as_float((uint32_t)w[i][1]);
+        h.n[i] = (uint32_t)(w[i][1] >> 32);
+        h.mass[i] = bits_f64(w[i][2]);
+        m = fmaxf(m, h.max[i]);
+        if (h.flags[i] & kLeft) worst = fmaxf(worst, h.edge[i]);
+        if ((h.flags[i] & kNoBins) && h.max[i] == -INFINITY) h.flags[i] &= ~kNoBins;   // nothing to count there
+        all |= h.flags[i];
+        total += (float)h.n[i];
     }
-    tm = block_sum(tm, s.part);
-    tn = block_sum(tn, s.part2);
-    __syncthreads();
-    if ((by_count ? tn : tm) < target) {
-        r.mass = tm;
-        r.count = tn;
-        r.hi = argmax_key((float)((mb - (kBins - 1)) / 8.0), -1) - 1;   // below the last bin's lower edge
-        return r;
+    h.m = group_max<64>(m);
+    h.worst = group_max<64>(worst);
+    h.nan = __any(all & kNaN);
+    h.no_bins = __any(all & kNoBins);
+    h.left = __any(all & kLeft);
+    h.total = (int)group_sum<64>(total);   // (exact: at most 2^16)
+    return h;
+}
+// the listed keys of all chunks into LDS, a wave a chunk (n[], offset by the sums before)
+__device__ __forceinline__ void load_list(SampleLds &s, const char *rec0, int n_chunks, const uint32_t (&n)[2]) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int off[2];
+    const double i0 = wave_scan_f64((double)n[0]), i1 = wave_scan_f64((double)n[1]);
+    off[0] = (int)(i0 - (double)n[0]);
+    off[1] = (int)(i1 - (double)n[1]) + (int)read_lane_f64(i0, 63);
+    for (int c = wave; c < n_chunks; c += kThreads / 64) {
+        const int nc = __builtin_amdgcn_readlane((int)(c < 64 ? n[0] : n[1]), c & 63);
+        const int at = __builtin_amdgcn_readlane(c < 64 ? off[0] : off[1], c & 63);
+        for (int i = lane; i < nc; i += 64) s.list[at + i] = get64(rec0 + (size_t)c * kSampleRecord + kHead + 8 * i);
     }
-    const int b = crossing(s, kBins, by_count, target, r, &n), j = kBins - 1 - b;
-    // keys of values in [(mb - j) / 8, (mb - j + 1) / 8): every index (the image of an edge with the index field at 0)
-    const uint64_t edge = (uint64_t)0xffffffffu << 32;
-    r.lo = argmax_key((float)((mb - j) / 8.0), 0) & edge;
-    r.hi = (argmax_key((float)((mb - j + 1) / 8.0), 0) & edge) - 1;
-    return r;
 }
 
 // The draw: the first entry with which the running kept mass exceeds u * (sum of c_mass), c_mass[] each chunk's.
 template <typename T>
-__device__ int draw(const Row<T> &row, uint64_t t, double u) {
-    SampleLds &s = *row.s;
+__device__ __forceinline__ int draw(const Row<T> &row, uint64_t t, double u) {
+    SampleLds &s = lds();
     const int tid = threadIdx.x;
     if (tid < 64) {
         double z = 0.0;
@@ -449,56 +484,106 @@ __device__ int draw(const Row<T> &row, uint64_t t, double u) {
 
 // A row with a small top-k, all candidates in the list (n of them, the k-th largest among them).
 template <typename T>
-__device__ void finish_list(const Row<T> &row, const SampleArgs &a, int b, size_t r, int n) {
-    SampleLds &s = *row.s;
-    const int tid = threadIdx.x, k = min(a.top_k[b], n);
-    Range all = {0, ~(uint64_t)0, 0.0, 0.0};
-    if (tid == 0) s.num[3] = n;
-    __syncthreads();
-    const uint64_t t = n > k ? select(row, all, true, (double)k, n, true) : 0;
-    // the k kept, ordered by rank: keys to mass[], weights behind them
+__device__ __forceinline__ void finish_list(const Row<T> &row, const SampleArgs &a, int b, size_t r, int n) {
+    SampleLds &s = lds();
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, k = min(a.top_k[b], n);
+    constexpr int kSort = 512;
+    uint64_t *some = s.mass, *sorted = s.mass + kSort;
+    // down to few: by bins of 1/8 below the maximum, or, where those hold too many, by narrowing to the k-th
+    uint64_t t = 0;
+    int n_some = n;
+    if (n > kSort / 2) {
+        const float mb = floorf(row.m * 8.f);
+        if (tid < kBins) s.cnt[tid] = 0;
+        if (tid == 0) s.num[3] = n;
+        __syncthreads();
+        for (int i = tid; i < n; i += kThreads) atomicAdd(&s.cnt[(int)fminf(mb - floorf(key_value(s.list[i]) * 8.f), kBins - 1)], 1u);
+        __syncthreads();
+        if (wave == 0) {
+            double before;
+            const int j = first_reaching([&](int i) { return (double)s.cnt[i]; }, (double)k, &before);
+            if (lane == 0) {
+                s.num[0] = j;
+                s.num[1] = (int)before + (int)s.cnt[j];
+            }
+        }
+        __syncthreads();
+        n_some = s.num[1];
+        t = argmax_key((mb - (float)s.num[0]) * 0.125f, 0) & ((uint64_t)0xffffffffu << 32);
+        if (s.num[0] == kBins - 1) t = 0, n_some = n;
+        __syncthreads();
+        if (n_some > kSort) {
+            Range all = {0, ~(uint64_t)0, 0.0, 0.0};
+            t = n > k ? select<false>(row, all, true, (double)k, n) : 0;
+        }
+    }
     if (tid == 0) s.num[2] = 0;
     __syncthreads();
     for (int i = tid; i < n; i += kThreads)
-        if (s.list[i] >= t) s.mass[atomicAdd(&s.num[2], 1)] = s.list[i];
+        if (s.list[i] >= t) some[atomicAdd(&s.num[2], 1)] = s.list[i];
     __syncthreads();
-    uint64_t *sorted = s.mass + kListK, *ws = s.mass + 2 * kListK;
-    if (tid < k) {
-        const uint64_t mine = s.mass[tid];
+    n_some = s.num[2];   // k of them at least, 512 at most
+    static_assert(2 * kSort <= kThreads, "two threads an entry");
+    {
+        const int e = tid >> 1, half = tid & 1;
+        const uint64_t mine = e < n_some ? some[e] : 0;
         int rank = 0;
-        for (int j = 0; j < k; ++j) rank += s.mass[j] > mine ? 1 : 0;
-        sorted[rank] = mine;
-        ws[rank] = f64_bits(weight(key_value(mine), row.m, row.c));
+        for (int j = half; j < n_some; j += 2) rank += some[j] > mine ? 1 : 0;
+        rank += __shfl_xor(rank, 1);
+        if (e < n_some && half == 0) sorted[rank] = mine;
     }
     __syncthreads();
-    const double w = tid < k ? bits_f64(ws[tid]) : 0.0;
-    const double before = block_scan(w, s.part), total = block_sum(w, s.part2);
-    const bool keep = tid < k && (a.top_p[b] >= 1.0 || before < a.top_p[b] * total) && w >= a.min_p[b];
-    const int kept = __syncthreads_count(keep);   // a prefix
-    const double z = block_sum(keep ? w : 0.0, s.part);
-    if (tid == 0) s.num[0] = 0x7fffffff, s.num[1] = -1;
-    __syncthreads();
-    if (keep) {
-        const int v = key_index(sorted[tid]);
-        if (a.probs) store_agent(a.probs + r * row.V + v, (float)(w / z));
-        if (a.tok) {
-            // running mass in index order, summed in the order of the values
-            double upto = 0.0;
-            for (int j = 0; j < kept; ++j) upto += key_index(sorted[j]) <= v ? bits_f64(ws[j]) : 0.0;
-            if (w > 0.0) {
-                if (upto > (double)a.u[r] * z) atomicMin(&s.num[0], v);
-                atomicMax(&s.num[1], v);
-            }
+    // from here on one wave, two entries a lane in order
+    if (wave != 0) return;
+    static_assert(kListK <= 128, "two a lane");
+    uint64_t key[2];
+    double w[2];
+    #pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const bool in = 2 * lane + i < k;
+        key[i] = in ? sorted[2 * lane + i] : 0;
+        w[i] = in ? weight(key_value(key[i]), row.m, row.c) : 0.0;
+    }
+    const double incl = wave_scan_f64(w[0] + w[1]), total = read_lane_f64(incl, 63);
+    const double before[2] = {incl - (w[0] + w[1]), incl - w[1]};
+    bool keep[2];
+    #pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        keep[i] = 2 * lane + i < k && (a.top_p[b] >= 1.0 || before[i] < a.top_p[b] * total) && w[i] >= a.min_p[b];
+        w[i] = keep[i] ? w[i] : 0.0;
+    }
+    const double z = __longlong_as_double((long long)wave_fold_u64(f64_bits(w[0] + w[1]), add_f64_bits));
+    const int kept = (int)__popcll(__ballot(keep[0])) + (int)__popcll(__ballot(keep[1]));   // a prefix
+    const double inv = 1.0 / z, target = a.tok ? (double)a.u[r] * z : 0.0;
+    int v[2];
+    double upto[2] = {0.0, 0.0};   // running mass in index order, summed in the order of the values
+    #pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        v[i] = key_index(key[i]);
+        if (keep[i] && a.probs) store_agent(a.probs + r * row.V + v[i], (float)(w[i] * inv));
+    }
+    if (!a.tok) return;
+    for (int j = 0; j < kept; ++j) {
+        const int vj = __builtin_amdgcn_readlane(v[j & 1], j >> 1);
+        const double wj = read_lane_f64(w[j & 1], j >> 1);
+        #pragma unroll
+        for (int i = 0; i < 2; ++i) upto[i] += vj <= v[i] ? wj : 0.0;
+    }
+    int first = 0x7fffffff, last = -1;
+    #pragma unroll
+    for (int i = 0; i < 2; ++i)
+        if (w[i] > 0.0) {
+            if (upto[i] > target) first = min(first, v[i]);
+            last = max(last, v[i]);
         }
-    }
-    __syncthreads();
-    if (tid == 0 && a.tok) a.tok[r] = s.num[0] != 0x7fffffff ? s.num[0] : s.num[1];
+    const int f = (int)(0xffffffffu - wave_max_u32(0xffffffffu - (uint32_t)first)), l = (int)wave_max_u32((uint32_t)(last + 1)) - 1;
+    if (lane == 0) a.tok[r] = f != 0x7fffffff ? f : l;
 }
 
 // kept mass of every chunk into c_mass[]; returns their sum
 template <typename T>
-__device__ double chunk_masses(const Row<T> &row, uint64_t t) {
-    SampleLds &s = *row.s;
+__device__ __forceinline__ double chunk_masses(const Row<T> &row, uint64_t t) {
+    SampleLds &s = lds();
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     double *part = reinterpret_cast<double *>(s.list);   // [chunk][wave]
     static_assert(kSampleMaxChunks * 16 <= kList, "partial sums fit the list");
@@ -526,77 +611,154 @@ __device__ double chunk_masses(const Row<T> &row, uint64_t t) {
     return z;
 }
 
+// The least key whose value's weight reaches p (0 < p <= 1): 64 places at a time, by every wave.
+__device__ __forceinline__ uint64_t least_weight(float m, double c, double p) {
+    uint32_t lo = 0, hi = (uint32_t)(argmax_key(m, 0) >> 32);   // hi reaches it; the answer is in [lo, hi]
+    while (lo < hi) {
+        const uint32_t span = hi - lo, step = span / 64 + 1;
+        const uint32_t at = lo + min(span, (uint32_t)(threadIdx.x & 63) * step);
+        const float v = key_value((uint64_t)at << 32);
+        const unsigned long long ok = __ballot(v == v && weight(v, m, c) >= p);   // (images below -inf's are NaN)
+        const int l = ok ? __ffsll((long long)ok) - 1 : 64;
+        const uint32_t was = lo;
+        if (l > 0) lo = was + min(span, (uint32_t)(l - 1) * step) + 1;
+        if (l < 64) hi = was + min(span, (uint32_t)l * step);
+        else lo = min(lo, hi);
+    }
+    return (uint64_t)lo << 32;
+}
+
 template <typename T>
-__global__ __launch_bounds__(kThreads) void sample_kernel(const SampleArgs a) {
-    __shared__ SampleLds s;
+__device__ __forceinline__ Row<T> row_of(const SampleArgs &a, int r) {
+    return Row<T>{reinterpret_cast<const T *>(a.logits) + (size_t)r * a.V, a.V, a.n_chunks, 0.f, a.c[r / a.T]};
+}
+// whether this workgroup is the row's last to get here; what it stored at device scope is visible then
+__device__ __forceinline__ bool row_last(const SampleArgs &a, int r, SampleLds &s) {
+    wait_vm_stores();
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        unsigned *cnt = a.counters + (size_t)r * kCounterStride;
+        const int last = arrive(cnt) == (unsigned)(a.n_chunks - 1);
+        if (last) reset_counter(cnt);
+        s.num[3] = last;
+    }
+    __syncthreads();
+    const bool last = s.num[3];
+    __syncthreads();
+    return last;
+}
+
+// A row by passes over it, by one workgroup: what the bins or the lists did not hold.  Not inlined: the kernels keep
+// their registers (64, for two workgroups per CU) and its spills stay in it.
+template <typename T> struct SolveJob {
+    Row<T> row;
+    double top_p, min_p, u;
+    int32_t *tok;     // or null
+    float *over;      // the row's distribution, zeros so far, where no other launch writes it
+    RowResult *out;
+    int top_k;
+};
+template <typename T>
+__device__ __noinline__ void solve_row(const SolveJob<T> j) {
+    const int tid = threadIdx.x;
+    const Row<T> row = j.row;
+    uint64_t t = 0;
+    for (int pass = 0; pass < 2; ++pass) {   // top-k, then top-p of its mass
+        const bool by_count = pass == 0;
+        if (by_count ? j.top_k == 0 : j.top_p >= 1.0) continue;
+        const double target = by_count ? (double)j.top_k : j.top_p * chunk_masses(row, t);
+        Range g = {0, ~(uint64_t)0, 0.0, 0.0};
+        t = max(t, select<true>(row, g, by_count, target, 0));
+    }
+    if (j.min_p > 0.0) t = max(t, least_weight(row.m, row.c, j.min_p));
+    const double kept = chunk_masses(row, t);
+    if (j.tok) {
+        const int v = draw(row, t, j.u);
+        if (tid == 0) *j.tok = v;
+    }
+    if (j.over)
+        row.each([&](float v, int i) {
+            if (argmax_key(v, i) >= t) store_agent(j.over + i, (float)(weight(v, row.m, row.c) * (1.0 / kept)));
+        });
+    if (tid == 0) *j.out = RowResult{t, kept, 0.0, 0.f, 0.f, row.m, kRowDone};
+}
+template <typename T>
+__device__ __forceinline__ SolveJob<T> solve_job(const SampleArgs &a, const Row<T> &row, int r) {
+    const int b = r / a.T, k = a.top_k[b];
+    return SolveJob<T>{row, a.top_p[b], a.min_p[b], a.tok ? (double)a.u[r] : 0.0, a.tok ? a.tok + r : nullptr,
+                       a.probs && k > 0 && k <= kListK ? a.probs + (size_t)r * a.V : nullptr, a.rows + r, k};
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads, 8) void sample_kernel(const SampleArgs a) {
+    SampleLds &s = lds();
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int rows = a.B * a.T, r = blockIdx.x % rows, chunk = blockIdx.x / rows, b = r / a.T;
     const int top_k = a.top_k[b];
     const bool listed = top_k > 0 && top_k <= kListK;
     const bool binned = !listed && (top_k > 0 || a.top_p[b] < 1.0);
-    Row<T> row = {reinterpret_cast<const T *>(a.logits) + (size_t)r * a.V, a.V, a.n_chunks, 0.f, a.c[b], &s};
+    Row<T> row = row_of<T>(a, r);
     char *rec0 = a.records + (size_t)r * a.n_chunks * kSampleRecord, *rec = rec0 + (size_t)chunk * kSampleRecord;
 
-    // ---- this chunk: maximum, NaN, bins ----
+    // ---- this chunk: maximum, NaN ----
     const int e0 = chunk * kSampleChunk + tid * kRun;
     float x[kRun];
     load_run(row.x, e0, a.V, x);
-    float m = -INFINITY;
+    float mine = -INFINITY;
     bool nan = false;
     #pragma unroll
     for (int i = 0; i < kRun; ++i) {
         nan |= x[i] != x[i];
-        m = fmaxf(m, x[i]);
+        mine = fmaxf(mine, x[i]);
     }
-    m = group_max<64>(m);
+    float m = group_max<64>(mine);
     nan = __any(nan);
     if (lane == 0) {
-        s.c_max[wave] = m;
-        s.c_flags[wave] = nan ? 1 : 0;
+        s.fmx[wave] = m;
+        s.flag[wave] = nan ? kNaN : 0;
     }
     if (tid < kBins) s.mass[tid] = 0, s.cnt[tid] = 0;
     if (tid == 0) s.num[0] = 0, s.num[1] = 0;
+    if (listed && a.probs) zero_run(a.probs + (size_t)r * a.V, e0, a.V);
     __syncthreads();
-    m = s.c_max[0];
-    uint32_t flags = s.c_flags[0];
+    m = s.fmx[0];
+    uint32_t flags = s.flag[0];
     #pragma unroll
     for (int k = 1; k < kThreads / 64; ++k) {
-        m = fmaxf(m, s.c_max[k]);
-        flags |= s.c_flags[k];
+        m = fmaxf(m, s.fmx[k]);
+        flags |= s.flag[k];
     }
     const float mb = floorf(m * 8.f);
-    if (!(fabsf(m) < 0x1p20f)) flags |= 2;   // (bins of 1/8 are exact below 2^21)
+    if (!(fabsf(m) < 0x1p20f)) flags |= kNoBins;   // (bins of 1/8 are exact below 2^21)
     float edge = INFINITY;
     uint32_t n_out = 0;
     double mass = 0.0;
     if (listed) {
-        if (!(flags & 2)) {
-            #pragma unroll
-            for (int i = 0; i < kRun; ++i) {
-                const float j = mb - floorf(x[i] * 8.f);
-                if (j < (float)kBins) atomicAdd(&s.cnt[(int)j], 1u);
-            }
-            __syncthreads();
-            if (wave == 0) {   // the bin with which top_k are reached, or the last
-                double v[kBins / 64], sum = 0.0;
-                #pragma unroll
-                for (int i = 0; i < kBins / 64; ++i) {
-                    v[i] = (double)s.cnt[lane * (kBins / 64) + i];
-                    sum += v[i];
+        if (!(flags & kNoBins)) {
+            // the threads' maxima by bins; where fewer than top_k of them are in the bins, every entry
+            int at;
+            for (int every = 0;; every = 1) {
+                if (!every) {
+                    const float j = mb - floorf(mine * 8.f);
+                    if (j < (float)kBins) atomicAdd(&s.cnt[(int)j], 1u);
+                } else {
+                    #pragma unroll
+                    for (int i = 0; i < kRun; ++i) {
+                        const float j = mb - floorf(x[i] * 8.f);
+                        if (j < (float)kBins && x[i] != mine) atomicAdd(&s.cnt[(int)j], 1u);   // (fewer than there are: harmless)
+                    }
                 }
-                double run = wave_scan_f64(sum) - sum;
-                int at = kBins - 1;
-                for (int i = kBins / 64 - 1; i >= 0; --i) {
-                    double upto = run;
-                    for (int k = 0; k <= i; ++k) upto += v[k];
-                    if (upto >= (double)top_k) at = lane * (kBins / 64) + i;
+                __syncthreads();
+                if (wave == 0) {
+                    double before;
+                    const int j = first_reaching([&](int i) { return (double)s.cnt[i]; }, (double)top_k, &before);
+                    if (lane == 0) s.num[2] = before + (double)s.cnt[j] >= (double)top_k ? j : kBins;
                 }
-                at = (int)(0xffffffffu - (uint32_t)wave_fold_u64((uint64_t)(0xffffffffu - (uint32_t)at),
-                                                                 [](uint64_t p, uint64_t q) { return p > q ? p : q; }));
-                if (lane == 0) s.num[2] = at;
+                __syncthreads();
+                at = s.num[2];
+                if (at < kBins || every) break;
             }
-            __syncthreads();
-            const int at = s.num[2];
+            at = min(at, kBins - 1);   // fewer than top_k in the bins: all of them
             edge = (mb - (float)at) * 0.125f;
             bool left = false;
             #pragma unroll
@@ -611,30 +773,30 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const SampleArgs a) {
             if (left) s.num[1] = 1;
             __syncthreads();
             n_out = (uint32_t)s.num[0];
-            if (n_out > (uint32_t)kEmit) flags |= 4, edge = INFINITY, n_out = 0;
-            else if (s.num[1]) flags |= 4;
+            if (n_out > (uint32_t)kEmit) flags |= kLeft, edge = INFINITY, n_out = 0;
+            else if (s.num[1]) flags |= kLeft;
         } else if (m > -INFINITY) {
-            flags |= 4;   // candidates only by the row's last workgroup
+            flags |= kLeft;   // (edge +inf) candidates only by the row's last workgroup
         }
-        if (a.probs) zero_run(a.probs + (size_t)r * a.V, e0, a.V);
     } else {
         #pragma unroll
         for (int i = 0; i < kRun; ++i) {
-            const double w = e0 + i < a.V ? weight(x[i], m, row.c) : 0.0;
-            mass += m == -INFINITY ? 0.0 : w;
-            if (binned && !(flags & 2)) {
+            const double w = e0 + i < a.V && m > -INFINITY ? weight(x[i], m, row.c) : 0.0;
+            mass += w;
+            if (binned && !(flags & kNoBins)) {
                 const float j = mb - floorf(x[i] * 8.f);
-                if (j < (float)kBins && e0 + i < a.V) {
+                if (j < (float)kBins) {   // (not -inf, so not past the row's end)
                     atomicAdd((unsigned long long *)&s.mass[(int)j], (unsigned long long)(w * (1.0 / kBinUnit) + 0.5));
-                    atomicAdd(&s.cnt[(int)j], 1u);
+                    if (top_k > 0) atomicAdd(&s.cnt[(int)j], 1u);
                 }
             }
         }
         mass = block_sum(mass, s.part);   // (its barrier stands behind the atomics)
         if (binned && tid < kBins) {
             put64(rec + kHead + 8 * tid, s.mass[tid]);
-            __hip_atomic_store(reinterpret_cast<uint32_t *>(rec + kHead + 8 * kBins) + tid, s.cnt[tid], __ATOMIC_RELAXED,
-                               __HIP_MEMORY_SCOPE_AGENT);
+            if (top_k > 0)
+                __hip_atomic_store(reinterpret_cast<uint32_t *>(rec + kHead + 8 * kBins) + tid, s.cnt[tid], __ATOMIC_RELAXED,
+                                   __HIP_MEMORY_SCOPE_AGENT);
         }
     }
     if (tid == 0) {
@@ -642,182 +804,240 @@ __global__ __launch_bounds__(kThreads) void sample_kernel(const SampleArgs a) {
         put64(rec + 8, (uint64_t)__float_as_uint(edge) | (uint64_t)n_out << 32);
         put64(rec + 16, f64_bits(mass));
     }
-    wait_vm_stores();
-    __syncthreads();
-    if (tid == 0) {
-        unsigned *cnt = a.counters + (size_t)r * kCounterStride;
-        const int last = arrive(cnt) == (unsigned)(a.n_chunks - 1);
-        if (last) reset_counter(cnt);
-        s.num[3] = last;
-    }
-    __syncthreads();
-    if (!s.num[3]) return;
+    if (!row_last(a, r, s)) return;
 
     // ---- the row's last workgroup ----
-    if (tid < a.n_chunks) {
-        const char *p = rec0 + (size_t)tid * kSampleRecord;
-        const uint64_t h0 = get64(p), h1 = get64(p + 8), h2 = get64(p + 16);
-        s.c_max[tid] = __uint_as_float((uint32_t)h0);
-        s.c_flags[tid] = (uint32_t)(h0 >> 32);
-        s.c_edge[tid] = __uint_as_float((uint32_t)h1);
-        s.c_n[tid] = (uint32_t)(h1 >> 32);
-        s.c_mass[tid] = bits_f64(h2);
-    }
-    __syncthreads();
-    m = -INFINITY;
-    flags = 0;
-    int n = 0;
-    for (int c = 0; c < a.n_chunks; ++c) {
-        m = fmaxf(m, s.c_max[c]);
-        flags |= s.c_flags[c];
-        n += (int)s.c_n[c];
-    }
-    row.m = m;
-    RowResult *out = a.rows + r;
-    if ((flags & 1) || m == -INFINITY) {   // no distribution
+    const Heads h = load_heads(rec0, a.n_chunks);
+    m = row.m = h.m;
+    RowResult out = {0, 0, 0.0, 0.f, 0.f, m, kRowDone};
+    if (h.nan || m == -INFINITY) {   // no distribution
         if (tid == 0) {
             if (a.tok) a.tok[r] = -1;
-            if (!listed) *out = RowResult{~(uint64_t)0, 1.0, 0.f, 0};
+            out.mode = kRowNone;
+            a.rows[r] = out;
         }
         return;
     }
-    if (listed && n <= kList) {
-        // the candidates, in whatever order: chunk by chunk, a wave each
-        int at = 0;
-        for (int c = 0; c < a.n_chunks; ++c) {
-            const int nc = (int)s.c_n[c];
-            if (c % (kThreads / 64) == wave)
-                for (int i = lane; i < nc; i += 64) s.list[at + i] = get64(rec0 + (size_t)c * kSampleRecord + kHead + 8 * i);
-            at += nc;
-        }
-        __syncthreads();
+    if (listed) {
         // What a chunk left out lies below its edge: harmless where the k-th candidate does not.
-        bool complete = true;
-        if (flags & 4) {
-            float worst = -INFINITY;
-            for (int c = 0; c < a.n_chunks; ++c)
-                if (s.c_flags[c] & 4) worst = fmaxf(worst, s.c_edge[c]);
-            complete = false;
-            if (worst < INFINITY) {
+        bool complete = h.total <= kList && !(h.worst == INFINITY);
+        if (complete) {
+            load_list(s, rec0, a.n_chunks, h.n);
+            __syncthreads();
+            if (h.left) {
                 int above = 0;
-                for (int i = tid; i < n; i += kThreads) above += key_value(s.list[i]) >= worst ? 1 : 0;
+                for (int i = tid; i < h.total; i += kThreads) above += key_value(s.list[i]) >= h.worst ? 1 : 0;
                 complete = block_sum((double)above, s.part) >= (double)top_k;
-                __syncthreads();
             }
         }
         if (complete) {
-            finish_list(row, a, b, r, n);
+            if (tid == 0) a.rows[r] = out;
+            finish_list(row, a, b, r, h.total);
             return;
         }
-    }
-    // ---- any row: threshold and mass ----
-    uint64_t t = 0;
-    double kept;
-    bool have = false;   // c_mass[] holds the kept masses
-    if (!listed) {
-        __syncthreads();
-        if (tid < a.n_chunks) s.c_mass[tid] = s.c_max[tid] == -INFINITY ? 0.0 : s.c_mass[tid] * weight(s.c_max[tid], m, row.c);
-        __syncthreads();
-        kept = 0.0;
-        for (int c = 0; c < a.n_chunks; ++c) kept += s.c_mass[c];
-        have = true;
-    } else {
-        kept = chunk_masses(row, 0);
-    }
-    bool bins = binned;
-    if (bins)
-        for (int c = 0; c < a.n_chunks; ++c) bins = bins && (!(s.c_flags[c] & 2) || s.c_max[c] == -INFINITY);
-    const Range whole = {0, ~(uint64_t)0, 0.0, 0.0};
-    if (top_k > 0 && top_k < a.V) {
-        if (bins) merge_bins(s, rec0, a.n_chunks, m, row.c);
-        Range g = bins ? by_bins(s, m, true, (double)top_k) : whole;
-        t = select(row, g, true, (double)top_k, 0, false);
-        kept = g.mass;
-        have = false;
-    }
-    if (a.top_p[b] < 1.0) {
-        const double target = a.top_p[b] * kept;
-        if (bins) merge_bins(s, rec0, a.n_chunks, m, row.c);
-        Range g = bins ? by_bins(s, m, false, target) : whole;
-        const uint64_t tp = select(row, g, false, target, 0, false);
-        if (tp > t) {
-            t = tp;
-            kept = g.mass;
-        }
-        have = false;
-    }
-    const double min_p = a.min_p[b];
-    if (min_p > 0.0 && (t == 0 || weight(key_value(t), m, row.c) < min_p)) {
-        // the least value whose weight reaches min_p, by bisection over the ordered images
-        uint32_t lo = 0, hi = (uint32_t)(argmax_key(m, 0) >> 32);   // hi reaches it
-        while (lo < hi) {
-            const uint32_t mid = lo + (hi - lo) / 2;
-            const float v = key_value((uint64_t)mid << 32);
-            if (v == v && weight(v, m, row.c) >= min_p) hi = mid;
-            else lo = mid + 1;
-        }
-        t = (uint64_t)hi << 32;
-        kept = chunk_masses(row, t);
-        have = true;
-    }
-    if (a.tok && !a.probs) {
-        if (!have) kept = chunk_masses(row, t);
-        const int v = draw(row, t, (double)a.u[r]);
-        if (tid == 0) a.tok[r] = v;
+        solve_row<T>(solve_job(a, row, r));
         return;
-    }
-    if (listed) {   // (no second launch for it) its distribution, over the zeros
-        if (a.tok) {
-            if (!have) kept = chunk_masses(row, t);
-            const int v = draw(row, t, (double)a.u[r]);
+    } else {
+        // the chunks' masses against the row's maximum
+        double cm[2];
+        #pragma unroll
+        for (int i = 0; i < 2; ++i) cm[i] = h.max[i] == -INFINITY ? 0.0 : h.mass[i] * weight(h.max[i], m, row.c);
+        if (wave == 0) {
+            #pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (lane + 64 * i < a.n_chunks) {
+                    s.c_mass[lane + 64 * i] = cm[i];
+                    s.c_max[lane + 64 * i] = h.max[i];
+                }
+        }
+        out.mass = __longlong_as_double((long long)wave_fold_u64(f64_bits(cm[0] + cm[1]), add_f64_bits));
+        __syncthreads();
+        const double min_p = a.min_p[b];
+        if (min_p > 0.0) out.t = least_weight(m, row.c, min_p);   // so far: no entry below it stays
+        if (binned) {
+            if (h.no_bins) {
+                out.mode = kRowSlow;
+            } else {
+                // the row's bins: bin j of a chunk whose maximum lies d bins lower is the row's j + d
+                const int j = tid & (kBins - 1);
+                const float rb = floorf(m * 8.f);
+                double w = 0.0;
+                uint32_t n = 0;
+                #pragma unroll 4
+                for (int k = tid / kBins; k < a.n_chunks; k += kThreads / kBins) {
+                    const float top = s.c_max[k], d = rb - floorf(top * 8.f);
+                    const bool in = top > -INFINITY && (float)j >= d;
+                    const char *q = rec0 + (size_t)k * kSampleRecord + kHead;
+                    const int jc = in ? j - (int)d : 0;
+                    const double x = (double)get64(q + 8 * jc);
+                    w += in ? x * kBinUnit * weight(top, m, row.c) : 0.0;
+                    if (top_k > 0) {
+                        const uint32_t y = __hip_atomic_load(reinterpret_cast<uint32_t *>(const_cast<char *>(q) + 8 * kBins + 4 * jc),
+                                                             __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                        n += in ? y : 0;
+                    }
+                }
+                s.list[tid] = f64_bits(top_k > 0 ? (double)n : w);
+                __syncthreads();
+                if (wave == 0) {
+                    auto bin = [&](int i) {
+                        return bits_f64(s.list[i]) + bits_f64(s.list[i + kBins]) + bits_f64(s.list[i + 2 * kBins]) + bits_f64(s.list[i + 3 * kBins]);
+                    };
+                    const double target = top_k > 0 ? (double)top_k : a.top_p[b] * out.mass;
+                    double before;
+                    const int i = first_reaching(bin, target, &before);
+                    const bool in = before + bin(i) >= target;   // else it is reached below the last bin
+                    out.lo = in ? (rb - (float)i) * 0.125f : -INFINITY;
+                    out.hi = (rb - (in ? (float)(i - 1) : (float)(kBins - 1))) * 0.125f;
+                    // where min-p ends above it, only that counts
+                    const float tv = key_value(out.t);
+                    if (out.t > 0 && tv >= out.hi) out.lo = out.hi = tv;
+                    out.mode = kRowCut;
+                    out.target = target;
+                    if (lane == 0) a.rows[r] = out;
+                }
+                return;
+            }
+        } else if (min_p > 0.0) {
+            out.lo = out.hi = key_value(out.t);
+            out.mode = kRowCut;
+        } else if (a.tok) {
+            const int v = draw(row, 0, (double)a.u[r]);
             if (tid == 0) a.tok[r] = v;
         }
-        float *p = a.probs + (size_t)r * a.V;
-        row.each([&](float v, int i) {
-            if (argmax_key(v, i) >= t) store_agent(p + i, (float)(weight(v, m, row.c) / kept));
-        });
-        return;
     }
-    if (tid == 0) *out = RowResult{t, kept, m, 1};
+    if (tid == 0) a.rows[r] = out;
 }
 
-// The distributions of the rows that the first launch only decided, and their draws.
+// The second launch: the entries of each undecided row's range, the mass above it, the cut, and the draw.
+template <typename T>
+__global__ __launch_bounds__(kThreads, 8) void sample_cut_kernel(const SampleArgs a) {
+    SampleLds &s = lds();
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int rows = a.B * a.T, r = blockIdx.x % rows, chunk = blockIdx.x / rows, b = r / a.T;
+    const RowResult res = a.rows[r];
+    if (res.mode != kRowCut && (res.mode != kRowSlow || chunk > 0)) return;
+    Row<T> row = row_of<T>(a, r);
+    row.m = res.m;
+    if (res.mode == kRowSlow) {
+        solve_row<T>(solve_job(a, row, r));
+        return;
+    }
+    char *rec0 = a.records + (size_t)r * a.n_chunks * kSampleRecord, *rec = rec0 + (size_t)chunk * kSampleRecord;
+    const int e0 = chunk * kSampleChunk + tid * kRun;
+    float x[kRun];
+    load_run(row.x, e0, a.V, x);
+    if (tid == 0) s.num[0] = 0, s.num[1] = 0;
+    __syncthreads();
+    double above = 0.0;
+    int n_above = 0;
+    #pragma unroll
+    for (int i = 0; i < kRun; ++i) {
+        const bool up = x[i] >= res.hi && e0 + i < a.V;
+        if (__any(up)) above += up ? weight(x[i], res.m, row.c) : 0.0;
+        n_above += up ? 1 : 0;
+        if (x[i] < res.hi && x[i] >= res.lo && e0 + i < a.V) {
+            const int p = atomicAdd(&s.num[0], 1);
+            if (p < kEmit) put64(rec + kHead + 8 * p, argmax_key(x[i], e0 + i));
+        }
+    }
+    if (a.top_k[b] > 0) {
+        const int n = (int)group_sum<64>((float)n_above);
+        if (lane == 0 && n > 0) atomicAdd(&s.num[1], n);
+    }
+    above = block_sum(above, s.part);   // (its barrier stands behind the atomics)
+    if (tid == 0) {
+        put64(rec, (uint64_t)(uint32_t)s.num[0] | (uint64_t)(uint32_t)s.num[1] << 32);
+        put64(rec + 16, f64_bits(above));
+    }
+    if (!row_last(a, r, s)) return;
+
+    // ---- the row's last workgroup ----
+    uint32_t n[2];
+    float total = 0.f;
+    double mass = 0.0, count = 0.0;
+    bool over = false;
+    #pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const bool in = lane + 64 * i < a.n_chunks;
+        const uint64_t h0 = in ? get64(rec0 + (size_t)(lane + 64 * i) * kSampleRecord) : 0;
+        const double up = in ? bits_f64(get64(rec0 + (size_t)(lane + 64 * i) * kSampleRecord + 16)) : 0.0;
+        n[i] = (uint32_t)h0;
+        over |= n[i] > (uint32_t)kEmit;
+        total += (float)n[i];
+        mass += up;
+        count += (double)(uint32_t)(h0 >> 32);
+        if (tid < 64 && in) {
+            s.c_mass[lane + 64 * i] = up;
+            s.c_fix[lane + 64 * i] = 0;
+        }
+    }
+    const int all = (int)group_sum<64>(total);
+    if (__any(over) || all > kList || (a.top_k[b] > 0 && a.top_p[b] < 1.0)) {
+        solve_row<T>(solve_job(a, row, r));
+        return;
+    }
+    mass = __longlong_as_double((long long)wave_fold_u64(f64_bits(mass), add_f64_bits));
+    count = __longlong_as_double((long long)wave_fold_u64(f64_bits(count), add_f64_bits));
+    load_list(s, rec0, a.n_chunks, n);
+    if (tid == 0) s.num[3] = all;
+    __syncthreads();
+    uint64_t t = res.t;
+    if (res.lo < res.hi) {
+        const uint64_t edge = (uint64_t)0xffffffffu << 32;
+        Range g = {argmax_key(res.lo, 0) & edge, (argmax_key(res.hi, 0) & edge) - 1, mass, count};
+        t = max(t, select<false>(row, g, a.top_k[b] > 0, res.target, all));
+    }
+    // each chunk's kept mass: above the range, and the listed entries that stay
+    for (int i = tid; i < all; i += kThreads) {
+        const uint64_t k = s.list[i];
+        if (k >= t)
+            atomicAdd((unsigned long long *)&s.c_fix[key_index(k) / kSampleChunk],
+                      (unsigned long long)(weight(key_value(k), row.m, row.c) * (1.0 / kBinUnit) + 0.5));
+    }
+    __syncthreads();
+    double kept = 0.0;
+    #pragma unroll
+    for (int i = 0; i < 2; ++i)
+        if (lane + 64 * i < a.n_chunks) kept += s.c_mass[lane + 64 * i] + (double)s.c_fix[lane + 64 * i] * kBinUnit;
+    kept = __longlong_as_double((long long)wave_fold_u64(f64_bits(kept), add_f64_bits));
+    __syncthreads();
+    if (tid < a.n_chunks) s.c_mass[tid] += (double)s.c_fix[tid] * kBinUnit;
+    __syncthreads();
+    if (a.tok) {
+        const int v = draw(row, t, (double)a.u[r]);
+        if (tid == 0) a.tok[r] = v;
+    }
+    if (tid == 0) {
+        RowResult out = res;
+        out.t = t;
+        out.mass = kept;
+        out.mode = kRowDone;
+        a.rows[r] = out;
+    }
+}
+
+// The third launch: the distributions of the rows that were not finished from their list.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void sample_emit_kernel(const SampleArgs a) {
-    __shared__ SampleLds s;
     const int tid = threadIdx.x;
     const int rows = a.B * a.T, r = blockIdx.x % rows, chunk = blockIdx.x / rows, b = r / a.T;
     if (a.top_k[b] > 0 && a.top_k[b] <= kListK) return;
-    const RowResult res = a.rows[r];
-    Row<T> row = {reinterpret_cast<const T *>(a.logits) + (size_t)r * a.V, a.V, a.n_chunks, res.m, a.c[b], &s};
     const int e0 = chunk * kSampleChunk + tid * kRun;
+    const RowResult res = a.rows[r];
     float x[kRun], p[kRun];
-    load_run(row.x, e0, a.V, x);
-    double sum = 0.0;
+    load_run(reinterpret_cast<const T *>(a.logits) + (size_t)r * a.V, e0, a.V, x);
+    const float tv = key_value(res.t);   // the row has no NaN
+    const uint32_t ti = (uint32_t)key_index(res.t);   // (a bound of values: past every index)
+    const bool any = res.mode == kRowDone;
+    const double c = a.c[b], inv = 1.0 / res.mass;
     #pragma unroll
     for (int i = 0; i < kRun; ++i) {
-        const double w = res.valid && e0 + i < a.V && argmax_key(x[i], e0 + i) >= res.t ? weight(x[i], res.m, row.c) : 0.0;
-        sum += w;
-        p[i] = (float)(w / res.mass);
+        const bool stays = any && (res.t == 0 || x[i] > tv || (x[i] == tv && (uint32_t)(e0 + i) <= ti));
+        p[i] = 0.f;
+        if (__any(stays)) p[i] = stays ? (float)(weight(x[i], res.m, c) * inv) : 0.f;
     }
     store_run(a.probs + (size_t)r * a.V, e0, a.V, p);
-    if (!a.tok || !res.valid) return;
-    sum = block_sum(sum, s.part);
-    char *rec0 = a.records + (size_t)r * a.n_chunks * kSampleRecord;
-    if (tid == 0) {
-        put64(rec0 + (size_t)chunk * kSampleRecord + 24, f64_bits(sum));
-        wait_vm_stores();
-        unsigned *cnt = a.counters + (size_t)r * kCounterStride;
-        const int last = arrive(cnt) == (unsigned)(a.n_chunks - 1);
-        if (last) reset_counter(cnt);
-        s.num[3] = last;
-    }
-    __syncthreads();
-    if (!s.num[3]) return;
-    if (tid < a.n_chunks) s.c_mass[tid] = bits_f64(get64(rec0 + (size_t)tid * kSampleRecord + 24));
-    __syncthreads();
-    const int v = draw(row, res.t, (double)a.u[r]);
-    if (tid == 0) a.tok[r] = v;
 }
 
 // ------------------------------------------------------------------ host ----
@@ -831,13 +1051,23 @@ template <typename T>
 static hipError_t launch_sample_t(const SampleArgs &a, hipStream_t st) {
     const dim3 grid((unsigned)(a.B * a.T) * (unsigned)a.n_chunks), block(kThreads);
     hipLaunchKernelGGL((sample_kernel<T>), grid, block, 0, st, a);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || !a.probs) return e;
-    bool emit = false;
-    for (int b = 0; b < a.B; ++b) emit |= a.top_k[b] == 0 || a.top_k[b] > kListK;
-    if (!emit) return e;
-    hipLaunchKernelGGL((sample_emit_kernel<T>), grid, block, 0, st, a);
-    return hipGetLastError();
+    hipError_t e = hipGetLastError();
+    // rows with a small top-k are finished there; plain ones have nothing to cut
+    bool cut = false, emit = false;
+    for (int b = 0; b < a.B; ++b) {
+        const bool listed = a.top_k[b] > 0 && a.top_k[b] <= kListK;
+        cut |= !listed && (a.top_k[b] > 0 || a.top_p[b] < 1.0 || a.min_p[b] > 0.0);
+        emit |= a.probs && !listed;
+    }
+    if (e == hipSuccess && cut) {
+        hipLaunchKernelGGL((sample_cut_kernel<T>), grid, block, 0, st, a);
+        e = hipGetLastError();
+    }
+    if (e == hipSuccess && emit) {
+        hipLaunchKernelGGL((sample_emit_kernel<T>), grid, block, 0, st, a);
+        e = hipGetLastError();
+    }
+    return e;
 }
 
 hipError_t launch_sample(const SampleArgs &a, int dtype, hipStream_t st) {
