@@ -41,7 +41,7 @@
 namespace mad {
 
 constexpr int kThreads = 1024, kRun = kSampleChunk / kThreads;   // entries of a thread: consecutive
-constexpr int kBins = 256, kBuckets = 2048, kList = 4096, kFinal = 64;
+constexpr int kBins = 256, kBuckets = 2048, kList = 4096, kFinal = 128, kSort = 512;
 constexpr double kBinUnit = 0x1p-50, kRowUnit = 0x1p-43;   // 8192 and 2^20 weights of at most 1 fit 63 bits
 
 // 2^y for y <= 0 (y > -1000): the Taylor series of 2^f, |f| <= 1/2, to 12th order: below 2e-16 relative
@@ -239,6 +239,21 @@ __device__ __forceinline__ int crossing(SampleLds &s, int nb, bool by_count, dou
     return b;
 }
 
+// n different keys (512 at most) into descending order: each counts the larger ones, by 8 threads or 2
+__device__ __forceinline__ void sort_down(const uint64_t *from, uint64_t *to, int n) {
+    static_assert(kFinal * 8 <= kThreads && kSort * 2 <= kThreads, "threads for each key");
+    const int sh = n <= kFinal ? 3 : 1, e = threadIdx.x >> sh, part = threadIdx.x & ((1 << sh) - 1);
+    const uint64_t mine = e < n ? from[e] : 0;
+    int rank = 0;
+    for (int j = part; j < n; j += 1 << sh) rank += from[j] > mine ? 1 : 0;
+    rank += __shfl_xor(rank, 1);
+    if (sh == 3) {
+        rank += __shfl_xor(rank, 2);
+        rank += __shfl_xor(rank, 4);
+    }
+    if (e < n && part == 0) to[rank] = mine;
+}
+
 // The entry at which `target` is reached, among the keys of r: its key (or the end of r, where rounding leaves
 // nothing in it); r.mass and r.count become what lies at and above it.  STREAM: out of the row; else out of the list,
 // which holds n keys of r.
@@ -263,8 +278,27 @@ __device__ __forceinline__ uint64_t select(const Row<T> &row, Range &r, bool by_
             in_list = n <= kList;
             __syncthreads();
         }
-        // The keys of the list that are still in the range; few enough are put in order by one wave.
+        // The keys of the list that are still in the range: few enough are put in order.
         if (in_list && n <= kFinal) break;
+        if (in_list) {   // to the keys that are there (equal values differ in a few bits of their indices only)
+            if (tid == 0) s.key[0] = ~(uint64_t)0, s.key[1] = 0;
+            __syncthreads();
+            uint64_t lo = ~(uint64_t)0, hi = 0;
+            const int all = s.num[3];
+            for (int i = tid; i < all; i += kThreads) {
+                const uint64_t k = s.list[i];
+                if (k >= r.lo && k <= r.hi) lo = min(lo, k), hi = max(hi, k);
+            }
+            lo = wave_fold_u64(lo, [](uint64_t x, uint64_t y) { return x < y ? x : y; });
+            hi = wave_fold_u64(hi, [](uint64_t x, uint64_t y) { return x > y ? x : y; });
+            if ((tid & 63) == 0 && lo <= hi) {
+                atomicMin((unsigned long long *)&s.key[0], (unsigned long long)lo);
+                atomicMax((unsigned long long *)&s.key[1], (unsigned long long)hi);
+            }
+            __syncthreads();
+            r.lo = s.key[0];
+            r.hi = s.key[1];
+        }
         int sh = 64 - __clzll((long long)(r.hi - r.lo)) - 11;   // 2048 buckets (a range of one key holds one entry)
         if (sh < 0) sh = 0;
         for (int b = tid; b < kBuckets; b += kThreads) s.mass[b] = 0, s.cnt[b] = 0;
@@ -291,7 +325,7 @@ __device__ __forceinline__ uint64_t select(const Row<T> &row, Range &r, bool by_
         r.hi = min(r.hi, lo + (((uint64_t)1 << sh) - 1));
         r.lo = lo;
     }
-    // at most 64: wave 0 orders them by rank and sums in order
+    // at most 128: ordered by rank, then wave 0 sums them in order, two a lane
     if (tid == 0) s.num[2] = 0;
     __syncthreads();
     const int all = s.num[3];
@@ -299,12 +333,7 @@ __device__ __forceinline__ uint64_t select(const Row<T> &row, Range &r, bool by_
         if (s.list[i] >= r.lo && s.list[i] <= r.hi) s.mass[atomicAdd(&s.num[2], 1)] = s.list[i];
     __syncthreads();
     const int f = s.num[2];
-    if (tid < f) {
-        const uint64_t mine = s.mass[tid];
-        int rank = 0;
-        for (int j = 0; j < f; ++j) rank += s.mass[j] > mine ? 1 : 0;
-        s.mass[kFinal + rank] = mine;
-    }
+    sort_down(s.mass, s.mass + kSort, f);
     if (tid == 0 && f == 0) {   // nothing there (a mass reached only but for rounding): all above the range
         s.key[0] = r.hi + 1;
         s.res[0] = r.mass;
@@ -312,16 +341,24 @@ __device__ __forceinline__ uint64_t select(const Row<T> &row, Range &r, bool by_
     }
     __syncthreads();
     if (tid < 64 && f > 0) {
-        const uint64_t k = tid < f ? s.mass[kFinal + tid] : 0;
-        const double w = tid < f ? weight(key_value(k), row.m, row.c) : 0.0;
-        const double incl = wave_scan_f64(w);
-        const bool hit = tid < f && (by_count ? r.count + tid + 1 : r.mass + incl) >= target;
+        uint64_t k[2];
+        double w[2];
+        #pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            k[i] = 2 * tid + i < f ? s.mass[kSort + 2 * tid + i] : 0;
+            w[i] = 2 * tid + i < f ? weight(key_value(k[i]), row.m, row.c) : 0.0;
+        }
+        const double incl1 = wave_scan_f64(w[0] + w[1]), incl0 = incl1 - w[1];
+        auto reached = [&](int i, double incl) {
+            return 2 * tid + i < f && (by_count ? r.count + (2 * tid + i + 1) : r.mass + incl) >= target;
+        };
+        const bool hit0 = reached(0, incl0), hit = hit0 || reached(1, incl1);
         const unsigned long long hm = __ballot(hit);
-        const int l = hm ? __ffsll((long long)hm) - 1 : f - 1;
+        const int l = hm ? __ffsll((long long)hm) - 1 : (f - 1) >> 1, i = hm ? !hit0 : (f - 1) & 1;
         if (tid == l) {
-            s.key[0] = k;
-            s.res[0] = r.mass + incl;
-            s.res[1] = r.count + tid + 1;
+            s.key[0] = i ? k[1] : k[0];
+            s.res[0] = r.mass + (i ? incl1 : incl0);
+            s.res[1] = r.count + (2 * tid + i + 1);
         }
     }
     __syncthreads();
@@ -410,8 +447,9 @@ __device__ __forceinline__ Heads load_heads(const char *rec0, int n_chunks) {
     h.total = (int)group_sum<64>(total);   // (exact: at most 2^16)
     return h;
 }
-// the listed keys of all chunks into LDS, a wave a chunk (n[], offset by the sums before)
-__device__ __forceinline__ void load_list(SampleLds &s, const char *rec0, int n_chunks, const uint32_t (&n)[2]) {
+// the listed keys of all chunks into LDS, a wave a chunk (n[], offset by the sums before); f(key) for each
+template <typename F>
+__device__ __forceinline__ void load_list(SampleLds &s, const char *rec0, int n_chunks, const uint32_t (&n)[2], F f) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int off[2];
     const double i0 = wave_scan_f64((double)n[0]), i1 = wave_scan_f64((double)n[1]);
@@ -420,7 +458,11 @@ __device__ __forceinline__ void load_list(SampleLds &s, const char *rec0, int n_
     for (int c = wave; c < n_chunks; c += kThreads / 64) {
         const int nc = __builtin_amdgcn_readlane((int)(c < 64 ? n[0] : n[1]), c & 63);
         const int at = __builtin_amdgcn_readlane(c < 64 ? off[0] : off[1], c & 63);
-        for (int i = lane; i < nc; i += 64) s.list[at + i] = get64(rec0 + (size_t)c * kSampleRecord + kHead + 8 * i);
+        for (int i = lane; i < nc; i += 64) {
+            const uint64_t k = get64(rec0 + (size_t)c * kSampleRecord + kHead + 8 * i);
+            s.list[at + i] = k;
+            f(k);
+        }
     }
 }
 
@@ -482,102 +524,90 @@ __device__ __forceinline__ int draw(const Row<T> &row, uint64_t t, double u) {
     return s.num[1] != 0x7fffffff ? s.num[1] : s.num[2];
 }
 
-// A row with a small top-k, all candidates in the list (n of them, the k-th largest among them).
+// A row with a small top-k, all candidates in the list (n of them, the k-th largest among them), and counted in cnt[]
+// by bins of 1/8 below the maximum, the last bin open.
 template <typename T>
 __device__ __forceinline__ void finish_list(const Row<T> &row, const SampleArgs &a, int b, size_t r, int n) {
     SampleLds &s = lds();
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, k = min(a.top_k[b], n);
-    constexpr int kSort = 512;
     uint64_t *some = s.mass, *sorted = s.mass + kSort;
-    // down to few: by bins of 1/8 below the maximum, or, where those hold too many, by narrowing to the k-th
-    uint64_t t = 0;
-    int n_some = n;
-    if (n > kSort / 2) {
-        const float mb = floorf(row.m * 8.f);
-        if (tid < kBins) s.cnt[tid] = 0;
-        if (tid == 0) s.num[3] = n;
-        __syncthreads();
-        for (int i = tid; i < n; i += kThreads) atomicAdd(&s.cnt[(int)fminf(mb - floorf(key_value(s.list[i]) * 8.f), kBins - 1)], 1u);
-        __syncthreads();
-        if (wave == 0) {
-            double before;
-            const int j = first_reaching([&](int i) { return (double)s.cnt[i]; }, (double)k, &before);
-            if (lane == 0) {
-                s.num[0] = j;
-                s.num[1] = (int)before + (int)s.cnt[j];
-            }
-        }
-        __syncthreads();
-        n_some = s.num[1];
-        t = argmax_key((mb - (float)s.num[0]) * 0.125f, 0) & ((uint64_t)0xffffffffu << 32);
-        if (s.num[0] == kBins - 1) t = 0, n_some = n;
-        __syncthreads();
-        if (n_some > kSort) {
-            Range all = {0, ~(uint64_t)0, 0.0, 0.0};
-            t = n > k ? select<false>(row, all, true, (double)k, n) : 0;
+    // down to few: the bins that hold k, or, where those hold too many, down to the k-th itself
+    if (wave == 0) {
+        double before;
+        const int j = first_reaching([&](int i) { return (double)s.cnt[i]; }, (double)k, &before);
+        if (lane == 0) {
+            s.num[0] = j;
+            s.num[1] = (int)before + (int)s.cnt[j];
+            s.num[2] = 0;
+            s.num[3] = n;
         }
     }
-    if (tid == 0) s.num[2] = 0;
     __syncthreads();
+    uint64_t t = 0;
+    if (s.num[0] < kBins - 1) t = argmax_key((floorf(row.m * 8.f) - (float)s.num[0]) * 0.125f, 0) & ((uint64_t)0xffffffffu << 32);
+    if (s.num[1] > kSort) {
+        __syncthreads();
+        Range all = {0, ~(uint64_t)0, 0.0, 0.0};
+        t = n > k ? select<false>(row, all, true, (double)k, n) : 0;
+        if (tid == 0) s.num[2] = 0;
+        __syncthreads();
+    }
     for (int i = tid; i < n; i += kThreads)
         if (s.list[i] >= t) some[atomicAdd(&s.num[2], 1)] = s.list[i];
     __syncthreads();
-    n_some = s.num[2];   // k of them at least, 512 at most
-    static_assert(2 * kSort <= kThreads, "two threads an entry");
-    {
-        const int e = tid >> 1, half = tid & 1;
-        const uint64_t mine = e < n_some ? some[e] : 0;
-        int rank = 0;
-        for (int j = half; j < n_some; j += 2) rank += some[j] > mine ? 1 : 0;
-        rank += __shfl_xor(rank, 1);
-        if (e < n_some && half == 0) sorted[rank] = mine;
-    }
+    sort_down(some, sorted, s.num[2]);   // k of them at least, 512 at most
     __syncthreads();
-    // from here on one wave, two entries a lane in order
-    if (wave != 0) return;
+    // one wave applies the filters, two entries a lane in order
     static_assert(kListK <= 128, "two a lane");
-    uint64_t key[2];
-    double w[2];
-    #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const bool in = 2 * lane + i < k;
-        key[i] = in ? sorted[2 * lane + i] : 0;
-        w[i] = in ? weight(key_value(key[i]), row.m, row.c) : 0.0;
-    }
-    const double incl = wave_scan_f64(w[0] + w[1]), total = read_lane_f64(incl, 63);
-    const double before[2] = {incl - (w[0] + w[1]), incl - w[1]};
-    bool keep[2];
-    #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        keep[i] = 2 * lane + i < k && (a.top_p[b] >= 1.0 || before[i] < a.top_p[b] * total) && w[i] >= a.min_p[b];
-        w[i] = keep[i] ? w[i] : 0.0;
-    }
-    const double z = __longlong_as_double((long long)wave_fold_u64(f64_bits(w[0] + w[1]), add_f64_bits));
-    const int kept = (int)__popcll(__ballot(keep[0])) + (int)__popcll(__ballot(keep[1]));   // a prefix
-    const double inv = 1.0 / z, target = a.tok ? (double)a.u[r] * z : 0.0;
-    int v[2];
-    double upto[2] = {0.0, 0.0};   // running mass in index order, summed in the order of the values
-    #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        v[i] = key_index(key[i]);
-        if (keep[i] && a.probs) store_agent(a.probs + r * row.V + v[i], (float)(w[i] * inv));
+    if (wave == 0) {
+        uint64_t key[2];
+        double w[2];
+        #pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const bool in = 2 * lane + i < k;
+            key[i] = in ? sorted[2 * lane + i] : 0;
+            w[i] = in ? weight(key_value(key[i]), row.m, row.c) : 0.0;
+        }
+        const double incl = wave_scan_f64(w[0] + w[1]), total = read_lane_f64(incl, 63);
+        const double before[2] = {incl - (w[0] + w[1]), incl - w[1]};
+        bool keep[2];
+        #pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            keep[i] = 2 * lane + i < k && (a.top_p[b] >= 1.0 || before[i] < a.top_p[b] * total) && w[i] >= a.min_p[b];
+            w[i] = keep[i] ? w[i] : 0.0;
+        }
+        const double z = __longlong_as_double((long long)wave_fold_u64(f64_bits(w[0] + w[1]), add_f64_bits));
+        const int kept = (int)__popcll(__ballot(keep[0])) + (int)__popcll(__ballot(keep[1]));   // a prefix
+        const double inv = 1.0 / z;
+        #pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            if (keep[i] && a.probs) store_agent(a.probs + r * row.V + key_index(key[i]), (float)(w[i] * inv));
+            s.list[2 * lane + i] = f64_bits(w[i]);
+            s.cnt[2 * lane + i] = (uint32_t)key_index(key[i]);
+        }
+        if (lane == 0) {
+            s.num[0] = kept;
+            s.num[1] = 0x7fffffff;
+            s.num[2] = -1;
+            s.res[0] = a.tok ? (double)a.u[r] * z : 0.0;
+        }
     }
     if (!a.tok) return;
-    for (int j = 0; j < kept; ++j) {
-        const int vj = __builtin_amdgcn_readlane(v[j & 1], j >> 1);
-        const double wj = read_lane_f64(w[j & 1], j >> 1);
-        #pragma unroll
-        for (int i = 0; i < 2; ++i) upto[i] += vj <= v[i] ? wj : 0.0;
+    __syncthreads();
+    // the running mass up to each entry in index order, eight threads an entry
+    const int kept = s.num[0], e = tid >> 3, part = tid & 7;
+    const uint32_t v = s.cnt[e];
+    double upto = 0.0;
+    for (int j = part; j < kept; j += 8) upto += s.cnt[j] <= v ? bits_f64(s.list[j]) : 0.0;
+    upto += __shfl_xor(upto, 1);
+    upto += __shfl_xor(upto, 2);
+    upto += __shfl_xor(upto, 4);
+    if (e < kept && part == 0 && s.list[e] != 0) {
+        if (upto > s.res[0]) atomicMin(&s.num[1], (int)v);
+        atomicMax(&s.num[2], (int)v);
     }
-    int first = 0x7fffffff, last = -1;
-    #pragma unroll
-    for (int i = 0; i < 2; ++i)
-        if (w[i] > 0.0) {
-            if (upto[i] > target) first = min(first, v[i]);
-            last = max(last, v[i]);
-        }
-    const int f = (int)(0xffffffffu - wave_max_u32(0xffffffffu - (uint32_t)first)), l = (int)wave_max_u32((uint32_t)(last + 1)) - 1;
-    if (lane == 0) a.tok[r] = f != 0x7fffffff ? f : l;
+    __syncthreads();
+    if (tid == 0) a.tok[r] = s.num[1] != 0x7fffffff ? s.num[1] : s.num[2];
 }
 
 // kept mass of every chunk into c_mass[]; returns their sum
@@ -696,7 +726,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(const SampleArgs a)
     const int rows = a.B * a.T, r = blockIdx.x % rows, chunk = blockIdx.x / rows, b = r / a.T;
     const int top_k = a.top_k[b];
     const bool listed = top_k > 0 && top_k <= kListK;
-    const bool binned = !listed && (top_k > 0 || a.top_p[b] < 1.0);
+    const bool binned = !listed && (top_k > 0 || a.top_p[b] < 1.0 || a.min_p[b] > 0.0);
     Row<T> row = row_of<T>(a, r);
     char *rec0 = a.records + (size_t)r * a.n_chunks * kSampleRecord, *rec = rec0 + (size_t)chunk * kSampleRecord;
 
@@ -804,6 +834,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(const SampleArgs a)
         put64(rec + 8, (uint64_t)__float_as_uint(edge) | (uint64_t)n_out << 32);
         put64(rec + 16, f64_bits(mass));
     }
+    if (listed && tid < kBins) s.cnt[tid] = 0;   // (its last reader is behind a barrier)
     if (!row_last(a, r, s)) return;
 
     // ---- the row's last workgroup ----
@@ -822,7 +853,10 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(const SampleArgs a)
         // What a chunk left out lies below its edge: harmless where the k-th candidate does not.
         bool complete = h.total <= kList && !(h.worst == INFINITY);
         if (complete) {
-            load_list(s, rec0, a.n_chunks, h.n);
+            const float rb = floorf(m * 8.f);
+            load_list(s, rec0, a.n_chunks, h.n, [&](uint64_t k) {
+                atomicAdd(&s.cnt[(int)fminf(rb - floorf(key_value(k) * 8.f), kBins - 1)], 1u);
+            });
             __syncthreads();
             if (h.left) {
                 int above = 0;
@@ -848,6 +882,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(const SampleArgs a)
                 if (lane + 64 * i < a.n_chunks) {
                     s.c_mass[lane + 64 * i] = cm[i];
                     s.c_max[lane + 64 * i] = h.max[i];
+                    s.c_fix[lane + 64 * i] = f64_bits(h.max[i] == -INFINITY ? 0.0 : kBinUnit * weight(h.max[i], m, row.c));
                 }
         }
         out.mass = __longlong_as_double((long long)wave_fold_u64(f64_bits(cm[0] + cm[1]), add_f64_bits));
@@ -858,49 +893,49 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(const SampleArgs a)
             if (h.no_bins) {
                 out.mode = kRowSlow;
             } else {
-                // the row's bins: bin j of a chunk whose maximum lies d bins lower is the row's j + d
-                const int j = tid & (kBins - 1);
-                const float rb = floorf(m * 8.f);
-                double w = 0.0;
-                uint32_t n = 0;
-                #pragma unroll 4
-                for (int k = tid / kBins; k < a.n_chunks; k += kThreads / kBins) {
-                    const float top = s.c_max[k], d = rb - floorf(top * 8.f);
-                    const bool in = top > -INFINITY && (float)j >= d;
-                    const char *q = rec0 + (size_t)k * kSampleRecord + kHead;
-                    const int jc = in ? j - (int)d : 0;
-                    const double x = (double)get64(q + 8 * jc);
-                    w += in ? x * kBinUnit * weight(top, m, row.c) : 0.0;
-                    if (top_k > 0) {
-                        const uint32_t y = __hip_atomic_load(reinterpret_cast<uint32_t *>(const_cast<char *>(q) + 8 * kBins + 4 * jc),
-                                                             __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                        n += in ? y : 0;
+                out.mode = kRowCut;
+                const float rb = floorf(m * 8.f), low = (rb - (float)(kBins - 1)) * 0.125f;   // low: the bins' end
+                out.target = top_k > 0 ? (double)top_k : a.top_p[b] < 1.0 ? a.top_p[b] * out.mass : -1.0;
+                out.hi = -INFINITY;
+                if (out.target >= 0.0) {
+                    // the row's bins: bin j of a chunk whose maximum lies d bins lower is the row's j + d
+                    const int j = tid & (kBins - 1);
+                    double w = 0.0;
+                    uint32_t n = 0;
+                    #pragma unroll 4
+                    for (int k = tid / kBins; k < a.n_chunks; k += kThreads / kBins) {
+                        const float top = s.c_max[k], d = rb - floorf(top * 8.f);
+                        const bool in = top > -INFINITY && (float)j >= d;
+                        const char *q = rec0 + (size_t)k * kSampleRecord + kHead;
+                        const int jc = in ? j - (int)d : 0;
+                        const double x = (double)get64(q + 8 * jc);
+                        w += in ? x * bits_f64(s.c_fix[k]) : 0.0;
+                        if (top_k > 0) {
+                            const uint32_t y = __hip_atomic_load(reinterpret_cast<uint32_t *>(const_cast<char *>(q) + 8 * kBins + 4 * jc),
+                                                                 __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                            n += in ? y : 0;
+                        }
                     }
-                }
-                s.list[tid] = f64_bits(top_k > 0 ? (double)n : w);
-                __syncthreads();
-                if (wave == 0) {
+                    s.list[tid] = f64_bits(top_k > 0 ? (double)n : w);
+                    __syncthreads();
+                    if (wave != 0) return;
                     auto bin = [&](int i) {
                         return bits_f64(s.list[i]) + bits_f64(s.list[i + kBins]) + bits_f64(s.list[i + 2 * kBins]) + bits_f64(s.list[i + 3 * kBins]);
                     };
-                    const double target = top_k > 0 ? (double)top_k : a.top_p[b] * out.mass;
                     double before;
-                    const int i = first_reaching(bin, target, &before);
-                    const bool in = before + bin(i) >= target;   // else it is reached below the last bin
-                    out.lo = in ? (rb - (float)i) * 0.125f : -INFINITY;
-                    out.hi = (rb - (in ? (float)(i - 1) : (float)(kBins - 1))) * 0.125f;
-                    // where min-p ends above it, only that counts
-                    const float tv = key_value(out.t);
-                    if (out.t > 0 && tv >= out.hi) out.lo = out.hi = tv;
-                    out.mode = kRowCut;
-                    out.target = target;
-                    if (lane == 0) a.rows[r] = out;
+                    const int i = first_reaching(bin, out.target, &before);
+                    const bool in = before + bin(i) >= out.target;   // else it is reached below the last bin
+                    out.lo = in ? (rb - (float)i) * 0.125f : -3.402823466e38f;   // (an entry of -inf has no mass)
+                    out.hi = in ? (rb - (float)(i - 1)) * 0.125f : low;
                 }
-                return;
+                // where min-p ends above it, only that counts: its bin's entries down to it
+                const float tv = key_value(out.t);
+                if (out.t > 0 && tv >= out.hi) {
+                    out.lo = tv;
+                    out.hi = fmaxf((floorf(tv * 8.f) + 1.f) * 0.125f, low);
+                    out.target = -1.0;
+                }
             }
-        } else if (min_p > 0.0) {
-            out.lo = out.hi = key_value(out.t);
-            out.mode = kRowCut;
         } else if (a.tok) {
             const int v = draw(row, 0, (double)a.u[r]);
             if (tid == 0) a.tok[r] = v;
@@ -927,27 +962,38 @@ __global__ __launch_bounds__(kThreads, 8) void sample_cut_kernel(const SampleArg
     const int e0 = chunk * kSampleChunk + tid * kRun;
     float x[kRun];
     load_run(row.x, e0, a.V, x);
-    if (tid == 0) s.num[0] = 0, s.num[1] = 0;
-    __syncthreads();
+    // what lies above the range: the chunk's bins up to there (read before the keys take their place)
     double above = 0.0;
-    int n_above = 0;
+    uint32_t n_above = 0;
+    if (tid < 64) {
+        const float top = __uint_as_float((uint32_t)get64(rec)), ups = floorf(top * 8.f) - res.hi * 8.f;   // the last bin above
+        uint64_t q = 0;
+        #pragma unroll
+        for (int i = 0; i < kBins / 64; ++i) {
+            const uint64_t y = get64(rec + kHead + 8 * (lane + 64 * i));
+            const bool up = (float)(lane + 64 * i) <= ups;
+            q += up ? y : 0;
+            if (a.top_k[b] > 0) {
+                const uint32_t z = __hip_atomic_load(reinterpret_cast<uint32_t *>(rec + kHead + 8 * kBins) + lane + 64 * i, __ATOMIC_RELAXED,
+                                                     __HIP_MEMORY_SCOPE_AGENT);
+                n_above += up ? z : 0;
+            }
+        }
+        q = wave_fold_u64(q, [](uint64_t x, uint64_t y) { return x + y; });
+        n_above = (uint32_t)group_sum<64>((float)n_above);   // (exact: at most 8192)
+        above = q ? (double)q * kBinUnit * weight(top, res.m, row.c) : 0.0;
+    }
+    if (tid == 0) s.num[0] = 0;
+    __syncthreads();
     #pragma unroll
-    for (int i = 0; i < kRun; ++i) {
-        const bool up = x[i] >= res.hi && e0 + i < a.V;
-        if (__any(up)) above += up ? weight(x[i], res.m, row.c) : 0.0;
-        n_above += up ? 1 : 0;
+    for (int i = 0; i < kRun; ++i)
         if (x[i] < res.hi && x[i] >= res.lo && e0 + i < a.V) {
             const int p = atomicAdd(&s.num[0], 1);
             if (p < kEmit) put64(rec + kHead + 8 * p, argmax_key(x[i], e0 + i));
         }
-    }
-    if (a.top_k[b] > 0) {
-        const int n = (int)group_sum<64>((float)n_above);
-        if (lane == 0 && n > 0) atomicAdd(&s.num[1], n);
-    }
-    above = block_sum(above, s.part);   // (its barrier stands behind the atomics)
+    __syncthreads();
     if (tid == 0) {
-        put64(rec, (uint64_t)(uint32_t)s.num[0] | (uint64_t)(uint32_t)s.num[1] << 32);
+        put64(rec, (uint64_t)(uint32_t)s.num[0] | (uint64_t)n_above << 32);
         put64(rec + 16, f64_bits(above));
     }
     if (!row_last(a, r, s)) return;
@@ -979,11 +1025,11 @@ __global__ __launch_bounds__(kThreads, 8) void sample_cut_kernel(const SampleArg
     }
     mass = __longlong_as_double((long long)wave_fold_u64(f64_bits(mass), add_f64_bits));
     count = __longlong_as_double((long long)wave_fold_u64(f64_bits(count), add_f64_bits));
-    load_list(s, rec0, a.n_chunks, n);
+    load_list(s, rec0, a.n_chunks, n, [](uint64_t) {});
     if (tid == 0) s.num[3] = all;
     __syncthreads();
     uint64_t t = res.t;
-    if (res.lo < res.hi) {
+    if (res.target >= 0.0) {
         const uint64_t edge = (uint64_t)0xffffffffu << 32;
         Range g = {argmax_key(res.lo, 0) & edge, (argmax_key(res.hi, 0) & edge) - 1, mass, count};
         t = max(t, select<false>(row, g, a.top_k[b] > 0, res.target, all));
