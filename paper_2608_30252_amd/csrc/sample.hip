@@ -125,6 +125,13 @@ __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
 __device__ __forceinline__ uint64_t f64_bits(double v) { return (uint64_t)__double_as_longlong(v); }
 __device__ __forceinline__ double bits_f64(uint64_t v) { return __longlong_as_double((long long)v); }
 
+// what is the same in every lane, in scalar registers (64 vector registers are all that two workgroups per CU leave)
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ float uniform(float v) { return __uint_as_float(uniform(__float_as_uint(v))); }
+__device__ __forceinline__ uint64_t uniform(uint64_t v) { return (uint64_t)uniform((uint32_t)(v >> 32)) << 32 | uniform((uint32_t)v); }
+__device__ __forceinline__ double uniform(double v) { return bits_f64(uniform(f64_bits(v))); }
+
 // A chunk's record in the workspace: a header of 32 bytes, then keys, or the bins' masses and counts.
 //   first launch:  maximum, flags | edge, keys | mass          second: count and keys | mass above the range
 constexpr int kHead = 32;
@@ -135,6 +142,8 @@ struct SampleLds {
     uint64_t list[kList];       // gathered keys
     uint64_t mass[kBuckets];    // histogram: masses (integers), or doubles' bits
     uint32_t cnt[kBuckets];
+    double bucket_mass[kBins];
+    uint32_t bucket_cnt[kBins];
     double c_mass[kSampleMaxChunks];    // per chunk: kept mass; against the row's maximum
     uint64_t c_fix[kSampleMaxChunks];   // the same of listed entries, in units of 2^-50
     float c_max[kSampleMaxChunks];
@@ -172,6 +181,15 @@ __device__ __forceinline__ double block_scan(double v, double *part) {
     return s;
 }
 
+// The workgroup's least `first` and greatest `last`, where both rise with the thread (0x7fffffff, -1: none): one lane of
+// a wave for each (an LDS atomic of 64 lanes on one word takes as long as 64).
+__device__ __forceinline__ void first_and_last(int first, int last, int *least, int *greatest) {
+    const int lane = threadIdx.x & 63;
+    const unsigned long long f = __ballot(first != 0x7fffffff), l = __ballot(last >= 0);
+    if (f && lane == __ffsll((long long)f) - 1) atomicMin(least, first);
+    if (l && lane == 63 - __clzll((long long)l)) atomicMax(greatest, last);
+}
+
 // One row, by one workgroup.
 template <typename T> struct Row {
     const T *x;
@@ -204,39 +222,77 @@ struct Range {
     double mass, count;   // above hi
 };
 
-// Finds in the histogram mass/cnt (nb buckets, highest keys last; masses as doubles' bits) the first bucket from the
-// top with which `target` of the measure is reached on top of what r holds, or the last that is not empty.  Returns
-// it (-1: all are empty) and adds what lies above it to r.  *n: its entries.
-__device__ __forceinline__ int crossing(SampleLds &s, int nb, bool by_count, double target, Range &r, int *n) {
-    const int tid = threadIdx.x, b0 = nb - 1 - 2 * tid, b1 = b0 - 1;   // two buckets a thread, from the top
-    const double m0 = b0 >= 0 ? bits_f64(s.mass[b0]) : 0.0, m1 = b1 >= 0 ? bits_f64(s.mass[b1]) : 0.0;
-    const double n0 = b0 >= 0 ? (double)s.cnt[b0] : 0.0, n1 = b1 >= 0 ? (double)s.cnt[b1] : 0.0;
-    if (tid == 0) s.num[0] = 0x7fffffff, s.num[1] = -1;
-    const double em = block_scan(m0 + m1, s.part), en = block_scan(n0 + n1, s.part2);
-    const double before = by_count ? r.count + en : r.mass + em, v0 = by_count ? n0 : m0, v1 = by_count ? n1 : m1;
-    int at = 0x7fffffff, some = -1;
-    if (n1 > 0.0) some = 2 * tid + 1;
-    else if (n0 > 0.0) some = 2 * tid;
-    if (n1 > 0.0 && before + v0 + v1 >= target) at = 2 * tid + 1;
-    if (n0 > 0.0 && before + v0 >= target) at = 2 * tid;
-    if (at != 0x7fffffff) atomicMin(&s.num[0], at);
-    if (some >= 0) atomicMax(&s.num[1], some);
-    __syncthreads();
-    const int pos = s.num[0] != 0x7fffffff ? s.num[0] : s.num[1];
-    if (pos >= 0 && (pos >> 1) == tid) {
-        const bool second = pos & 1;
-        s.res[0] = em + (second ? m0 : 0.0);
-        s.res[1] = en + (second ? n0 : 0.0);
-        s.num[2] = (int)(second ? n1 : n0);
+// Finds in the histogram mass/cnt (256 buckets of 8 parts each, the highest keys last; masses as integers of `unit`)
+// the first bucket from the top with which `target` of the measure is reached on top of what r holds, or the last that
+// is not empty.  PARTS: the part of it.  Returns its number and adds what lies above it to r; *n: its entries.
+template <bool PARTS>
+__device__ __forceinline__ int crossing(SampleLds &s, double unit, bool by_count, double target, Range &r, int *n) {
+    constexpr int P = kBuckets / kBins, Q = kBins / 64;
+    const int tid = threadIdx.x;
+    if (tid < kBins) {
+        uint64_t m = 0;
+        uint32_t c = 0;
+        #pragma unroll
+        for (int p = 0; p < P; ++p) m += s.mass[tid * P + p], c += s.cnt[tid * P + p];
+        s.bucket_mass[kBins - 1 - tid] = (double)m * unit;
+        s.bucket_cnt[kBins - 1 - tid] = c;
     }
     __syncthreads();
-    if (pos < 0) return -1;
-    r.mass += s.res[0];
-    r.count += s.res[1];
-    *n = s.num[2];
-    const int b = nb - 1 - pos;
+    if (tid < 64) {   // four buckets a lane, from the top
+        double m[Q], c[Q], sm = 0.0, sc = 0.0;
+        #pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            m[q] = s.bucket_mass[tid * Q + q];
+            c[q] = (double)s.bucket_cnt[tid * Q + q];
+            sm += m[q];
+            sc += c[q];
+        }
+        double um = r.mass + (wave_scan_f64(sm) - sm), uc = r.count + (wave_scan_f64(sc) - sc);   // above lane's first
+        double hm = 0.0, hc = 0.0, lm = 0.0, lc = 0.0;
+        int hit = -1, last = -1;
+        #pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            if (c[q] > 0.0) {
+                last = q, lm = um, lc = uc;
+                if (hit < 0 && (by_count ? uc + c[q] : um + m[q]) >= target) hit = q, hm = um, hc = uc;
+            }
+            um += m[q];
+            uc += c[q];
+        }
+        const unsigned long long hits = __ballot(hit >= 0), some = __ballot(last >= 0);
+        const int l = hits ? __ffsll((long long)hits) - 1 : some ? 63 - __clzll((long long)some) : 0;
+        if (tid == l) {
+            int at = kBins - 1 - (tid * Q + (hits ? hit : max(last, 0)));
+            double am = hits ? hm : lm, ac = hits ? hc : lc;
+            int in = (int)s.bucket_cnt[kBins - 1 - at];
+            if constexpr (PARTS) {
+                int part = -1;
+                double pm = 0.0, pc = 0.0;
+                for (int p = P - 1; p >= 0; --p) {
+                    const double xc = (double)s.cnt[at * P + p], xm = (double)s.mass[at * P + p] * unit;
+                    if (xc > 0.0) {
+                        part = p, pm = am, pc = ac;
+                        if ((by_count ? ac + xc : am + xm) >= target) break;
+                    }
+                    am += xm;
+                    ac += xc;
+                }
+                at = at * P + max(part, 0);
+                am = pm;
+                ac = pc;
+                in = (int)s.cnt[at];
+            }
+            s.num[0] = at;
+            s.num[2] = in;
+            s.res[0] = am;
+            s.res[1] = ac;
+        }
+    }
     __syncthreads();
-    return b;
+    r.mass = uniform(s.res[0]);
+    r.count = uniform(s.res[1]);
+    *n = uniform(s.num[2]);
+    return uniform(s.num[0]);   // (what follows writes none of these before a barrier)
 }
 
 // n different keys (512 at most) into descending order: each counts the larger ones, by 8 threads or 2
@@ -280,11 +336,21 @@ __device__ __forceinline__ uint64_t select(const Row<T> &row, Range &r, bool by_
         }
         // The keys of the list that are still in the range: few enough are put in order.
         if (in_list && n <= kFinal) break;
-        if (in_list) {   // to the keys that are there (equal values differ in a few bits of their indices only)
-            if (tid == 0) s.key[0] = ~(uint64_t)0, s.key[1] = 0;
-            __syncthreads();
+        for (int b = tid; b < kBuckets; b += kThreads) s.mass[b] = 0, s.cnt[b] = 0;
+        if (tid == 0) s.key[0] = ~(uint64_t)0, s.key[1] = 0;
+        __syncthreads();
+        const double unit = in_list ? kBinUnit : kRowUnit, per = 1.0 / unit;
+        auto count = [&](int at, float x) {
+            atomicAdd(&s.cnt[at], 1u);
+            atomicAdd((unsigned long long *)&s.mass[at], (unsigned long long)(weight(x, row.m, row.c) * per + 0.5));
+        };
+        int sh, at;
+        if (in_list) {
+            // To the keys that are there: equal values differ in a few bits of their indices only.  Then 256 buckets,
+            // each in 8 parts by lane: equal values go to one bucket.
+            const int all = uniform(s.num[3]);
             uint64_t lo = ~(uint64_t)0, hi = 0;
-            const int all = s.num[3];
+            #pragma unroll 1
             for (int i = tid; i < all; i += kThreads) {
                 const uint64_t k = s.list[i];
                 if (k >= r.lo && k <= r.hi) lo = min(lo, k), hi = max(hi, k);
@@ -296,43 +362,39 @@ __device__ __forceinline__ uint64_t select(const Row<T> &row, Range &r, bool by_
                 atomicMax((unsigned long long *)&s.key[1], (unsigned long long)hi);
             }
             __syncthreads();
-            r.lo = s.key[0];
-            r.hi = s.key[1];
-        }
-        int sh = 64 - __clzll((long long)(r.hi - r.lo)) - 11;   // 2048 buckets (a range of one key holds one entry)
-        if (sh < 0) sh = 0;
-        for (int b = tid; b < kBuckets; b += kThreads) s.mass[b] = 0, s.cnt[b] = 0;
-        __syncthreads();
-        const double unit = in_list ? kBinUnit : kRowUnit, per = 1.0 / unit;
-        auto count = [&](uint64_t k, float x) {
-            if (k >= r.lo && k <= r.hi) {
-                const int b = (int)((k - r.lo) >> sh);
-                atomicAdd(&s.cnt[b], 1u);
-                atomicAdd((unsigned long long *)&s.mass[b], (unsigned long long)(weight(x, row.m, row.c) * per + 0.5));
+            r.lo = uniform(s.key[0]);
+            r.hi = uniform(s.key[1]);
+            sh = max(64 - __clzll((long long)(r.hi - r.lo)) - 8, 0);
+            #pragma unroll 1
+            for (int i = tid; i < all; i += kThreads) {
+                const uint64_t k = s.list[i];
+                if (k >= r.lo && k <= r.hi) count((int)((k - r.lo) >> sh) * (kBuckets / kBins) + (tid & 7), key_value(k));
             }
-        };
-        if (in_list) {
-            const int all = s.num[3];
-            for (int i = tid; i < all; i += kThreads) count(s.list[i], key_value(s.list[i]));
-        } else if constexpr (STREAM) {
-            row.each([&](float x, int i) { count(argmax_key(x, i), x); });
+            __syncthreads();
+            at = crossing<false>(s, unit, by_count, target, r, &n);
+        } else {
+            sh = max(64 - __clzll((long long)(r.hi - r.lo)) - 11, 0);   // 2048 buckets (a range of one key holds one entry)
+            if constexpr (STREAM)
+                row.each([&](float x, int i) {
+                    const uint64_t k = argmax_key(x, i);
+                    if (k >= r.lo && k <= r.hi) count((int)((k - r.lo) >> sh), x);
+                });
+            __syncthreads();
+            at = crossing<true>(s, unit, by_count, target, r, &n);
         }
-        __syncthreads();
-        for (int b = tid; b < kBuckets; b += kThreads) s.mass[b] = f64_bits((double)s.mass[b] * unit);
-        __syncthreads();
-        const int b = crossing(s, kBuckets, by_count, target, r, &n);
-        const uint64_t lo = r.lo + ((uint64_t)b << sh);
-        r.hi = min(r.hi, lo + (((uint64_t)1 << sh) - 1));
+        const uint64_t lo = r.lo + ((uint64_t)at << sh);
+        r.hi = lo + min(r.hi - lo, ((uint64_t)1 << sh) - 1);   // (no sum past 64 bits)
         r.lo = lo;
     }
     // at most 128: ordered by rank, then wave 0 sums them in order, two a lane
-    if (tid == 0) s.num[2] = 0;
+    if (tid == 0) s.num[1] = 0;
     __syncthreads();
-    const int all = s.num[3];
+    const int all = uniform(s.num[3]);
+    #pragma unroll 1
     for (int i = tid; i < all; i += kThreads)
-        if (s.list[i] >= r.lo && s.list[i] <= r.hi) s.mass[atomicAdd(&s.num[2], 1)] = s.list[i];
+        if (s.list[i] >= r.lo && s.list[i] <= r.hi) s.mass[atomicAdd(&s.num[1], 1)] = s.list[i];
     __syncthreads();
-    const int f = s.num[2];
+    const int f = uniform(s.num[1]);
     sort_down(s.mass, s.mass + kSort, f);
     if (tid == 0 && f == 0) {   // nothing there (a mass reached only but for rounding): all above the range
         s.key[0] = r.hi + 1;
@@ -362,9 +424,9 @@ __device__ __forceinline__ uint64_t select(const Row<T> &row, Range &r, bool by_
         }
     }
     __syncthreads();
-    r.mass = s.res[0];
-    r.count = s.res[1];
-    const uint64_t t = s.key[0];
+    r.mass = uniform(s.res[0]);
+    r.count = uniform(s.res[1]);
+    const uint64_t t = uniform(s.key[0]);
     __syncthreads();
     return t;
 }
@@ -439,12 +501,12 @@ __device__ __forceinline__ Heads load_heads(const char *rec0, int n_chunks) {
         all |= h.flags[i];
         total += (float)h.n[i];
     }
-    h.m = group_max<64>(m);
-    h.worst = group_max<64>(worst);
+    h.m = uniform(group_max<64>(m));
+    h.worst = uniform(group_max<64>(worst));
     h.nan = __any(all & kNaN);
     h.no_bins = __any(all & kNoBins);
     h.left = __any(all & kLeft);
-    h.total = (int)group_sum<64>(total);   // (exact: at most 2^16)
+    h.total = uniform((int)group_sum<64>(total));   // (exact: at most 2^16)
     return h;
 }
 // the listed keys of all chunks into LDS, a wave a chunk (n[], offset by the sums before); f(key) for each
@@ -496,8 +558,8 @@ __device__ __forceinline__ int draw(const Row<T> &row, uint64_t t, double u) {
         }
     }
     __syncthreads();
-    const int e0 = s.num[0] * kSampleChunk + tid * kRun;
-    const double target = s.res[0];
+    const int e0 = uniform(s.num[0]) * kSampleChunk + tid * kRun;
+    const double target = uniform(s.res[0]);
     float x[kRun];
     load_run(row.x, e0, row.V, x);
     double w[kRun], sum = 0.0;
@@ -518,10 +580,16 @@ __device__ __forceinline__ int draw(const Row<T> &row, uint64_t t, double u) {
         for (int k = 0; k <= i; ++k) upto += w[k];
         if (w[i] > 0.0 && upto > target) first = e0 + i;
     }
-    if (first != 0x7fffffff) atomicMin(&s.num[1], first);
-    if (last >= 0) atomicMax(&s.num[2], last);
+    first_and_last(first, last, &s.num[1], &s.num[2]);
     __syncthreads();
     return s.num[1] != 0x7fffffff ? s.num[1] : s.num[2];
+}
+
+// the k-th key of the list of n (seldom asked for: kept out of its callers' registers)
+__device__ __noinline__ uint64_t nth_of_list(float m, double c, int k, int n) {
+    const Row<float> row = {nullptr, 0, 0, m, c};
+    Range all = {0, ~(uint64_t)0, 0.0, 0.0};
+    return select<false>(row, all, true, (double)k, n);
 }
 
 // A row with a small top-k, all candidates in the list (n of them, the k-th largest among them), and counted in cnt[]
@@ -547,8 +615,7 @@ __device__ __forceinline__ void finish_list(const Row<T> &row, const SampleArgs 
     if (s.num[0] < kBins - 1) t = argmax_key((floorf(row.m * 8.f) - (float)s.num[0]) * 0.125f, 0) & ((uint64_t)0xffffffffu << 32);
     if (s.num[1] > kSort) {
         __syncthreads();
-        Range all = {0, ~(uint64_t)0, 0.0, 0.0};
-        t = n > k ? select<false>(row, all, true, (double)k, n) : 0;
+        t = n > k ? nth_of_list(row.m, row.c, k, n) : 0;
         if (tid == 0) s.num[2] = 0;
         __syncthreads();
     }
@@ -758,6 +825,8 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(const SampleArgs a)
         m = fmaxf(m, s.fmx[k]);
         flags |= s.flag[k];
     }
+    m = uniform(m);
+    flags = uniform(flags);
     const float mb = floorf(m * 8.f);
     if (!(fabsf(m) < 0x1p20f)) flags |= kNoBins;   // (bins of 1/8 are exact below 2^21)
     float edge = INFINITY;
@@ -950,7 +1019,9 @@ __global__ __launch_bounds__(kThreads, 8) void sample_cut_kernel(const SampleArg
     SampleLds &s = lds();
     const int tid = threadIdx.x, lane = tid & 63;
     const int rows = a.B * a.T, r = blockIdx.x % rows, chunk = blockIdx.x / rows, b = r / a.T;
-    const RowResult res = a.rows[r];
+    RowResult res = a.rows[r];
+    res.t = uniform(res.t), res.target = uniform(res.target), res.lo = uniform(res.lo), res.hi = uniform(res.hi);
+    res.m = uniform(res.m), res.mode = uniform(res.mode);
     if (res.mode != kRowCut && (res.mode != kRowSlow || chunk > 0)) return;
     Row<T> row = row_of<T>(a, r);
     row.m = res.m;
@@ -1018,12 +1089,13 @@ __global__ __launch_bounds__(kThreads, 8) void sample_cut_kernel(const SampleArg
             s.c_fix[lane + 64 * i] = 0;
         }
     }
-    const int all = (int)group_sum<64>(total);
+    const int all = uniform((int)group_sum<64>(total));
     if (__any(over) || all > kList || (a.top_k[b] > 0 && a.top_p[b] < 1.0)) {
         solve_row<T>(solve_job(a, row, r));
         return;
     }
     mass = __longlong_as_double((long long)wave_fold_u64(f64_bits(mass), add_f64_bits));
+    mass = uniform(mass);
     count = __longlong_as_double((long long)wave_fold_u64(f64_bits(count), add_f64_bits));
     load_list(s, rec0, a.n_chunks, n, [](uint64_t) {});
     if (tid == 0) s.num[3] = all;
@@ -1035,6 +1107,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_cut_kernel(const SampleArg
         t = max(t, select<false>(row, g, a.top_k[b] > 0, res.target, all));
     }
     // each chunk's kept mass: above the range, and the listed entries that stay
+    #pragma unroll 1
     for (int i = tid; i < all; i += kThreads) {
         const uint64_t k = s.list[i];
         if (k >= t)
@@ -1046,7 +1119,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_cut_kernel(const SampleArg
     #pragma unroll
     for (int i = 0; i < 2; ++i)
         if (lane + 64 * i < a.n_chunks) kept += s.c_mass[lane + 64 * i] + (double)s.c_fix[lane + 64 * i] * kBinUnit;
-    kept = __longlong_as_double((long long)wave_fold_u64(f64_bits(kept), add_f64_bits));
+    kept = uniform(__longlong_as_double((long long)wave_fold_u64(f64_bits(kept), add_f64_bits)));
     __syncthreads();
     if (tid < a.n_chunks) s.c_mass[tid] += (double)s.c_fix[tid] * kBinUnit;
     __syncthreads();
