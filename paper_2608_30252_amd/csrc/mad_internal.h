@@ -236,7 +236,7 @@ struct SampleArgs {
     char *records;         // [B * T][n_chunks] of kSampleRecord bytes
     unsigned *counters;    // line r: arrivals of row r's workgroups
     int B, T, V, n_chunks;
-    double c[kMaxB];       // log2 e / temperature
+    double c[kMaxB];       // 64 log2 e / temperature
     double top_p[kMaxB], min_p[kMaxB];
     int top_k[kMaxB];      // 0: off
 };

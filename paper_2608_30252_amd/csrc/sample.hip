@@ -44,29 +44,36 @@ constexpr int kThreads = 1024, kRun = kSampleChunk / kThreads;   // entries of a
 constexpr int kBins = 256, kBuckets = 2048, kList = 4096, kFinal = 128, kSort = 512;
 constexpr double kBinUnit = 0x1p-50, kRowUnit = 0x1p-43;   // 8192 and 2^20 weights of at most 1 fit 63 bits
 
-// 2^y for y <= 0 (y > -1000): the Taylor series of 2^f, |f| <= 1/2, to 12th order: below 2e-16 relative
-__device__ __forceinline__ double exp2_neg(double y) {
-    const double n = rint(y), f = (y - n) * 0.6931471805599453;
-    double p = 1.0 / 479001600.0;
-    p = fma(p, f, 1.0 / 39916800.0);
-    p = fma(p, f, 1.0 / 3628800.0);
-    p = fma(p, f, 1.0 / 362880.0);
-    p = fma(p, f, 1.0 / 40320.0);
-    p = fma(p, f, 1.0 / 5040.0);
-    p = fma(p, f, 1.0 / 720.0);
-    p = fma(p, f, 1.0 / 120.0);
-    p = fma(p, f, 1.0 / 24.0);
-    p = fma(p, f, 1.0 / 6.0);
-    p = fma(p, f, 0.5);
+// 2^(j / 64), 0 <= j < 64: squared up from the Taylor series at a 2^-7th of the exponent (below 2e-16 relative), at
+// compile time
+struct Exp2Table {
+    double v[64];
+    constexpr Exp2Table() : v() {
+        for (int j = 0; j < 64; ++j) {
+            const double f = 0.6931471805599453 * j / 64;   // 0 <= f < ln 2
+            double p = 1.0;
+            for (int k = 20; k > 0; --k) p = 1.0 + p * f / k;
+            v[j] = p;
+        }
+    }
+};
+__constant__ const Exp2Table kExp2 = Exp2Table();
+
+// The weight of x against the maximum m (+inf against +inf: 1), c64 = 64 log2 e / temperature: with
+// (x - m) c64 = n + f, |f| <= 1/2, it is 2^(n / 64) from the table and 2^(f / 64) by its series (to f^5: 4e-17 relative).
+// In double: half the operations of a series alone.
+__device__ __forceinline__ double weight(float x, float m, double c64, const double *table) {
+    constexpr double k1 = 0.6931471805599453 / 64, k2 = k1 * k1 / 2, k3 = k2 * k1 / 3, k4 = k3 * k1 / 4, k5 = k4 * k1 / 5;
+    const double y = fmax(((double)x - (double)m) * c64, -64000.0);   // (a NaN of inf - inf: -64000)
+    const double n = rint(y), f = y - n;
+    double p = fma(k5, f, k4);
+    p = fma(p, f, k3);
+    p = fma(p, f, k2);
+    p = fma(p, f, k1);
     p = fma(p, f, 1.0);
-    p = fma(p, f, 1.0);
-    return ldexp(p, (int)n);
-}
-// weight of x against the maximum m (+inf against +inf: 1)
-__device__ __forceinline__ double weight(float x, float m, double c) {
-    const double y = ((double)x - (double)m) * c;
-    const double w = exp2_neg(y > -1000.0 ? y : -1000.0);
-    return x == m ? 1.0 : y > -1000.0 ? w : 0.0;
+    const int i = (int)n;
+    const double w = ldexp(p * table[i & 63], i >> 6);
+    return x == m ? 1.0 : y > -64000.0 ? w : 0.0;
 }
 // the value that a key holds
 __device__ __forceinline__ float key_value(uint64_t k) {
@@ -142,6 +149,7 @@ struct SampleLds {
     uint64_t list[kList];       // gathered keys
     uint64_t mass[kBuckets];    // histogram: masses (integers), or doubles' bits
     uint32_t cnt[kBuckets];
+    double exp2[64];   // kExp2
     double bucket_mass[kBins];
     uint32_t bucket_cnt[kBins];
     double c_mass[kSampleMaxChunks];    // per chunk: kept mass; against the row's maximum
@@ -195,7 +203,7 @@ template <typename T> struct Row {
     const T *x;
     int V, n_chunks;
     float m;       // maximum
-    double c;      // log2 e / temperature
+    double c;      // 64 log2 e / temperature
 
     // f(value, index) for every entry; four chunks in flight
     template <typename F> __device__ __forceinline__ void each(F f) const {
@@ -342,7 +350,7 @@ __device__ __forceinline__ uint64_t select(const Row<T> &row, Range &r, bool by_
         const double unit = in_list ? kBinUnit : kRowUnit, per = 1.0 / unit;
         auto count = [&](int at, float x) {
             atomicAdd(&s.cnt[at], 1u);
-            atomicAdd((unsigned long long *)&s.mass[at], (unsigned long long)(weight(x, row.m, row.c) * per + 0.5));
+            atomicAdd((unsigned long long *)&s.mass[at], (unsigned long long)(weight(x, row.m, row.c, s.exp2) * per + 0.5));
         };
         int sh, at;
         if (in_list) {
@@ -408,7 +416,7 @@ __device__ __forceinline__ uint64_t select(const Row<T> &row, Range &r, bool by_
         #pragma unroll
         for (int i = 0; i < 2; ++i) {
             k[i] = 2 * tid + i < f ? s.mass[kSort + 2 * tid + i] : 0;
-            w[i] = 2 * tid + i < f ? weight(key_value(k[i]), row.m, row.c) : 0.0;
+            w[i] = 2 * tid + i < f ? weight(key_value(k[i]), row.m, row.c, s.exp2) : 0.0;
         }
         const double incl1 = wave_scan_f64(w[0] + w[1]), incl0 = incl1 - w[1];
         auto reached = [&](int i, double incl) {
@@ -566,7 +574,7 @@ __device__ __forceinline__ int draw(const Row<T> &row, uint64_t t, double u) {
     int last = -1;
     #pragma unroll
     for (int i = 0; i < kRun; ++i) {
-        w[i] = e0 + i < row.V && argmax_key(x[i], e0 + i) >= t ? weight(x[i], row.m, row.c) : 0.0;
+        w[i] = e0 + i < row.V && argmax_key(x[i], e0 + i) >= t ? weight(x[i], row.m, row.c, s.exp2) : 0.0;
         sum += w[i];
         if (w[i] > 0.0) last = e0 + i;
     }
@@ -633,7 +641,7 @@ __device__ __forceinline__ void finish_list(const Row<T> &row, const SampleArgs 
         for (int i = 0; i < 2; ++i) {
             const bool in = 2 * lane + i < k;
             key[i] = in ? sorted[2 * lane + i] : 0;
-            w[i] = in ? weight(key_value(key[i]), row.m, row.c) : 0.0;
+            w[i] = in ? weight(key_value(key[i]), row.m, row.c, s.exp2) : 0.0;
         }
         const double incl = wave_scan_f64(w[0] + w[1]), total = read_lane_f64(incl, 63);
         const double before[2] = {incl - (w[0] + w[1]), incl - w[1]};
@@ -692,7 +700,7 @@ __device__ __forceinline__ double chunk_masses(const Row<T> &row, uint64_t t) {
         double w = 0.0;
         #pragma unroll
         for (int i = 0; i < kRun; ++i)
-            if (e + i < row.V && argmax_key(x[i], e + i) >= t) w += weight(x[i], row.m, row.c);
+            if (e + i < row.V && argmax_key(x[i], e + i) >= t) w += weight(x[i], row.m, row.c, s.exp2);
         w = __longlong_as_double((long long)wave_fold_u64(f64_bits(w), add_f64_bits));
         if (lane == 0) part[c * 16 + wave] = w;
     }
@@ -710,12 +718,13 @@ __device__ __forceinline__ double chunk_masses(const Row<T> &row, uint64_t t) {
 
 // The least key whose value's weight reaches p (0 < p <= 1): 64 places at a time, by every wave.
 __device__ __forceinline__ uint64_t least_weight(float m, double c, double p) {
+    SampleLds &s = lds();
     uint32_t lo = 0, hi = (uint32_t)(argmax_key(m, 0) >> 32);   // hi reaches it; the answer is in [lo, hi]
     while (lo < hi) {
         const uint32_t span = hi - lo, step = span / 64 + 1;
         const uint32_t at = lo + min(span, (uint32_t)(threadIdx.x & 63) * step);
         const float v = key_value((uint64_t)at << 32);
-        const unsigned long long ok = __ballot(v == v && weight(v, m, c) >= p);   // (images below -inf's are NaN)
+        const unsigned long long ok = __ballot(v == v && weight(v, m, c, s.exp2) >= p);   // (images below -inf's are NaN)
         const int l = ok ? __ffsll((long long)ok) - 1 : 64;
         const uint32_t was = lo;
         if (l > 0) lo = was + min(span, (uint32_t)(l - 1) * step) + 1;
@@ -757,7 +766,9 @@ template <typename T> struct SolveJob {
 };
 template <typename T>
 __device__ __noinline__ void solve_row(const SolveJob<T> j) {
+    SampleLds &s = lds();
     const int tid = threadIdx.x;
+    __syncthreads();
     const Row<T> row = j.row;
     uint64_t t = 0;
     for (int pass = 0; pass < 2; ++pass) {   // top-k, then top-p of its mass
@@ -775,7 +786,7 @@ __device__ __noinline__ void solve_row(const SolveJob<T> j) {
     }
     if (j.over)
         row.each([&](float v, int i) {
-            if (argmax_key(v, i) >= t) store_agent(j.over + i, (float)(weight(v, row.m, row.c) * (1.0 / kept)));
+            if (argmax_key(v, i) >= t) store_agent(j.over + i, (float)(weight(v, row.m, row.c, s.exp2) * (1.0 / kept)));
         });
     if (tid == 0) *j.out = RowResult{t, kept, 0.0, 0.f, 0.f, row.m, kRowDone};
 }
@@ -815,6 +826,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(const SampleArgs a)
         s.flag[wave] = nan ? kNaN : 0;
     }
     if (tid < kBins) s.mass[tid] = 0, s.cnt[tid] = 0;
+    if (tid < 64) s.exp2[tid] = kExp2.v[tid];
     if (tid == 0) s.num[0] = 0, s.num[1] = 0;
     if (listed && a.probs) zero_run(a.probs + (size_t)r * a.V, e0, a.V);
     __syncthreads();
@@ -880,7 +892,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(const SampleArgs a)
     } else {
         #pragma unroll
         for (int i = 0; i < kRun; ++i) {
-            const double w = e0 + i < a.V && m > -INFINITY ? weight(x[i], m, row.c) : 0.0;
+            const double w = e0 + i < a.V && m > -INFINITY ? weight(x[i], m, row.c, s.exp2) : 0.0;
             mass += w;
             if (binned && !(flags & kNoBins)) {
                 const float j = mb - floorf(x[i] * 8.f);
@@ -944,14 +956,14 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(const SampleArgs a)
         // the chunks' masses against the row's maximum
         double cm[2];
         #pragma unroll
-        for (int i = 0; i < 2; ++i) cm[i] = h.max[i] == -INFINITY ? 0.0 : h.mass[i] * weight(h.max[i], m, row.c);
+        for (int i = 0; i < 2; ++i) cm[i] = h.max[i] == -INFINITY ? 0.0 : h.mass[i] * weight(h.max[i], m, row.c, s.exp2);
         if (wave == 0) {
             #pragma unroll
             for (int i = 0; i < 2; ++i)
                 if (lane + 64 * i < a.n_chunks) {
                     s.c_mass[lane + 64 * i] = cm[i];
                     s.c_max[lane + 64 * i] = h.max[i];
-                    s.c_fix[lane + 64 * i] = f64_bits(h.max[i] == -INFINITY ? 0.0 : kBinUnit * weight(h.max[i], m, row.c));
+                    s.c_fix[lane + 64 * i] = f64_bits(h.max[i] == -INFINITY ? 0.0 : kBinUnit * weight(h.max[i], m, row.c, s.exp2));
                 }
         }
         out.mass = __longlong_as_double((long long)wave_fold_u64(f64_bits(cm[0] + cm[1]), add_f64_bits));
@@ -1025,6 +1037,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_cut_kernel(const SampleArg
     if (res.mode != kRowCut && (res.mode != kRowSlow || chunk > 0)) return;
     Row<T> row = row_of<T>(a, r);
     row.m = res.m;
+    if (tid < 64) s.exp2[tid] = kExp2.v[tid];   // (read by this wave alone before the next barrier)
     if (res.mode == kRowSlow) {
         solve_row<T>(solve_job(a, row, r));
         return;
@@ -1052,7 +1065,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_cut_kernel(const SampleArg
         }
         q = wave_fold_u64(q, [](uint64_t x, uint64_t y) { return x + y; });
         n_above = (uint32_t)group_sum<64>((float)n_above);   // (exact: at most 8192)
-        above = q ? (double)q * kBinUnit * weight(top, res.m, row.c) : 0.0;
+        above = q ? (double)q * kBinUnit * weight(top, res.m, row.c, s.exp2) : 0.0;
     }
     if (tid == 0) s.num[0] = 0;
     __syncthreads();
@@ -1112,7 +1125,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_cut_kernel(const SampleArg
         const uint64_t k = s.list[i];
         if (k >= t)
             atomicAdd((unsigned long long *)&s.c_fix[key_index(k) / kSampleChunk],
-                      (unsigned long long)(weight(key_value(k), row.m, row.c) * (1.0 / kBinUnit) + 0.5));
+                      (unsigned long long)(weight(key_value(k), row.m, row.c, s.exp2) * (1.0 / kBinUnit) + 0.5));
     }
     __syncthreads();
     double kept = 0.0;
@@ -1146,6 +1159,9 @@ __global__ __launch_bounds__(kThreads) void sample_emit_kernel(const SampleArgs 
     const RowResult res = a.rows[r];
     float x[kRun], p[kRun];
     load_run(reinterpret_cast<const T *>(a.logits) + (size_t)r * a.V, e0, a.V, x);
+    __shared__ double table[64];
+    if (tid < 64) table[tid] = kExp2.v[tid];
+    __syncthreads();
     const float tv = key_value(res.t);   // the row has no NaN
     const uint32_t ti = (uint32_t)key_index(res.t);   // (a bound of values: past every index)
     const bool any = res.mode == kRowDone;
@@ -1154,7 +1170,7 @@ __global__ __launch_bounds__(kThreads) void sample_emit_kernel(const SampleArgs 
     for (int i = 0; i < kRun; ++i) {
         const bool stays = any && (res.t == 0 || x[i] > tv || (x[i] == tv && (uint32_t)(e0 + i) <= ti));
         p[i] = 0.f;
-        if (__any(stays)) p[i] = stays ? (float)(weight(x[i], res.m, c) * inv) : 0.f;
+        if (__any(stays)) p[i] = stays ? (float)(weight(x[i], res.m, c, table) * inv) : 0.f;
     }
     store_run(a.probs + (size_t)r * a.V, e0, a.V, p);
 }
