@@ -42,6 +42,7 @@ namespace mad {
 
 constexpr int kThreads = 1024, kRun = kSampleChunk / kThreads;   // entries of a thread: consecutive
 constexpr int kBins = 256, kBuckets = 2048, kList = 4096, kFinal = 128, kSort = 512;
+constexpr int kUnknown = 0x7fffffff;
 constexpr double kBinUnit = 0x1p-50, kRowUnit = 0x1p-43;   // 8192 and 2^20 weights of at most 1 fit 63 bits
 
 // 2^(j / 64), 0 <= j < 64: squared up from the Taylor series at a 2^-7th of the exponent (below 2e-16 relative), at
@@ -319,15 +320,15 @@ __device__ __forceinline__ void sort_down(const uint64_t *from, uint64_t *to, in
 }
 
 // The entry at which `target` is reached, among the keys of r: its key (or the end of r, where rounding leaves
-// nothing in it); r.mass and r.count become what lies at and above it.  STREAM: out of the row; else out of the list,
-// which holds n keys of r.
+// nothing in it); r.mass and r.count become what lies at and above it.  r holds n keys (or as many as there are, where
+// that is not known).  STREAM: out of the row, through the list as soon as that takes them; else out of the list.
 template <bool STREAM, typename T>
 __device__ __forceinline__ uint64_t select(const Row<T> &row, Range &r, bool by_count, double target, int n) {
     SampleLds &s = lds();
     const int tid = threadIdx.x;
     bool in_list = !STREAM;
     for (;;) {
-        if constexpr (STREAM) if (!in_list) {   // into the list, if it takes them
+        if constexpr (STREAM) if (!in_list && n <= kList) {   // into the list
             if (tid == 0) s.num[3] = 0;
             __syncthreads();
             row.each([&](float x, int i) {
@@ -338,8 +339,8 @@ __device__ __forceinline__ uint64_t select(const Row<T> &row, Range &r, bool by_
                 }
             });
             __syncthreads();
-            n = s.num[3];
-            in_list = n <= kList;
+            n = uniform(s.num[3]);
+            in_list = true;
             __syncthreads();
         }
         // The keys of the list that are still in the range: few enough are put in order.
@@ -763,6 +764,12 @@ template <typename T> struct SolveJob {
     float *over;      // the row's distribution, zeros so far, where no other launch writes it
     RowResult *out;
     int top_k;
+    // where the first filter (top-k, else top-p) ends, as far as it is known: `n` keys, none to search for where
+    // target < 0; and min-p's bound
+    Range range;
+    double target;
+    uint64_t least;
+    int n;
 };
 template <typename T>
 __device__ __noinline__ void solve_row(const SolveJob<T> j) {
@@ -771,14 +778,19 @@ __device__ __noinline__ void solve_row(const SolveJob<T> j) {
     __syncthreads();
     const Row<T> row = j.row;
     uint64_t t = 0;
-    for (int pass = 0; pass < 2; ++pass) {   // top-k, then top-p of its mass
-        const bool by_count = pass == 0;
-        if (by_count ? j.top_k == 0 : j.top_p >= 1.0) continue;
-        const double target = by_count ? (double)j.top_k : j.top_p * chunk_masses(row, t);
-        Range g = {0, ~(uint64_t)0, 0.0, 0.0};
-        t = max(t, select<true>(row, g, by_count, target, 0));
+    bool known = j.n < kUnknown;
+    if (!known || j.target >= 0.0) {
+        for (int pass = 0; pass < 2; ++pass) {   // top-k, then top-p of its mass
+            const bool by_count = pass == 0;
+            if (by_count ? j.top_k == 0 : j.top_p >= 1.0) continue;
+            Range g = known ? j.range : Range{0, ~(uint64_t)0, 0.0, 0.0};
+            const double target = known ? j.target : by_count ? (double)j.top_k : j.top_p * chunk_masses(row, t);
+            t = max(t, select<true>(row, g, by_count, target, known ? j.n : kUnknown));
+            known = false;   // (the other filter's place is not)
+        }
     }
-    if (j.min_p > 0.0) t = max(t, least_weight(row.m, row.c, j.min_p));
+    if (j.least > 0) t = max(t, j.least);
+    else if (j.min_p > 0.0) t = max(t, least_weight(row.m, row.c, j.min_p));
     const double kept = chunk_masses(row, t);
     if (j.tok) {
         const int v = draw(row, t, j.u);
@@ -794,7 +806,8 @@ template <typename T>
 __device__ __forceinline__ SolveJob<T> solve_job(const SampleArgs &a, const Row<T> &row, int r) {
     const int b = r / a.T, k = a.top_k[b];
     return SolveJob<T>{row, a.top_p[b], a.min_p[b], a.tok ? (double)a.u[r] : 0.0, a.tok ? a.tok + r : nullptr,
-                       a.probs && k > 0 && k <= kListK ? a.probs + (size_t)r * a.V : nullptr, a.rows + r, k};
+                       a.probs && k > 0 && k <= kListK ? a.probs + (size_t)r * a.V : nullptr, a.rows + r, k,
+                       Range{0, 0, 0.0, 0.0}, -1.0, 0, kUnknown};
 }
 
 template <typename T>
@@ -884,6 +897,34 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(const SampleArgs a)
             if (left) s.num[1] = 1;
             __syncthreads();
             n_out = (uint32_t)s.num[0];
+            if (n_out > (uint32_t)kEmit && m - edge > 0x1p-100f) {
+                // too many (a flat distribution): by 256 bins from there to the maximum, all entries counted
+                wait_vm_stores();   // (other threads write over these keys)
+                __syncthreads();
+                const float per = 256.f / (m - edge);
+                auto place = [&](float v) { return kBins - 1 - min((int)((v - edge) * per), kBins - 1); };   // (falls with v)
+                if (tid < kBins) s.cnt[tid] = 0;
+                if (tid == 0) s.num[0] = 0;
+                __syncthreads();
+                #pragma unroll
+                for (int i = 0; i < kRun; ++i)
+                    if (x[i] >= edge) atomicAdd(&s.cnt[place(x[i])], 1u);
+                __syncthreads();
+                if (wave == 0) {
+                    double before;
+                    const int j = first_reaching([&](int i) { return (double)s.cnt[i]; }, (double)top_k, &before);
+                    if (lane == 0) s.num[2] = j;
+                }
+                __syncthreads();
+                #pragma unroll
+                for (int i = 0; i < kRun; ++i)
+                    if (x[i] >= edge && place(x[i]) <= s.num[2]) {
+                        const int p = atomicAdd(&s.num[0], 1);
+                        if (p < kEmit) put64(rec + kHead + 8 * p, argmax_key(x[i], e0 + i));
+                    }
+                __syncthreads();
+                n_out = (uint32_t)s.num[0];
+            }
             if (n_out > (uint32_t)kEmit) flags |= kLeft, edge = INFINITY, n_out = 0;
             else if (s.num[1]) flags |= kLeft;
         } else if (m > -INFINITY) {
@@ -1103,20 +1144,24 @@ __global__ __launch_bounds__(kThreads, 8) void sample_cut_kernel(const SampleArg
         }
     }
     const int all = uniform((int)group_sum<64>(total));
+    mass = uniform(__longlong_as_double((long long)wave_fold_u64(f64_bits(mass), add_f64_bits)));
+    count = uniform(__longlong_as_double((long long)wave_fold_u64(f64_bits(count), add_f64_bits)));
+    const uint64_t bits = (uint64_t)0xffffffffu << 32;
+    Range g = {argmax_key(res.lo, 0) & bits, (argmax_key(res.hi, 0) & bits) - 1, mass, count};
     if (__any(over) || all > kList || (a.top_k[b] > 0 && a.top_p[b] < 1.0)) {
-        solve_row<T>(solve_job(a, row, r));
+        SolveJob<T> job = solve_job(a, row, r);
+        job.range = g;
+        job.target = res.target;
+        job.least = res.t;
+        job.n = a.top_k[b] > 0 && a.top_p[b] < 1.0 && res.target < 0.0 ? kUnknown : all;   // (top-p of top-k's mass all the same)
+        solve_row<T>(job);
         return;
     }
-    mass = __longlong_as_double((long long)wave_fold_u64(f64_bits(mass), add_f64_bits));
-    mass = uniform(mass);
-    count = __longlong_as_double((long long)wave_fold_u64(f64_bits(count), add_f64_bits));
     load_list(s, rec0, a.n_chunks, n, [](uint64_t) {});
     if (tid == 0) s.num[3] = all;
     __syncthreads();
     uint64_t t = res.t;
     if (res.target >= 0.0) {
-        const uint64_t edge = (uint64_t)0xffffffffu << 32;
-        Range g = {argmax_key(res.lo, 0) & edge, (argmax_key(res.hi, 0) & edge) - 1, mass, count};
         t = max(t, select<false>(row, g, a.top_k[b] > 0, res.target, all));
     }
     // each chunk's kept mass: above the range, and the listed entries that stay

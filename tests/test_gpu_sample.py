@@ -27,6 +27,8 @@ def _logits(kind, shape, seed):
         return (2.2 * x).scatter_(-1, at, head)
     if kind == "flat":       # thousands of entries to a bin
         return 0.01 * x
+    if kind == "body":
+        return 0.5 * x
     if kind == "wide":       # a few entries to many bins, most below the window of 32
         return 30 * x
     if kind == "ties":       # eight values only
@@ -93,6 +95,15 @@ def test_distributions(dtype, kind):
                             dict(top_p=0.6, min_p=0.2), dict(), dict(temperature=0), dict(temperature=40.0, top_k=60))):
         _run(kind, (2, 1, 17000), dtype, 10 + i, probs=i % 2 == 0, **kw)
         _run(kind, (1, 2, 700), dtype, 30 + i, **kw)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_more_entries_to_a_bin_than_are_listed(dtype):
+    # thousands within an eighth: the range where a filter ends is searched on in the row, for two filters one after the
+    # other; where min-p ends above top-k, top-p is still of top-k's mass
+    for i, kw in enumerate((dict(top_p=0.9), dict(top_p=0.6, temperature=0.3), dict(top_k=3000), dict(top_k=3000, top_p=0.8),
+                            dict(top_k=3000, top_p=0.8, min_p=0.5), dict(top_k=200, top_p=0.3, min_p=0.9), dict(min_p=0.1), dict(top_k=128))):
+        _run("body", (2, 1, 40000), dtype, 50 + i, **kw)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
