@@ -594,7 +594,8 @@ def sample(logits: torch.Tensor, u: Optional[torch.Tensor] = None, temperature=1
     for name, v in (("temperature", temperature), ("top_k", top_k), ("top_p", top_p), ("min_p", min_p)):
         v = [v] * B if not hasattr(v, "__len__") else v
         _need(len(v) == B, f"{name} needs one entry per sequence")
-        settings.append((_host_i32 if name == "top_k" else _host_f64)(v, B))
+        # (a top-k beyond every vocabulary keeps all; one beyond 32 bits must not wrap)
+        settings.append(_host_i32([max(-1, min(int(k), 2 ** 31 - 1)) for k in v], B) if name == "top_k" else _host_f64(v, B))
     _contiguous(logits=logits, u=u, tok=tok, probs=probs)
     _same_device(dev, u=u, tok=tok, probs=probs)
     dt = _dtype_code(logits)

@@ -518,7 +518,8 @@ int mad_kv8_append(const void *k_new, const void *v_new, const int32_t *n, int B
         a.row[b].y = len;
         a.row[b].z = nb;
         if (nb > 0) blocks += (len + nb - 1) / kv->block - len / kv->block + 1;
-        if (blocks * 2 * Hkv > 0x7fffffff) return fail(MAD_EINVAL, "too many blocks in one call");
+        if (blocks * 2 * Hkv > 0xffffff)   // (a launch has fewer than 2^32 threads, 256 a block)
+            return fail(MAD_EINVAL, "rows in %lld blocks of %d KV heads: more than a call takes", (long long)blocks, Hkv);
     }
     for (int b = B; b < MAD_MAX_BATCH; ++b) a.row[b].x = (int)blocks;
     if (blocks == 0) return ok();

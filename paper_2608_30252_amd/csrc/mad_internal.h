@@ -240,6 +240,7 @@ struct SampleArgs {
     double top_p[kMaxB], min_p[kMaxB];
     int top_k[kMaxB];      // 0: off
 };
+static_assert(kMaxB * 64 <= kCounterLines, "a counter line per row, T <= 64");
 size_t sample_ws_bytes(int B, int T, int V);
 hipError_t launch_sample(const SampleArgs &a, int dtype, hipStream_t st);
 

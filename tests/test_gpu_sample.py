@@ -97,6 +97,17 @@ def test_distributions(dtype, kind):
         _run(kind, (1, 2, 700), dtype, 30 + i, **kw)
 
 
+def test_a_top_k_beyond_32_bits_keeps_all():
+    mad = _mad()
+    x, u = _logits("model", (2, 1, 5000), 3).cuda(), torch.rand((2, 1), device="cuda")
+    want = mad.sample(x, u, probs=torch.empty_like(x))
+    for k in (5000, 2 ** 31 - 1, 2 ** 32, 2 ** 32 + 1, [2 ** 40, 0]):
+        got = mad.sample(x, u, top_k=k, probs=torch.empty_like(x))
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    with pytest.raises(mad.MadError):
+        mad.sample(x, u, top_k=-2 ** 32)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_more_entries_to_a_bin_than_are_listed(dtype):
     # thousands within an eighth: the range where a filter ends is searched on in the row, for two filters one after the

@@ -105,6 +105,11 @@ def test_append_refuses(mad):
     assert _append(mad, v, n_cap=45) == mad.MAD_EINVAL           # 20 + 45 > 64
     assert "exceeds cap" in mad._load_library().mad_last_error().decode()
     assert _append(mad, v, i32(0, 45), n_cap=45) == mad.MAD_EINVAL
+    cap = 1 << 26                                                # 2^22 blocks of 2 heads, K and V: 2^24 workgroups
+    huge = _view(mad, cap=cap, head_stride=cap * 64, seq_stride=2 * cap * 64, scale_head_stride=cap // 16, scale_seq_stride=cap // 8,
+                 len=i32(0, 0))
+    assert _append(mad, huge, i32(0, cap), n_cap=cap) == mad.MAD_EINVAL
+    assert "more than a call takes" in mad._load_library().mad_last_error().decode()
     shared = _view(mad, seq_stride=0, scale_seq_stride=0)
     assert _append(mad, shared) == mad.MAD_EINVAL                # two sequences write one buffer
     assert _append(mad, v, i32(0, 0)) == mad.MAD_OK              # nothing to do: nothing is launched
