@@ -784,7 +784,7 @@ int mad_sample(const void *logits, int dtype, const float *u, const double *temp
         if (!(p > 0.0) || p > 1.0) return fail(MAD_EINVAL, "top_p[%d]=%g outside (0, 1]", b, p);
         if (!(mp >= 0.0) || mp > 1.0) return fail(MAD_EINVAL, "min_p[%d]=%g outside [0, 1]", b, mp);
         const bool greedy = t == 0.0;   // the first entry of the order, whatever the filters
-        a.c[b] = 64.0 * 1.4426950408889634 / (greedy ? 1.0 : t);
+        a.c[b] = fmin(256.0 * 1.4426950408889634 / (greedy ? 1.0 : t), 1e300);   // (finite)
         a.top_k[b] = greedy ? 1 : k < V ? k : 0;
         a.top_p[b] = greedy ? 1.0 : p;
         a.min_p[b] = greedy ? 0.0 : mp;

@@ -151,6 +151,12 @@ __device__ __forceinline__ void lane_pair_u64(uint64_t v, uint64_t &a, uint64_t 
         b = ((uint64_t)h[1] << 32) | l[1];
     }
 }
+// The same value, computed from here on: keeps the addresses that a rare part of the kernel derives from it out of
+// registers in the loop (the compiler would form them once, ahead of it).
+__device__ __forceinline__ int here(int v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
 // f folded over the 64 lanes, the same value in every lane: pairs within a
 // quad, then the two quads of 8 lanes (half mirror), the two 8s of a row
 // (mirror), the two 16s of 32 lanes, the two 32s.  Every lane combines the same

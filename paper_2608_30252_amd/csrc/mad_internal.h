@@ -236,10 +236,14 @@ struct SampleArgs {
     char *records;         // [B * T][n_chunks] of kSampleRecord bytes
     unsigned *counters;    // line r: arrivals of row r's workgroups
     int B, T, V, n_chunks;
-    double c[kMaxB];       // 64 log2 e / temperature
+    double c[kMaxB];       // 256 log2 e / temperature
     double top_p[kMaxB], min_p[kMaxB];
     int top_k[kMaxB];      // 0: off
+    // (set by launch_sample) the second launch's chunks to a workgroup and workgroups to a row; its sequences and the third's
+    int cut_per_group, cut_groups, n_cut, n_emit;
+    uint8_t cut[kMaxB], emit[kMaxB];
 };
+static_assert(kMaxB <= 256, "sequence numbers in a byte");
 static_assert(kMaxB * 64 <= kCounterLines, "a counter line per row, T <= 64");
 size_t sample_ws_bytes(int B, int T, int V);
 hipError_t launch_sample(const SampleArgs &a, int dtype, hipStream_t st);

@@ -38,20 +38,23 @@
 #include "mad_device.h"
 #include "mad_internal.h"
 
+#include <algorithm>
+
 namespace mad {
 
 constexpr int kThreads = 1024, kRun = kSampleChunk / kThreads;   // entries of a thread: consecutive
 constexpr int kBins = 256, kBuckets = 2048, kList = 4096, kFinal = 128, kSort = 512;
+constexpr int kResident = 512;   // workgroups at a time: two for each of the 256 CUs (64 KB of LDS, 2048 threads)
 constexpr int kUnknown = 0x7fffffff;
 constexpr double kBinUnit = 0x1p-50, kRowUnit = 0x1p-43;   // 8192 and 2^20 weights of at most 1 fit 63 bits
 
-// 2^(j / 64), 0 <= j < 64: squared up from the Taylor series at a 2^-7th of the exponent (below 2e-16 relative), at
-// compile time
+// 2^(j / 256), 0 <= j < 256, from the Taylor series at compile time (below 2e-16 relative)
+constexpr int kTable = 256;
 struct Exp2Table {
-    double v[64];
+    double v[kTable];
     constexpr Exp2Table() : v() {
-        for (int j = 0; j < 64; ++j) {
-            const double f = 0.6931471805599453 * j / 64;   // 0 <= f < ln 2
+        for (int j = 0; j < kTable; ++j) {
+            const double f = 0.6931471805599453 * j / kTable;   // 0 <= f < ln 2
             double p = 1.0;
             for (int k = 20; k > 0; --k) p = 1.0 + p * f / k;
             v[j] = p;
@@ -60,21 +63,40 @@ struct Exp2Table {
 };
 __constant__ const Exp2Table kExp2 = Exp2Table();
 
-// The weight of x against the maximum m (+inf against +inf: 1), c64 = 64 log2 e / temperature: with
-// (x - m) c64 = n + f, |f| <= 1/2, it is 2^(n / 64) from the table and 2^(f / 64) by its series (to f^5: 4e-17 relative).
-// In double: half the operations of a series alone.
-__device__ __forceinline__ double weight(float x, float m, double c64, const double *table) {
-    constexpr double k1 = 0.6931471805599453 / 64, k2 = k1 * k1 / 2, k3 = k2 * k1 / 3, k4 = k3 * k1 / 4, k5 = k4 * k1 / 5;
-    const double y = fmax(((double)x - (double)m) * c64, -64000.0);   // (a NaN of inf - inf: -64000)
-    const double n = rint(y), f = y - n;
-    double p = fma(k5, f, k4);
-    p = fma(p, f, k3);
-    p = fma(p, f, k2);
-    p = fma(p, f, k1);
+// The weight of x against the maximum m, c = 256 log2 e / temperature: with (x - m) c = n + f, |f| <= 1/2, it is
+// 2^(n / 256) from the table and 2^(f / 256) by its series (to f^4: 4e-17 relative).  In double, at half the operations
+// of a series alone; the coefficients are in scalar registers, formed where they are used: the compiler would keep a
+// copy of each in vector registers all through the kernel, of which there are 64, and have them spilled.
+struct Series {
+    double k1, k2, k3, k4;
+};
+__device__ __forceinline__ Series series() {
+    constexpr double k1 = 0.6931471805599453 / kTable, k2 = k1 * k1 / 2, k3 = k2 * k1 / 3, k4 = k3 * k1 / 4;
+    Series s = {k1, k2, k3, k4};
+    asm volatile("" : "+s"(s.k1), "+s"(s.k2), "+s"(s.k3), "+s"(s.k4));
+    return s;
+}
+// m finite, x not above it (a NaN or -inf: 2^-1000)
+__device__ __forceinline__ double weight_finite(float x, double m, double c, const double *table, const Series &s) {
+    const double y = fmax(((double)x - m) * c, -1000.0 * kTable);
+    const double t = y + 0x1.8p52;   // n in the low bits
+    const double f = y - (t - 0x1.8p52);
+    double p = fma(s.k4, f, s.k3);
+    p = fma(p, f, s.k2);
+    p = fma(p, f, s.k1);
     p = fma(p, f, 1.0);
-    const int i = (int)n;
-    const double w = ldexp(p * table[i & 63], i >> 6);
-    return x == m ? 1.0 : y > -64000.0 ? w : 0.0;
+    const int n = (int)__double_as_longlong(t);
+    const uint64_t w = (uint64_t)__double_as_longlong(p * table[n & (kTable - 1)]);
+    return __longlong_as_double((long long)(w + ((uint64_t)(uint32_t)((n >> 8) << 20) << 32)));   // times 2^(n >> 8)
+}
+// any m and x (+inf against +inf: 1; below 2^-1000: 0)
+__device__ __forceinline__ double weight(float x, float m, double c, const double *table) {
+    const double y = ((double)x - (double)m) * c;
+    return x == m ? 1.0 : y > -1000.0 * kTable ? weight_finite(x, (double)m, c, table, series()) : 0.0;
+}
+// w (<= 1) as an integer of 1 / per, to nearest; per a power of two up to 2^50: from the low mantissa bits of a sum with 2^52
+__device__ __forceinline__ unsigned long long units(double w, double per) {
+    return (unsigned long long)__double_as_longlong(fma(w, per, 0x1p52)) - (unsigned long long)__double_as_longlong(0x1p52);
 }
 // the value that a key holds
 __device__ __forceinline__ float key_value(uint64_t k) {
@@ -82,24 +104,46 @@ __device__ __forceinline__ float key_value(uint64_t k) {
     return __uint_as_float((o & 0x80000000u) ? o ^ 0x80000000u : ~o);
 }
 
-// a thread's run of kRun entries from entry e on (unaligned 16-byte loads; -inf past V)
-__device__ __forceinline__ void load_run(const float *row, int e, int V, float (&x)[kRun]) {
-    if (e + kRun <= V) {
-        __builtin_memcpy(x, row + e, kRun * 4);
-    } else {
-        #pragma unroll
-        for (int i = 0; i < kRun; ++i) x[i] = e + i < V ? row[e + i] : -INFINITY;
+// A thread's run of kRun entries from entry e on (unaligned 16-byte loads; -inf past V), as it is loaded: the next
+// chunk's is in flight while this one's is worked on.
+template <typename T> struct Run;
+template <> struct Run<float> {
+    float v[kRun];
+    __device__ __forceinline__ void load(const float *row, int e, int V) {
+        if (e + kRun <= V) {
+            __builtin_memcpy(v, row + e, kRun * 4);
+        } else {
+            #pragma unroll
+            for (int i = 0; i < kRun; ++i) v[i] = e + i < V ? row[e + i] : -INFINITY;
+        }
     }
-}
-__device__ __forceinline__ void load_run(const bf16_t *row, int e, int V, float (&x)[kRun]) {
-    if (e + kRun <= V) {
-        uint4 u;
-        __builtin_memcpy(&u, row + e, kRun * 2);
-        unpack16(u, x, bf16_t());
-    } else {
+    __device__ __forceinline__ void unpack(float (&x)[kRun]) const {
         #pragma unroll
-        for (int i = 0; i < kRun; ++i) x[i] = e + i < V ? bf16_to_f32(row[e + i].bits) : -INFINITY;
+        for (int i = 0; i < kRun; ++i) x[i] = v[i];
     }
+};
+template <> struct Run<bf16_t> {
+    uint4 v;
+    __device__ __forceinline__ void load(const bf16_t *row, int e, int V) {
+        if (e + kRun <= V) {
+            __builtin_memcpy(&v, row + e, kRun * 2);
+        } else {
+            uint32_t w[kRun / 2];
+            #pragma unroll
+            for (int i = 0; i < kRun / 2; ++i) {
+                const uint32_t lo = e + 2 * i < V ? row[e + 2 * i].bits : 0xff80u, hi = e + 2 * i + 1 < V ? row[e + 2 * i + 1].bits : 0xff80u;
+                w[i] = lo | hi << 16;
+            }
+            v = uint4{w[0], w[1], w[2], w[3]};
+        }
+    }
+    __device__ __forceinline__ void unpack(float (&x)[kRun]) const { unpack16(v, x, bf16_t()); }
+};
+template <typename T>
+__device__ __forceinline__ void load_run(const T *row, int e, int V, float (&x)[kRun]) {
+    Run<T> run;
+    run.load(row, e, V);
+    run.unpack(x);
 }
 // Zeros at device scope: the row's last workgroup, perhaps behind another L2, writes over some of them in this launch
 // (at device scope too).
@@ -150,7 +194,7 @@ struct SampleLds {
     uint64_t list[kList];       // gathered keys
     uint64_t mass[kBuckets];    // histogram: masses (integers), or doubles' bits
     uint32_t cnt[kBuckets];
-    double exp2[64];   // kExp2
+    double exp2[kTable];   // kExp2
     double bucket_mass[kBins];
     uint32_t bucket_cnt[kBins];
     double c_mass[kSampleMaxChunks];    // per chunk: kept mass; against the row's maximum
@@ -204,7 +248,7 @@ template <typename T> struct Row {
     const T *x;
     int V, n_chunks;
     float m;       // maximum
-    double c;      // 64 log2 e / temperature
+    double c;      // 256 log2 e / temperature
 
     // f(value, index) for every entry; four chunks in flight
     template <typename F> __device__ __forceinline__ void each(F f) const {
@@ -351,7 +395,7 @@ __device__ __forceinline__ uint64_t select(const Row<T> &row, Range &r, bool by_
         const double unit = in_list ? kBinUnit : kRowUnit, per = 1.0 / unit;
         auto count = [&](int at, float x) {
             atomicAdd(&s.cnt[at], 1u);
-            atomicAdd((unsigned long long *)&s.mass[at], (unsigned long long)(weight(x, row.m, row.c, s.exp2) * per + 0.5));
+            atomicAdd((unsigned long long *)&s.mass[at], units(weight(x, row.m, row.c, s.exp2), per));
         };
         int sh, at;
         if (in_list) {
@@ -740,12 +784,12 @@ __device__ __forceinline__ Row<T> row_of(const SampleArgs &a, int r) {
     return Row<T>{reinterpret_cast<const T *>(a.logits) + (size_t)r * a.V, a.V, a.n_chunks, 0.f, a.c[r / a.T]};
 }
 // whether this workgroup is the row's last to get here; what it stored at device scope is visible then
-__device__ __forceinline__ bool row_last(const SampleArgs &a, int r, SampleLds &s) {
+__device__ __forceinline__ bool row_last(const SampleArgs &a, int r, int groups, SampleLds &s) {
     wait_vm_stores();
     __syncthreads();
     if (threadIdx.x == 0) {
         unsigned *cnt = a.counters + (size_t)r * kCounterStride;
-        const int last = arrive(cnt) == (unsigned)(a.n_chunks - 1);
+        const int last = arrive(cnt) == (unsigned)(groups - 1);
         if (last) reset_counter(cnt);
         s.num[3] = last;
     }
@@ -814,7 +858,7 @@ template <typename T>
 __global__ __launch_bounds__(kThreads, 8) void sample_kernel(const SampleArgs a) {
     SampleLds &s = lds();
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int rows = a.B * a.T, r = blockIdx.x % rows, chunk = blockIdx.x / rows, b = r / a.T;
+    const int rows = a.B * a.T, chunk = blockIdx.x / rows, r = blockIdx.x - chunk * rows, b = r / a.T;
     const int top_k = a.top_k[b];
     const bool listed = top_k > 0 && top_k <= kListK;
     const bool binned = !listed && (top_k > 0 || a.top_p[b] < 1.0 || a.min_p[b] > 0.0);
@@ -825,6 +869,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(const SampleArgs a)
     const int e0 = chunk * kSampleChunk + tid * kRun;
     float x[kRun];
     load_run(row.x, e0, a.V, x);
+    if (tid < kTable) s.exp2[tid] = kExp2.v[tid];
     float mine = -INFINITY;
     bool nan = false;
     #pragma unroll
@@ -839,7 +884,6 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(const SampleArgs a)
         s.flag[wave] = nan ? kNaN : 0;
     }
     if (tid < kBins) s.mass[tid] = 0, s.cnt[tid] = 0;
-    if (tid < 64) s.exp2[tid] = kExp2.v[tid];
     if (tid == 0) s.num[0] = 0, s.num[1] = 0;
     if (listed && a.probs) zero_run(a.probs + (size_t)r * a.V, e0, a.V);
     __syncthreads();
@@ -931,16 +975,26 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(const SampleArgs a)
             flags |= kLeft;   // (edge +inf) candidates only by the row's last workgroup
         }
     } else {
-        #pragma unroll
-        for (int i = 0; i < kRun; ++i) {
-            const double w = e0 + i < a.V && m > -INFINITY ? weight(x[i], m, row.c, s.exp2) : 0.0;
-            mass += w;
-            if (binned && !(flags & kNoBins)) {
-                const float j = mb - floorf(x[i] * 8.f);
-                if (j < (float)kBins) {   // (not -inf, so not past the row's end)
-                    atomicAdd((unsigned long long *)&s.mass[(int)j], (unsigned long long)(w * (1.0 / kBinUnit) + 0.5));
-                    if (top_k > 0) atomicAdd(&s.cnt[(int)j], 1u);
+        if (m == INFINITY) {
+            #pragma unroll
+            for (int i = 0; i < kRun; ++i) mass += x[i] == m ? 1.0 : 0.0;
+        } else if (m > -INFINITY) {   // (what is past the row's end is -inf: as good as 0)
+            const Series terms = series();
+            const double md = (double)m;
+            const int mi = (int)mb;   // (where there are bins)
+            #pragma unroll
+            for (int i = 0; i < kRun; ++i) {
+                const double w = weight_finite(x[i], md, row.c, s.exp2, terms);
+                mass += w;
+                if (binned && !(flags & kNoBins)) {
+                    const float low = floorf(x[i] * 8.f);
+                    if (mb - low < (float)kBins) {   // (not -inf)
+                        const int j = mi - (int)low;
+                        atomicAdd((unsigned long long *)&s.mass[j], units(w, 1.0 / kBinUnit));
+                        if (top_k > 0) atomicAdd(&s.cnt[j], 1u);
+                    }
                 }
+                if (i % 2 == 1) __builtin_amdgcn_sched_barrier(0);   // (few temporaries at a time)
             }
         }
         mass = block_sum(mass, s.part);   // (its barrier stands behind the atomics)
@@ -957,7 +1011,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(const SampleArgs a)
         put64(rec + 16, f64_bits(mass));
     }
     if (listed && tid < kBins) s.cnt[tid] = 0;   // (its last reader is behind a barrier)
-    if (!row_last(a, r, s)) return;
+    if (!row_last(a, r, a.n_chunks, s)) return;
 
     // ---- the row's last workgroup ----
     const Heads h = load_heads(rec0, a.n_chunks);
@@ -1071,57 +1125,65 @@ template <typename T>
 __global__ __launch_bounds__(kThreads, 8) void sample_cut_kernel(const SampleArgs a) {
     SampleLds &s = lds();
     const int tid = threadIdx.x, lane = tid & 63;
-    const int rows = a.B * a.T, r = blockIdx.x % rows, chunk = blockIdx.x / rows, b = r / a.T;
+    const int rows = a.n_cut * a.T, part = blockIdx.x / rows, i_cut = blockIdx.x - part * rows, b = a.cut[i_cut / a.T];
+    const int r = b * a.T + i_cut % a.T, chunk0 = part * a.cut_per_group, chunk1 = min(chunk0 + a.cut_per_group, a.n_chunks);
     RowResult res = a.rows[r];
     res.t = uniform(res.t), res.target = uniform(res.target), res.lo = uniform(res.lo), res.hi = uniform(res.hi);
     res.m = uniform(res.m), res.mode = uniform(res.mode);
-    if (res.mode != kRowCut && (res.mode != kRowSlow || chunk > 0)) return;
+    if (res.mode != kRowCut && (res.mode != kRowSlow || part > 0)) return;
     Row<T> row = row_of<T>(a, r);
     row.m = res.m;
-    if (tid < 64) s.exp2[tid] = kExp2.v[tid];   // (read by this wave alone before the next barrier)
+    if (tid < kTable) s.exp2[tid] = kExp2.v[tid];
     if (res.mode == kRowSlow) {
         solve_row<T>(solve_job(a, row, r));
         return;
     }
-    char *rec0 = a.records + (size_t)r * a.n_chunks * kSampleRecord, *rec = rec0 + (size_t)chunk * kSampleRecord;
-    const int e0 = chunk * kSampleChunk + tid * kRun;
-    float x[kRun];
-    load_run(row.x, e0, a.V, x);
-    // what lies above the range: the chunk's bins up to there (read before the keys take their place)
-    double above = 0.0;
-    uint32_t n_above = 0;
-    if (tid < 64) {
-        const float top = __uint_as_float((uint32_t)get64(rec)), ups = floorf(top * 8.f) - res.hi * 8.f;   // the last bin above
+    char *rec0 = a.records + (size_t)r * a.n_chunks * kSampleRecord;
+    Run<T> next;
+    next.load(row.x, chunk0 * kSampleChunk + tid * kRun, a.V);
+    for (int chunk = chunk0; chunk < chunk1; ++chunk) {
+        const int e0 = chunk * kSampleChunk + tid * kRun;
+        float x[kRun];
+        next.unpack(x);
+        if (chunk + 1 < chunk1) next.load(row.x, e0 + kSampleChunk, a.V);   // in flight meanwhile
+        char *rec = rec0 + (size_t)chunk * kSampleRecord;
+        // what lies above the range: the chunk's bins up to there (read before the keys take their place)
         uint64_t q = 0;
-        #pragma unroll
-        for (int i = 0; i < kBins / 64; ++i) {
-            const uint64_t y = get64(rec + kHead + 8 * (lane + 64 * i));
-            const bool up = (float)(lane + 64 * i) <= ups;
-            q += up ? y : 0;
-            if (a.top_k[b] > 0) {
-                const uint32_t z = __hip_atomic_load(reinterpret_cast<uint32_t *>(rec + kHead + 8 * kBins) + lane + 64 * i, __ATOMIC_RELAXED,
-                                                     __HIP_MEMORY_SCOPE_AGENT);
-                n_above += up ? z : 0;
+        uint32_t n_above = 0;
+        float top = 0.f;
+        if (tid < 64) {
+            top = __uint_as_float((uint32_t)get64(rec));
+            const float ups = floorf(top * 8.f) - res.hi * 8.f;   // the last bin above
+            #pragma unroll
+            for (int i = 0; i < kBins / 64; ++i) {
+                const uint64_t y = get64(rec + kHead + 8 * (lane + 64 * i));
+                const bool up = (float)(lane + 64 * i) <= ups;
+                q += up ? y : 0;
+                if (a.top_k[b] > 0) {
+                    const uint32_t z = __hip_atomic_load(reinterpret_cast<uint32_t *>(rec + kHead + 8 * kBins) + lane + 64 * i, __ATOMIC_RELAXED,
+                                                         __HIP_MEMORY_SCOPE_AGENT);
+                    n_above += up ? z : 0;
+                }
             }
+            q = wave_fold_u64(q, [](uint64_t x, uint64_t y) { return x + y; });
+            n_above = (uint32_t)group_sum<64>((float)n_above);   // (exact: at most 8192)
         }
-        q = wave_fold_u64(q, [](uint64_t x, uint64_t y) { return x + y; });
-        n_above = (uint32_t)group_sum<64>((float)n_above);   // (exact: at most 8192)
-        above = q ? (double)q * kBinUnit * weight(top, res.m, row.c, s.exp2) : 0.0;
-    }
-    if (tid == 0) s.num[0] = 0;
-    __syncthreads();
-    #pragma unroll
-    for (int i = 0; i < kRun; ++i)
-        if (x[i] < res.hi && x[i] >= res.lo && e0 + i < a.V) {
-            const int p = atomicAdd(&s.num[0], 1);
-            if (p < kEmit) put64(rec + kHead + 8 * p, argmax_key(x[i], e0 + i));
+        if (tid == 0) s.num[0] = 0;
+        __syncthreads();
+        #pragma unroll
+        for (int i = 0; i < kRun; ++i)
+            if (x[i] < res.hi && x[i] >= res.lo && e0 + i < a.V) {
+                const int p = atomicAdd(&s.num[0], 1);
+                if (p < kEmit) put64(rec + kHead + 8 * p, argmax_key(x[i], e0 + i));
+            }
+        __syncthreads();
+        if (tid == 0) {
+            put64(rec, (uint64_t)(uint32_t)s.num[0] | (uint64_t)n_above << 32);
+            put64(rec + 16, f64_bits(q ? (double)q * kBinUnit * weight(top, res.m, row.c, s.exp2) : 0.0));
         }
-    __syncthreads();
-    if (tid == 0) {
-        put64(rec, (uint64_t)(uint32_t)s.num[0] | (uint64_t)n_above << 32);
-        put64(rec + 16, f64_bits(above));
+        __syncthreads();   // (the count is read)
     }
-    if (!row_last(a, r, s)) return;
+    if (!row_last(a, r, a.cut_groups, s)) return;
 
     // ---- the row's last workgroup ----
     uint32_t n[2];
@@ -1170,7 +1232,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_cut_kernel(const SampleArg
         const uint64_t k = s.list[i];
         if (k >= t)
             atomicAdd((unsigned long long *)&s.c_fix[key_index(k) / kSampleChunk],
-                      (unsigned long long)(weight(key_value(k), row.m, row.c, s.exp2) * (1.0 / kBinUnit) + 0.5));
+                      units(weight(key_value(k), row.m, row.c, s.exp2), 1.0 / kBinUnit));
     }
     __syncthreads();
     double kept = 0.0;
@@ -1198,14 +1260,14 @@ __global__ __launch_bounds__(kThreads, 8) void sample_cut_kernel(const SampleArg
 template <typename T>
 __global__ __launch_bounds__(kThreads) void sample_emit_kernel(const SampleArgs a) {
     const int tid = threadIdx.x;
-    const int rows = a.B * a.T, r = blockIdx.x % rows, chunk = blockIdx.x / rows, b = r / a.T;
-    if (a.top_k[b] > 0 && a.top_k[b] <= kListK) return;
+    const int rows = a.n_emit * a.T, chunk = blockIdx.x / rows, i_emit = blockIdx.x - chunk * rows, b = a.emit[i_emit / a.T];
+    const int r = b * a.T + i_emit % a.T;
     const int e0 = chunk * kSampleChunk + tid * kRun;
     const RowResult res = a.rows[r];
     float x[kRun], p[kRun];
     load_run(reinterpret_cast<const T *>(a.logits) + (size_t)r * a.V, e0, a.V, x);
-    __shared__ double table[64];
-    if (tid < 64) table[tid] = kExp2.v[tid];
+    __shared__ double table[kTable];
+    if (tid < kTable) table[tid] = kExp2.v[tid];
     __syncthreads();
     const float tv = key_value(res.t);   // the row has no NaN
     const uint32_t ti = (uint32_t)key_index(res.t);   // (a bound of values: past every index)
@@ -1229,28 +1291,36 @@ size_t sample_ws_bytes(int B, int T, int V) {
 
 template <typename T>
 static hipError_t launch_sample_t(const SampleArgs &a, hipStream_t st) {
-    const dim3 grid((unsigned)(a.B * a.T) * (unsigned)a.n_chunks), block(kThreads);
-    hipLaunchKernelGGL((sample_kernel<T>), grid, block, 0, st, a);
+    const unsigned T_ = (unsigned)a.T;
+    hipLaunchKernelGGL((sample_kernel<T>), dim3(a.B * T_ * a.n_chunks), dim3(kThreads), 0, st, a);
     hipError_t e = hipGetLastError();
-    // rows with a small top-k are finished there; plain ones have nothing to cut
-    bool cut = false, emit = false;
-    for (int b = 0; b < a.B; ++b) {
-        const bool listed = a.top_k[b] > 0 && a.top_k[b] <= kListK;
-        cut |= !listed && (a.top_k[b] > 0 || a.top_p[b] < 1.0 || a.min_p[b] > 0.0);
-        emit |= a.probs && !listed;
-    }
-    if (e == hipSuccess && cut) {
-        hipLaunchKernelGGL((sample_cut_kernel<T>), grid, block, 0, st, a);
+    if (e == hipSuccess && a.n_cut > 0) {
+        hipLaunchKernelGGL((sample_cut_kernel<T>), dim3(a.n_cut * T_ * a.cut_groups), dim3(kThreads), 0, st, a);
         e = hipGetLastError();
     }
-    if (e == hipSuccess && emit) {
-        hipLaunchKernelGGL((sample_emit_kernel<T>), grid, block, 0, st, a);
+    if (e == hipSuccess && a.n_emit > 0) {
+        hipLaunchKernelGGL((sample_emit_kernel<T>), dim3(a.n_emit * T_ * a.n_chunks), dim3(kThreads), 0, st, a);
         e = hipGetLastError();
     }
     return e;
 }
 
-hipError_t launch_sample(const SampleArgs &a, int dtype, hipStream_t st) {
+// Chunks of a row to a workgroup: as many as leave every workgroup resident at once.
+static void split_rows(int rows, int n_chunks, int *per_group, int *groups) {
+    *per_group = std::min((int)(((int64_t)rows * n_chunks + kResident - 1) / kResident), n_chunks);
+    *groups = (n_chunks + *per_group - 1) / *per_group;
+}
+
+hipError_t launch_sample(const SampleArgs &args, int dtype, hipStream_t st) {
+    SampleArgs a = args;
+    // rows with a small top-k are finished in the first launch; plain ones have nothing to cut
+    a.n_cut = a.n_emit = 0;
+    for (int b = 0; b < a.B; ++b) {
+        if (a.top_k[b] > 0 && a.top_k[b] <= kListK) continue;
+        if (a.top_k[b] > 0 || a.top_p[b] < 1.0 || a.min_p[b] > 0.0) a.cut[a.n_cut++] = (uint8_t)b;
+        if (a.probs) a.emit[a.n_emit++] = (uint8_t)b;
+    }
+    split_rows(std::max(a.n_cut, 1) * a.T, a.n_chunks, &a.cut_per_group, &a.cut_groups);
     return dtype == MAD_BF16 ? launch_sample_t<bf16_t>(a, st) : launch_sample_t<float>(a, st);
 }
 

@@ -120,13 +120,6 @@ __device__ __forceinline__ f16x8_v codes_f16(uint32_t lo, uint32_t hi) {
 // 0x80 in every byte that is a NaN code
 __device__ __forceinline__ uint32_t nan_codes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 
-// The same value, computed from here on: keeps the addresses that a rare part of the kernel derives from it out of
-// registers in the loop (the compiler would form them once, ahead of it).
-__device__ __forceinline__ int here(int v) {
-    asm volatile("" : "+v"(v));
-    return v;
-}
-
 struct KvScales {
     uint64_t k, v;
     int64_t seq, head;
