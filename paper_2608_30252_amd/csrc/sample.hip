@@ -198,9 +198,9 @@ struct SampleLds {
     double bucket_mass[kBins];
     uint32_t bucket_cnt[kBins];
     double c_mass[kSampleMaxChunks];    // per chunk: kept mass; against the row's maximum
-    uint64_t c_fix[kSampleMaxChunks];   // the same of listed entries, in units of 2^-50
-    float c_max[kSampleMaxChunks];
-    double part[16], part2[16];   // one per wave
+    double c_unit[kSampleMaxChunks];    // what its bins' units are against the row's maximum
+    float c_max[kSampleMaxChunks];      // its maximum; or where its keys begin in the list
+    double part[16];   // one per wave
     double res[4];
     uint64_t key[4];
     float fmx[16];
@@ -573,6 +573,7 @@ __device__ __forceinline__ void load_list(SampleLds &s, const char *rec0, int n_
     for (int c = wave; c < n_chunks; c += kThreads / 64) {
         const int nc = __builtin_amdgcn_readlane((int)(c < 64 ? n[0] : n[1]), c & 63);
         const int at = __builtin_amdgcn_readlane(c < 64 ? off[0] : off[1], c & 63);
+        if (lane == 0) s.c_max[c] = (float)at;
         for (int i = lane; i < nc; i += 64) {
             const uint64_t k = get64(rec0 + (size_t)c * kSampleRecord + kHead + 8 * i);
             s.list[at + i] = k;
@@ -617,9 +618,16 @@ __device__ __forceinline__ int draw(const Row<T> &row, uint64_t t, double u) {
     load_run(row.x, e0, row.V, x);
     double w[kRun], sum = 0.0;
     int last = -1;
+    const bool finite = row.m < INFINITY;
+    const Series terms = series();
     #pragma unroll
     for (int i = 0; i < kRun; ++i) {
-        w[i] = e0 + i < row.V && argmax_key(x[i], e0 + i) >= t ? weight(x[i], row.m, row.c, s.exp2) : 0.0;
+        const bool in = e0 + i < row.V && argmax_key(x[i], e0 + i) >= t && (finite ? x[i] > -INFINITY : x[i] == row.m);
+        w[i] = 0.0;
+        if (__any(in)) {
+            const double y = finite ? weight_finite(x[i], (double)row.m, row.c, s.exp2, terms) : 1.0;
+            w[i] = in && y > 0x1p-999 ? y : 0.0;
+        }
         sum += w[i];
         if (w[i] > 0.0) last = e0 + i;
     }
@@ -1058,7 +1066,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(const SampleArgs a)
                 if (lane + 64 * i < a.n_chunks) {
                     s.c_mass[lane + 64 * i] = cm[i];
                     s.c_max[lane + 64 * i] = h.max[i];
-                    s.c_fix[lane + 64 * i] = f64_bits(h.max[i] == -INFINITY ? 0.0 : kBinUnit * weight(h.max[i], m, row.c, s.exp2));
+                    s.c_unit[lane + 64 * i] = h.max[i] == -INFINITY ? 0.0 : kBinUnit * weight(h.max[i], m, row.c, s.exp2);
                 }
         }
         out.mass = __longlong_as_double((long long)wave_fold_u64(f64_bits(cm[0] + cm[1]), add_f64_bits));
@@ -1085,7 +1093,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(const SampleArgs a)
                         const char *q = rec0 + (size_t)k * kSampleRecord + kHead;
                         const int jc = in ? j - (int)d : 0;
                         const double x = (double)get64(q + 8 * jc);
-                        w += in ? x * bits_f64(s.c_fix[k]) : 0.0;
+                        w += in ? x * s.c_unit[k] : 0.0;
                         if (top_k > 0) {
                             const uint32_t y = __hip_atomic_load(reinterpret_cast<uint32_t *>(const_cast<char *>(q) + 8 * kBins + 4 * jc),
                                                                  __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -1124,7 +1132,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(const SampleArgs a)
 template <typename T>
 __global__ __launch_bounds__(kThreads, 8) void sample_cut_kernel(const SampleArgs a) {
     SampleLds &s = lds();
-    const int tid = threadIdx.x, lane = tid & 63;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int rows = a.n_cut * a.T, part = blockIdx.x / rows, i_cut = blockIdx.x - part * rows, b = a.cut[i_cut / a.T];
     const int r = b * a.T + i_cut % a.T, chunk0 = part * a.cut_per_group, chunk1 = min(chunk0 + a.cut_per_group, a.n_chunks);
     RowResult res = a.rows[r];
@@ -1202,7 +1210,6 @@ __global__ __launch_bounds__(kThreads, 8) void sample_cut_kernel(const SampleArg
         count += (double)(uint32_t)(h0 >> 32);
         if (tid < 64 && in) {
             s.c_mass[lane + 64 * i] = up;
-            s.c_fix[lane + 64 * i] = 0;
         }
     }
     const int all = uniform((int)group_sum<64>(total));
@@ -1226,23 +1233,24 @@ __global__ __launch_bounds__(kThreads, 8) void sample_cut_kernel(const SampleArg
     if (res.target >= 0.0) {
         t = max(t, select<false>(row, g, a.top_k[b] > 0, res.target, all));
     }
-    // each chunk's kept mass: above the range, and the listed entries that stay
-    #pragma unroll 1
-    for (int i = tid; i < all; i += kThreads) {
-        const uint64_t k = s.list[i];
-        if (k >= t)
-            atomicAdd((unsigned long long *)&s.c_fix[key_index(k) / kSampleChunk],
-                      units(weight(key_value(k), row.m, row.c, s.exp2), 1.0 / kBinUnit));
+    // each chunk's kept mass: above the range, and the listed entries that stay (a wave a chunk)
+    for (int c = wave; c < a.n_chunks; c += kThreads / 64) {
+        const int nc = __builtin_amdgcn_readlane((int)(c < 64 ? n[0] : n[1]), c & 63), at = (int)s.c_max[c];
+        unsigned long long sum = 0;
+        #pragma unroll 1
+        for (int i = lane; i < nc; i += 64) {
+            const uint64_t k = s.list[at + i];
+            sum += k >= t ? units(weight(key_value(k), row.m, row.c, s.exp2), 1.0 / kBinUnit) : 0;
+        }
+        sum = wave_fold_u64(sum, [](uint64_t x, uint64_t y) { return x + y; });
+        if (lane == 0) s.c_mass[c] += (double)sum * kBinUnit;
     }
     __syncthreads();
     double kept = 0.0;
     #pragma unroll
     for (int i = 0; i < 2; ++i)
-        if (lane + 64 * i < a.n_chunks) kept += s.c_mass[lane + 64 * i] + (double)s.c_fix[lane + 64 * i] * kBinUnit;
+        if (lane + 64 * i < a.n_chunks) kept += s.c_mass[lane + 64 * i];
     kept = uniform(__longlong_as_double((long long)wave_fold_u64(f64_bits(kept), add_f64_bits)));
-    __syncthreads();
-    if (tid < a.n_chunks) s.c_mass[tid] += (double)s.c_fix[tid] * kBinUnit;
-    __syncthreads();
     if (a.tok) {
         const int v = draw(row, t, (double)a.u[r]);
         if (tid == 0) a.tok[r] = v;
