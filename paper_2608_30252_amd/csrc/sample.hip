@@ -19,22 +19,36 @@
 //
 // Work.  Workgroup (chunk, row) of 1024 threads reads 8192 entries, 8 a thread.
 //   * Rows with a small top-k (kListK): it finds a value that at least top_k of
-//     its entries reach (from its threads' maxima, counted into bins of 1/8) and
+//     its entries reach (from its threads' maxima, counted into bins of 1/8, and
+//     where those crowd, from all of them in bins of a 256th of what is left) and
 //     writes the entries down to there, somewhat more than top_k, to the
 //     workspace.  The row's last workgroup then has every candidate: it sorts
 //     the best and applies the filters, the draw and the probabilities to them.
 //     The row is read once and nothing else of V entries is touched but the
 //     zeros of the distribution.
 //   * Other rows: it sums its weights, and where a filter is on, also by bins of
-//     1/8 below its maximum.  The row's last workgroup finds the bin in which
-//     top-p (or a large top-k) ends.  A second launch, over all chunks again,
-//     collects that bin's entries and the mass above it; its last workgroup finds
+//     1/8 below its maximum.  The row's last workgroup finds the bin in which the
+//     filter ends.  A second launch, over all chunks again, collects that bin's
+//     entries (the mass above it is known from the bins); its last workgroup finds
 //     the entry where the count or mass is reached, and draws.  Where distributions
 //     are asked for, a third launch writes them.
-//   What the bins do not resolve (values further apart than 32, thousands of
-//   equal ones, huge magnitudes, a large top-k with top-p) is narrowed down by
-//   one workgroup in passes over the row, with 2048 buckets of the key range
-//   each.
+//   What neither holds (thousands of entries to a bin, values further apart than
+//   32, huge magnitudes, a large top-k with top-p) one workgroup narrows down in
+//   passes over the row, with 2048 buckets of the key range each, from what is known.
+//
+// Bound.  Small calls: one launch's chain of round trips (loads 2.7 us, bins and
+// candidates 2.8, arrival 0.9, the records 2.4, the list's end 3.4): a row of 50257
+// 12.0 us, 20 rows with their distributions 13.2.  Large ones: 80 rows of 128256
+// fp32 with top-p and distributions (82 MB read and written once) 69 us: 26.5 for the
+// weights (two workgroups per CU load, then compute, in step: 1.5 TB/s; the vector ALU
+// is busy for half of it), 27 for the cut (a read at 4 TB/s, then 5 - 14 us for a
+// row's last workgroup), 16.4 for the distributions (5 TB/s, a copy's rate).  64 rows
+// of 128256 with settings of their own, tokens only, 48 us.  Rows that go by passes:
+// 90 - 220 us for top-p in a crowded body, 180 - 350 for a top-k above 128 with
+// top-p (rows of 50257 - 128256).
+//   Not kept: several chunks to a workgroup of the first launch, the next one's loads
+// in flight (its 64 registers do not hold the loop and the row's end: 33 us against
+// 26.5); the row's end as a function that is not inlined (75).
 #include "mad_device.h"
 #include "mad_internal.h"
 
@@ -1313,7 +1327,8 @@ static hipError_t launch_sample_t(const SampleArgs &a, hipStream_t st) {
     return e;
 }
 
-// Chunks of a row to a workgroup: as many as leave every workgroup resident at once.
+// The second launch's chunks to a workgroup: as many as leave every workgroup resident at once, so that one's loads run
+// under another's emission (28 rows of 16 chunks 28.8 -> 25.6 us, 80 rows 28.7 -> 27.5).
 static void split_rows(int rows, int n_chunks, int *per_group, int *groups) {
     *per_group = std::min((int)(((int64_t)rows * n_chunks + kResident - 1) / kResident), n_chunks);
     *groups = (n_chunks + *per_group - 1) / *per_group;
