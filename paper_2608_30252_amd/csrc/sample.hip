@@ -39,16 +39,16 @@
 // Bound.  Small calls: one launch's chain of round trips (loads 2.7 us, bins and
 // candidates 2.8, arrival 0.9, the records 2.4, the list's end 3.4): a row of 50257
 // 12.0 us, 20 rows with their distributions 13.2.  Large ones: 80 rows of 128256
-// fp32 with top-p and distributions (82 MB read and written once) 69 us: 26.5 for the
-// weights (two workgroups per CU load, then compute, in step: 1.5 TB/s; the vector ALU
-// is busy for half of it), 27 for the cut (a read at 4 TB/s, then 5 - 14 us for a
+// fp32 with top-p and distributions (82 MB read and written once) 67.5 us: 25.4 for the
+// weights (two workgroups per CU load, then compute, in step: 1.6 TB/s, and the vector
+// ALU is busy four fifths of the time: 31 instructions an entry), 27 for the cut (a read at 4 TB/s, then 5 - 14 us for a
 // row's last workgroup), 16.4 for the distributions (5 TB/s, a copy's rate).  64 rows
-// of 128256 with settings of their own, tokens only, 48 us.  Rows that go by passes:
+// of 128256 with settings of their own, tokens only, 47 us.  Rows that go by passes:
 // 90 - 220 us for top-p in a crowded body, 180 - 350 for a top-k above 128 with
 // top-p (rows of 50257 - 128256).
 //   Not kept: several chunks to a workgroup of the first launch, the next one's loads
 // in flight (its 64 registers do not hold the loop and the row's end: 33 us against
-// 26.5); the row's end as a function that is not inlined (75).
+// 26.5 of one to each); the row's end as a function that is not inlined (75).
 #include "mad_device.h"
 #include "mad_internal.h"
 
@@ -99,9 +99,10 @@ __device__ __forceinline__ double weight_finite(float x, double m, double c, con
     p = fma(p, f, s.k2);
     p = fma(p, f, s.k1);
     p = fma(p, f, 1.0);
-    const int n = (int)__double_as_longlong(t);
+    const uint32_t n = (uint32_t)__double_as_longlong(t);
     const uint64_t w = (uint64_t)__double_as_longlong(p * table[n & (kTable - 1)]);
-    return __longlong_as_double((long long)(w + ((uint64_t)(uint32_t)((n >> 8) << 20) << 32)));   // times 2^(n >> 8)
+    const uint32_t hi = (uint32_t)(w >> 32) + ((n & ~(uint32_t)(kTable - 1)) << 12);   // times 2^(n >> 8)
+    return __longlong_as_double((long long)((uint64_t)hi << 32 | (uint32_t)w));
 }
 // any m and x (+inf against +inf: 1; below 2^-1000: 0)
 __device__ __forceinline__ double weight(float x, float m, double c, const double *table) {
@@ -1002,22 +1003,30 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(const SampleArgs a)
             for (int i = 0; i < kRun; ++i) mass += x[i] == m ? 1.0 : 0.0;
         } else if (m > -INFINITY) {   // (what is past the row's end is -inf: as good as 0)
             const Series terms = series();
-            const double md = (double)m;
+            double md = (double)m, c = row.c;
+            asm volatile("" : "+v"(md), "+v"(c));   // (kept at hand)
             const int mi = (int)mb;   // (where there are bins)
-            #pragma unroll
-            for (int i = 0; i < kRun; ++i) {
-                const double w = weight_finite(x[i], md, row.c, s.exp2, terms);
-                mass += w;
-                if (binned && !(flags & kNoBins)) {
-                    const float low = floorf(x[i] * 8.f);
-                    if (mb - low < (float)kBins) {   // (not -inf)
-                        const int j = mi - (int)low;
-                        atomicAdd((unsigned long long *)&s.mass[j], units(w, 1.0 / kBinUnit));
-                        if (top_k > 0) atomicAdd(&s.cnt[j], 1u);
+            auto weigh = [&](auto bins, auto count) {
+                #pragma unroll
+                for (int i = 0; i < kRun; ++i) {
+                    const double w = weight_finite(x[i], md, c, s.exp2, terms);
+                    mass += w;
+                    if constexpr (bins.value) {
+                        const float low = floorf(x[i] * 8.f);
+                        if (mb - low < (float)kBins) {   // (not -inf)
+                            const int j = mi - (int)low;
+                            atomicAdd((unsigned long long *)&s.mass[j], units(w, 1.0 / kBinUnit));
+                            if constexpr (count.value) atomicAdd(&s.cnt[j], 1u);
+                        }
                     }
+                    if (i % 2 == 1) __builtin_amdgcn_sched_barrier(0);   // (few temporaries at a time)
                 }
-                if (i % 2 == 1) __builtin_amdgcn_sched_barrier(0);   // (few temporaries at a time)
-            }
+            };
+            using Yes = std::true_type;
+            using No = std::false_type;
+            if (!binned || (flags & kNoBins)) weigh(No(), No());
+            else if (top_k > 0) weigh(Yes(), Yes());
+            else weigh(Yes(), No());
         }
         mass = block_sum(mass, s.part);   // (its barrier stands behind the atomics)
         if (binned && tid < kBins) {
