@@ -32,9 +32,11 @@
 //     entries (the mass above it is known from the bins); its last workgroup finds
 //     the entry where the count or mass is reached, and draws.  Where distributions
 //     are asked for, a third launch writes them.
-//   What neither holds (thousands of entries to a bin, values further apart than
-//   32, huge magnitudes, a large top-k with top-p) one workgroup narrows down in
-//   passes over the row, with 2048 buckets of the key range each, from what is known.
+//   * Rows with a large top-k and a top-p: top-p's bin is known only behind the k-th
+//     entry, so the row's last workgroup collects both bins' entries itself.
+//   What none of these holds (thousands of entries to a bin, values further apart
+//   than 32, huge magnitudes) one workgroup narrows down in passes over the row, with
+//   2048 buckets of the key range each, from what is known.
 //
 // Bound.  Small calls: one launch's chain of round trips (loads 2.7 us, bins and
 // candidates 2.8, arrival 0.9, the records 2.4, the list's end 3.4): a row of 50257
@@ -43,9 +45,10 @@
 // weights (two workgroups per CU load, then compute, in step: 1.6 TB/s, and the vector
 // ALU is busy four fifths of the time: 31 instructions an entry), 27 for the cut (a read at 4 TB/s, then 5 - 14 us for a
 // row's last workgroup), 16.4 for the distributions (5 TB/s, a copy's rate).  64 rows
-// of 128256 with settings of their own, tokens only, 47 us.  Rows that go by passes:
-// 90 - 220 us for top-p in a crowded body, 180 - 350 for a top-k above 128 with
-// top-p (rows of 50257 - 128256).
+// of 128256 with settings of their own, tokens only, 47 us.  A top-k of 200
+// with top-p, tokens only: a row of 50257 65 us, 16 rows of 128256 85.  Rows that go
+// by passes: 78 - 160 for top-p in a crowded body, 90 - 330 where all entries are
+// within 1/8 (the same sizes).
 //   Not kept: several chunks to a workgroup of the first launch, the next one's loads
 // in flight (its 64 registers do not hold the loop and the row's end: 33 us against
 // 26.5 of one to each); the row's end as a function that is not inlined (75).
@@ -186,6 +189,9 @@ __device__ __forceinline__ void put64(void *p, uint64_t v) {
     __hip_atomic_store(reinterpret_cast<uint64_t *>(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 __device__ __forceinline__ uint64_t get64(const void *p) { return load_agent64(reinterpret_cast<const uint64_t *>(p)); }
+__device__ __forceinline__ uint32_t get32(const void *p) {
+    return __hip_atomic_load(reinterpret_cast<uint32_t *>(const_cast<void *>(p)), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
 __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
     return (uint32_t)wave_fold_u64(v, [](uint64_t x, uint64_t y) { return x > y ? x : y; });
 }
@@ -837,6 +843,7 @@ template <typename T> struct SolveJob {
     double target;
     uint64_t least;
     int n;
+    const char *rec0;   // the row's records
 };
 template <typename T>
 __device__ __noinline__ void solve_row(const SolveJob<T> j) {
@@ -874,8 +881,144 @@ __device__ __forceinline__ SolveJob<T> solve_job(const SampleArgs &a, const Row<
     const int b = r / a.T, k = a.top_k[b];
     return SolveJob<T>{row, a.top_p[b], a.min_p[b], a.tok ? (double)a.u[r] : 0.0, a.tok ? a.tok + r : nullptr,
                        a.probs && k > 0 && k <= kListK ? a.probs + (size_t)r * a.V : nullptr, a.rows + r, k,
-                       Range{0, 0, 0.0, 0.0}, -1.0, 0, kUnknown};
+                       Range{0, 0, 0.0, 0.0}, -1.0, 0, kUnknown, a.records + (size_t)r * a.n_chunks * kSampleRecord};
 }
+
+// A row with a large top-k and a top-p (whose target is known only behind top-k), from its chunks' bins (c_max and
+// c_unit are set), by its last workgroup: for each filter the bin in which it ends, that bin's entries from the row, and
+// among them the place; then the draw.
+template <typename T>
+__device__ __noinline__ void cut_row(const SolveJob<T> job) {
+    SampleLds &s = lds();
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const Row<T> row = job.row;
+    const char *rec0 = job.rec0;
+    const uint64_t least = job.least;
+    double total = 0.0;
+    const float rb = floorf(row.m * 8.f), low = (rb - (float)(kBins - 1)) * 0.125f;   // low: the bins' end
+    const uint64_t bits = (uint64_t)0xffffffffu << 32;
+    uint64_t t = least;
+    float lo, hi = -INFINITY;   // the values listed
+    int all = 0;
+    for (int pass = 0; pass < 3; ++pass) {   // top-k, top-p of its mass, and where another key than top-p's is the end, its bin
+        const bool by_count = pass == 0;
+        double target = -1.0;
+        if (pass < 2) {
+            target = by_count ? (double)job.top_k : job.top_p * total;
+            // the row's bins: bin j of a chunk whose maximum lies d bins lower is the row's j + d
+            const int j = tid & (kBins - 1);
+            double w = 0.0;
+            uint32_t n = 0;
+            #pragma unroll 4
+            for (int k = tid / kBins; k < row.n_chunks; k += kThreads / kBins) {
+                const float top = s.c_max[k], d = rb - floorf(top * 8.f);
+                const bool in = top > -INFINITY && (float)j >= d;
+                const char *q = rec0 + (size_t)k * kSampleRecord + kHead;
+                const int jc = in ? j - (int)d : 0;
+                if (by_count) n += in ? get32(q + 8 * kBins + 4 * jc) : 0;
+                else w += in ? (double)get64(q + 8 * jc) * s.c_unit[k] : 0.0;
+            }
+            s.list[tid] = f64_bits(by_count ? (double)n : w);
+            __syncthreads();
+            if (wave == 0) {
+                auto bin = [&](int i) {
+                    return bits_f64(s.list[i]) + bits_f64(s.list[i + kBins]) + bits_f64(s.list[i + 2 * kBins]) + bits_f64(s.list[i + 3 * kBins]);
+                };
+                double before;
+                const int i = first_reaching(bin, target, &before);
+                if (lane == 0) s.num[0] = before + bin(i) >= target ? i : kBins;   // kBins: reached below the last bin
+            }
+            __syncthreads();
+            const int i = uniform(s.num[0]);
+            lo = i < kBins ? (rb - (float)i) * 0.125f : -3.402823466e38f;   // (an entry of -inf has no mass)
+            hi = (rb - (float)(i - 1)) * 0.125f;
+            // where min-p ends above top-p's bin, only that counts
+            if (key_value(least) >= hi && !by_count) continue;
+        } else {
+            const float tv = key_value(t);
+            if (tv < hi) break;
+            lo = tv;
+            hi = fmaxf((floorf(tv * 8.f) + 1.f) * 0.125f, low);
+        }
+        // what lies above the range, chunk by chunk (a wave a chunk), and the entries in it
+        __syncthreads();
+        if (tid == 0) s.num[1] = 0, s.num[3] = 0;
+        __syncthreads();
+        for (int c = wave; c < row.n_chunks; c += kThreads / 64) {
+            const float ups = floorf(s.c_max[c] * 8.f) - hi * 8.f;   // the last bin above
+            const char *q = rec0 + (size_t)c * kSampleRecord + kHead;
+            uint64_t sum = 0;
+            uint32_t n = 0;
+            #pragma unroll
+            for (int i = 0; i < kBins / 64; ++i) {
+                const bool up = (float)(lane + 64 * i) <= ups;
+                const uint64_t y = get64(q + 8 * (lane + 64 * i));
+                sum += up ? y : 0;
+                if (by_count) {
+                    const uint32_t z = get32(q + 8 * kBins + 4 * (lane + 64 * i));
+                    n += up ? z : 0;
+                }
+            }
+            sum = wave_fold_u64(sum, [](uint64_t x, uint64_t y) { return x + y; });
+            if (by_count) n = (uint32_t)group_sum<64>((float)n);   // (exact: at most 8192)
+            if (lane == 0) {
+                s.c_mass[c] = (double)sum * s.c_unit[c];
+                if (by_count) atomicAdd(&s.num[1], (int)n);
+            }
+        }
+        row.each([&](float x, int i) {
+            if (x >= lo && x < hi) {
+                const int p = atomicAdd(&s.num[3], 1);
+                if (p < kList) s.list[p] = argmax_key(x, i);
+            }
+        });
+        __syncthreads();
+        all = uniform(s.num[3]);
+        double above = 0.0;
+        #pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (lane + 64 * i < row.n_chunks) above += s.c_mass[lane + 64 * i];
+        above = uniform(__longlong_as_double((long long)wave_fold_u64(f64_bits(above), add_f64_bits)));
+        Range g = {argmax_key(lo, 0) & bits, (argmax_key(hi, 0) & bits) - 1, above, (double)uniform(s.num[1])};
+        if (all > kList) {
+            SolveJob<T> rest = job;
+            if (pass == 0) rest.range = g, rest.target = target, rest.n = all;   // (else top-k's place is behind)
+            solve_row<T>(rest);
+            return;
+        }
+        if (target >= 0.0) {
+            t = max(t, select<false>(row, g, by_count, target, all));
+            if (by_count) total = g.mass;   // at and above the k-th
+        }
+    }
+    // each chunk's kept mass: above the range, and the listed entries that stay
+    uint64_t *fix = reinterpret_cast<uint64_t *>(s.c_unit);   // (whose values are not needed any more)
+    __syncthreads();
+    if (tid < kSampleMaxChunks) fix[tid] = 0;
+    __syncthreads();
+    #pragma unroll 1
+    for (int i = tid; i < all; i += kThreads) {
+        const uint64_t k = s.list[i];
+        if (k >= t)
+            atomicAdd((unsigned long long *)&fix[key_index(k) / kSampleChunk], units(weight(key_value(k), row.m, row.c, s.exp2), 1.0 / kBinUnit));
+    }
+    __syncthreads();
+    if (tid < row.n_chunks) s.c_mass[tid] += (double)fix[tid] * kBinUnit;
+    __syncthreads();
+    double kept = 0.0;
+    #pragma unroll
+    for (int i = 0; i < 2; ++i)
+        if (lane + 64 * i < row.n_chunks) kept += s.c_mass[lane + 64 * i];
+    kept = uniform(__longlong_as_double((long long)wave_fold_u64(f64_bits(kept), add_f64_bits)));
+    if (job.tok) {
+        const int v = draw(row, t, job.u);
+        if (tid == 0) *job.tok = v;
+    }
+    if (tid == 0) *job.out = RowResult{t, kept, 0.0, 0.f, 0.f, row.m, kRowDone};
+}
+
+// rows that the first launch ends though their candidates are not listed
+__host__ __device__ inline bool both_filters(int top_k, double top_p) { return top_k > kListK && top_p < 1.0; }
 
 template <typename T>
 __global__ __launch_bounds__(kThreads, 8) void sample_kernel(const SampleArgs a) {
@@ -1097,6 +1240,13 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(const SampleArgs a)
         const double min_p = a.min_p[b];
         if (min_p > 0.0) out.t = least_weight(m, row.c, min_p);   // so far: no entry below it stays
         if (binned) {
+            if (both_filters(top_k, a.top_p[b])) {
+                SolveJob<T> job = solve_job(a, row, r);
+                job.least = out.t;
+                if (h.no_bins) solve_row<T>(job);
+                else cut_row<T>(job);
+                return;
+            }
             if (h.no_bins) {
                 out.mode = kRowSlow;
             } else {
@@ -1240,12 +1390,12 @@ __global__ __launch_bounds__(kThreads, 8) void sample_cut_kernel(const SampleArg
     count = uniform(__longlong_as_double((long long)wave_fold_u64(f64_bits(count), add_f64_bits)));
     const uint64_t bits = (uint64_t)0xffffffffu << 32;
     Range g = {argmax_key(res.lo, 0) & bits, (argmax_key(res.hi, 0) & bits) - 1, mass, count};
-    if (__any(over) || all > kList || (a.top_k[b] > 0 && a.top_p[b] < 1.0)) {
+    if (__any(over) || all > kList) {
         SolveJob<T> job = solve_job(a, row, r);
         job.range = g;
         job.target = res.target;
         job.least = res.t;
-        job.n = a.top_k[b] > 0 && a.top_p[b] < 1.0 && res.target < 0.0 ? kUnknown : all;   // (top-p of top-k's mass all the same)
+        job.n = all;
         solve_row<T>(job);
         return;
     }
@@ -1345,11 +1495,11 @@ static void split_rows(int rows, int n_chunks, int *per_group, int *groups) {
 
 hipError_t launch_sample(const SampleArgs &args, int dtype, hipStream_t st) {
     SampleArgs a = args;
-    // rows with a small top-k are finished in the first launch; plain ones have nothing to cut
+    // rows with a small top-k, or with top-k and top-p, are finished in the first launch; plain ones have nothing to cut
     a.n_cut = a.n_emit = 0;
     for (int b = 0; b < a.B; ++b) {
         if (a.top_k[b] > 0 && a.top_k[b] <= kListK) continue;
-        if (a.top_k[b] > 0 || a.top_p[b] < 1.0 || a.min_p[b] > 0.0) a.cut[a.n_cut++] = (uint8_t)b;
+        if ((a.top_k[b] > 0 || a.top_p[b] < 1.0 || a.min_p[b] > 0.0) && !both_filters(a.top_k[b], a.top_p[b])) a.cut[a.n_cut++] = (uint8_t)b;
         if (a.probs) a.emit[a.n_emit++] = (uint8_t)b;
     }
     split_rows(std::max(a.n_cut, 1) * a.T, a.n_chunks, &a.cut_per_group, &a.cut_groups);

@@ -97,6 +97,19 @@ def test_distributions(dtype, kind):
         _run(kind, (1, 2, 700), dtype, 30 + i, **kw)
 
 
+@pytest.mark.parametrize("kind", ["model", "body", "wide", "ties", "masked", "lowest", "spike"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_filters_of_any_strength_together(dtype, kind):
+    # top-k of 1 .. V with top-p close to 0, in between and close to 1, and a min-p above and below both
+    rng = np.random.default_rng(len(kind))
+    for i in range(12):
+        V = int(rng.choice([300, 9000, 20000]))
+        kw = dict(temperature=float(np.exp(rng.normal(0, 0.7))), top_k=int(np.exp(rng.uniform(0, np.log(V)))),
+                  top_p=float(rng.choice([rng.uniform(0, 1), 1 - 10 ** rng.uniform(-6, -2), 10 ** rng.uniform(-6, -2)])),
+                  min_p=float(rng.choice([0.0, 10 ** rng.uniform(-6, 0)])))
+        _run(kind, (2, 2, V), dtype, 70 + i, probs=i % 2 == 0, **kw)
+
+
 def test_a_top_k_beyond_32_bits_keeps_all():
     mad = _mad()
     x, u = _logits("model", (2, 1, 5000), 3).cuda(), torch.rand((2, 1), device="cuda")
