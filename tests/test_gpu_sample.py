@@ -137,6 +137,15 @@ def test_sizes(V, dtype):
         _run("model", (1, 2 if V < 60000 else 1, V), dtype, V + i, probs=i != 3, **kw)
 
 
+@pytest.mark.parametrize("V", [600001, 1 << 20])
+def test_the_largest_vocabularies(V):
+    # more chunks than a wave has lanes; all of them
+    for i, kw in enumerate((dict(top_k=128, top_p=0.9), dict(top_p=0.95), dict(top_k=1000), dict(top_k=1000, top_p=0.5), dict(min_p=0.01),
+                            dict(), dict(temperature=0))):
+        _run("model", (1, 1, V), ("bf16", "f32")[i % 2], 90 + i, probs=i % 3 == 0, **kw)
+    _run("body", (1, 1, V), "f32", 97, top_p=0.9)
+
+
 def test_every_sequence_its_own_settings():
     B = 64
     kw = dict(temperature=[0.0 if b % 7 == 0 else 0.5 + 0.02 * b for b in range(B)], top_k=[(0, 30, 200, 1, 5000)[b % 5] for b in range(B)],
@@ -200,7 +209,9 @@ def test_the_same_bits_every_time():
     mad = _mad()
     x = _logits("model", (4, 2, 50257), 58).cuda()
     u = torch.rand(4, 2, device="cuda")
-    for kw in (dict(top_k=100, top_p=0.9), dict(top_p=0.95), dict(top_k=900), dict()):
+    body = _logits("body", (4, 2, 50257), 59).cuda()      # (by passes over the row)
+    for x, kw in ((x, dict(top_k=100, top_p=0.9)), (x, dict(top_p=0.95)), (x, dict(top_k=900)), (x, dict()), (x, dict(top_k=900, top_p=0.7)),
+                  (body, dict(top_p=0.9)), (body, dict(top_k=9000, top_p=0.9))):
         first = None
         for _ in range(5):
             tok, p = mad.sample(x, u, probs=torch.empty_like(x), **kw)
