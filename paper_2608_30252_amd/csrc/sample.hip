@@ -43,12 +43,12 @@
 // 12.0 us, 20 rows with their distributions 13.2.  Large ones: 80 rows of 128256
 // fp32 with top-p and distributions (82 MB read and written once) 67.5 us: 25.4 for the
 // weights (two workgroups per CU load, then compute, in step: 1.6 TB/s, and the vector
-// ALU is busy four fifths of the time: 31 instructions an entry), 27 for the cut (a read at 4 TB/s, then 5 - 14 us for a
-// row's last workgroup), 16.4 for the distributions (5 TB/s, a copy's rate).  64 rows
-// of 128256 with settings of their own, tokens only, 47 us.  A top-k of 200
-// with top-p, tokens only: a row of 50257 65 us, 16 rows of 128256 85.  Rows that go
-// by passes: 78 - 160 for top-p in a crowded body, 90 - 330 where all entries are
-// within 1/8 (the same sizes).
+// ALU is busy four fifths of the time: 31 instructions an entry), 27 for the cut (a
+// read at 4 TB/s, then 5 - 14 us for a row's last workgroup), 16.4 for the
+// distributions (5 TB/s, a copy's rate).  64 rows of 128256 with settings of their own,
+// tokens only, 47 us.  A top-k of 200 with top-p, tokens only: a row of 50257 65 us,
+// 16 rows of 128256 85.  Rows that go by passes: 78 - 160 for top-p in a crowded body,
+// 90 - 330 where all entries are within 1/8 (the same sizes).
 //   Not kept: several chunks to a workgroup of the first launch, the next one's loads
 // in flight (its 64 registers do not hold the loop and the row's end: 33 us against
 // 26.5 of one to each); the row's end as a function that is not inlined (75).
@@ -191,9 +191,6 @@ __device__ __forceinline__ void put64(void *p, uint64_t v) {
 __device__ __forceinline__ uint64_t get64(const void *p) { return load_agent64(reinterpret_cast<const uint64_t *>(p)); }
 __device__ __forceinline__ uint32_t get32(const void *p) {
     return __hip_atomic_load(reinterpret_cast<uint32_t *>(const_cast<void *>(p)), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
-    return (uint32_t)wave_fold_u64(v, [](uint64_t x, uint64_t y) { return x > y ? x : y; });
 }
 __device__ __forceinline__ uint64_t f64_bits(double v) { return (uint64_t)__double_as_longlong(v); }
 __device__ __forceinline__ double bits_f64(uint64_t v) { return __longlong_as_double((long long)v); }
