@@ -266,8 +266,8 @@ typedef struct mad_kv8_view {
  *   code  = e4m3(x / scale), round to nearest even; an element that is not
  *           finite is stored as NaN
  * Where the scale grows, the block's rows below len[b] are written again with
- * it, e4m3(code * old scale / scale): the scales are powers of two, so this is
- * exact but for codes that get below 2^-6.  A block's scale never falls while
+ * it, e4m3(code * old scale / scale): between powers of two, as this call writes
+ * them, that is exact but for codes that get below 2^-6.  A block's scale never falls while
  * it holds rows, also not by a rollback.  Rows and scales of other blocks, and
  * rows from len[b] + n[b] on, are left as they are.
  *   k_new, v_new  device [B][n_cap][Hkv][d], dtype; rows from n[b] on are not read
@@ -363,10 +363,10 @@ int mad_accept_stochastic(const float *p, const float *q, const int32_t *draft_t
  *   u       device float32 [B][T] uniforms in [0, 1); NULL if tok is
  *   temperature, top_k, top_p, min_p   HOST arrays [B] (double, top_k int32);
  *           NULL: 1, 0, 1 and 0
- *   tok     device int32 [B][T] or NULL;  probs  device float32 [B][T][V] or NULL (not both)
+ *   tok     device int32 [B][T] or NULL;  probs  device float32 [B][T][V] or NULL (one of them is given)
  * temperature >= 0 and finite, top_k >= 0, 0 < top_p <= 1, 0 <= min_p <= 1;
- * T <= 64, V <= 2^20.  probs must not overlap logits.  Rows may start at any address that suits their
- * type.  Workspace MAD_OP_SAMPLE.
+ * T <= 64, V <= 2^20.  probs must not overlap logits.  Rows may start at any
+ * address that suits their type.  Workspace MAD_OP_SAMPLE, 256-byte aligned.
  */
 int mad_sample(const void *logits, int dtype, const float *u, const double *temperature, const int32_t *top_k,
                const double *top_p, const double *min_p, int B, int T, int V, int32_t *tok, float *probs, void *ws,
