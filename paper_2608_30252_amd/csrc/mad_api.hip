@@ -788,6 +788,7 @@ int mad_sample(const void *logits, int dtype, const float *u, const double *temp
         a.top_k[b] = greedy ? 1 : k < V ? k : 0;
         a.top_p[b] = greedy ? 1.0 : p;
         a.min_p[b] = greedy ? 0.0 : mp;
+        a.drop[b] = a.min_p[b] > 0.0 ? 256.0 * log2(a.min_p[b]) / a.c[b] : 0.0;
     }
     const size_t need = mad::sample_ws_bytes(B, T, V);
     if (!ws) return fail(MAD_EWS, "workspace required (%zu bytes)", need);

@@ -238,6 +238,7 @@ struct SampleArgs {
     int B, T, V, n_chunks;
     double c[kMaxB];       // 256 log2 e / temperature
     double top_p[kMaxB], min_p[kMaxB];
+    double drop[kMaxB];    // where min-p ends, above the maximum (<= 0): log(min_p) * temperature
     int top_k[kMaxB];      // 0: off
     // (set by launch_sample) the second launch's chunks to a workgroup and workgroups to a row; its sequences and the third's
     int cut_per_group, cut_groups, n_cut, n_emit;

@@ -26,6 +26,8 @@
 //     the best and applies the filters, the draw and the probabilities to them.
 //     The row is read once and nothing else of V entries is touched but the
 //     zeros of the distribution.
+//   * Rows with min-p alone likewise: a chunk's candidates are what min-p leaves
+//     against its own maximum (the row's leaves no more of them).
 //   * Other rows: it sums its weights, and where a filter is on, also by bins of
 //     1/8 below its maximum.  The row's last workgroup finds the bin in which the
 //     filter ends.  A second launch, over all chunks again, collects that bin's
@@ -47,8 +49,9 @@
 // read at 4 TB/s, then 5 - 14 us for a row's last workgroup), 16.4 for the
 // distributions (5 TB/s, a copy's rate).  64 rows of 128256 with settings of their own,
 // tokens only, 47 us.  A top-k of 200 with top-p, tokens only: a row of 50257 65 us,
-// 16 rows of 128256 85.  Rows that go by passes: 78 - 160 for top-p in a crowded body,
-// 90 - 330 where all entries are within 1/8 (the same sizes).
+// 16 rows of 128256 85; min-p alone 14.5 and 15.8 (by the bins 23 and 24).  Rows that
+// go by passes: 78 - 160 for top-p in a crowded body, 48 - 76 for min-p there, 90 - 330
+// for the other filters where all entries are within 1/8 (the same sizes).
 //   Not kept: several chunks to a workgroup of the first launch, the next one's loads
 // in flight (its 64 registers do not hold the loop and the row's end: 33 us against
 // 26.5 of one to each); the row's end as a function that is not inlined (75).
@@ -206,7 +209,8 @@ __device__ __forceinline__ double uniform(double v) { return bits_f64(uniform(f6
 //   first launch:  maximum, flags | edge, keys | mass          second: count and keys | mass above the range
 constexpr int kHead = 32;
 static_assert(kHead + kBins * 12 <= (int)kSampleRecord && kHead + kEmit * 8 <= (int)kSampleRecord, "chunk record");
-constexpr uint32_t kNaN = 1, kNoBins = 2, kLeft = 4;   // flags: a NaN; magnitudes beyond the bins; candidates left out below `edge`
+// flags: a NaN; magnitudes beyond the bins; candidates left out below `edge` (min-p's: up to it)
+constexpr uint32_t kNaN = 1, kNoBins = 2, kLeft = 4;
 
 struct SampleLds {
     uint64_t list[kList];       // gathered keys
@@ -756,6 +760,31 @@ __device__ __forceinline__ void finish_list(const Row<T> &row, const SampleArgs 
     if (tid == 0) a.tok[r] = s.num[1] != 0x7fffffff ? s.num[1] : s.num[2];
 }
 
+// The listed entries that stay (n[]: a chunk's, as in load_list) to their chunks' masses, a wave a chunk; returns the
+// sum over the row.
+template <typename T>
+__device__ __forceinline__ double add_listed(const Row<T> &row, const uint32_t (&n)[2], uint64_t t) {
+    SampleLds &s = lds();
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int c = wave; c < row.n_chunks; c += kThreads / 64) {
+        const int nc = __builtin_amdgcn_readlane((int)(c < 64 ? n[0] : n[1]), c & 63), at = (int)s.c_max[c];
+        unsigned long long sum = 0;
+        #pragma unroll 1
+        for (int i = lane; i < nc; i += 64) {
+            const uint64_t k = s.list[at + i];
+            sum += k >= t ? units(weight(key_value(k), row.m, row.c, s.exp2), 1.0 / kBinUnit) : 0;
+        }
+        sum = wave_fold_u64(sum, [](uint64_t x, uint64_t y) { return x + y; });
+        if (lane == 0) s.c_mass[c] += (double)sum * kBinUnit;
+    }
+    __syncthreads();
+    double kept = 0.0;
+    #pragma unroll
+    for (int i = 0; i < 2; ++i)
+        if (lane + 64 * i < row.n_chunks) kept += s.c_mass[lane + 64 * i];
+    return uniform(__longlong_as_double((long long)wave_fold_u64(f64_bits(kept), add_f64_bits)));
+}
+
 // kept mass of every chunk into c_mass[]; returns their sum
 template <typename T>
 __device__ __forceinline__ double chunk_masses(const Row<T> &row, uint64_t t) {
@@ -1014,6 +1043,8 @@ __device__ __noinline__ void cut_row(const SolveJob<T> job) {
     if (tid == 0) *job.out = RowResult{t, kept, 0.0, 0.f, 0.f, row.m, kRowDone};
 }
 
+// rows whose one filter is min-p: what stays is known from the maximum
+__host__ __device__ inline bool min_p_only(int top_k, double top_p, double min_p) { return top_k == 0 && top_p >= 1.0 && min_p > 0.0; }
 // rows that the first launch ends though their candidates are not listed
 __host__ __device__ inline bool both_filters(int top_k, double top_p) { return top_k > kListK && top_p < 1.0; }
 
@@ -1024,7 +1055,8 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(const SampleArgs a)
     const int rows = a.B * a.T, chunk = blockIdx.x / rows, r = blockIdx.x - chunk * rows, b = r / a.T;
     const int top_k = a.top_k[b];
     const bool listed = top_k > 0 && top_k <= kListK;
-    const bool binned = !listed && (top_k > 0 || a.top_p[b] < 1.0 || a.min_p[b] > 0.0);
+    const bool floored = min_p_only(top_k, a.top_p[b], a.min_p[b]);
+    const bool binned = !listed && !floored && (top_k > 0 || a.top_p[b] < 1.0);
     Row<T> row = row_of<T>(a, r);
     char *rec0 = a.records + (size_t)r * a.n_chunks * kSampleRecord, *rec = rec0 + (size_t)chunk * kSampleRecord;
 
@@ -1137,6 +1169,23 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(const SampleArgs a)
         } else if (m > -INFINITY) {
             flags |= kLeft;   // (edge +inf) candidates only by the row's last workgroup
         }
+    } else if (floored) {
+        // what min-p leaves against this chunk's maximum (the row's leaves no more), with a margin for the roundings here
+        const double bound = (double)m + a.drop[b];
+        edge = (float)(bound - 1e-6 * (fabs((double)m) + fabs(a.drop[b])) - 1e-40);
+        if (fabsf(m) < 1e30f && edge > -1e30f) {
+            #pragma unroll
+            for (int i = 0; i < kRun; ++i)
+                if (x[i] >= edge) {
+                    const int p = atomicAdd(&s.num[0], 1);
+                    if (p < kEmit) put64(rec + kHead + 8 * p, argmax_key(x[i], e0 + i));
+                }
+            __syncthreads();
+            n_out = (uint32_t)s.num[0];
+            if (n_out > (uint32_t)kEmit) flags |= kLeft, edge = m, n_out = 0;   // (none of them may stay in the row)
+        } else if (m > -INFINITY) {
+            flags |= kLeft, edge = INFINITY;   // by the row's last workgroup
+        }
     } else {
         if (m == INFINITY) {
             #pragma unroll
@@ -1218,6 +1267,22 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(const SampleArgs a)
         }
         solve_row<T>(solve_job(a, row, r));
         return;
+    } else if (floored) {
+        out.t = least_weight(m, row.c, a.min_p[b]);
+        if (h.total > kList || (h.left && h.worst >= key_value(out.t))) {
+            SolveJob<T> job = solve_job(a, row, r);
+            job.least = out.t;
+            solve_row<T>(job);
+            return;
+        }
+        load_list(s, rec0, a.n_chunks, h.n, [](uint64_t) {});
+        if (tid < a.n_chunks) s.c_mass[tid] = 0.0;
+        __syncthreads();
+        out.mass = add_listed(row, h.n, out.t);
+        if (a.tok) {
+            const int v = draw(row, out.t, (double)a.u[r]);
+            if (tid == 0) a.tok[r] = v;
+        }
     } else {
         // the chunks' masses against the row's maximum
         double cm[2];
@@ -1302,7 +1367,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(const SampleArgs a)
 template <typename T>
 __global__ __launch_bounds__(kThreads, 8) void sample_cut_kernel(const SampleArgs a) {
     SampleLds &s = lds();
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63;
     const int rows = a.n_cut * a.T, part = blockIdx.x / rows, i_cut = blockIdx.x - part * rows, b = a.cut[i_cut / a.T];
     const int r = b * a.T + i_cut % a.T, chunk0 = part * a.cut_per_group, chunk1 = min(chunk0 + a.cut_per_group, a.n_chunks);
     RowResult res = a.rows[r];
@@ -1403,24 +1468,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_cut_kernel(const SampleArg
     if (res.target >= 0.0) {
         t = max(t, select<false>(row, g, a.top_k[b] > 0, res.target, all));
     }
-    // each chunk's kept mass: above the range, and the listed entries that stay (a wave a chunk)
-    for (int c = wave; c < a.n_chunks; c += kThreads / 64) {
-        const int nc = __builtin_amdgcn_readlane((int)(c < 64 ? n[0] : n[1]), c & 63), at = (int)s.c_max[c];
-        unsigned long long sum = 0;
-        #pragma unroll 1
-        for (int i = lane; i < nc; i += 64) {
-            const uint64_t k = s.list[at + i];
-            sum += k >= t ? units(weight(key_value(k), row.m, row.c, s.exp2), 1.0 / kBinUnit) : 0;
-        }
-        sum = wave_fold_u64(sum, [](uint64_t x, uint64_t y) { return x + y; });
-        if (lane == 0) s.c_mass[c] += (double)sum * kBinUnit;
-    }
-    __syncthreads();
-    double kept = 0.0;
-    #pragma unroll
-    for (int i = 0; i < 2; ++i)
-        if (lane + 64 * i < a.n_chunks) kept += s.c_mass[lane + 64 * i];
-    kept = uniform(__longlong_as_double((long long)wave_fold_u64(f64_bits(kept), add_f64_bits)));
+    const double kept = add_listed(row, n, t);   // (above the range, and the listed entries that stay)
     if (a.tok) {
         const int v = draw(row, t, (double)a.u[r]);
         if (tid == 0) a.tok[r] = v;
@@ -1492,11 +1540,12 @@ static void split_rows(int rows, int n_chunks, int *per_group, int *groups) {
 
 hipError_t launch_sample(const SampleArgs &args, int dtype, hipStream_t st) {
     SampleArgs a = args;
-    // rows with a small top-k, or with top-k and top-p, are finished in the first launch; plain ones have nothing to cut
+    // rows with a small top-k, with top-k and top-p, or with min-p alone are finished in the first launch; plain ones have
+    // nothing to cut
     a.n_cut = a.n_emit = 0;
     for (int b = 0; b < a.B; ++b) {
         if (a.top_k[b] > 0 && a.top_k[b] <= kListK) continue;
-        if ((a.top_k[b] > 0 || a.top_p[b] < 1.0 || a.min_p[b] > 0.0) && !both_filters(a.top_k[b], a.top_p[b])) a.cut[a.n_cut++] = (uint8_t)b;
+        if ((a.top_k[b] > 0 || a.top_p[b] < 1.0) && !both_filters(a.top_k[b], a.top_p[b])) a.cut[a.n_cut++] = (uint8_t)b;
         if (a.probs) a.emit[a.n_emit++] = (uint8_t)b;
     }
     split_rows(std::max(a.n_cut, 1) * a.T, a.n_chunks, &a.cut_per_group, &a.cut_groups);

@@ -137,6 +137,16 @@ def test_sizes(V, dtype):
         _run("model", (1, 2 if V < 60000 else 1, V), dtype, V + i, probs=i != 3, **kw)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_min_p_alone(dtype):
+    # few to a chunk; chunks whose own best would leave hundreds, none of which the row keeps; rows that keep thousands;
+    # next to all; all but the masked
+    for i, (kind, kw) in enumerate((("model", dict(min_p=0.1)), ("model", dict(min_p=0.02, temperature=1.2)), ("model", dict(min_p=1e-3, temperature=1.5)),
+                                    ("model", dict(min_p=1e-12)), ("masked", dict(min_p=1e-9)), ("lowest", dict(min_p=1e-300)), ("body", dict(min_p=0.3)),
+                                    ("wide", dict(min_p=1e-4, temperature=30.0)), ("infinite", dict(min_p=0.5)), ("huge", dict(min_p=0.01)))):
+        _run(kind, (2, 2, 40000), dtype, 120 + i, probs=i % 2 == 0, **kw)
+
+
 @pytest.mark.parametrize("V", [600001, 1 << 20])
 def test_the_largest_vocabularies(V):
     # more chunks than a wave has lanes; all of them
