@@ -1082,15 +1082,8 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(const SampleArgs a)
     if (tid == 0) s.num[0] = 0, s.num[1] = 0;
     if (listed && a.probs) zero_run(a.probs + (size_t)r * a.V, e0, a.V);
     __syncthreads();
-    m = s.fmx[0];
-    uint32_t flags = s.flag[0];
-    #pragma unroll
-    for (int k = 1; k < kThreads / 64; ++k) {
-        m = fmaxf(m, s.fmx[k]);
-        flags |= s.flag[k];
-    }
-    m = uniform(m);
-    flags = uniform(flags);
+    m = uniform(group_max<16>(s.fmx[lane & 15]));
+    uint32_t flags = __any(s.flag[lane & 15] != 0) ? kNaN : 0;
     const float mb = floorf(m * 8.f);
     if (!(fabsf(m) < 0x1p20f)) flags |= kNoBins;   // (bins of 1/8 are exact below 2^21)
     float edge = INFINITY;
@@ -1217,7 +1210,11 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(const SampleArgs a)
             else if (top_k > 0) weigh(Yes(), Yes());
             else weigh(Yes(), No());
         }
-        mass = block_sum(mass, s.part);   // (its barrier stands behind the atomics)
+        // (wave 0 alone needs the sum)
+        mass = __longlong_as_double((long long)wave_fold_u64(f64_bits(mass), add_f64_bits));
+        if (lane == 0) s.part[wave] = mass;
+        __syncthreads();
+        if (wave == 0) mass = __longlong_as_double((long long)wave_fold_u64(lane < 16 ? f64_bits(s.part[lane]) : 0, add_f64_bits));
         if (binned && tid < kBins) {
             put64(rec + kHead + 8 * tid, s.mass[tid]);
             if (top_k > 0)
