@@ -42,8 +42,8 @@
 //
 // Bound.  Small calls: one launch's chain of round trips (loads 2.7 us, bins and
 // candidates 2.8, arrival 0.9, the records 2.4, the list's end 3.4): a row of 50257
-// 12.0 us, 20 rows with their distributions 13.2.  Large ones: 80 rows of 128256
-// fp32 with top-p and distributions (82 MB read and written once) 67.5 us: 25.4 for the
+// 11.5 us, 20 rows with their distributions 12.8.  Large ones: 80 rows of 128256
+// fp32 with top-p and distributions (82 MB read and written once) 66.6 us: 24.2 for the
 // weights (two workgroups per CU load, then compute, in step: 1.6 TB/s, and the vector
 // ALU is busy four fifths of the time: 31 instructions an entry), 27 for the cut (a
 // read at 4 TB/s, then 5 - 14 us for a row's last workgroup), 16.4 for the
