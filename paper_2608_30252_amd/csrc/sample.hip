@@ -14,8 +14,11 @@
 //   p_v = w_v [key(v) >= t] / mass.  The draw is the smallest v whose running
 //   mass, in index order, exceeds u times the whole.
 // Masses that are summed in no fixed order (histograms, by LDS atomics) are
-// integers, in units of 2^-50 (2^-43 over a whole row): their sums do not depend
-// on the order.
+// integers: their sums do not depend on the order.  Entries of equal value all
+// round the same way, and a filter may end among thousands of them at a tiny
+// weight, so the units go down with the weights: a bin's unit with the bin, a
+// list's with its largest weight, and sums over a whole row keep what the unit
+// leaves in a second integer.
 //
 // Work.  Workgroup (chunk, row) of 1024 threads reads 8192 entries, 8 a thread.
 //   * Rows with a small top-k (kListK): it finds a value that at least top_k of
@@ -66,7 +69,10 @@ constexpr int kThreads = 1024, kRun = kSampleChunk / kThreads;   // entries of a
 constexpr int kBins = 256, kBuckets = 2048, kList = 4096, kFinal = 128, kSort = 512;
 constexpr int kResident = 512;   // workgroups at a time: two for each of the 256 CUs (64 KB of LDS, 2048 threads)
 constexpr int kUnknown = 0x7fffffff;
-constexpr double kBinUnit = 0x1p-50, kRowUnit = 0x1p-43;   // 8192 and 2^20 weights of at most 1 fit 63 bits
+// 8192 weights of at most 1 in units of 2^-50, and 2^20 in units of 2^-43, come to 2^63 at most.  Weights of a whole row
+// may lie far below its largest, and equal ones are all rounded the same way, so what a unit of 2^-43 leaves of each is
+// counted too, in units of 2^-86 (signed, 2^62 at most): a sum is exact to 2^-67, far below a double's step.
+constexpr double kBinUnit = 0x1p-50, kRowUnit = 0x1p-43, kRestUnit = 0x1p-86;
 
 // 2^(j / 256), 0 <= j < 256, from the Taylor series at compile time (below 2e-16 relative)
 constexpr int kTable = 256;
@@ -118,6 +124,26 @@ __device__ __forceinline__ double weight(float x, float m, double c, const doubl
 // w (<= 1) as an integer of 1 / per, to nearest; per a power of two up to 2^50: from the low mantissa bits of a sum with 2^52
 __device__ __forceinline__ unsigned long long units(double w, double per) {
     return (unsigned long long)__double_as_longlong(fma(w, per, 0x1p52)) - (unsigned long long)__double_as_longlong(0x1p52);
+}
+// what units(w, per) leaves of w, in its 2^43rd part (signed)
+__device__ __forceinline__ long long rest_units(double w, double per) {
+    const double whole = fma(w, per, 0x1p52) - 0x1p52;
+    return __double_as_longlong(fma(fma(w, per, -whole), 0x1p43, 0x1.8p52)) - __double_as_longlong(0x1.8p52);
+}
+// The bins' masses, each in a unit of its own.  With k = c / 2048, the binades of weight that a bin of 1/8 spans, an entry
+// of bin j has a weight of at most 2^-e, e = floor((j - 1) k), and of at least 2^-(j + 1) k; it is counted in 2^-(50 + e),
+// that is to 2^-(50 - 2 k) of itself (2^-49 at temperature 1), where 8192 of one value all round the same way.  k is cut
+// off at 3 1/2 (temperature 0.0515), where a bin's weights are gone within 15 bins.  `step` is k with 20 bits behind the
+// point, so that 2^(50 + e) is a multiply-add and a mask on a double's high word.
+__device__ __forceinline__ uint32_t bin_step(double c) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)(fmin(c, 3.5 * 2048) * 512.0)); }
+__device__ __forceinline__ uint32_t bin_per_high(int j, uint32_t step) {
+    return (__umul24((uint32_t)j, step) + ((1073u << 20) - step)) & 0xfff00000u;
+}
+__device__ __forceinline__ double bin_per(int j, uint32_t step) {
+    return __longlong_as_double((long long)((uint64_t)bin_per_high(j, step) << 32));
+}
+__device__ __forceinline__ double bin_unit(int j, uint32_t step) {
+    return __longlong_as_double((long long)((uint64_t)((2046u << 20) - bin_per_high(j, step)) << 32));
 }
 // the value that a key holds
 __device__ __forceinline__ float key_value(uint64_t k) {
@@ -220,7 +246,7 @@ struct SampleLds {
     double bucket_mass[kBins];
     uint32_t bucket_cnt[kBins];
     double c_mass[kSampleMaxChunks];    // per chunk: kept mass; against the row's maximum
-    double c_unit[kSampleMaxChunks];    // what its bins' units are against the row's maximum
+    double c_unit[kSampleMaxChunks];    // the weight of its maximum: what its bins' masses are against the row's
     float c_max[kSampleMaxChunks];      // its maximum; or where its keys begin in the list
     double part[16];   // one per wave
     double res[4];
@@ -230,6 +256,7 @@ struct SampleLds {
     int num[4];
 };
 static_assert(sizeof(SampleLds) <= 64 * 1024, "static LDS");
+static_assert(kBuckets <= kList && 2 * kSampleMaxChunks <= kBuckets, "second sums");
 __device__ __forceinline__ SampleLds &lds() {
     __shared__ SampleLds s;
     return s;
@@ -299,17 +326,21 @@ struct Range {
 
 // Finds in the histogram mass/cnt (256 buckets of 8 parts each, the highest keys last; masses as integers of `unit`)
 // the first bucket from the top with which `target` of the measure is reached on top of what r holds, or the last that
-// is not empty.  PARTS: the part of it.  Returns its number and adds what lies above it to r; *n: its entries.
+// is not empty.  PARTS: the part of it, with what the masses leave in the list's place (integers of kRestUnit).  Returns
+// its number and adds what lies above it to r; *n: its entries.
 template <bool PARTS>
 __device__ __forceinline__ int crossing(SampleLds &s, double unit, bool by_count, double target, Range &r, int *n) {
     constexpr int P = kBuckets / kBins, Q = kBins / 64;
     const int tid = threadIdx.x;
     if (tid < kBins) {
-        uint64_t m = 0;
+        uint64_t m = 0, rest = 0;
         uint32_t c = 0;
         #pragma unroll
-        for (int p = 0; p < P; ++p) m += s.mass[tid * P + p], c += s.cnt[tid * P + p];
-        s.bucket_mass[kBins - 1 - tid] = (double)m * unit;
+        for (int p = 0; p < P; ++p) {
+            m += s.mass[tid * P + p], c += s.cnt[tid * P + p];
+            if constexpr (PARTS) rest += s.list[tid * P + p];
+        }
+        s.bucket_mass[kBins - 1 - tid] = (double)m * unit + (double)(int64_t)rest * kRestUnit;
         s.bucket_cnt[kBins - 1 - tid] = c;
     }
     __syncthreads();
@@ -344,7 +375,7 @@ __device__ __forceinline__ int crossing(SampleLds &s, double unit, bool by_count
                 int part = -1;
                 double pm = 0.0, pc = 0.0;
                 for (int p = P - 1; p >= 0; --p) {
-                    const double xc = (double)s.cnt[at * P + p], xm = (double)s.mass[at * P + p] * unit;
+                    const double xc = (double)s.cnt[at * P + p], xm = (double)s.mass[at * P + p] * unit + (double)(int64_t)s.list[at * P + p] * kRestUnit;
                     if (xc > 0.0) {
                         part = p, pm = am, pc = ac;
                         if ((by_count ? ac + xc : am + xm) >= target) break;
@@ -411,14 +442,12 @@ __device__ __forceinline__ uint64_t select(const Row<T> &row, Range &r, bool by_
         }
         // The keys of the list that are still in the range: few enough are put in order.
         if (in_list && n <= kFinal) break;
-        for (int b = tid; b < kBuckets; b += kThreads) s.mass[b] = 0, s.cnt[b] = 0;
+        for (int b = tid; b < kBuckets; b += kThreads) {
+            s.mass[b] = 0, s.cnt[b] = 0;
+            if constexpr (STREAM) if (!in_list) s.list[b] = 0;
+        }
         if (tid == 0) s.key[0] = ~(uint64_t)0, s.key[1] = 0;
         __syncthreads();
-        const double unit = in_list ? kBinUnit : kRowUnit, per = 1.0 / unit;
-        auto count = [&](int at, float x) {
-            atomicAdd(&s.cnt[at], 1u);
-            atomicAdd((unsigned long long *)&s.mass[at], units(weight(x, row.m, row.c, s.exp2), per));
-        };
         int sh, at;
         if (in_list) {
             // To the keys that are there: equal values differ in a few bits of their indices only.  Then 256 buckets,
@@ -440,10 +469,19 @@ __device__ __forceinline__ uint64_t select(const Row<T> &row, Range &r, bool by_
             r.lo = uniform(s.key[0]);
             r.hi = uniform(s.key[1]);
             sh = max(64 - __clzll((long long)(r.hi - r.lo)) - 8, 0);
+            // in 2^-50 of the power of two above the largest weight here (2^-900 at least, which none is near)
+            const double top = fmax(((double)key_value(r.hi) - (double)row.m) * row.c, -900.0 * kTable);
+            const int e = key_value(r.hi) == row.m ? 0 : (int)floor(top * (1.0 / kTable)) + 1;
+            const double unit = bits_f64((uint64_t)(1023 - 50 + e) << 52);
+            const double per = 1.0 / unit;
             #pragma unroll 1
             for (int i = tid; i < all; i += kThreads) {
                 const uint64_t k = s.list[i];
-                if (k >= r.lo && k <= r.hi) count((int)((k - r.lo) >> sh) * (kBuckets / kBins) + (tid & 7), key_value(k));
+                if (k >= r.lo && k <= r.hi) {
+                    const int b = (int)((k - r.lo) >> sh) * (kBuckets / kBins) + (tid & 7);
+                    atomicAdd(&s.cnt[b], 1u);
+                    atomicAdd((unsigned long long *)&s.mass[b], units(weight(key_value(k), row.m, row.c, s.exp2), per));
+                }
             }
             __syncthreads();
             at = crossing<false>(s, unit, by_count, target, r, &n);
@@ -452,10 +490,16 @@ __device__ __forceinline__ uint64_t select(const Row<T> &row, Range &r, bool by_
             if constexpr (STREAM)
                 row.each([&](float x, int i) {
                     const uint64_t k = argmax_key(x, i);
-                    if (k >= r.lo && k <= r.hi) count((int)((k - r.lo) >> sh), x);
+                    if (k >= r.lo && k <= r.hi) {
+                        const int b = (int)((k - r.lo) >> sh);
+                        const double w = weight(x, row.m, row.c, s.exp2);
+                        atomicAdd(&s.cnt[b], 1u);
+                        atomicAdd((unsigned long long *)&s.mass[b], units(w, 1.0 / kRowUnit));
+                        atomicAdd((unsigned long long *)&s.list[b], (unsigned long long)rest_units(w, 1.0 / kRowUnit));
+                    }
                 });
             __syncthreads();
-            at = crossing<true>(s, unit, by_count, target, r, &n);
+            at = crossing<true>(s, kRowUnit, by_count, target, r, &n);
         }
         const uint64_t lo = r.lo + ((uint64_t)at << sh);
         r.hi = lo + min(r.hi - lo, ((uint64_t)1 << sh) - 1);   // (no sum past 64 bits)
@@ -768,14 +812,17 @@ __device__ __forceinline__ double add_listed(const Row<T> &row, const uint32_t (
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     for (int c = wave; c < row.n_chunks; c += kThreads / 64) {
         const int nc = __builtin_amdgcn_readlane((int)(c < 64 ? n[0] : n[1]), c & 63), at = (int)s.c_max[c];
-        unsigned long long sum = 0;
+        unsigned long long sum = 0, rest = 0;   // (at most 4096 entries)
         #pragma unroll 1
         for (int i = lane; i < nc; i += 64) {
             const uint64_t k = s.list[at + i];
-            sum += k >= t ? units(weight(key_value(k), row.m, row.c, s.exp2), 1.0 / kBinUnit) : 0;
+            const double w = k >= t ? weight(key_value(k), row.m, row.c, s.exp2) : 0.0;
+            sum += units(w, 1.0 / kBinUnit);
+            rest += (unsigned long long)rest_units(w, 1.0 / kBinUnit);
         }
         sum = wave_fold_u64(sum, [](uint64_t x, uint64_t y) { return x + y; });
-        if (lane == 0) s.c_mass[c] += (double)sum * kBinUnit;
+        rest = wave_fold_u64(rest, [](uint64_t x, uint64_t y) { return x + y; });
+        if (lane == 0) s.c_mass[c] += (double)sum * kBinUnit + (double)(int64_t)rest * (kBinUnit * 0x1p-43);
     }
     __syncthreads();
     double kept = 0.0;
@@ -785,9 +832,10 @@ __device__ __forceinline__ double add_listed(const Row<T> &row, const uint32_t (
     return uniform(__longlong_as_double((long long)wave_fold_u64(f64_bits(kept), add_f64_bits)));
 }
 
-// kept mass of every chunk into c_mass[]; returns their sum
+// kept mass of every chunk into c_mass[]; returns their sum.  (Not inlined into the passes over a row, whose registers it
+// would share: 48 us a row of 50257 with min-p among near-equal entries, 58 inlined.)
 template <typename T>
-__device__ __forceinline__ double chunk_masses(const Row<T> &row, uint64_t t) {
+__device__ __noinline__ double chunk_masses(const Row<T> row, uint64_t t) {
     SampleLds &s = lds();
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     double *part = reinterpret_cast<double *>(s.list);   // [chunk][wave]
@@ -942,7 +990,7 @@ __device__ __noinline__ void cut_row(const SolveJob<T> job) {
                 const char *q = rec0 + (size_t)k * kSampleRecord + kHead;
                 const int jc = in ? j - (int)d : 0;
                 if (by_count) n += in ? get32(q + 8 * kBins + 4 * jc) : 0;
-                else w += in ? (double)get64(q + 8 * jc) * s.c_unit[k] : 0.0;
+                else w += in ? bits_f64(get64(q + 8 * jc)) * s.c_unit[k] : 0.0;
             }
             s.list[tid] = f64_bits(by_count ? (double)n : w);
             __syncthreads();
@@ -973,22 +1021,22 @@ __device__ __noinline__ void cut_row(const SolveJob<T> job) {
         for (int c = wave; c < row.n_chunks; c += kThreads / 64) {
             const float ups = floorf(s.c_max[c] * 8.f) - hi * 8.f;   // the last bin above
             const char *q = rec0 + (size_t)c * kSampleRecord + kHead;
-            uint64_t sum = 0;
+            double sum = 0.0;
             uint32_t n = 0;
             #pragma unroll
             for (int i = 0; i < kBins / 64; ++i) {
                 const bool up = (float)(lane + 64 * i) <= ups;
-                const uint64_t y = get64(q + 8 * (lane + 64 * i));
-                sum += up ? y : 0;
+                const double y = bits_f64(get64(q + 8 * (lane + 64 * i)));
+                sum += up ? y : 0.0;
                 if (by_count) {
                     const uint32_t z = get32(q + 8 * kBins + 4 * (lane + 64 * i));
                     n += up ? z : 0;
                 }
             }
-            sum = wave_fold_u64(sum, [](uint64_t x, uint64_t y) { return x + y; });
+            sum = wave_sum_f64(sum);
             if (by_count) n = (uint32_t)group_sum<64>((float)n);   // (exact: at most 8192)
             if (lane == 0) {
-                s.c_mass[c] = (double)sum * s.c_unit[c];
+                s.c_mass[c] = sum * s.c_unit[c];
                 if (by_count) atomicAdd(&s.num[1], (int)n);
             }
         }
@@ -1018,18 +1066,21 @@ __device__ __noinline__ void cut_row(const SolveJob<T> job) {
         }
     }
     // each chunk's kept mass: above the range, and the listed entries that stay
-    uint64_t *fix = reinterpret_cast<uint64_t *>(s.c_unit);   // (whose values are not needed any more)
+    uint64_t *fix = s.mass, *rest = s.mass + kSampleMaxChunks;   // (the search's, which is over)
     __syncthreads();
-    if (tid < kSampleMaxChunks) fix[tid] = 0;
+    if (tid < 2 * kSampleMaxChunks) fix[tid] = 0;
     __syncthreads();
     #pragma unroll 1
     for (int i = tid; i < all; i += kThreads) {
         const uint64_t k = s.list[i];
-        if (k >= t)
-            atomicAdd((unsigned long long *)&fix[key_index(k) / kSampleChunk], units(weight(key_value(k), row.m, row.c, s.exp2), 1.0 / kBinUnit));
+        if (k >= t) {
+            const double w = weight(key_value(k), row.m, row.c, s.exp2);
+            atomicAdd((unsigned long long *)&fix[key_index(k) / kSampleChunk], units(w, 1.0 / kBinUnit));
+            atomicAdd((unsigned long long *)&rest[key_index(k) / kSampleChunk], (unsigned long long)rest_units(w, 1.0 / kBinUnit));
+        }
     }
     __syncthreads();
-    if (tid < row.n_chunks) s.c_mass[tid] += (double)fix[tid] * kBinUnit;
+    if (tid < row.n_chunks) s.c_mass[tid] += (double)fix[tid] * kBinUnit + (double)(int64_t)rest[tid] * (kBinUnit * 0x1p-43);
     __syncthreads();
     double kept = 0.0;
     #pragma unroll
@@ -1187,17 +1238,17 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(const SampleArgs a)
             const Series terms = series();
             double md = (double)m, c = row.c;
             asm volatile("" : "+v"(md), "+v"(c));   // (kept at hand)
-            const int mi = (int)mb;   // (where there are bins)
+            const uint32_t step = bin_step(row.c);
             auto weigh = [&](auto bins, auto count) {
                 #pragma unroll
                 for (int i = 0; i < kRun; ++i) {
                     const double w = weight_finite(x[i], md, c, s.exp2, terms);
                     mass += w;
                     if constexpr (bins.value) {
-                        const float low = floorf(x[i] * 8.f);
-                        if (mb - low < (float)kBins) {   // (not -inf)
-                            const int j = mi - (int)low;
-                            atomicAdd((unsigned long long *)&s.mass[j], units(w, 1.0 / kBinUnit));
+                        const float below = mb - floorf(x[i] * 8.f);
+                        if (below < (float)kBins) {   // (not -inf)
+                            const int j = (int)below;
+                            atomicAdd((unsigned long long *)&s.mass[j], units(w, bin_per(j, step)));
                             if constexpr (count.value) atomicAdd(&s.cnt[j], 1u);
                         }
                     }
@@ -1216,7 +1267,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(const SampleArgs a)
         __syncthreads();
         if (wave == 0) mass = __longlong_as_double((long long)wave_fold_u64(lane < 16 ? f64_bits(s.part[lane]) : 0, add_f64_bits));
         if (binned && tid < kBins) {
-            put64(rec + kHead + 8 * tid, s.mass[tid]);
+            put64(rec + kHead + 8 * tid, f64_bits((double)s.mass[tid] * bin_unit(tid, bin_step(row.c))));
             if (top_k > 0)
                 __hip_atomic_store(reinterpret_cast<uint32_t *>(rec + kHead + 8 * kBins) + tid, s.cnt[tid], __ATOMIC_RELAXED,
                                    __HIP_MEMORY_SCOPE_AGENT);
@@ -1291,7 +1342,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(const SampleArgs a)
                 if (lane + 64 * i < a.n_chunks) {
                     s.c_mass[lane + 64 * i] = cm[i];
                     s.c_max[lane + 64 * i] = h.max[i];
-                    s.c_unit[lane + 64 * i] = h.max[i] == -INFINITY ? 0.0 : kBinUnit * weight(h.max[i], m, row.c, s.exp2);
+                    s.c_unit[lane + 64 * i] = h.max[i] == -INFINITY ? 0.0 : weight(h.max[i], m, row.c, s.exp2);
                 }
         }
         out.mass = __longlong_as_double((long long)wave_fold_u64(f64_bits(cm[0] + cm[1]), add_f64_bits));
@@ -1324,7 +1375,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(const SampleArgs a)
                         const bool in = top > -INFINITY && (float)j >= d;
                         const char *q = rec0 + (size_t)k * kSampleRecord + kHead;
                         const int jc = in ? j - (int)d : 0;
-                        const double x = (double)get64(q + 8 * jc);
+                        const double x = bits_f64(get64(q + 8 * jc));
                         w += in ? x * s.c_unit[k] : 0.0;
                         if (top_k > 0) {
                             const uint32_t y = __hip_atomic_load(reinterpret_cast<uint32_t *>(const_cast<char *>(q) + 8 * kBins + 4 * jc),
@@ -1388,7 +1439,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_cut_kernel(const SampleArg
         if (chunk + 1 < chunk1) next.load(row.x, e0 + kSampleChunk, a.V);   // in flight meanwhile
         char *rec = rec0 + (size_t)chunk * kSampleRecord;
         // what lies above the range: the chunk's bins up to there (read before the keys take their place)
-        uint64_t q = 0;
+        double q = 0.0;
         uint32_t n_above = 0;
         float top = 0.f;
         if (tid < 64) {
@@ -1396,16 +1447,16 @@ __global__ __launch_bounds__(kThreads, 8) void sample_cut_kernel(const SampleArg
             const float ups = floorf(top * 8.f) - res.hi * 8.f;   // the last bin above
             #pragma unroll
             for (int i = 0; i < kBins / 64; ++i) {
-                const uint64_t y = get64(rec + kHead + 8 * (lane + 64 * i));
+                const double y = bits_f64(get64(rec + kHead + 8 * (lane + 64 * i)));
                 const bool up = (float)(lane + 64 * i) <= ups;
-                q += up ? y : 0;
+                q += up ? y : 0.0;
                 if (a.top_k[b] > 0) {
                     const uint32_t z = __hip_atomic_load(reinterpret_cast<uint32_t *>(rec + kHead + 8 * kBins) + lane + 64 * i, __ATOMIC_RELAXED,
                                                          __HIP_MEMORY_SCOPE_AGENT);
                     n_above += up ? z : 0;
                 }
             }
-            q = wave_fold_u64(q, [](uint64_t x, uint64_t y) { return x + y; });
+            q = wave_sum_f64(q);
             n_above = (uint32_t)group_sum<64>((float)n_above);   // (exact: at most 8192)
         }
         if (tid == 0) s.num[0] = 0;
@@ -1419,7 +1470,7 @@ __global__ __launch_bounds__(kThreads, 8) void sample_cut_kernel(const SampleArg
         __syncthreads();
         if (tid == 0) {
             put64(rec, (uint64_t)(uint32_t)s.num[0] | (uint64_t)n_above << 32);
-            put64(rec + 16, f64_bits(q ? (double)q * kBinUnit * weight(top, res.m, row.c, s.exp2) : 0.0));
+            put64(rec + 16, f64_bits(q > 0.0 ? q * weight(top, res.m, row.c, s.exp2) : 0.0));
         }
         __syncthreads();   // (the count is read)
     }
