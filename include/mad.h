@@ -286,7 +286,10 @@ int mad_kv8_append(const void *k_new, const void *v_new, const int32_t *n, int B
  * effect on it, NaN and infinite scores included.
  *   q    device [B][T][Hq][d], dtype     out  device [B][T][Hq][d], dtype
  *   lse  device fp32 [B][T][Hq] or NULL
- *   kv   scales 0 or positive normal numbers
+ *   kv   scales 0 or positive normal numbers, of any size beside each other: a
+ *        row's output is exact against what it weighs (terms below 2^-24 of its
+ *        largest lose precision).  Sums over a row's keys are formed in fp32:
+ *        the number of keys times the largest |value| below 2^124
  * T * G <= MAD_MAX_VERIFY_ROWS; d in {64, 128}; dtype BF16 or F32, both on the
  * matrix cores (F32: q as three bf16 terms, the probabilities as two fp16
  * terms, so that products keep fp32's precision).  Workspace MAD_OP_VERIFY.

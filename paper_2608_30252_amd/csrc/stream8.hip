@@ -14,13 +14,16 @@
 //                 (24 bits), three products to the same accumulator.
 //   O^T = V^T P^T fp16 x fp16.  fp16 keeps 3 bits more of a probability than
 //                 bf16 (2^-12 against 2^-9 relative, which against the output's own
-//                 2^-9 is nothing); its range is made up for by p' = 2^11 p vs / vref,
-//                 vref the largest V scale the wave has met in the unit.  m is the
-//                 running maximum to within 2^4: it is raised, and o scaled, only
-//                 where a score exceeds it by more (with 16 rows to a wave some
-//                 row's maximum grows in most steps, by little), so p' <= 2^15,
-//                 and fp16's precision holds down to p vs / vref = 2^-25.  fp32: a
-//                 second fp16 term holds what the first leaves (22 bits).
+//                 2^-9 is nothing); its range is made up for by p' = 2^11 p vs 2^(m - y),
+//                 y a row's largest x_j + log2 vs_j so far: V scales of any size meet
+//                 in one sum, each row's against what that row sees.  m and y are
+//                 whole numbers, so 2^(m - y) goes onto vs exactly (v_ldexp), and the
+//                 running maxima to within 2^4 (2^3): m is raised, and the sum of p
+//                 scaled, only where a score exceeds it by more, y, and o scaled,
+//                 likewise (with 16 rows to a wave some row's maximum grows in most
+//                 steps, by little), so p' <= 2^15, and fp16's precision holds down
+//                 to 2^-24 of the largest p vs.  fp32: a second fp16 term holds what
+//                 the first leaves (22 bits).
 //
 // Work decomposition.  As in stream.hip a unit is one (sequence, KV head) with
 // its T * G query rows, its keys are cut into slabs (16 KB of codes), and the
@@ -58,8 +61,9 @@ typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_v;
 typedef __attribute__((ext_vector_type(2))) float f32x2_v;
 typedef int v2i_t __attribute__((ext_vector_type(2)));
 
-constexpr float kPShift = 11.f;   // p' = 2^11 p
+constexpr float kPShift = 11.f;   // the running sums are of 2^11 p
 constexpr float kLazy = 4.f;      // the maximum is raised where a score exceeds it by more (log2 units)
+constexpr float kLazyV = 3.f;     // likewise that of the scores with their V scale's exponent (a scale is below 2 of those)
 
 // T: bf16_t or float (queries and output)
 template <int D, int NB, typename T>
@@ -301,12 +305,11 @@ __global__ __launch_bounds__(512, 1) void stream8_kernel(const Stream8Args args)
         }
 
         f32x4_v o[NB][DB];
-        float m_run[NB], l_run[NB];           // in log2 units; sum of p'
+        float m_run[NB], l_run[NB], y_run[NB];   // m in log2 units; sum of 2^11 p; y
         int lim[NB];                          // the last key that row 16 nb + lr sees
-        float vref = 0.f, inv_vref = 0.f;     // the largest V scale so far (the same in every lane)
         #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
-            m_run[nb] = -INFINITY;
+            m_run[nb] = y_run[nb] = -INFINITY;
             l_run[nb] = 0.f;
             lim[nb] = g.len - TT + min(16 * nb + lr, R - 1) / G;
             #pragma unroll
@@ -383,17 +386,8 @@ __global__ __launch_bounds__(512, 1) void stream8_kernel(const Stream8Args args)
                     if (n % 2 == 1 || !C::QREG) __builtin_amdgcn_sched_barrier(0);
                 }
                 __builtin_amdgcn_sched_barrier(0);
-                const float vm = max_over_row_lanes(vsc);
-                if (vm > vref) {   // the same in every lane
-                    inv_vref = 1.f / vm;
-                    const float down = vref * inv_vref;
-                    #pragma unroll
-                    for (int nb = 0; nb < NB; ++nb)
-                        #pragma unroll
-                        for (int db = 0; db < DB; ++db) o[nb][db] *= down;
-                    vref = vm;
-                }
-                const float rv = vsc * inv_vref, csk = cs * ksc;
+                const float csk = cs * ksc;
+                const float v_exp = (float)((int)(__float_as_uint(vsc) >> 23) - 127);   // (0: -127)
                 const int kg0 = 32 * kh + 8 * lg;   // this lane's first key of the chunk
                 const bool open = key + C::KPC - 1 <= open_to;   // every row sees the whole chunk
                 u32x4_v pk[NB], pl[C::F32 ? NB : 1];
@@ -409,16 +403,21 @@ __global__ __launch_bounds__(512, 1) void stream8_kernel(const Stream8Args args)
                     #pragma unroll
                     for (int j = 1; j < 8; ++j) mt = fmaxf(mt, sacc[nb][j >> 2][j & 3]);
                     mt = mt == -INFINITY ? mt : mt * csk;   // (csk may be 0)
-                    if (__any(mt > m_run[nb] + kLazy)) {
-                        // the four lanes of a row agree on its maximum; rows that stay have alpha 1
+                    if (__any(mt > fminf(m_run[nb] + kLazy, y_run[nb] + kLazyV - v_exp))) {
+                        // the four lanes of a row agree on its maxima; rows that stay have factors of 1
+                        const float yt = max_over_row_lanes(mt + v_exp);
                         mt = max_over_row_lanes(mt);
-                        const float mn = mt > m_run[nb] + kLazy ? mt : m_run[nb];
-                        const float alpha = mn == m_run[nb] ? 1.f : __builtin_amdgcn_exp2f(m_run[nb] - mn);
+                        const float mn = mt > m_run[nb] + kLazy ? ceilf(mt) : m_run[nb], yn = yt > y_run[nb] + kLazyV ? ceilf(yt) : y_run[nb];
+                        const float alpha = yn == y_run[nb] ? 1.f : __builtin_amdgcn_exp2f(y_run[nb] - yn);
+                        l_run[nb] *= mn == m_run[nb] ? 1.f : __builtin_amdgcn_exp2f(m_run[nb] - mn);
                         m_run[nb] = mn;
-                        l_run[nb] *= alpha;
+                        y_run[nb] = yn;
                         #pragma unroll
                         for (int db = 0; db < DB; ++db) o[nb][db] *= alpha;
                     }
+                    // (a whole number within some 140 of 0, or a NaN before the row's first key; where rv would pass 2^100, p
+                    // is below 2^-80)
+                    const float rv = fminf(__builtin_amdgcn_ldexpf(vsc, (int)fmaxf(m_run[nb] - y_run[nb], -1000.f)), 0x1p100f);
                     const float ms = m_run[nb] == -INFINITY ? -kPShift : m_run[nb] - kPShift;
                     float x[8];
                     #pragma unroll
@@ -496,13 +495,14 @@ __global__ __launch_bounds__(512, 1) void stream8_kernel(const Stream8Args args)
             key = g.key0 + wave * C::KPC;
             if (C::NST == 2 && key < g.key1) issue(g, key, 0);
         }
-        // each wave's (max, sum of p) per row, in log2 units (the sum is of p' = 2^11 p), and from all of them its factor
+        // each wave's (max, sum of p) per row, in log2 units, and from all of them its factor.  (The 2^11 of the running sums
+        // goes here: the values' sums need fp32's range.)
         const int x_lane = here(lane), x_lr = x_lane & 15, x_lg = x_lane >> 4;
         float2 *xml = reinterpret_cast<float2 *>(smem + C::OFF_ML);   // [8][RP]
         #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
             const float lt = sum_over_row_lanes(l_run[nb]);
-            if (x_lg == 0) xml[wave * C::RP + 16 * nb + x_lr] = make_float2(m_run[nb] - kPShift, lt);
+            if (x_lg == 0) xml[wave * C::RP + 16 * nb + x_lr] = make_float2(m_run[nb], lt * 0x1p-11f);
         }
         __syncthreads();   // (also: every wave is done with its stages and the queries)
         if (more) fetch_q(g);
@@ -520,7 +520,7 @@ __global__ __launch_bounds__(512, 1) void stream8_kernel(const Stream8Args args)
             const float mr = M[nb] == -INFINITY ? 0.f : M[nb];
             #pragma unroll
             for (int k = 0; k < C::NWV; ++k) L[nb] = fmaf(__builtin_amdgcn_exp2f(ml[k].x - mr), ml[k].y, L[nb]);
-            const float wt = __builtin_amdgcn_exp2f(m_run[nb] - kPShift - mr) * vref;
+            const float wt = __builtin_amdgcn_exp2f(y_run[nb] - kPShift - mr);
             #pragma unroll
             for (int db = 0; db < DB; ++db) o[nb][db] *= wt;
         }
