@@ -263,8 +263,8 @@ typedef struct mad_kv8_view {
  *   need  = the least 2^k, k >= -100, with |x| <= 448 * 2^k for every finite new
  *           element x of the block
  *   scale = max(its scale, need) if the block holds rows below len[b], else need
- *   code  = e4m3(x / scale), round to nearest even; an element that is not
- *           finite is stored as NaN
+ *   code  = e4m3(x / scale), the fp32 quotient rounded to nearest even; an
+ *           element that is not finite is stored as NaN
  * Where the scale grows, the block's rows below len[b] are written again with
  * it, e4m3(code * old scale / scale): between powers of two, as this call writes
  * them, that is exact but for codes that get below 2^-6.  A block's scale never falls while

@@ -118,8 +118,10 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(const Kv8AppendArgs a) 
             make_uint2(e4m3_x4(y[0], y[1], y[2], y[3]), e4m3_x4(y[4], y[5], y[6], y[7]));
     }
     if (r0 > 0 && !(s_old >= need)) {
-        // the scale grew (to a power of two): the block's earlier rows again
+        // the scale grew (to a power of two): the block's earlier rows again.  (The quotient of the scales first: it is
+        // exact, and code times old scale may be beyond fp32.)
         const int old = r0 * d8;
+        const float down = s_old * inv;
         for (int c = tid; c < old; c += 256) {
             uint2 *p = reinterpret_cast<uint2 *>(dst + (c >> sh) * a.d + ((c & (d8 - 1)) << 3));
             const uint2 u = *p;
@@ -127,7 +129,7 @@ __global__ __launch_bounds__(256) void kv8_append_kernel(const Kv8AppendArgs a) 
             #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const f32x2_v lo = __builtin_amdgcn_cvt_pk_f32_fp8(w[k], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w[k], true);
-                w[k] = e4m3_x4(lo.x * s_old * inv, lo.y * s_old * inv, hi.x * s_old * inv, hi.y * s_old * inv);
+                w[k] = e4m3_x4(lo.x * down, lo.y * down, hi.x * down, hi.y * down);
             }
             *p = make_uint2(w[0], w[1]);
         }
