@@ -592,7 +592,8 @@ def sample(logits: torch.Tensor, u: Optional[torch.Tensor] = None, temperature=1
     _need(probs is None or (probs.shape == (B, T, V) and probs.dtype == torch.float32), "probs must be float32 [B, T, V]")
     settings = []
     for name, v in (("temperature", temperature), ("top_k", top_k), ("top_p", top_p), ("min_p", min_p)):
-        v = [v] * B if not hasattr(v, "__len__") else v
+        one = not hasattr(v, "__len__") or getattr(v, "ndim", 1) == 0   # a number, also as a tensor or array without dimensions
+        v = [v] * B if one else v
         _need(len(v) == B, f"{name} needs one entry per sequence")
         # (a top-k beyond every vocabulary keeps all; one beyond 32 bits must not wrap)
         settings.append(_host_i32([max(-1, min(int(k), 2 ** 31 - 1)) for k in v], B) if name == "top_k" else _host_f64(v, B))
