@@ -21,8 +21,9 @@
  *     enqueued; on an error nothing is launched and no buffer is touched.
  *   - dtype: MAD_F32 or MAD_BF16 (inputs and outputs share it; arithmetic
  *     accumulates in fp32; lse outputs are always fp32).
- *   - `stream` is a hipStream_t (NULL = the default stream).  Calls enqueue
- *     work and return; nothing synchronises the host.
+ *   - `stream` is a hipStream_t (NULL = the default stream) of the current
+ *     device, which holds the tensors.  Calls enqueue work and return; nothing
+ *     synchronises the host.
  *   - Workspace `ws`: device scratch of at least mad_workspace_bytes(...)
  *     bytes.  It holds split partial results and arrival counters.  It must be
  *     zero-filled once before its first use; every call leaves the counters at

@@ -170,6 +170,22 @@ def _stream(device) -> ctypes.c_void_p:
     return ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)
 
 
+class _On:
+    """The library's entry points, called with `device` as the current one (each device has a default stream of its own,
+    and a launch on it goes to the current device)."""
+
+    def __init__(self, device):
+        self.index = device.index if device.type == "cuda" else -1   # -1: no change
+
+    def __getattr__(self, name):
+        entry = getattr(_load_library(), name)
+
+        def call(*args):
+            with torch.cuda.device(self.index):
+                return entry(*args)
+        return call
+
+
 def _host_i32(vals, n) -> ctypes.Array:
     arr = (ctypes.c_int32 * max(n, 1))()
     for j, x in enumerate(vals):
@@ -369,7 +385,7 @@ def draft_decode_attn(q: torch.Tensor, mem: Optional[KV], win: Optional[KV],
     # a given workspace has to hold the split partials; the library streams where it holds more
     nbytes = workspace_bytes(MAD_OP_DECODE if ws is None else MAD_OP_DECODE_LEAST, B, Hq, Hkv, d)
     w = _ws_for(q.device, nbytes, ws)
-    rc = _load_library().mad_draft_decode_attn(_ptr(q), B, Hq, Hkv, d, _dtype_code(q), float(scale),
+    rc = _On(q.device).mad_draft_decode_attn(_ptr(q), B, Hq, Hkv, d, _dtype_code(q), float(scale),
                                    ctypes.byref(mv) if mv is not None else None,
                                    ctypes.byref(wv) if wv is not None else None,
                                    _ptr(k_new), _ptr(v_new), _ptr(out), _ptr(lse),
@@ -386,11 +402,11 @@ def draft_decode_attn_noalloc(q: torch.Tensor, mem: Optional[KV], win: Optional[
     holds the split partials (no allocation by the library; out and lse are
     allocated here only when not given).  Calls on one GPU must not overlap."""
     B, Hq, Hkv, d, out, lse, scale, mv, wv = _decode_args(q, mem, win, k_new, v_new, out, lse, scale)
-    rc = _load_library().mad_draft_decode_attn_noalloc(_ptr(q), B, Hq, Hkv, d, _dtype_code(q), float(scale),
-                                                       ctypes.byref(mv) if mv is not None else None,
-                                                       ctypes.byref(wv) if wv is not None else None,
-                                                       _ptr(k_new), _ptr(v_new), _ptr(out), _ptr(lse),
-                                                       _stream(q.device))
+    rc = _On(q.device).mad_draft_decode_attn_noalloc(_ptr(q), B, Hq, Hkv, d, _dtype_code(q), float(scale),
+                                                     ctypes.byref(mv) if mv is not None else None,
+                                                     ctypes.byref(wv) if wv is not None else None,
+                                                     _ptr(k_new), _ptr(v_new), _ptr(out), _ptr(lse),
+                                                     _stream(q.device))
     _check(rc)
     return out, lse
 
@@ -413,11 +429,11 @@ def draft_step_attn(q: torch.Tensor, mem: Optional[KV], win: Optional[KV], k_new
     # a given workspace has to hold the split partials; the library streams where it holds more
     nbytes = workspace_bytes(MAD_OP_DECODE if ws is None else MAD_OP_DECODE_LEAST, B, Hq, Hkv, d)
     w = _ws_for(q.device, nbytes, ws)
-    rc = _load_library().mad_draft_step_attn(_ptr(q), B, Hq, Hkv, d, _dtype_code(q), float(scale),
-                                             ctypes.byref(mv) if mv is not None else None,
-                                             ctypes.byref(wv) if wv is not None else None,
-                                             _ptr(k_new), _ptr(v_new), modes, _ptr(out), _ptr(lse),
-                                             _ptr(w), w.numel(), _stream(q.device))
+    rc = _On(q.device).mad_draft_step_attn(_ptr(q), B, Hq, Hkv, d, _dtype_code(q), float(scale),
+                                           ctypes.byref(mv) if mv is not None else None,
+                                           ctypes.byref(wv) if wv is not None else None,
+                                           _ptr(k_new), _ptr(v_new), modes, _ptr(out), _ptr(lse),
+                                           _ptr(w), w.numel(), _stream(q.device))
     _check(rc)
     return out, lse
 
@@ -446,7 +462,7 @@ def memory_update(x: torch.Tensor, w_kv: torch.Tensor, pos, mem: KV, fire=None, 
     fire_arr = None
     if fire is not None:
         fire_arr = (ctypes.c_uint8 * B)(*[1 if f else 0 for f in fire])
-    rc = _load_library().mad_memory_update(_ptr(x), _ptr(w_kv), pos_arr, fire_arr, B, n_new, D, Hkv, d,
+    rc = _On(x.device).mad_memory_update(_ptr(x), _ptr(w_kv), pos_arr, fire_arr, B, n_new, D, Hkv, d,
                                _dtype_code(x), float(rope_base), ctypes.byref(mv), _stream(x.device))
     _check(rc)
 
@@ -482,8 +498,8 @@ def verify_attn(q: torch.Tensor, kv: KV, out=None, lse=None, scale: Optional[flo
     view = kv.view(B, Hkv, d, q.dtype, q.device, "kv")
     nbytes = workspace_bytes(MAD_OP_VERIFY, B, Hq, Hkv, d, T)
     w = _ws_for(q.device, nbytes, ws)
-    rc = _load_library().mad_verify_attn(_ptr(q), B, T, Hq, Hkv, d, _dtype_code(q), float(scale), ctypes.byref(view),
-                                         _ptr(out), _ptr(lse), _ptr(w), w.numel(), _stream(q.device))
+    rc = _On(q.device).mad_verify_attn(_ptr(q), B, T, Hq, Hkv, d, _dtype_code(q), float(scale), ctypes.byref(view),
+                                       _ptr(out), _ptr(lse), _ptr(w), w.numel(), _stream(q.device))
     _check(rc)
     return out, lse
 
@@ -512,10 +528,10 @@ def verify_attn_vt(q: torch.Tensor, k: torch.Tensor, vt: torch.Tensor, length, o
     _same_device(q.device, k=k, vt=vt)
     nbytes = workspace_bytes(MAD_OP_VERIFY, B, Hq, Hkv, d, T)
     w = _ws_for(q.device, nbytes, ws)
-    rc = _load_library().mad_verify_attn_vt(_ptr(q), B, T, Hq, Hkv, d, _dtype_code(q), float(scale), _ptr(k),
-                                            _ptr(vt), k.stride(0) if B > 1 else 0, k.stride(1), cap,
-                                            _host_i32(length, B), _ptr(out), _ptr(lse), _ptr(w), w.numel(),
-                                            _stream(q.device))
+    rc = _On(q.device).mad_verify_attn_vt(_ptr(q), B, T, Hq, Hkv, d, _dtype_code(q), float(scale), _ptr(k),
+                                          _ptr(vt), k.stride(0) if B > 1 else 0, k.stride(1), cap,
+                                          _host_i32(length, B), _ptr(out), _ptr(lse), _ptr(w), w.numel(),
+                                          _stream(q.device))
     _check(rc)
     return out, lse
 
@@ -535,8 +551,8 @@ def kv8_append(k_new: torch.Tensor, v_new: torch.Tensor, kv: KV8, n: Optional[Se
     _contiguous(k_new=k_new, v_new=v_new)
     _same_device(k_new.device, v_new=v_new)
     view = kv.view(B, Hkv, d, k_new.device, "kv")
-    _check(_load_library().mad_kv8_append(_ptr(k_new), _ptr(v_new), None if n is None else _host_i32(n, B), B, n_cap,
-                                          Hkv, d, _dtype_code(k_new), ctypes.byref(view), _stream(k_new.device)))
+    _check(_On(k_new.device).mad_kv8_append(_ptr(k_new), _ptr(v_new), None if n is None else _host_i32(n, B), B, n_cap,
+                                            Hkv, d, _dtype_code(k_new), ctypes.byref(view), _stream(k_new.device)))
 
 
 def verify_attn_kv8(q: torch.Tensor, kv: KV8, out=None, lse=None, scale: Optional[float] = None,
@@ -556,8 +572,8 @@ def verify_attn_kv8(q: torch.Tensor, kv: KV8, out=None, lse=None, scale: Optiona
     view = kv.view(B, Hkv, d, q.device, "kv")
     nbytes = workspace_bytes(MAD_OP_VERIFY, B, Hq, Hkv, d, T)
     w = _ws_for(q.device, nbytes, ws)
-    rc = _load_library().mad_verify_attn_kv8(_ptr(q), B, T, Hq, Hkv, d, _dtype_code(q), float(scale), ctypes.byref(view),
-                                             _ptr(out), _ptr(lse), _ptr(w), w.numel(), _stream(q.device))
+    rc = _On(q.device).mad_verify_attn_kv8(_ptr(q), B, T, Hq, Hkv, d, _dtype_code(q), float(scale), ctypes.byref(view),
+                                           _ptr(out), _ptr(lse), _ptr(w), w.numel(), _stream(q.device))
     _check(rc)
     return out, lse
 
@@ -601,8 +617,8 @@ def sample(logits: torch.Tensor, u: Optional[torch.Tensor] = None, temperature=1
     _same_device(dev, u=u, tok=tok, probs=probs)
     dt = _dtype_code(logits)
     w = _ws_for(dev, workspace_bytes(MAD_OP_SAMPLE, B, 1, 1, 64, T, V), ws)
-    _check(_load_library().mad_sample(_ptr(logits), dt, _ptr(u), *settings, B, T, V, _ptr(tok), _ptr(probs), _ptr(w),
-                                      w.numel(), _stream(dev)))
+    _check(_On(dev).mad_sample(_ptr(logits), dt, _ptr(u), *settings, B, T, V, _ptr(tok), _ptr(probs), _ptr(w),
+                               w.numel(), _stream(dev)))
     return tok, probs
 
 
@@ -629,7 +645,7 @@ def accept_greedy(logits: torch.Tensor, draft_tok: Optional[torch.Tensor], n_acc
     _same_device(dev, draft_tok=draft_tok, n_accept=n_accept, next_tok=next_tok)
     nbytes = workspace_bytes(MAD_OP_ACCEPT, B, 1, 1, 64, T, V)
     w = _ws_for(dev, nbytes, ws)
-    rc = _load_library().mad_accept_greedy(_ptr(logits), _dtype_code(logits), _ptr(draft_tok), B, T, V,
+    rc = _On(dev).mad_accept_greedy(_ptr(logits), _dtype_code(logits), _ptr(draft_tok), B, T, V,
                                _ptr(n_accept), _ptr(next_tok), _ptr(w), w.numel(), _stream(dev))
     _check(rc)
     return n_accept, next_tok
@@ -661,9 +677,8 @@ def accept_stochastic(p: torch.Tensor, q: Optional[torch.Tensor], draft_tok: Opt
     _same_device(dev, q=q, draft_tok=draft_tok, u=u, n_accept=n_accept, next_tok=next_tok)
     nbytes = workspace_bytes(MAD_OP_ACCEPT_STOCH, B, 1, 1, 64, T, V)
     w = _ws_for(dev, nbytes, ws)
-    lib = _load_library()
-    rc = lib.mad_accept_stochastic(_ptr(p), _ptr(q), _ptr(draft_tok), _ptr(u), B, T, V, _ptr(n_accept),
-                                   _ptr(next_tok), _ptr(w), w.numel(), _stream(dev))
+    rc = _On(dev).mad_accept_stochastic(_ptr(p), _ptr(q), _ptr(draft_tok), _ptr(u), B, T, V, _ptr(n_accept),
+                                        _ptr(next_tok), _ptr(w), w.numel(), _stream(dev))
     _check(rc)
     return n_accept, next_tok
 
@@ -708,7 +723,7 @@ def memory_prefill_attn(q_raw: torch.Tensor, q_slot: Optional[torch.Tensor], mem
     mv = mem.view(B, Hkv, d, q_raw.dtype, q_raw.device, "mem")
     rv = raw.view(B, Hkv, d, q_raw.dtype, q_raw.device, "raw")
     plen = _host_i32(P, B)
-    rc = _load_library().mad_memory_prefill_attn(
+    rc = _On(q_raw.device).mad_memory_prefill_attn(
         _ptr(q_raw), _ptr(q_slot), B, Hq, Hkv, d, _dtype_code(q_raw), float(scale), plen, q_cap, slot_cap,
         S, W, r, u, ctypes.byref(mv), ctypes.byref(rv), _ptr(out_raw), _ptr(lse_raw),
         _ptr(out_slot) if q_slot is not None else None, _ptr(lse_slot) if q_slot is not None else None,
@@ -742,9 +757,9 @@ def rmsnorm_qkv_rope(x: torch.Tensor, gamma: torch.Tensor, w_qkv: torch.Tensor, 
     _need(len(pos) == R, "pos needs one entry per row")
     _contiguous(x=x, gamma=gamma, w_qkv=w_qkv, q=q, k=k, v=v, xn=xn)
     _same_device(x.device, gamma=gamma, w_qkv=w_qkv, q=q, k=k, v=v, xn=xn)
-    rc = _load_library().mad_rmsnorm_qkv_rope(_ptr(x), _ptr(gamma), float(eps), _ptr(w_qkv), _host_i32(pos, R), R,
-                                              D, Hq, Hkv, d, float(rope_base), 1 if kv_from_row0 else 0, _ptr(q),
-                                              _ptr(k), _ptr(v), _ptr(xn), _stream(x.device))
+    rc = _On(x.device).mad_rmsnorm_qkv_rope(_ptr(x), _ptr(gamma), float(eps), _ptr(w_qkv), _host_i32(pos, R), R,
+                                            D, Hq, Hkv, d, float(rope_base), 1 if kv_from_row0 else 0, _ptr(q),
+                                            _ptr(k), _ptr(v), _ptr(xn), _stream(x.device))
     _check(rc)
     return q, k, v
 
@@ -764,7 +779,7 @@ def linear_residual(x: torch.Tensor, w: torch.Tensor, res: torch.Tensor, out: Op
           "x [R, D], w [N, D], res and out [R, N], bf16")
     _contiguous(x=x, w=w, res=res, out=out)
     _same_device(x.device, w=w, res=res, out=out)
-    _check(_load_library().mad_linear_residual(_ptr(x), _ptr(w), _ptr(res), R, D, N, _ptr(out), _stream(x.device)))
+    _check(_On(x.device).mad_linear_residual(_ptr(x), _ptr(w), _ptr(res), R, D, N, _ptr(out), _stream(x.device)))
     return out
 
 
@@ -784,8 +799,8 @@ def rmsnorm_swiglu(x: torch.Tensor, gamma: torch.Tensor, w_gate_up: torch.Tensor
           and out.shape == (R, Fd), "x [R, D], gamma [D], w_gate_up [2F, D], out [R, F], bf16")
     _contiguous(x=x, gamma=gamma, w_gate_up=w_gate_up, out=out)
     _same_device(x.device, gamma=gamma, w_gate_up=w_gate_up, out=out)
-    _check(_load_library().mad_rmsnorm_swiglu(_ptr(x), _ptr(gamma), float(eps), _ptr(w_gate_up), R, D, Fd,
-                                              _ptr(out), _stream(x.device)))
+    _check(_On(x.device).mad_rmsnorm_swiglu(_ptr(x), _ptr(gamma), float(eps), _ptr(w_gate_up), R, D, Fd,
+                                            _ptr(out), _stream(x.device)))
     return out
 
 
@@ -795,7 +810,7 @@ def probe_stream_read(src: torch.Tensor, sink: Optional[torch.Tensor] = None, n_
     """Stream-read the bytes of a contiguous device tensor (a contiguous range per workgroup,
     nontemporal 16-byte loads)."""
     _need(src.is_contiguous() and src.numel() * src.element_size() % 16 == 0, "src: contiguous, bytes % 16 == 0")
-    _check(_load_library().mad_probe_stream_read(_ptr(src), src.numel() * src.element_size(), _ptr(sink),
+    _check(_On(src.device).mad_probe_stream_read(_ptr(src), src.numel() * src.element_size(), _ptr(sink),
                                                  n_workgroups, _stream(src.device)))
 
 
@@ -803,18 +818,18 @@ def probe_shared_read(src: torch.Tensor, sink: Optional[torch.Tensor] = None, n_
                       threads: int = 256):
     """Every workgroup reads all bytes of a contiguous device tensor (L2-resident after the first touch)."""
     _need(src.is_contiguous() and src.numel() * src.element_size() % 16 == 0, "src: contiguous, bytes % 16 == 0")
-    _check(_load_library().mad_probe_shared_read(_ptr(src), src.numel() * src.element_size(), _ptr(sink),
+    _check(_On(src.device).mad_probe_shared_read(_ptr(src), src.numel() * src.element_size(), _ptr(sink),
                                                  n_workgroups, threads, _stream(src.device)))
 
 
 def probe_empty(n_workgroups: int = 256, threads: int = 256, device=None):
     """Launch an empty kernel (the launch floor)."""
     dev = torch.device(device or "cuda")
-    _check(_load_library().mad_probe_empty(n_workgroups, threads, _stream(dev)))
+    _check(_On(dev).mad_probe_empty(n_workgroups, threads, _stream(dev)))
 
 
 def probe_handoff_latency(buf: torch.Tensor, cycles: torch.Tensor, reps: int):
     """Time the hand-off primitives (see include/mad.h); cycles: int64 [8, reps] on the device."""
     _need(cycles.dtype == torch.int64 and cycles.shape == (8, reps) and cycles.is_contiguous(), "cycles [8, reps] int64")
-    _check(_load_library().mad_probe_handoff_latency(_ptr(buf), buf.numel() * buf.element_size(), _ptr(cycles),
+    _check(_On(buf.device).mad_probe_handoff_latency(_ptr(buf), buf.numel() * buf.element_size(), _ptr(cycles),
                                                      reps, _stream(buf.device)))

@@ -13,6 +13,8 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <ATen/core/Tensor.h>
+#include <c10/core/DeviceGuard.h>
+#include <c10/core/impl/VirtualGuardImpl.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cmath>
@@ -244,11 +246,19 @@ template <typename F> PyObject *guarded(F f) {
         Py_RETURN_NONE;
     }
 }
-#define RELEASED(call)         \
-    int rc;                    \
-    Py_BEGIN_ALLOW_THREADS     \
-    rc = (call);               \
-    Py_END_ALLOW_THREADS       \
+// The call, on the device of its tensors: each has a default stream of its own, and a launch on it goes to the current
+// device.  (Nothing to look up where the process sees one device: 0.2 us of a call's 4.)
+bool several_devices() {
+    static const bool several = c10::impl::VirtualGuardImpl(c10::DeviceType::CUDA).deviceCount() > 1;
+    return several;
+}
+#define RELEASED(call)                                     \
+    c10::OptionalDeviceGuard on_device;                    \
+    if (several_devices()) on_device.reset_device(dev);    \
+    int rc;                                                \
+    Py_BEGIN_ALLOW_THREADS                                 \
+    rc = (call);                                           \
+    Py_END_ALLOW_THREADS                                   \
     return rc
 
 float scale_of(PyObject *o, int64_t d) { return o == Py_None ? (float)std::pow((double)d, -0.5) : (float)as_double(o); }
@@ -301,7 +311,8 @@ PyObject *update(PyObject *, PyObject *const *a, Py_ssize_t n) {
     ORDINARY(6, plain_tensors(a, {0, 1}) && plain_rows(a[2]) && plain_kv(a[3]) && plain_flags(a[4]) && plain_real(a[5]));
     return guarded([&]() -> int {
         const at::Tensor &x = first(a[0]);
-        const at::Tensor &w = dense(a[1], x.device());
+        const at::Device dev = x.device();
+        const at::Tensor &w = dense(a[1], dev);
         need(x.dim() == 3);
         const int B = small(x.size(0)), nn = small(x.size(1)), D = small(x.size(2));
         need(B <= MAD_MAX_BATCH && (int64_t)B * nn <= MAD_MAX_UPDATE_ROWS && w.dim() == 2 && w.size(1) == D &&
@@ -328,7 +339,7 @@ PyObject *update(PyObject *, PyObject *const *a, Py_ssize_t n) {
         }
         const double base = as_double(a[5]);
         const int dt = dtype_code(x);
-        void *st = stream_of(x.device()), *xp = x.data_ptr(), *wp = w.data_ptr();
+        void *st = stream_of(dev), *xp = x.data_ptr(), *wp = w.data_ptr();
         const uint8_t *fp = a[4] != Py_None ? fire : nullptr;
         RELEASED(g.update(xp, wp, pos, fp, B, nn, D, (int)Hkv, d, dt, base, mv, st));
     });
