@@ -1362,39 +1362,36 @@ __global__ __launch_bounds__(kThreads, 8) void sample_kernel(const SampleArgs a)
             } else {
                 out.mode = kRowCut;
                 const float rb = floorf(m * 8.f), low = (rb - (float)(kBins - 1)) * 0.125f;   // low: the bins' end
-                out.target = top_k > 0 ? (double)top_k : a.top_p[b] < 1.0 ? a.top_p[b] * out.mass : -1.0;
-                out.hi = -INFINITY;
-                if (out.target >= 0.0) {
-                    // the row's bins: bin j of a chunk whose maximum lies d bins lower is the row's j + d
-                    const int j = tid & (kBins - 1);
-                    double w = 0.0;
-                    uint32_t n = 0;
-                    #pragma unroll 4
-                    for (int k = tid / kBins; k < a.n_chunks; k += kThreads / kBins) {
-                        const float top = s.c_max[k], d = rb - floorf(top * 8.f);
-                        const bool in = top > -INFINITY && (float)j >= d;
-                        const char *q = rec0 + (size_t)k * kSampleRecord + kHead;
-                        const int jc = in ? j - (int)d : 0;
-                        const double x = bits_f64(get64(q + 8 * jc));
-                        w += in ? x * s.c_unit[k] : 0.0;
-                        if (top_k > 0) {
-                            const uint32_t y = __hip_atomic_load(reinterpret_cast<uint32_t *>(const_cast<char *>(q) + 8 * kBins + 4 * jc),
-                                                                 __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                            n += in ? y : 0;
-                        }
+                out.target = top_k > 0 ? (double)top_k : a.top_p[b] * out.mass;
+                // the row's bins: bin j of a chunk whose maximum lies d bins lower is the row's j + d
+                const int j = tid & (kBins - 1);
+                double w = 0.0;
+                uint32_t n = 0;
+                #pragma unroll 4
+                for (int k = tid / kBins; k < a.n_chunks; k += kThreads / kBins) {
+                    const float top = s.c_max[k], d = rb - floorf(top * 8.f);
+                    const bool in = top > -INFINITY && (float)j >= d;
+                    const char *q = rec0 + (size_t)k * kSampleRecord + kHead;
+                    const int jc = in ? j - (int)d : 0;
+                    const double x = bits_f64(get64(q + 8 * jc));
+                    w += in ? x * s.c_unit[k] : 0.0;
+                    if (top_k > 0) {
+                        const uint32_t y = __hip_atomic_load(reinterpret_cast<uint32_t *>(const_cast<char *>(q) + 8 * kBins + 4 * jc),
+                                                             __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                        n += in ? y : 0;
                     }
-                    s.list[tid] = f64_bits(top_k > 0 ? (double)n : w);
-                    __syncthreads();
-                    if (wave != 0) return;
-                    auto bin = [&](int i) {
-                        return bits_f64(s.list[i]) + bits_f64(s.list[i + kBins]) + bits_f64(s.list[i + 2 * kBins]) + bits_f64(s.list[i + 3 * kBins]);
-                    };
-                    double before;
-                    const int i = first_reaching(bin, out.target, &before);
-                    const bool in = before + bin(i) >= out.target;   // else it is reached below the last bin
-                    out.lo = in ? (rb - (float)i) * 0.125f : -3.402823466e38f;   // (an entry of -inf has no mass)
-                    out.hi = in ? (rb - (float)(i - 1)) * 0.125f : low;
                 }
+                s.list[tid] = f64_bits(top_k > 0 ? (double)n : w);
+                __syncthreads();
+                if (wave != 0) return;
+                auto bin = [&](int i) {
+                    return bits_f64(s.list[i]) + bits_f64(s.list[i + kBins]) + bits_f64(s.list[i + 2 * kBins]) + bits_f64(s.list[i + 3 * kBins]);
+                };
+                double before;
+                const int i = first_reaching(bin, out.target, &before);
+                const bool in = before + bin(i) >= out.target;   // else it is reached below the last bin
+                out.lo = in ? (rb - (float)i) * 0.125f : -3.402823466e38f;   // (an entry of -inf has no mass)
+                out.hi = in ? (rb - (float)(i - 1)) * 0.125f : low;
                 // where min-p ends above it, only that counts: its bin's entries down to it
                 const float tv = key_value(out.t);
                 if (out.t > 0 && tv >= out.hi) {
