@@ -20,9 +20,10 @@
 // in flight together, and stay in registers from the maximum to the codes.
 // Heads are neighbours in the grid: a token's heads lie side by side in the
 // rows that are read.  Measured: two prompts of up to 16384 tokens, 8 heads of
-// 128, bf16, blocks of 128 (134 MB): 24.8 us, 5.4 TB/s (a copy's rate is 4.8 -
-// 5.1); a token, or five for each of 16 sequences: 2.6 - 3.1 us, a launch and
-// two dependent loads (the sequence's record, then its rows and the scale).
+// 128, bf16, blocks of 128 (122 MB counted, two thirds of it reads): 25 us, 4.9
+// TB/s (a copy's rate is 4.8 - 5.1); a token, or five for each of 16 sequences:
+// 2.7 - 3.1 us, a launch and two dependent loads (the sequence's record, then its
+// rows and the scale).
 #include "mad_device.h"
 #include "mad_internal.h"
 

@@ -43,18 +43,22 @@
 //   than 32, huge magnitudes) one workgroup narrows down in passes over the row, with
 //   2048 buckets of the key range each, from what is known.
 //
-// Bound.  Small calls: one launch's chain of round trips (loads 2.7 us, bins and
-// candidates 2.8, arrival 0.9, the records 2.4, the list's end 3.4): a row of 50257
-// 11.5 us, 20 rows with their distributions 12.8.  Large ones: 80 rows of 128256
-// fp32 with top-p and distributions (82 MB read and written once) 66.6 us: 24.2 for the
-// weights (two workgroups per CU load, then compute, in step: 1.6 TB/s, and the vector
-// ALU is busy four fifths of the time: 31 instructions an entry), 27 for the cut (a
-// read at 4 TB/s, then 5 - 14 us for a row's last workgroup), 16.4 for the
-// distributions (5 TB/s, a copy's rate).  64 rows of 128256 with settings of their own,
-// tokens only, 47 us.  A top-k of 200 with top-p, tokens only: a row of 50257 65 us,
-// 16 rows of 128256 85; min-p alone 14.5 and 15.8 (by the bins 23 and 24).  Rows that
-// go by passes: 78 - 160 for top-p in a crowded body, 48 - 76 for min-p there, 90 - 330
-// for the other filters where all entries are within 1/8 (the same sizes).
+// Bound.  Small calls: one launch's chain of round trips (with time stamps in the
+// kernel, 12.2 us in all: loads 2.7, bins and candidates 2.8, arrival 0.9, the records
+// 2.4, the list's end 3.4): a row of 50257 11.2 us, 20 rows with their distributions
+// 13.1.  Large ones: 80 rows of 128256 fp32 with top-p and distributions (82 MB read and
+// written once) 68.3 us: 24.4 for the weights (two workgroups per CU load, then compute,
+// in step: 1.8 TB/s, and the vector ALU is busy 86 % of the time: 60 instructions an
+// entry, 31 of them its weight, the others its bin's), 29 for the cut (a read at 4 TB/s,
+// then 5 - 14 us for a row's last workgroup), 16.5 for the distributions (5 TB/s, a copy's
+// rate).  64 rows of 128256 with settings of their own, tokens only, 47.5 us.  A top-k of
+// 200 with top-p, tokens only: a row of 50257 64 us, 16 rows of 128256 83; min-p alone
+// 14.8 and 16.4 (by the bins 23 and 24).  Rows that go by passes: 77 - 163 for top-p in a
+// crowded body, 49 - 76 for min-p there, 91 - 306 for the other filters where all entries
+// are within 1/8 (the same sizes).
+//   The bins' own units cost the first launch two instructions an entry (weights all
+// in 2^-50 of the largest: 67.9 us for the 80 rows, 46.1 for the 64, and wrong ends
+// among tiny weights).
 //   Not kept: several chunks to a workgroup of the first launch, the next one's loads
 // in flight (its 64 registers do not hold the loop and the row's end: 33 us against
 // 26.5 of one to each); the row's end as a function that is not inlined (75).

@@ -37,12 +37,18 @@
 // way), every row block's wave converted the codes again and the vector ALU was the
 // bound: 16 sequences of 600 .. 12000 keys (210 MB), 64/8 heads, 6 queries 86 us.
 // At a unit's end the waves' results are merged through the stages.
-//   Now that batch takes 56 - 61 us (3.6 TB/s; the chunks themselves arrive at 5.9), one
-// sequence of 32773 keys (67 MB), 40 query rows, 21 + 4.5 us, 317 keys 6.7.
+//   Now such batches take 59 - 71 us by their lengths (216 MB counted in 65, 3.3 TB/s;
+// the chunks themselves arrive at 5.9), one sequence of 32773 keys (68 MB), 40 query
+// rows, 22.5 and 4.5 for the merge, 317 keys 7.1 (kernel times; calls back to back are
+// 0.5 - 1.5 shorter).  The vector ALU is busy 50 - 57 % of the time in the long ones.
 // What is left beside the stream: some 5 us until every CU's first chunks are there,
 // 3.6 for a unit's exchange (48 rows: 200 KB through LDS), the pieces' merge, and
 // workgroups with up to a fifth more slabs than the mean.  Four waves a workgroup,
-// two workgroups per CU: 58.3 against 58.9, but 27.8 against 25.6 and 7.9 against 6.9.
+// two workgroups per CU, when V scales counted against the largest: 58.3 against 58.9
+// for one such batch, but 27.8 against 25.6 for 32773 keys and 7.9 against 6.9 for 317.
+//   The rows' own V reference (m, y above) takes 7 % more vector instructions than one
+// for the wave, 2 % of the long calls' time, and 0.1 us off the short ones, where it
+// spares the exchange between lanes for the largest scale.
 //   A K row's 16-byte chunk holds features 16 c .. 16 c + 15: the first 8 are one
 // 32-feature step's, the rest the next one's; the query fragments are read in
 // the same order.  V^T fragments (8 keys of one feature) come from transposing
