@@ -58,6 +58,7 @@ extern "C" {
 #define MAD_MAX_UPDATE_ROWS 64 /* B * n_new per mad_memory_update call */
 #define MAD_MAX_VERIFY_ROWS 64 /* T * (Hq / Hkv) per mad_verify_attn call */
 #define MAD_MAX_LAYER_ROWS 8   /* rows (raw token + slot tokens) per draft-layer linear map */
+#define MAD_MAX_TOP 64         /* alternatives per row of mad_token_logprobs */
 
 #define MAD_OP_DECODE 0
 #define MAD_OP_UPDATE 1 /* takes no workspace: 0 bytes */
@@ -66,6 +67,7 @@ extern "C" {
 #define MAD_OP_ACCEPT_STOCH 4
 #define MAD_OP_DECODE_LEAST 5
 #define MAD_OP_SAMPLE 6
+#define MAD_OP_LOGPROBS 7
 
 /*
  * A per-sequence, per-KV-head run of key/value rows in device memory.
@@ -299,6 +301,110 @@ int mad_verify_attn_kv8(const void *q, int B, int T, int Hq, int Hkv, int d, int
                         const mad_kv8_view *kv, void *out, float *lse, void *ws, size_t ws_bytes, void *stream);
 
 /*
+ * Rows of heads: row i of sequence b, head h lives at
+ *     p + b * seq_stride + i * row_stride + h * head_dim   (elements of dtype)
+ * so that the heads of a fused projection's output are views of it.  p is
+ * 16-byte aligned and the strides are multiples of 16 bytes, row_stride >= the
+ * heads times head_dim (each stride counts only where there is more than one
+ * sequence, one row).  What is written to must not overlap itself.
+ */
+typedef struct mad_rows {
+    void *p;
+    int64_t seq_stride;
+    int64_t row_stride;
+} mad_rows;
+
+/*
+ * Norms of queries and keys for each head, with the position rotation in the
+ * same pass: what a target's projection leaves becomes what the appends and the
+ * attention take.  For every row i < n[b] of sequence b and every head x of it,
+ * in fp32, rounded once:
+ *   y = x / sqrt(mean(x^2) + eps) * gamma       (gamma given; else y = x)
+ *   z = RoPE(y, pos)                            (rope_base > 0; else z = y), as
+ *       mad_memory_update rotates: pairs (j, j+d/2), angle pos * base^(-2j/d), fp64
+ *   q, q_out   Hq heads a row, or both NULL;   k, k_out   Hkv heads, or both NULL.
+ *              An output is its input (in place) or shares no element with an input.
+ *   q_gamma, k_gamma  device [d], dtype, or NULL: no norm
+ *   start   HOST int32[B]: row i is at position start[b] + i
+ *   pos     device int32 [B][n_cap], any values: the rows' positions.  With a
+ *           rotation one of start and pos is given, the other NULL.
+ *   n       HOST int32[B], 0 <= n[b] <= n_cap (NULL: n_cap); rows from n[b] on
+ *           are neither read nor written
+ * dtype F32 or BF16; d in {64, 128}.  The squares' sum is formed in fp32: |x| below 2^60.
+ * rope_base 0 (no rotation) or finite and above 1.  No workspace.
+ */
+int mad_qk_norm_rope(const mad_rows *q, const mad_rows *k, const mad_rows *q_out, const mad_rows *k_out, const void *q_gamma,
+                     const void *k_gamma, float eps, double rope_base, const int32_t *start, const int32_t *pos,
+                     const int32_t *n, int B, int n_cap, int Hq, int Hkv, int d, int dtype, void *stream);
+
+/*
+ * A 4-bit key/value cache (the OCP MX format of e2m1): codes of 0, 0.5, 1, 1.5,
+ * 2, 3, 4, 6 with a sign in bit 3, two to a byte, the even feature's in the low
+ * half, and one scale byte s for each row and 32 features, which stands for
+ * 2^(s - 127), 255 for NaN.  An element's value is its code's value times its
+ * scale.  Row i of sequence b, KV head h (strides in bytes):
+ *     codes   k + b * seq_stride + h * head_stride + i * head_dim / 2
+ *     scales  k_scale + b * scale_seq_stride + h * scale_head_stride + i * head_dim / 32
+ * and likewise v, v_scale.  seq_stride and scale_seq_stride may be 0 together
+ * (every sequence index aliases the same buffer; not for mad_kv4_append with
+ * B > 1).  k and v 16-byte aligned, their strides multiples of 16; the scales and
+ * their strides multiples of head_dim / 32; head_stride >= cap * head_dim / 2;
+ * scale_head_stride >= cap * head_dim / 32.
+ *   len    HOST int32[B], number of valid rows, 0 <= len <= cap
+ * Scales of valid rows: 0 .. 252 or 255 (values below 2^-126 may count as 0).
+ */
+typedef struct mad_kv4_view {
+    void *k;
+    void *v;
+    void *k_scale;
+    void *v_scale;
+    int64_t seq_stride;
+    int64_t head_stride;
+    int64_t scale_seq_stride;
+    int64_t scale_head_stride;
+    int32_t cap;
+    const int32_t *len;
+} mad_kv4_view;
+
+/*
+ * Append new rows to a 4-bit cache: rows len[b] .. len[b] + n[b] - 1 of every
+ * sequence b from k_new, v_new.  The caller then raises len[b] by n[b]; a
+ * rollback lowers it.  For each row, KV head, tensor and 32 features x:
+ *   scale = the least 2^k, -100 <= k <= 125, with |x| <= 6 * 2^k
+ *   code  = e2m1(x / scale), to nearest even, the sign kept (of zeros too);
+ *           |x| beyond 1.5 * 2^127 as that
+ *   an x that is not finite makes its 32 features NaN: scale byte 255, codes 0
+ * Other rows and their scales are left as they are.
+ *   k_new, v_new    Hkv heads a row, n_cap rows; rows from n[b] on are not read
+ *   k_held, v_held  both NULL, or rows like k_new (k_new and v_new themselves
+ *                   too) that receive the values that the cache now holds, exact
+ *                   in either type: what the rows' own attention in higher
+ *                   precision has to read to see what later steps see
+ *   n               HOST int32[B], 0 <= n[b] <= n_cap, len[b] + n[b] <= cap;
+ *                   NULL = n_cap for every sequence
+ * dtype F32 or BF16; d in {64, 128}.  No workspace.
+ */
+int mad_kv4_append(const mad_rows *k_new, const mad_rows *v_new, const mad_rows *k_held, const mad_rows *v_held,
+                   const int32_t *n, int B, int n_cap, int Hkv, int d, int dtype, const mad_kv4_view *kv, void *stream);
+
+/*
+ * Verify attention (mad_verify_attn) over a 4-bit cache; T = 1 is the decode
+ * step of a single token.  Query t sees rows 0 .. len[b]-T+t; one that sees no
+ * row (len[b] < T - t, a padded sequence with len[b] = 0 among them) gets out =
+ * 0 and lse = -inf.  Rows from len[b] on may hold anything; what a query does not
+ * see has no effect on it, NaN included.
+ *   q    device [B][T][Hq][d], dtype     out  device [B][T][Hq][d], dtype
+ *   lse  device fp32 [B][T][Hq] or NULL
+ * Sums over a row's keys are formed in fp32: the number of keys times the largest
+ * |value| below 2^124.  T * G <= MAD_MAX_VERIFY_ROWS; d in {64, 128}; dtype BF16
+ * or F32, both on the matrix cores (a cached value is exact in bf16; F32: q and
+ * the probabilities as three bf16 terms each, so that products keep fp32's
+ * precision).  Workspace MAD_OP_VERIFY.
+ */
+int mad_verify_attn_kv4(const void *q, int B, int T, int Hq, int Hkv, int d, int dtype, float scale,
+                        const mad_kv4_view *kv, void *out, float *lse, void *ws, size_t ws_bytes, void *stream);
+
+/*
  * Greedy accept/reject (Sec. 2.1; greedy decoding at temperature 0, Sec. 4.1).
  * For each sequence b, with am[t] = argmax_v logits[b][t][v] (ties -> lowest
  * index, a NaN ranks above every number):
@@ -375,6 +481,34 @@ int mad_accept_stochastic(const float *p, const float *q, const int32_t *draft_t
 int mad_sample(const void *logits, int dtype, const float *u, const double *temperature, const int32_t *top_k,
                const double *top_p, const double *min_p, int B, int T, int V, int32_t *tok, float *probs, void *ws,
                size_t ws_bytes, void *stream);
+
+/*
+ * Log probabilities of given tokens, with the rows' entropies and the most
+ * probable alternatives.  For each row (b, t) with logits x, and p the softmax
+ * of x / temperature[b]:
+ *   logp     = log p_v of v = tok[b][t]
+ *   rank     = the number of entries before v in the order by value, equal
+ *              values by the lower index first (0: the most probable)
+ *   entropy  = - sum p log p
+ *   top_tok, top_logp   the first top_n entries of that order and their log p
+ * A v outside [0, V) is no token: logp -inf, rank V.  -inf is an entry of
+ * probability 0 (log p = -inf); +inf takes the whole mass, shared by equal ones.
+ * A row with a NaN, or with nothing but -inf, has no distribution: logp, entropy
+ * and top_logp NaN, rank and top_tok -1.
+ *   logits  device, row (b, t) at logits + b * seq_stride + t * row_stride
+ *           (elements of dtype F32 or BF16, any alignment that suits the type;
+ *           a stride counts only where there is more than one).  The aligned
+ *           16-byte pieces that hold a row's ends are read whole.
+ *   tok     device int32 [B][T], or NULL: then logp and rank are NULL too
+ *   temperature   HOST double [B], finite and above 0; NULL: 1
+ *   logp, entropy   device float32 [B][T] or NULL;  rank  device int32 [B][T] or NULL
+ *   top_tok, top_logp   device int32, float32 [B][T][top_n]; NULL where top_n is 0
+ * 0 <= top_n <= min(V, MAD_MAX_TOP); B <= MAD_MAX_BATCH, B * T <= 2^22,
+ * V <= 2^20.  Workspace MAD_OP_LOGPROBS, 256-byte aligned.
+ */
+int mad_token_logprobs(const void *logits, int dtype, int64_t seq_stride, int64_t row_stride, const int32_t *tok,
+                       const double *temperature, int B, int T, int V, int top_n, float *logp, int32_t *rank,
+                       float *entropy, int32_t *top_tok, float *top_logp, void *ws, size_t ws_bytes, void *stream);
 
 /*
  * Memory-prefill attention (Sec. 3.3, prefill; the appendix on memory
@@ -489,6 +623,7 @@ int mad_probe_handoff_latency(void *buf, size_t buf_bytes, unsigned long long *c
  *   ACCEPT_STOCH: B, max_keys = V               (Hq, Hkv, d, T ignored)
  *   DECODE_LEAST: B, Hq, Hkv, d
  *   SAMPLE: B, T, max_keys = V                  (Hq, Hkv, d ignored)
+ *   LOGPROBS: B, T, max_keys = V                (Hq, Hkv, d ignored)
  * A decode call is accepted from DECODE_LEAST on, what its split partials take
  * (at most 68 KB for each of the B * Hkv units).  With less than DECODE a call
  * may run another kernel: the same sums in another order.

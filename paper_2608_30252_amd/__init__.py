@@ -17,7 +17,11 @@ Entry points (same names as the C ABI, without the ``mad_`` prefix):
                         (verify_attn_vt: the same over a transposed V cache)
     kv8_append          new K/V rows into an 8-bit cache (e4m3, a scale per block of tokens and KV head)
     verify_attn_kv8     verify attention over an 8-bit cache
+    qk_norm_rope        each head's RMS norm of queries and keys, and the rotation at their positions
+    kv4_append          new K/V rows into a 4-bit cache (e2m1, a power-of-two scale per row and 32 features)
+    verify_attn_kv4     verify attention over a 4-bit cache
     sample              temperature, top-k, top-p and min-p: tokens and their distributions
+    token_logprobs      given tokens' log probabilities and ranks, entropies, the most probable alternatives
     accept_greedy       greedy accept/reject
 """
 import ctypes
@@ -34,8 +38,9 @@ LIB_PATH = os.path.join(_HERE, "libmad.so")
 MAD_OK, MAD_EINVAL, MAD_ENOTSUP, MAD_EHIP, MAD_EWS = 0, -1, -2, -3, -4
 MAD_F32, MAD_BF16 = 0, 1
 MAD_OP_DECODE, MAD_OP_UPDATE, MAD_OP_VERIFY, MAD_OP_ACCEPT, MAD_OP_ACCEPT_STOCH, MAD_OP_DECODE_LEAST = 0, 1, 2, 3, 4, 5
-MAD_OP_SAMPLE = 6
+MAD_OP_SAMPLE, MAD_OP_LOGPROBS = 6, 7
 MAX_BATCH = 64
+MAX_TOP = 64
 
 _i32p = ctypes.POINTER(ctypes.c_int32)
 _u8p = ctypes.POINTER(ctypes.c_uint8)
@@ -53,6 +58,17 @@ class _KV8View(ctypes.Structure):
                 ("seq_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
                 ("scale_seq_stride", ctypes.c_int64), ("scale_head_stride", ctypes.c_int64),
                 ("cap", ctypes.c_int32), ("block", ctypes.c_int32), ("len", _i32p)]
+
+
+class _KV4View(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("seq_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("scale_seq_stride", ctypes.c_int64), ("scale_head_stride", ctypes.c_int64),
+                ("cap", ctypes.c_int32), ("len", _i32p)]
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("seq_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64)]
 
 
 _LIB = None
@@ -76,6 +92,11 @@ def _load_library():
     kv8p = ctypes.POINTER(_KV8View)
     lib.mad_kv8_append.argtypes = [vp, vp, _i32p, i, i, i, i, i, kv8p, vp]
     lib.mad_verify_attn_kv8.argtypes = [vp, i, i, i, i, i, i, f, kv8p, vp, vp, vp, sz, vp]
+    kv4p, rows = ctypes.POINTER(_KV4View), ctypes.POINTER(_Rows)
+    lib.mad_qk_norm_rope.argtypes = [rows, rows, rows, rows, vp, vp, f, d, _i32p, vp, _i32p, i, i, i, i, i, i, vp]
+    lib.mad_kv4_append.argtypes = [rows, rows, rows, rows, _i32p, i, i, i, i, i, kv4p, vp]
+    lib.mad_verify_attn_kv4.argtypes = [vp, i, i, i, i, i, i, f, kv4p, vp, vp, vp, sz, vp]
+    lib.mad_token_logprobs.argtypes = [vp, i, ctypes.c_int64, ctypes.c_int64, vp, _f64p, i, i, i, i, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.mad_sample.argtypes = [vp, i, vp, _f64p, _i32p, _f64p, _f64p, i, i, i, vp, vp, vp, sz, vp]
     lib.mad_accept_greedy.argtypes = [vp, i, vp, i, i, i, vp, vp, vp, sz, vp]
     lib.mad_accept_stochastic.argtypes = [vp, vp, vp, vp, i, i, i, vp, vp, vp, sz, vp]
@@ -96,6 +117,7 @@ def _load_library():
     lib.mad_version.restype = ctypes.c_char_p
     for fn in ("mad_draft_decode_attn", "mad_memory_update", "mad_verify_attn", "mad_verify_attn_vt", "mad_accept_greedy",
                "mad_kv8_append", "mad_verify_attn_kv8", "mad_sample",
+               "mad_qk_norm_rope", "mad_kv4_append", "mad_verify_attn_kv4", "mad_token_logprobs",
                "mad_accept_stochastic", "mad_draft_step_attn", "mad_draft_decode_attn_noalloc",
                "mad_memory_prefill_attn",
                "mad_rmsnorm_qkv_rope", "mad_linear_residual", "mad_rmsnorm_swiglu", "mad_probe_stream_read",
@@ -109,7 +131,8 @@ _FAST = None
 _FAST_ENTRIES = ("mad_draft_decode_attn", "mad_draft_step_attn", "mad_memory_update", "mad_verify_attn",
                  "mad_verify_attn_vt", "mad_accept_greedy", "mad_accept_stochastic", "mad_rmsnorm_qkv_rope",
                  "mad_linear_residual", "mad_rmsnorm_swiglu", "mad_workspace_bytes", "mad_kv8_append",
-                 "mad_verify_attn_kv8", "mad_sample")
+                 "mad_verify_attn_kv8", "mad_sample", "mad_qk_norm_rope", "mad_kv4_append", "mad_verify_attn_kv4",
+                 "mad_token_logprobs")
 
 
 class _CtypesOnly:
@@ -135,6 +158,7 @@ def _fast():
         _fastcall.bind(tuple(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in _FAST_ENTRIES), KV,
                        _default_ws, torch._C._cuda_getCurrentRawStream)
         _fastcall.bind_kv8(KV8)
+        _fastcall.bind_kv4(KV4)
         _FAST = _fastcall
     return _FAST
 
@@ -281,6 +305,61 @@ class KV8:
         many = k.shape[0] > 1
         return _KV8View(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), k.stride(0) if many else 0, k.stride(1),
                         ks.stride(0) if many else 0, ks.stride(1), k.shape[2], self.block, self._len)
+
+
+@dataclass
+class KV4:
+    """A 4-bit cache (OCP MX e2m1): K and V bytes [B, Hkv, cap, d / 2] in torch.uint8, two codes each, the even feature's in
+    the low half (any strides with contiguous rows, the same for both), the scale bytes of each row's groups of 32
+    features, torch.uint8 [B, Hkv, cap, d / 32] (2^(byte - 127), 255 NaN), and per-sequence host lengths."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+    length: Sequence[int]
+
+    @staticmethod
+    def empty(B, Hkv, cap, d, device="cuda"):
+        """A cache without rows.  Neither codes nor scales need a value before their rows are appended."""
+        mk = lambda n: torch.zeros((B, Hkv, cap, n), dtype=torch.uint8, device=device)   # noqa: E731
+        return KV4(mk(d // 2), mk(d // 2), mk(d // 32), mk(d // 32), [0] * B)
+
+    def view(self, B, Hkv=None, d=None, device=None, name="kv"):
+        """The C view of this cache for a call over B rows.  The batch dimension must be B, or 1 (every row then
+        aliases sequence 0); the KV heads, head_dim and device must match the call's."""
+        k, v, ks, vs = self.k, self.v, self.k_scale, self.v_scale
+        if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride():
+            raise ValueError(f"{name}: K and V must be [B, Hkv, cap, d / 2] tensors with identical strides")
+        if any(t.dtype != torch.uint8 for t in (k, v, ks, vs)):
+            raise ValueError(f"{name}: K, V and their scales must be torch.uint8")
+        if k.stride(3) != 1 or k.stride(2) != k.shape[3]:
+            raise ValueError(f"{name}: K/V rows must be contiguous")
+        if k.shape[0] not in (1, B):
+            raise ValueError(f"{name}: batch dimension {k.shape[0]} must be 1 or B={B}")
+        if Hkv is not None and k.shape[1] != Hkv:
+            raise ValueError(f"{name}: {k.shape[1]} KV heads, the call has {Hkv}")
+        if d is not None and 2 * k.shape[3] != d:
+            raise ValueError(f"{name}: head_dim {2 * k.shape[3]}, the call has {d}")
+        want = (*k.shape[:3], k.shape[3] // 16)
+        if ks.shape != want or vs.shape != want or ks.stride() != vs.stride() or ks.stride(3) != 1 or ks.stride(2) != want[3]:
+            raise ValueError(f"{name}: scales must be [B, Hkv, cap, d / 32] = {want}, with contiguous rows and identical strides")
+        for t in (k, v, ks, vs):
+            if device is not None and t.device != device:
+                raise ValueError(f"{name}: tensors on {t.device}, the call is on {device}")
+        if len(self.length) < B:
+            raise ValueError(f"{name}: lengths need one entry per row ({B})")
+        self._len = _host_i32(self.length, B)
+        many = k.shape[0] > 1
+        return _KV4View(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), k.stride(0) if many else 0, k.stride(1),
+                        ks.stride(0) if many else 0, ks.stride(1), k.shape[2], self._len)
+
+
+def _rows(t, name):
+    """The C view of rows of heads [B, n, H, d] whose heads lie one after the other (or None)."""
+    if t is None:
+        return None
+    _need(t.stride(3) == 1 and (t.shape[2] == 1 or t.stride(2) == t.shape[3]), f"{name}: a row's heads must be contiguous")
+    return ctypes.byref(_Rows(t.data_ptr(), t.stride(0), t.stride(1)))
 
 
 def _need(cond, msg):
@@ -578,6 +657,98 @@ def verify_attn_kv8(q: torch.Tensor, kv: KV8, out=None, lse=None, scale: Optiona
     return out, lse
 
 
+def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], pos=None, q_gamma: Optional[torch.Tensor] = None,
+                 k_gamma: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                 k_out: Optional[torch.Tensor] = None, n: Optional[Sequence[int]] = None, eps: float = 1e-5,
+                 rope_base: Optional[float] = 500000.0):
+    """q [B, n_cap, Hq, d] and k [B, n_cap, Hkv, d] (either may be None; views of a fused projection as they are) ->
+    (q_out, k_out): each head's RMS norm times gamma [d] (None: no norm), then the rotation at pos: a host list of each
+    sequence's first position, or an int32 tensor [B, n_cap] of the rows' own.  rope_base None: no rotation.  Only rows
+    below n[b] are read and written (without n, all).  An output may be its input."""
+    rc = (_FAST or _fast()).qk_norm_rope(q, k, pos, q_gamma, k_gamma, q_out, k_out, n, eps, rope_base)
+    if rc is not None:
+        _check(rc)
+        return q_out, k_out
+    like = q if q is not None else k
+    _need(like is not None, "neither q nor k is given")
+    for name, x in (("q", q), ("k", k)):
+        _need(x is None or (x.dim() == 4 and x.shape[:2] == like.shape[:2] and x.shape[3] == like.shape[3]
+                            and x.dtype == like.dtype), f"{name} must be [B, n_cap, heads, d], q and k alike")
+    B, n_cap, _, d = like.shape
+    dev = like.device
+    if q is not None and q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    if k is not None and k_out is None:
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=dev)
+    for name, x, y, g in (("q", q, q_out, q_gamma), ("k", k, k_out, k_gamma)):
+        _need((x is None) == (y is None), f"{name}_out goes with {name}")
+        _need(x is not None or g is None, f"{name}_gamma goes with {name}")
+        _need(x is None or (y.shape == x.shape and y.dtype == x.dtype), f"{name}_out must match {name}")
+        _need(g is None or (g.shape == (d,) and g.dtype == like.dtype and g.is_contiguous()), f"{name}_gamma must be [d] of {like.dtype}")
+    _need(n is None or len(n) == B, "n needs one entry per sequence")
+    start = rows_pos = None
+    if rope_base is not None:
+        _need(pos is not None, "the rotation needs pos")
+        if isinstance(pos, torch.Tensor) and pos.dim() == 2:
+            _need(pos.shape == (B, n_cap) and pos.dtype == torch.int32 and pos.is_contiguous(), "pos must be int32 [B, n_cap], contiguous")
+            rows_pos = pos
+        else:
+            _need(len(pos) == B, "pos needs one first position per sequence")
+            start = _host_i32(pos, B)
+    _same_device(dev, q=q, k=k, q_out=q_out, k_out=k_out, q_gamma=q_gamma, k_gamma=k_gamma, pos=rows_pos)
+    _check(_On(dev).mad_qk_norm_rope(_rows(q, "q"), _rows(k, "k"), _rows(q_out, "q_out"), _rows(k_out, "k_out"), _ptr(q_gamma),
+                                     _ptr(k_gamma), float(eps), 0.0 if rope_base is None else float(rope_base), start,
+                                     _ptr(rows_pos), None if n is None else _host_i32(n, B), B, n_cap,
+                                     0 if q is None else q.shape[2], 0 if k is None else k.shape[2], d, _dtype_code(like),
+                                     _stream(dev)))
+    return q_out, k_out
+
+
+def kv4_append(k_new: torch.Tensor, v_new: torch.Tensor, kv: KV4, n: Optional[Sequence[int]] = None,
+               k_held: Optional[torch.Tensor] = None, v_held: Optional[torch.Tensor] = None):
+    """Appends rows 0 .. n[b]-1 of k_new, v_new [B, n_cap, Hkv, d] (all of them without n; views of a fused projection as
+    they are) to a 4-bit cache, at rows kv.length[b] .. of every sequence.  k_held and v_held, like k_new and v_new (or
+    those themselves), receive the values that the cache now holds.  The caller then raises its lengths."""
+    rc = (_FAST or _fast()).kv4_append(k_new, v_new, kv, n, k_held, v_held)
+    if rc is not None:
+        _check(rc)
+        return
+    _need(k_new.dim() == 4, "k_new must be [B, n_cap, Hkv, d]")
+    _need((k_held is None) == (v_held is None), "k_held and v_held go together")
+    for name, x in (("v_new", v_new), ("k_held", k_held), ("v_held", v_held)):
+        _need(x is None or (x.shape == k_new.shape and x.dtype == k_new.dtype), f"{name} must match k_new's shape and dtype")
+    B, n_cap, Hkv, d = k_new.shape
+    _need(n is None or len(n) == B, "n needs one entry per sequence")
+    _same_device(k_new.device, v_new=v_new, k_held=k_held, v_held=v_held)
+    view = kv.view(B, Hkv, d, k_new.device, "kv")
+    _check(_On(k_new.device).mad_kv4_append(_rows(k_new, "k_new"), _rows(v_new, "v_new"), _rows(k_held, "k_held"),
+                                            _rows(v_held, "v_held"), None if n is None else _host_i32(n, B), B, n_cap, Hkv,
+                                            d, _dtype_code(k_new), ctypes.byref(view), _stream(k_new.device)))
+
+
+def verify_attn_kv4(q: torch.Tensor, kv: KV4, out=None, lse=None, scale: Optional[float] = None,
+                    ws: Optional[torch.Tensor] = None):
+    """verify_attn over a 4-bit cache: q [B, T, Hq, d] (bf16 or fp32), query t sees rows 0 .. kv.length[b]-T+t
+    (T = 1: a single token's attention).  Returns (out [B, T, Hq, d], lse [B, T, Hq]); a query that sees no row has
+    out 0 and lse -inf."""
+    if out is not None and lse is not None:
+        rc = (_FAST or _fast()).verify4(q, kv, out, lse, scale, ws)
+        if rc is not None:
+            _check(rc)
+            return out, lse
+    out, lse, scale = _verify_out(q, out, lse, scale)
+    B, T, Hq, d = q.shape
+    Hkv = kv.k.shape[1]
+    _need(Hkv >= 1 and Hq % Hkv == 0, f"Hq={Hq} must be a multiple of the KV heads {Hkv}")
+    view = kv.view(B, Hkv, d, q.device, "kv")
+    nbytes = workspace_bytes(MAD_OP_VERIFY, B, Hq, Hkv, d, T)
+    w = _ws_for(q.device, nbytes, ws)
+    rc = _On(q.device).mad_verify_attn_kv4(_ptr(q), B, T, Hq, Hkv, d, _dtype_code(q), float(scale), ctypes.byref(view),
+                                           _ptr(out), _ptr(lse), _ptr(w), w.numel(), _stream(q.device))
+    _check(rc)
+    return out, lse
+
+
 def _host_f64(vals, n) -> ctypes.Array:
     return (ctypes.c_double * n)(*[float(x) for x in vals])
 
@@ -620,6 +791,53 @@ def sample(logits: torch.Tensor, u: Optional[torch.Tensor] = None, temperature=1
     _check(_On(dev).mad_sample(_ptr(logits), dt, _ptr(u), *settings, B, T, V, _ptr(tok), _ptr(probs), _ptr(w),
                                w.numel(), _stream(dev)))
     return tok, probs
+
+
+def token_logprobs(logits: torch.Tensor, tok: Optional[torch.Tensor] = None, top_n: int = 0, temperature=1.0,
+                   logp: Optional[torch.Tensor] = None, rank: Optional[torch.Tensor] = None,
+                   entropy: Optional[torch.Tensor] = None, top_tok: Optional[torch.Tensor] = None,
+                   top_logp: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+    """logits [B, T, V] (fp32 or bf16; any strides with contiguous rows, logits[:, :-1] among them) and tokens int32
+    [B, T] -> (logp, rank, entropy, top_tok, top_logp): the tokens' log probabilities at the temperature (a number, or one
+    per sequence) and their ranks (0: the most probable), [B, T]; each row's entropy; the top_n (up to 64) most probable
+    entries and their log probabilities, [B, T, top_n].  Without tok logp and rank are None, without top_n the last two.
+    A tok outside the vocabulary has logp -inf and rank V; a row without a distribution (a NaN, nothing but -inf) has NaN,
+    rank and top_tok -1."""
+    rc = (_FAST or _fast()).logprobs(logits, tok, top_n, temperature, logp, rank, entropy, top_tok, top_logp, ws)
+    if rc is not None:
+        _check(rc)
+        return logp, rank, entropy, top_tok, top_logp
+    _need(logits.dim() == 3, "logits must be [B, T, V]")
+    B, T, V = logits.shape
+    dev = logits.device
+    top_n = int(top_n)
+    _need(V == 1 or logits.stride(2) == 1, "logits' rows must be contiguous")
+    _need(tok is not None or (logp is None and rank is None), "logp and rank need tok")
+    _need(top_n > 0 or (top_tok is None and top_logp is None), "top_tok and top_logp need top_n")
+    _need(0 <= top_n <= min(V, MAX_TOP), f"top_n={top_n} outside [0, min(V, {MAX_TOP})]")
+    f32, i32 = dict(dtype=torch.float32, device=dev), dict(dtype=torch.int32, device=dev)
+    if tok is not None:
+        logp = torch.empty((B, T), **f32) if logp is None else logp
+        rank = torch.empty((B, T), **i32) if rank is None else rank
+    entropy = torch.empty((B, T), **f32) if entropy is None else entropy
+    if top_n > 0:
+        top_tok = torch.empty((B, T, top_n), **i32) if top_tok is None else top_tok
+        top_logp = torch.empty((B, T, top_n), **f32) if top_logp is None else top_logp
+    for name, x, shape, dt in (("tok", tok, (B, T), torch.int32), ("logp", logp, (B, T), torch.float32),
+                               ("rank", rank, (B, T), torch.int32), ("entropy", entropy, (B, T), torch.float32),
+                               ("top_tok", top_tok, (B, T, top_n), torch.int32),
+                               ("top_logp", top_logp, (B, T, top_n), torch.float32)):
+        _need(x is None or (x.shape == shape and x.dtype == dt), f"{name} must be {dt} {shape}")
+    one = not hasattr(temperature, "__len__") or getattr(temperature, "ndim", 1) == 0
+    temps = [temperature] * B if one else temperature
+    _need(len(temps) == B, "temperature needs one entry per sequence")
+    _contiguous(tok=tok, logp=logp, rank=rank, entropy=entropy, top_tok=top_tok, top_logp=top_logp)
+    _same_device(dev, tok=tok, logp=logp, rank=rank, entropy=entropy, top_tok=top_tok, top_logp=top_logp)
+    w = _ws_for(dev, workspace_bytes(MAD_OP_LOGPROBS, B, 1, 1, 64, T, V), ws)
+    _check(_On(dev).mad_token_logprobs(_ptr(logits), _dtype_code(logits), logits.stride(0), logits.stride(1), _ptr(tok),
+                                       _host_f64(temps, B), B, T, V, top_n, _ptr(logp), _ptr(rank), _ptr(entropy),
+                                       _ptr(top_tok), _ptr(top_logp), _ptr(w), w.numel(), _stream(dev)))
+    return logp, rank, entropy, top_tok, top_logp
 
 
 def accept_greedy(logits: torch.Tensor, draft_tok: Optional[torch.Tensor], n_accept=None, next_tok=None,

@@ -40,8 +40,12 @@ struct Entry {
     decltype(&mad_kv8_append) kv8_append;
     decltype(&mad_verify_attn_kv8) verify8;
     decltype(&mad_sample) sample;
+    decltype(&mad_qk_norm_rope) norm_rope;
+    decltype(&mad_kv4_append) kv4_append;
+    decltype(&mad_verify_attn_kv4) verify4;
+    decltype(&mad_token_logprobs) logprobs;
 } g;
-PyObject *g_kv, *g_kv8, *g_ws, *g_stream;   // classes KV and KV8, the default workspaces' dict, the raw-stream getter
+PyObject *g_kv, *g_kv8, *g_kv4, *g_ws, *g_stream;   // classes KV, KV8 and KV4, the default workspaces' dict, the raw-stream getter
 PyObject *s_k, *s_v, *s_length, *s_start, *s_buf, *s_k_scale, *s_v_scale, *s_block;
 
 struct Unhandled {};   // thrown for every call the Python path has to take
@@ -137,6 +141,7 @@ bool plain_tensors(PyObject *const *a, std::initializer_list<int> at) {
         if (!THPVariable_CheckExact(a[i])) return false;
     return true;
 }
+bool plain_kv4(PyObject *o) { return Py_TYPE(o) == (PyTypeObject *)g_kv4 && plain_attr(o, s_length, false); }
 #define ORDINARY(n_args, cond) \
     if (n != (n_args) || !(cond)) Py_RETURN_NONE
 
@@ -204,6 +209,47 @@ struct View8 {
         return &c;
     }
 };
+
+struct View4 {
+    mad_kv4_view c;
+    int32_t len[MAD_MAX_BATCH];
+    // KV4 `o` for B rows of [Hkv, cap, d] (Hkv < 0: any, returned in Hkv)
+    mad_kv4_view *read(PyObject *o, int B, int64_t *Hkv, int64_t d, const at::Device &dev) {
+        need(Py_TYPE(o) == (PyTypeObject *)g_kv4 && B >= 1 && B <= MAD_MAX_BATCH);
+        Ref ko(PyObject_GetAttr(o, s_k)), vo(PyObject_GetAttr(o, s_v)), kso(PyObject_GetAttr(o, s_k_scale)),
+            vso(PyObject_GetAttr(o, s_v_scale)), lo(PyObject_GetAttr(o, s_length));
+        const at::Tensor &k = tensor(ko.p), &v = tensor(vo.p), &ks = tensor(kso.p), &vs = tensor(vso.p);
+        need(k.dim() == 4 && k.sizes() == v.sizes() && k.strides() == v.strides());
+        need(k.scalar_type() == at::kByte && v.scalar_type() == at::kByte && ks.scalar_type() == at::kByte && vs.scalar_type() == at::kByte);
+        need(k.stride(3) == 1 && k.stride(2) == k.size(3));
+        need(k.size(0) == 1 || k.size(0) == B);
+        if (*Hkv < 0) *Hkv = k.size(1);
+        need(k.size(1) == *Hkv && 2 * k.size(3) == d);
+        c.cap = small(k.size(2));
+        need(shape(ks, {k.size(0), *Hkv, c.cap, d / 32}) && vs.sizes() == ks.sizes() && ks.strides() == vs.strides());
+        need(ks.stride(3) == 1 && ks.stride(2) == d / 32);
+        need(k.device() == dev && v.device() == dev && ks.device() == dev && vs.device() == dev);
+        ints(lo.p, B, len);
+        const bool many = k.size(0) > 1;
+        c.k = k.data_ptr();
+        c.v = v.data_ptr();
+        c.k_scale = ks.data_ptr();
+        c.v_scale = vs.data_ptr();
+        c.seq_stride = many ? k.stride(0) : 0;
+        c.head_stride = k.stride(1);
+        c.scale_seq_stride = many ? ks.stride(0) : 0;
+        c.scale_head_stride = ks.stride(1);
+        c.len = len;
+        return &c;
+    }
+};
+
+// rows of heads [B, n_cap, H, d] whose heads lie one after the other
+mad_rows rows_of(const at::Tensor &t, const at::Device &dev) {
+    need(t.dim() == 4 && t.device() == dev && t.is_cuda() && t.layout() == at::kStrided && t.stride(3) == 1 &&
+         (t.size(2) == 1 || t.stride(2) == t.size(3)));
+    return {t.data_ptr(), t.stride(0), t.stride(1)};
+}
 
 void *stream_of(const at::Device &dev) {
     Ref index(PyLong_FromLong(dev.index()));
@@ -536,6 +582,159 @@ PyObject *sample(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+// qk_norm_rope(q | None, k | None, pos, q_gamma | None, k_gamma | None, q_out, k_out, n | None, eps, rope_base | None)
+PyObject *qk_norm_rope(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    auto maybe = [&](int i) { return a[i] == Py_None || THPVariable_CheckExact(a[i]); };
+    ORDINARY(10, maybe(0) && maybe(1) && (a[0] != Py_None || a[1] != Py_None) && maybe(3) && maybe(4) &&
+                     (a[5] != Py_None || a[0] == Py_None) && (a[6] != Py_None || a[1] == Py_None) && maybe(5) && maybe(6) &&
+                     (a[7] == Py_None || plain_ints(a[7])) && plain_real(a[8]) && (a[9] == Py_None || plain_real(a[9])) &&
+                     (a[9] == Py_None || plain_ints(a[2]) || THPVariable_CheckExact(a[2])));
+    return guarded([&]() -> int {
+        const at::Tensor &like = tensor(a[0] != Py_None ? a[0] : a[1]);
+        const at::Device dev = like.device();
+        need(like.dim() == 4);
+        const int B = small(like.size(0)), n_cap = small(like.size(1)), d = small(like.size(3));
+        need(B >= 1 && B <= MAD_MAX_BATCH);
+        mad_rows in[2], out[2];
+        void *gamma[2] = {nullptr, nullptr};
+        int heads[2] = {0, 0};
+        for (int i = 0; i < 2; ++i) {
+            if (a[i] == Py_None) {
+                need(a[3 + i] == Py_None && a[5 + i] == Py_None);
+                continue;
+            }
+            const at::Tensor &x = tensor(a[i]), &y = tensor(a[5 + i]);
+            in[i] = rows_of(x, dev);
+            out[i] = rows_of(y, dev);
+            heads[i] = small(x.size(2));
+            need(x.size(0) == B && x.size(1) == n_cap && x.size(3) == d && x.scalar_type() == like.scalar_type());
+            need(y.sizes() == x.sizes() && y.scalar_type() == x.scalar_type());
+            if (a[3 + i] != Py_None) {
+                const at::Tensor &gm = dense(a[3 + i], dev);
+                need(shape(gm, {d}) && gm.scalar_type() == like.scalar_type());
+                gamma[i] = gm.data_ptr();
+            }
+        }
+        int32_t start[MAD_MAX_BATCH], rows[MAD_MAX_BATCH];
+        const int32_t *sp = nullptr, *pp = nullptr, *np = nullptr;
+        double base = 0.0;
+        if (a[9] != Py_None) {
+            base = as_double(a[9]);
+            if (THPVariable_CheckExact(a[2])) {
+                const at::Tensor &p = dense(a[2], dev);
+                need(shape(p, {B, n_cap}) && p.scalar_type() == at::kInt);
+                pp = (const int32_t *)p.data_ptr();
+            } else {
+                ints(a[2], B, start);
+                sp = start;
+            }
+        }
+        if (a[7] != Py_None) {
+            ints(a[7], B, rows);
+            np = rows;
+        }
+        const float eps = (float)as_double(a[8]);
+        const int dt = dtype_code(like);
+        void *st = stream_of(dev);
+        const bool q = a[0] != Py_None, k = a[1] != Py_None;
+        RELEASED(g.norm_rope(q ? &in[0] : nullptr, k ? &in[1] : nullptr, q ? &out[0] : nullptr, k ? &out[1] : nullptr, gamma[0], gamma[1],
+                             eps, base, sp, pp, np, B, n_cap, heads[0], heads[1], d, dt, st));
+    });
+}
+
+// kv4_append(k_new, v_new, kv, n | None, k_held | None, v_held | None)
+PyObject *kv4_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    ORDINARY(6, plain_tensors(a, {0, 1}) && plain_kv4(a[2]) && (a[3] == Py_None || plain_ints(a[3])) &&
+                    ((a[4] == Py_None && a[5] == Py_None) || plain_tensors(a, {4, 5})));
+    return guarded([&]() -> int {
+        const at::Tensor &k = tensor(a[0]), &v = tensor(a[1]);
+        const at::Device dev = k.device();
+        mad_rows r[4] = {rows_of(k, dev), rows_of(v, dev)};
+        need(v.sizes() == k.sizes() && v.scalar_type() == k.scalar_type());
+        const bool held = a[4] != Py_None;
+        for (int i = 2; held && i < 4; ++i) {
+            const at::Tensor &t = tensor(a[2 + i]);
+            need(t.sizes() == k.sizes() && t.scalar_type() == k.scalar_type());
+            r[i] = rows_of(t, dev);
+        }
+        const int B = small(k.size(0)), n_cap = small(k.size(1)), d = small(k.size(3));
+        int64_t Hkv = small(k.size(2));
+        View4 kv;
+        mad_kv4_view *c = kv.read(a[2], B, &Hkv, d, dev);
+        int32_t rows[MAD_MAX_BATCH];
+        if (a[3] != Py_None) ints(a[3], B, rows);
+        const int32_t *np = a[3] != Py_None ? rows : nullptr;
+        const int dt = dtype_code(k);
+        void *st = stream_of(dev);
+        RELEASED(g.kv4_append(&r[0], &r[1], held ? &r[2] : nullptr, held ? &r[3] : nullptr, np, B, n_cap, (int)Hkv, d, dt, c, st));
+    });
+}
+
+// verify4(q, kv, out, lse, scale, ws)
+PyObject *verify4(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    ORDINARY(6, plain_tensors(a, {0, 2, 3}) && plain_kv4(a[1]) && (a[4] == Py_None || plain_real(a[4])));
+    return guarded([&]() -> int {
+        const at::Tensor &q = first(a[0]);
+        const at::Device dev = q.device();
+        need(q.dim() == 4);
+        const int B = small(q.size(0)), T = small(q.size(1)), Hq = small(q.size(2)), d = small(q.size(3));
+        int64_t Hkv = -1;
+        View4 kv;
+        mad_kv4_view *v = kv.read(a[1], B, &Hkv, d, dev);
+        need(Hkv >= 1 && Hq % Hkv == 0);
+        const at::Tensor &out = dense(a[2], dev), &lse = dense(a[3], dev);
+        need(out.sizes() == q.sizes() && out.scalar_type() == q.scalar_type());
+        need(shape(lse, {B, T, Hq}) && lse.scalar_type() == at::kFloat);
+        const float scale = scale_of(a[4], d);
+        void *st = stream_of(dev);
+        const Scratch ws(a[5], dev, st, g.ws_bytes(MAD_OP_VERIFY, B, Hq, (int)Hkv, d, T, 0));
+        const int dt = dtype_code(q);
+        void *qp = q.data_ptr(), *op = out.data_ptr();
+        float *lp = (float *)lse.data_ptr();
+        RELEASED(g.verify4(qp, B, T, Hq, (int)Hkv, d, dt, scale, v, op, lp, ws.p, ws.n, st));
+    });
+}
+
+// logprobs(logits, tok | None, top_n, temperature, logp, rank, entropy, top_tok, top_logp, ws): every output there is given
+PyObject *logprobs(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    ORDINARY(10, plain_tensors(a, {0, 6}) && PyLong_CheckExact(a[2]) && plain_reals(a[3]) &&
+                     (a[1] == Py_None ? a[4] == Py_None && a[5] == Py_None : plain_tensors(a, {1, 4, 5})) &&
+                     ((a[7] == Py_None && a[8] == Py_None) || plain_tensors(a, {7, 8})));
+    return guarded([&]() -> int {
+        const at::Tensor &x = tensor(a[0]);
+        const at::Device dev = x.device();
+        need(x.dim() == 3 && x.is_cuda() && x.layout() == at::kStrided);
+        const int B = small(x.size(0)), T = small(x.size(1)), V = small(x.size(2)), top = as_int(a[2]);
+        need(B >= 1 && B <= MAD_MAX_BATCH && (V == 1 || x.stride(2) == 1));
+        need(top >= 0 && top <= MAD_MAX_TOP && top <= V && (top > 0) == (a[7] != Py_None));
+        double temp[MAD_MAX_BATCH];
+        reals(a[3], B, temp);
+        auto f32 = [&](PyObject *o, std::initializer_list<int64_t> want) {
+            const at::Tensor &t = dense(o, dev);
+            need(shape(t, want) && t.scalar_type() == at::kFloat);
+            return (float *)t.data_ptr();
+        };
+        const int32_t *tok = nullptr;
+        float *lp = nullptr, *ent = f32(a[6], {B, T}), *tl = nullptr;
+        int32_t *rank = nullptr, *tt = nullptr;
+        if (a[1] != Py_None) {
+            tok = (const int32_t *)i32(a[1], dev, {B, T}).data_ptr();
+            lp = f32(a[4], {B, T});
+            rank = (int32_t *)i32(a[5], dev, {B, T}).data_ptr();
+        }
+        if (top > 0) {
+            tt = (int32_t *)i32(a[7], dev, {B, T, top}).data_ptr();
+            tl = f32(a[8], {B, T, top});
+        }
+        void *st = stream_of(dev);
+        const Scratch ws(a[9], dev, st, g.ws_bytes(MAD_OP_LOGPROBS, B, 1, 1, 64, T, V));
+        const int dt = dtype_code(x);
+        void *xp = x.data_ptr();
+        const int64_t seq = x.stride(0), row = x.stride(1);
+        RELEASED(g.logprobs(xp, dt, seq, row, tok, temp, B, T, V, top, lp, rank, ent, tt, tl, ws.p, ws.n, st));
+    });
+}
+
 // stoch(p, q, draft, u, n_accept, next_tok, ws)
 PyObject *stoch(PyObject *, PyObject *const *a, Py_ssize_t n) {
     ORDINARY(7, plain_tensors(a, {0, 1, 2, 3, 4, 5}));
@@ -649,10 +848,18 @@ PyObject *bind_kv8(PyObject *, PyObject *kv8) {
     Py_RETURN_NONE;
 }
 
+// bind_kv4(KV4)
+PyObject *bind_kv4(PyObject *, PyObject *kv4) {
+    Py_INCREF(kv4);
+    Py_XSETREF(g_kv4, kv4);
+    Py_RETURN_NONE;
+}
+
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, nullptr}, {"bind_kv8", bind_kv8, METH_O, nullptr}, FAST(attn), FAST(update), FAST(verify), FAST(verify_vt),
+PyMethodDef methods[] = {{"bind", bind, METH_VARARGS, nullptr}, {"bind_kv8", bind_kv8, METH_O, nullptr},
+                         {"bind_kv4", bind_kv4, METH_O, nullptr}, FAST(attn), FAST(update), FAST(verify), FAST(verify_vt),
                          FAST(greedy), FAST(stoch), FAST(qkv), FAST(linear), FAST(swiglu), FAST(kv8_append),
-                         FAST(verify8), FAST(sample), {nullptr, nullptr, 0, nullptr}};
+                         FAST(verify8), FAST(sample), FAST(qk_norm_rope), FAST(kv4_append), FAST(verify4), FAST(logprobs), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -107,6 +107,53 @@ int check_view8(const mad_kv8_view *v, int B, int Hkv, int d) {
     return MAD_OK;
 }
 
+// Validate a 4-bit view for B sequences.
+int check_view4(const mad_kv4_view *v, int B, int Hkv, int d) {
+    if (!v) return fail(MAD_EINVAL, "null kv");
+    if (!v->k || !v->v || !v->k_scale || !v->v_scale) return fail(MAD_EINVAL, "kv: null k, v, k_scale or v_scale");
+    if (!aligned16(v->k) || !aligned16(v->v)) return fail(MAD_EINVAL, "kv: k/v not 16-byte aligned");
+    const int sr = d / 32;   // scale bytes of a row
+    if (((uintptr_t)v->k_scale | (uintptr_t)v->v_scale) & (uintptr_t)(sr - 1))
+        return fail(MAD_EINVAL, "kv: scales not %d-byte aligned", sr);
+    if (v->cap < 1) return fail(MAD_EINVAL, "kv: cap=%d", v->cap);
+    if (!v->len) return fail(MAD_EINVAL, "kv: null len");
+    if (v->seq_stride < 0 || v->head_stride < (int64_t)v->cap * (d / 2) || v->seq_stride % 16 || v->head_stride % 16)
+        return fail(MAD_EINVAL, "kv: bad strides (seq %lld, head %lld) for cap %d, d %d", (long long)v->seq_stride,
+                    (long long)v->head_stride, v->cap, d);
+    if (v->scale_seq_stride < 0 || v->scale_head_stride < (int64_t)v->cap * sr || v->scale_seq_stride % sr || v->scale_head_stride % sr)
+        return fail(MAD_EINVAL, "kv: bad scale strides (seq %lld, head %lld) for cap %d, d %d",
+                    (long long)v->scale_seq_stride, (long long)v->scale_head_stride, v->cap, d);
+    if ((v->seq_stride == 0) != (v->scale_seq_stride == 0) && B > 1)
+        return fail(MAD_EINVAL, "kv: codes and scales are shared by all sequences, or neither");
+    if (B > 1 && v->seq_stride != 0 && (v->seq_stride < (int64_t)Hkv * v->head_stride ||
+                                        v->scale_seq_stride < (int64_t)Hkv * v->scale_head_stride))
+        return fail(MAD_EINVAL, "kv: seq_stride %lld (scales %lld) overlaps heads", (long long)v->seq_stride,
+                    (long long)v->scale_seq_stride);
+    for (int b = 0; b < B; ++b)
+        if (v->len[b] < 0 || v->len[b] > v->cap)
+            return fail(MAD_EINVAL, "kv: len[%d]=%d outside [0, cap=%d]", b, v->len[b], v->cap);
+    return MAD_OK;
+}
+
+// Validate rows of heads of n_cap rows each; `written`: they must not overlap each other.
+int check_rows(const mad_rows *r, const char *name, int B, int n_cap, int heads, int d, int dtype, bool written, mad::RowsArg *a) {
+    if (!r->p) return fail(MAD_EINVAL, "null %s", name);
+    if (!aligned16(r->p)) return fail(MAD_EINVAL, "%s not 16-byte aligned", name);
+    const int vec = 16 / elem_size(dtype);
+    const int64_t width = (int64_t)heads * d, most = (int64_t)1 << 40;
+    const int64_t row = n_cap > 1 ? r->row_stride : width, seq = B > 1 ? r->seq_stride : 0;
+    if (row % vec || seq % vec || row < width || row > most || seq < 0 || seq > most)
+        return fail(MAD_EINVAL, "%s: bad strides (seq %lld, row %lld) for %d heads of %d", name, (long long)r->seq_stride,
+                    (long long)r->row_stride, heads, d);
+    // sequence after sequence, or row after row with the sequences inside
+    if (written && B > 1 && seq < (n_cap - 1) * row + width && (seq < width || (n_cap > 1 && row < (B - 1) * seq + width)))
+        return fail(MAD_EINVAL, "%s: strides (seq %lld, row %lld) make rows overlap", name, (long long)r->seq_stride, (long long)r->row_stride);
+    a->p = r->p;
+    a->seq = seq;
+    a->row = row;
+    return MAD_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -133,6 +180,9 @@ size_t mad_workspace_bytes(int op, int B, int Hq, int Hkv, int d, int T, int max
         case MAD_OP_SAMPLE:   // B, T, max_keys = V
             if (B < 1 || B > MAD_MAX_BATCH || T < 1 || T > 64 || max_keys < 1 || max_keys > mad::kSampleMaxV) return 0;
             return mad::sample_ws_bytes(B, T, max_keys);
+        case MAD_OP_LOGPROBS:   // B, T, max_keys = V
+            if (B < 1 || B > MAD_MAX_BATCH || T < 1 || (int64_t)B * T > mad::kLogprobMaxRows || max_keys < 1 || max_keys > mad::kLogprobMaxV) return 0;
+            return mad::logprobs_ws_bytes(B * T, max_keys);
         case MAD_OP_ACCEPT:   // B, T, max_keys = V
             if (B < 1 || B > MAD_MAX_BATCH || T < 1 || T > mad::kAcceptMaxT || max_keys < 1) return 0;
             return mad::accept_ws_bytes(B, T, max_keys);
@@ -582,6 +632,151 @@ int mad_verify_attn_kv8(const void *q, int B, int T, int Hq, int Hkv, int d, int
     return hip_status(mad::launch_stream8(a, dtype, d, (hipStream_t)stream), "8-bit verify launch");
 }
 
+int mad_qk_norm_rope(const mad_rows *q, const mad_rows *k, const mad_rows *q_out, const mad_rows *k_out, const void *q_gamma,
+                     const void *k_gamma, float eps, double rope_base, const int32_t *start, const int32_t *pos,
+                     const int32_t *n, int B, int n_cap, int Hq, int Hkv, int d, int dtype, void *stream) {
+    if (B < 1 || B > MAD_MAX_BATCH) return fail(MAD_EINVAL, "B=%d outside [1, %d]", B, MAD_MAX_BATCH);
+    if (n_cap < 1) return fail(MAD_EINVAL, "n_cap=%d", n_cap);
+    if (dtype != MAD_F32 && dtype != MAD_BF16) return fail(MAD_ENOTSUP, "dtype %d not supported", dtype);
+    if (d != 64 && d != 128) return fail(MAD_ENOTSUP, "head_dim %d not supported (64 or 128)", d);
+    if (!q && !k) return fail(MAD_EINVAL, "neither q nor k is given");
+    if ((!q) != (!q_out) || (!k) != (!k_out)) return fail(MAD_EINVAL, "q goes with q_out, k with k_out");
+    if ((q && (Hq < 1 || Hq > 4096)) || (k && (Hkv < 1 || Hkv > 4096))) return fail(MAD_EINVAL, "Hq=%d, Hkv=%d outside [1, 4096]", Hq, Hkv);
+    if (!aligned16(q_gamma) || !aligned16(k_gamma)) return fail(MAD_EINVAL, "q_gamma/k_gamma not 16-byte aligned");
+    if (!(eps >= 0.f) || isinf(eps)) return fail(MAD_EINVAL, "eps must be finite and >= 0");
+    const bool rotate = rope_base != 0.0;
+    if (rotate && (!(rope_base > 1.0) || isinf(rope_base))) return fail(MAD_EINVAL, "rope_base=%g must be 0 or finite and > 1", rope_base);
+    if (rotate && (!start) == (!pos)) return fail(MAD_EINVAL, "one of start and pos has to be given");
+    if ((uintptr_t)pos & 3) return fail(MAD_EINVAL, "pos not 4-byte aligned");
+    mad::NormRopeArgs a;
+    memset(&a, 0, sizeof(a));
+    int rc;
+    if (q && ((rc = check_rows(q, "q", B, n_cap, Hq, d, dtype, false, &a.q)) || (rc = check_rows(q_out, "q_out", B, n_cap, Hq, d, dtype, true, &a.q_out))))
+        return rc;
+    if (k && ((rc = check_rows(k, "k", B, n_cap, Hkv, d, dtype, false, &a.k)) || (rc = check_rows(k_out, "k_out", B, n_cap, Hkv, d, dtype, true, &a.k_out))))
+        return rc;
+    int64_t tokens = 0;
+    for (int b = 0; b < B; ++b) {
+        const int nb = n ? n[b] : n_cap;
+        if (nb < 0 || nb > n_cap) return fail(MAD_EINVAL, "n[%d]=%d outside [0, n_cap=%d]", b, nb, n_cap);
+        if (rotate && start && (int64_t)start[b] + nb - 1 > INT32_MAX) return fail(MAD_EINVAL, "start[%d]=%d + n=%d beyond 32 bits", b, start[b], nb);
+        a.row[b].x = (int)tokens;
+        a.row[b].y = start ? start[b] : 0;
+        tokens += nb;
+        if (tokens > 1 << 24) return fail(MAD_EINVAL, "%lld rows: more than a call takes", (long long)tokens);
+    }
+    for (int b = B; b < MAD_MAX_BATCH; ++b) a.row[b].x = (int)tokens;
+    if (tokens == 0) return ok();
+    a.q_gamma = q_gamma;
+    a.k_gamma = k_gamma;
+    a.pos = pos;
+    a.eps = eps;
+    a.rotate = rotate ? 1 : 0;
+    a.n_cap = n_cap;
+    a.Hq = q ? Hq : 0;
+    a.Hkv = k ? Hkv : 0;
+    a.tokens = (int)tokens;
+    for (int j = 0; rotate && j < d / 2; ++j) a.theta[j] = pow(rope_base, -2.0 * j / d);
+    return hip_status(mad::launch_norm_rope(a, dtype, d, (hipStream_t)stream), "norm and rotation launch");
+}
+
+int mad_kv4_append(const mad_rows *k_new, const mad_rows *v_new, const mad_rows *k_held, const mad_rows *v_held,
+                   const int32_t *n, int B, int n_cap, int Hkv, int d, int dtype, const mad_kv4_view *kv, void *stream) {
+    if (B < 1 || B > MAD_MAX_BATCH) return fail(MAD_EINVAL, "B=%d outside [1, %d]", B, MAD_MAX_BATCH);
+    if (n_cap < 1) return fail(MAD_EINVAL, "n_cap=%d", n_cap);
+    if (Hkv < 1 || Hkv > 4096) return fail(MAD_EINVAL, "Hkv=%d outside [1, 4096]", Hkv);
+    if (dtype != MAD_F32 && dtype != MAD_BF16) return fail(MAD_ENOTSUP, "dtype %d not supported", dtype);
+    if (d != 64 && d != 128) return fail(MAD_ENOTSUP, "head_dim %d not supported (64 or 128)", d);
+    if (!k_new || !v_new) return fail(MAD_EINVAL, "null k_new or v_new");
+    if ((!k_held) != (!v_held)) return fail(MAD_EINVAL, "k_held and v_held must both be given or both null");
+    mad::Kv4AppendArgs a;
+    memset(&a, 0, sizeof(a));
+    int rc;
+    if ((rc = check_rows(k_new, "k_new", B, n_cap, Hkv, d, dtype, false, &a.k_new)) ||
+        (rc = check_rows(v_new, "v_new", B, n_cap, Hkv, d, dtype, false, &a.v_new)))
+        return rc;
+    if (k_held && ((rc = check_rows(k_held, "k_held", B, n_cap, Hkv, d, dtype, true, &a.k_held)) ||
+                   (rc = check_rows(v_held, "v_held", B, n_cap, Hkv, d, dtype, true, &a.v_held))))
+        return rc;
+    if ((rc = check_view4(kv, B, Hkv, d))) return rc;
+    if (B > 1 && (kv->seq_stride == 0 || kv->scale_seq_stride == 0))
+        return fail(MAD_EINVAL, "kv: sequences that share one buffer cannot all append to it");
+    // a thread takes four pieces where that leaves enough workgroups
+    int64_t rows = 0;
+    for (int b = 0; b < B; ++b) {
+        const int nb = n ? n[b] : n_cap, len = kv->len[b];
+        if (nb < 0 || nb > n_cap) return fail(MAD_EINVAL, "n[%d]=%d outside [0, n_cap=%d]", b, nb, n_cap);
+        if ((int64_t)len + nb > kv->cap)
+            return fail(MAD_EINVAL, "kv: len[%d]=%d + n=%d exceeds cap %d", b, len, nb, kv->cap);
+        rows += nb;
+    }
+    a.pieces = rows / mad::kv4_tile(d, 4) * 2 * Hkv >= mad::kKv4WideTiles ? 4 : 1;
+    const int tile = mad::kv4_tile(d, a.pieces);
+    int64_t tiles = 0;
+    for (int b = 0; b < B; ++b) {
+        a.row[b].x = (int)tiles;
+        a.row[b].y = kv->len[b];
+        a.row[b].z = n ? n[b] : n_cap;
+        tiles += ((int64_t)a.row[b].z + tile - 1) / tile;
+        if (tiles * 2 * Hkv > 0xffffff)   // (a launch has fewer than 2^32 threads, 256 a tile)
+            return fail(MAD_EINVAL, "%lld rows of %d KV heads: more than a call takes", (long long)rows, Hkv);
+    }
+    for (int b = B; b < MAD_MAX_BATCH; ++b) a.row[b].x = (int)tiles;
+    if (tiles == 0) return ok();
+    a.k = kv->k;
+    a.v = kv->v;
+    a.k_scale = kv->k_scale;
+    a.v_scale = kv->v_scale;
+    a.seq = kv->seq_stride;
+    a.head = kv->head_stride;
+    a.s_seq = kv->scale_seq_stride;
+    a.s_head = kv->scale_head_stride;
+    a.Hkv = Hkv;
+    a.tiles = (int)tiles;
+    return hip_status(mad::launch_kv4_append(a, dtype, d, (hipStream_t)stream), "kv4 append launch");
+}
+
+int mad_verify_attn_kv4(const void *q, int B, int T, int Hq, int Hkv, int d, int dtype, float scale,
+                        const mad_kv4_view *kv, void *out, float *lse, void *ws, size_t ws_bytes, void *stream) {
+    int rc = check_heads(B, Hq, Hkv, d, dtype);
+    if (rc) return rc;
+    const int G = Hq / Hkv;
+    if (T < 1 || T * G > MAD_MAX_VERIFY_ROWS)
+        return fail(MAD_EINVAL, "T=%d: T*G=%d must be in [1, %d]", T, T * G, MAD_MAX_VERIFY_ROWS);
+    if (!q || !out) return fail(MAD_EINVAL, "null q or out");
+    if (!aligned16(q) || !aligned16(out)) return fail(MAD_EINVAL, "q/out not 16-byte aligned");
+    if ((uintptr_t)lse & 3) return fail(MAD_EINVAL, "lse not 4-byte aligned");
+    if (!(scale > 0.f) || isinf(scale)) return fail(MAD_EINVAL, "scale must be positive and finite");
+    if ((rc = check_view4(kv, B, Hkv, d))) return rc;
+    const size_t need = mad::verify_ws_bytes(B, Hq, Hkv, d, T);
+    if (!ws) return fail(MAD_EWS, "workspace required (%zu bytes)", need);
+    if (ws_bytes < need) return fail(MAD_EWS, "workspace %zu bytes < %zu", ws_bytes, need);
+    if (!aligned16(ws)) return fail(MAD_EINVAL, "workspace not 16-byte aligned");
+    mad::Stream4Args a;
+    memset(&a, 0, sizeof(a));
+    a.q = q;
+    a.k = kv->k;
+    a.v = kv->v;
+    a.k_scale = kv->k_scale;
+    a.v_scale = kv->v_scale;
+    a.kind = mad::kStream4;
+    a.out = out;
+    a.lse = lse;
+    a.seq = kv->seq_stride;
+    a.head = kv->head_stride;
+    a.s_seq = kv->scale_seq_stride;
+    a.s_head = kv->scale_head_stride;
+    a.part = (float *)((char *)ws + mad::kCounterRegionBytes);
+    a.counters = (unsigned *)ws;
+    a.scale_log2 = scale * 1.4426950408889634f;
+    a.cap = kv->cap;
+    a.Hq = Hq;
+    a.G = G;
+    a.T = T;
+    mad::plan_stream(a, B, Hkv, d, kv->len);
+    return hip_status(mad::launch_stream4(a, dtype, d, (hipStream_t)stream), "4-bit verify launch");
+}
+
 int mad_memory_prefill_attn(const void *q_raw, const void *q_slot, int B, int Hq, int Hkv, int d, int dtype,
                             float scale, const int32_t *P, int q_cap, int slot_cap, int S, int W, int r, int u,
                             const mad_kv_view *mem, const mad_kv_view *raw, void *out_raw, float *lse_raw,
@@ -806,6 +1001,57 @@ int mad_sample(const void *logits, int dtype, const float *u, const double *temp
     a.V = V;
     a.n_chunks = (V + mad::kSampleChunk - 1) / mad::kSampleChunk;
     return hip_status(mad::launch_sample(a, dtype, (hipStream_t)stream), "sample launch");
+}
+
+int mad_token_logprobs(const void *logits, int dtype, int64_t seq_stride, int64_t row_stride, const int32_t *tok,
+                       const double *temperature, int B, int T, int V, int top_n, float *logp, int32_t *rank,
+                       float *entropy, int32_t *top_tok, float *top_logp, void *ws, size_t ws_bytes, void *stream) {
+    if (B < 1 || B > MAD_MAX_BATCH) return fail(MAD_EINVAL, "B=%d outside [1, %d]", B, MAD_MAX_BATCH);
+    if (T < 1 || (int64_t)B * T > mad::kLogprobMaxRows) return fail(MAD_EINVAL, "T=%d: B*T outside [1, %d]", T, mad::kLogprobMaxRows);
+    if (V < 1 || V > mad::kLogprobMaxV) return fail(MAD_EINVAL, "V=%d outside [1, %d]", V, mad::kLogprobMaxV);
+    if (top_n < 0 || top_n > MAD_MAX_TOP || top_n > V) return fail(MAD_EINVAL, "top_n=%d outside [0, min(V, %d)]", top_n, MAD_MAX_TOP);
+    if (dtype != MAD_F32 && dtype != MAD_BF16) return fail(MAD_ENOTSUP, "dtype %d not supported", dtype);
+    if (!logits) return fail(MAD_EINVAL, "null logits");
+    const size_t esz = dtype == MAD_BF16 ? 2 : 4;
+    if (((uintptr_t)logits & (esz - 1)) ||
+        (((uintptr_t)tok | (uintptr_t)logp | (uintptr_t)rank | (uintptr_t)entropy | (uintptr_t)top_tok | (uintptr_t)top_logp) & 3))
+        return fail(MAD_EINVAL, "logits, tok or an output not aligned to their type");
+    const int64_t seq = B > 1 ? seq_stride : 0, row = T > 1 ? row_stride : 0, most = (int64_t)1 << 40;
+    if (seq < 0 || row < 0 || seq > most || row > most)
+        return fail(MAD_EINVAL, "bad strides (seq %lld, row %lld)", (long long)seq_stride, (long long)row_stride);
+    if (!tok && (logp || rank)) return fail(MAD_EINVAL, "logp and rank need tok");
+    if ((top_n > 0) != (top_tok != nullptr) || (top_n > 0) != (top_logp != nullptr))
+        return fail(MAD_EINVAL, "top_tok and top_logp go with top_n");
+    if (!logp && !rank && !entropy && !top_tok) return fail(MAD_EINVAL, "no output is given");
+    mad::LogprobArgs a;
+    memset(&a, 0, sizeof(a));
+    for (int b = 0; b < B; ++b) {
+        const double t = temperature ? temperature[b] : 1.0;
+        if (!(t > 0.0) || isinf(t)) return fail(MAD_EINVAL, "temperature[%d]=%g must be finite and > 0", b, t);
+        a.c[b] = (float)fmax(fmin(1.4426950408889634 / t, 1e30), 1e-30);   // (0 and inf would make NaN of differences)
+    }
+    const size_t need = mad::logprobs_ws_bytes(B * T, V);
+    if (!ws) return fail(MAD_EWS, "workspace required (%zu bytes)", need);
+    if (ws_bytes < need) return fail(MAD_EWS, "workspace %zu bytes < %zu", ws_bytes, need);
+    if (((uintptr_t)ws & 255u) != 0) return fail(MAD_EINVAL, "workspace not 256-byte aligned");
+    a.logits = logits;
+    a.seq = seq;
+    a.row = row;
+    a.tok = tok;
+    a.logp = logp;
+    a.rank = rank;
+    a.entropy = entropy;
+    a.top_tok = top_tok;
+    a.top_logp = top_logp;
+    a.counters = (unsigned *)ws;
+    a.records = (mad::LogprobRecord *)((char *)ws + mad::kCounterRegionBytes);
+    a.rows = B * T;
+    a.T = T;
+    a.V = V;
+    a.top_n = top_n;
+    a.n_chunks = mad::logprob_chunks(V);
+    a.splits = mad::logprob_splits(a.rows, V);
+    return hip_status(mad::launch_logprobs(a, dtype, (hipStream_t)stream), "logprobs launch");
 }
 
 int mad_accept_stochastic(const float *p, const float *q, const int32_t *draft_tok, const float *u, int B, int T,

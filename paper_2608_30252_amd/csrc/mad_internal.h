@@ -86,8 +86,8 @@ constexpr int kMergeBytes = 128 << 10;      // LDS for the pieces of a unit that
 constexpr int kMergeInLaunch = 48 << 10;    // such pieces where the units are few (plan_stream)
 
 // verify over a cache of K and V rows; over K rows and V^T (one run of cap keys per feature);
-// the draft's decode: memory rows, window ring, new token (T = 1); verify over an 8-bit cache
-enum { kStreamRows = 0, kStreamVT = 1, kStreamDraft = 2, kStream8 = 3 };
+// the draft's decode: memory rows, window ring, new token (T = 1); verify over an 8-bit cache, a 4-bit one
+enum { kStreamRows = 0, kStreamVT = 1, kStreamDraft = 2, kStream8 = 3, kStream4 = 4 };
 
 struct StreamArgs {
     const void *q, *k, *v;    // draft: k and v are the memory rows
@@ -146,6 +146,47 @@ struct Stream8Args : StreamArgs {
     int log2_block;
 };
 hipError_t launch_stream8(const Stream8Args &a, int dtype, int d, hipStream_t st);
+
+// ------------------------------------------------------------------ rope ----
+struct RowsArg {
+    void *p;             // null: absent
+    int64_t seq, row;    // element strides
+};
+// queries' and keys' norms and rotation (rope.hip)
+constexpr int kRopeWholeTokens = 2048;   // calls of this many tokens: a wave takes all heads of its token
+struct NormRopeArgs {
+    RowsArg q, k, q_out, k_out;
+    const void *q_gamma, *k_gamma;
+    const int32_t *pos;      // device [B][n_cap] or null: the rows' start
+    float eps;
+    int rotate, n_cap, Hq, Hkv;
+    int tokens;              // new rows over all sequences
+    int items, groups, rounds;   // (set by launch_norm_rope) waves' items, to a token; rounds of heads to an item
+    double theta[64];
+    int4 row[kMaxB];         // tokens before row b, first position; past the last row: the end
+};
+hipError_t launch_norm_rope(NormRopeArgs &a, int dtype, int d, hipStream_t st);
+
+// ------------------------------------------------------------------- kv4 ----
+// new rows into the 4-bit cache (kv4.hip)
+constexpr int kKv4WideTiles = 1024;   // calls of this many workgroups with four pieces to a thread take them
+__host__ __device__ constexpr int kv4_tile(int d, int pieces) { return 2048 / d * pieces; }   // rows of a workgroup
+struct Kv4AppendArgs {
+    RowsArg k_new, v_new, k_held, v_held;
+    void *k, *v, *k_scale, *v_scale;
+    int64_t seq, head, s_seq, s_head;
+    int Hkv, pieces;         // pieces of 8 features per thread: 1 or 4
+    int tiles;               // of one head over all rows
+    int4 row[kMaxB];         // tiles before row b, length, new rows; past the last row: the end
+};
+hipError_t launch_kv4_append(const Kv4AppendArgs &a, int dtype, int d, hipStream_t st);
+
+// attention over the 4-bit cache (stream4.hip)
+struct Stream4Args : StreamArgs {
+    const void *k_scale, *v_scale;
+    int64_t s_seq, s_head;
+};
+hipError_t launch_stream4(const Stream4Args &a, int dtype, int d, hipStream_t st);
 
 // ----------------------------------------------------------------- layer ----
 constexpr int kMaxLinRows = MAD_MAX_LAYER_ROWS;
@@ -248,6 +289,38 @@ static_assert(kMaxB <= 256, "sequence numbers in a byte");
 static_assert(kMaxB * 64 <= kCounterLines, "a counter line per row, T <= 64");
 size_t sample_ws_bytes(int B, int T, int V);
 hipError_t launch_sample(const SampleArgs &a, int dtype, hipStream_t st);
+
+// -------------------------------------------------------------- logprobs ----
+constexpr int kLogprobChunk = 8192;                            // entries of a workgroup's step
+constexpr int kLogprobSplits = 16;                             // workgroups to a row, at most
+constexpr int kLogprobMaxV = 1 << 20, kLogprobMaxRows = 1 << 22;
+constexpr int kLogprobWgs = 2048;                              // workgroups that a call of few rows is split into, about
+struct LogprobRecord {   // one workgroup's part of a row
+    double s, u;
+    float m;
+    int above, inf, best_n;
+    uint64_t best[MAD_MAX_TOP];
+};
+struct LogprobArgs {
+    const void *logits;
+    int64_t seq, row;        // element strides
+    const int32_t *tok;      // [B][T] or null
+    float *logp, *entropy, *top_logp;
+    int32_t *rank, *top_tok;
+    LogprobRecord *records;  // [rows][splits]
+    unsigned *counters;      // line r: arrivals of row r's workgroups
+    int rows, T, V, top_n, n_chunks, splits;
+    float c[kMaxB];          // log2 e / temperature
+};
+// chunks of a row (a row may begin up to 7 entries into its first 16 bytes)
+inline int logprob_chunks(int V) { return (V + 7 + kLogprobChunk - 1) / kLogprobChunk; }
+inline int logprob_splits(int rows, int V) {
+    if (rows > kCounterLines / 4) return 1;
+    const int want = kLogprobWgs / rows, most = logprob_chunks(V) < kLogprobSplits ? logprob_chunks(V) : kLogprobSplits;
+    return want < 1 ? 1 : want < most ? want : most;
+}
+size_t logprobs_ws_bytes(int rows, int V);
+hipError_t launch_logprobs(const LogprobArgs &a, int dtype, hipStream_t st);
 
 // ws layout helpers: counters first (256-byte aligned), then partials.
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
