@@ -298,7 +298,8 @@ constexpr int kLogprobWgs = 2048;                              // workgroups tha
 struct LogprobRecord {   // one workgroup's part of a row
     double s, u;
     float m;
-    int above, inf, best_n;
+    int above;
+    int64_t inf;
     uint64_t best[MAD_MAX_TOP];
 };
 struct LogprobArgs {

@@ -127,6 +127,17 @@ def test_temperatures(temperature):
     _check(_logits((1, 3, 50257), "bf16", 9), _tok(1, 3, 50257), 8, temperature)
 
 
+@pytest.mark.parametrize("scale", [1.0, 2.0 ** 20, 2.0 ** 26, 2.0 ** 30, 1e36])
+def test_differences_of_far_logits_are_exact(scale):
+    """Values a few units in the last place apart, around where the sums' reference changes its form and far beyond."""
+    g = torch.Generator().manual_seed(14)
+    near = torch.randint(0, 12, (1, 2, 20001), generator=g).float()
+    x = scale * (0.6931471805599453 * (1 + near * 2.0 ** -23))
+    x[0, 1] *= -1
+    for temperature in (1.0, scale * 2.0 ** -23, scale * 2.0 ** -21):
+        _check(x, _tok(1, 2, 20001), 30, temperature)
+
+
 def test_sharp_and_shifted_rows():
     x = _logits((1, 4, 50257), "f32", 10)
     x[0, 0, 77] += 60.0                                     # a certain token
