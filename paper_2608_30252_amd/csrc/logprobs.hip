@@ -1,14 +1,15 @@
 // logprobs.hip -- log probabilities of given tokens, ranks, entropies and the
 // most probable alternatives, from the logits in one read.
 //
-// Mathematics, for a row's logits x, c = log2 e / temperature, M near max x c:
+// Mathematics, for a row's logits x, c = log2 e / temperature, M not far from max x c:
 //   d_v = x_v c - M,  e_v = 2^d_v,  s = sum e,  u = sum e d
 //   log p_v = ln 2 * (d_v - log2 s);   entropy = ln 2 * (log2 s - u / s)
 //   rank = entries above the token's logit, and equal ones before it.
-// M is max x times c as fp32 rounds it, so that d is one fused operation with one
-// rounding whatever the logits' offset.  A thread keeps M, s and u of what it has
-// seen, raises M at most once per step of 16 entries, and sums within a step in
-// fp32, over steps and threads in fp64.
+// M is some entry times c as fp32 rounds it, so that d is one fused operation with
+// one rounding whatever the logits' offset.  A thread keeps M, s and u of what it
+// has seen, raises M where a step of 32 entries exceeds it by more than 8 (log2
+// units: few steps do), and sums within a step in fp32, over steps and threads in
+// fp64.
 //
 // The first top_n of the order: each wave keeps its largest 64 keys (value, then
 // index) sorted, one to a lane.  An entry above the wave's top_n-th, and above what
@@ -16,10 +17,10 @@
 // and a shift by one lane; few entries of a row come that far.  Before there are
 // top_n: the top_n-th largest of 64 maxima of disjoint groups (lane l of every
 // wave), which top_n entries at least reach.  The same bound, of the lanes' maxima,
-// thins a step in which many entries are above the list (a rising row).  At the end an entry's place
-// among the waves' lists is counted by binary searches.
+// thins a step in which many entries are above the list (a rising row).  At the end the places
+// of what the waves have above the bound are counted.
 //
-// Work: a workgroup takes a run of a row's chunks of 8192, its waves 1024 of each
+// Work: a workgroup takes a run of a row's chunks of 8192, its waves 2048 of each
 // and no barrier between the first chunk and the last; with few rows, more
 // workgroups to a row, whose results the last of them to arrive joins.
 #include "mad_device.h"
@@ -29,16 +30,18 @@ namespace mad {
 
 namespace {
 
-constexpr int kWg = 512, kEntries = 16;   // threads, entries of a thread and step
+constexpr int kWg = 256, kEntries = 32;   // threads, entries of a thread and step
+constexpr int kWaves = kWg / 64;
 static_assert(kWg * kEntries == kLogprobChunk, "");
-constexpr int kMany = 64;                 // entries of a step above the list that are thinned first
+constexpr int kMany = 24;                 // lanes with entries above the list from which on a step is thinned first
+constexpr float kLag = 8.f;               // M is raised where a step's largest x c is above it by more (log2 units)
 constexpr float kNear = 0x1p26f;          // |m| c below which M is m c as rounded
 
-// Sums relative to M, which m alone tells: below kNear m c as fp32 rounds it (within 2 of m c: d <= 2), else m c exactly, formed
+// Sums relative to M, which m alone tells: below kNear m c as fp32 rounds it (within 2 of it), else m c exactly, formed
 // in differences only.
 struct Stats {
     double s, u;
-    float m;        // the largest entry
+    float m;        // -inf: nothing yet
 };
 // M of a less M of b (a <= b)
 __device__ __forceinline__ float lower(float a, float b, float c) {
@@ -48,6 +51,11 @@ __device__ __forceinline__ float lower(float a, float b, float c) {
     return fabsf(mb) < kNear ? ma - mb : fmaf(-b, c, ma);
 }
 
+// the next number below (-inf: itself)
+__device__ __forceinline__ float next_below(float x) {
+    const uint32_t u = __float_as_uint(x);
+    return x == 0.f ? __uint_as_float(0x80000001u) : x == -INFINITY ? x : __uint_as_float(x > 0.f ? u - 1 : u + 1);
+}
 __device__ __forceinline__ uint32_t order_of(float x) { return (uint32_t)(argmax_key(x, 0) >> 32); }
 __device__ __forceinline__ float value_of(uint64_t key) {
     const uint32_t o = (uint32_t)(key >> 32);
@@ -59,15 +67,22 @@ __device__ __forceinline__ uint64_t read_lane_u64(uint64_t v, int l) {
 }
 __device__ __forceinline__ uint64_t max_u64(uint64_t a, uint64_t b) { return a > b ? a : b; }
 
-// the n-th largest of the lanes' values
-__device__ __forceinline__ uint32_t nth_of_lanes(uint32_t g, int n) {
+// A value that n of the lanes' values reach: the n-th largest of the maxima of 16, 32 or 64 groups of lanes, at least
+// four for each that is looked for where there are so many (fewer groups are a shorter chain, and a looser bound).
+__device__ __forceinline__ uint32_t reached_by(uint32_t g, int n) {
+    if (n <= 16) g = max(g, (uint32_t)__shfl_xor((int)g, 32));
+    if (n <= 4) g = max(g, (uint32_t)__shfl_xor((int)g, 16));
+    const int groups = n <= 4 ? 16 : n <= 16 ? 32 : 64;
     int above = 0;
-    #pragma unroll 8
-    for (int l = 0; l < 64; ++l) {
-        const uint32_t o = __builtin_amdgcn_readlane(g, l);
-        above += o > g || (o == g && l < (int)(threadIdx.x & 63)) ? 1 : 0;
-    }
-    return __builtin_amdgcn_readlane(g, __builtin_ctzll(__ballot(above == n - 1)));
+    for (int l = 0; l < groups; l += 16)
+        #pragma unroll
+        for (int k = 0; k < 16; ++k) above += (uint32_t)__builtin_amdgcn_readlane((int)g, l + k) > g ? 1 : 0;
+    // the least value with fewer than n above it
+    uint32_t least = above < n ? g : 0xffffffffu;
+    #pragma unroll
+    for (int k = 1; k < 16; k <<= 1) least = min(least, (uint32_t)__shfl_xor((int)least, k));
+    least = min(least, (uint32_t)__shfl_xor((int)least, 16));
+    return min(least, (uint32_t)__shfl_xor((int)least, 32));
 }
 
 // the lanes' sums together, in every lane
@@ -81,44 +96,42 @@ __device__ __forceinline__ Stats wave_join(Stats a, float c) {
     return a;
 }
 
-// the place of x in a list of n keys, the largest first: how many are above
-__device__ __forceinline__ int place(const uint64_t *list, int n, uint64_t x) {
-    int lo = 0, hi = n;
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        const bool up = list[mid] > x;
-        lo = up ? mid + 1 : lo;
-        hi = up ? hi : mid;
-    }
-    return lo;
-}
-
 struct Shared {
-    uint64_t list[kLogprobSplits][MAD_MAX_TOP], best[MAD_MAX_TOP];
+    uint64_t list[kLogprobSplits * MAD_MAX_TOP], best[MAD_MAX_TOP];
     uint64_t bound;
-    uint32_t group[8][64];
-    double s[8], u[8];
-    float m[8];
-    int above[8], inf[8];
+    int count;
+    uint32_t group[kWaves][64];
+    double s[kWaves], u[kWaves];
+    float m[kWaves];
+    int above[kWaves], inf[kWaves];
     int last;
 };
-static_assert(kLogprobSplits >= 8, "a list for each wave");
+static_assert(kLogprobSplits >= kWaves, "a list for each wave");
 
-// The first n of the order among `lists` lists of up to n sorted keys (0: none) into best.
-__device__ __forceinline__ void join_lists(Shared &sh, int lists, int n) {
-    for (int i = threadIdx.x; i < lists * n; i += kWg) {
-        const int l = i / n, k = i - l * n;
-        const uint64_t x = sh.list[l][k];
-        int at = k;
-        for (int o = 0; o < lists; ++o) at += o == l ? 0 : place(sh.list[o], n, x);
-        if (x != 0 && at < n) sh.best[at] = x;   // (keys differ: their index is in them)
+// The first n of the order among list[0 .. count) into best (behind a barrier).  An entry's place is the number of keys
+// above it (keys differ: their index is in them).
+__device__ __forceinline__ void first_of_list(Shared &sh, int count, int n) {
+    for (int i = threadIdx.x; i < count; i += kWg) {
+        const uint64_t x = sh.list[i];
+        int at = 0;
+        #pragma unroll 4
+        for (int k = 0; k < count; ++k) at += sh.list[k] > x ? 1 : 0;
+        if (at < n) sh.best[at] = x;
     }
+}
+// a lane's key goes into the list if `in`
+__device__ __forceinline__ void to_list(Shared &sh, uint64_t key, bool in) {
+    const uint64_t lanes = __ballot(in);
+    int at = 0;
+    if ((threadIdx.x & 63) == 0) at = atomicAdd(&sh.count, __popcll(lanes));
+    at = __builtin_amdgcn_readfirstlane(at) + __popcll(lanes & ((1ull << (threadIdx.x & 63)) - 1));
+    if (in) sh.list[at] = key;
 }
 
 }  // namespace
 
 template <typename T, bool TOP>
-__global__ __launch_bounds__(kWg, 6) void logprobs_kernel(const LogprobArgs a) {
+__global__ __launch_bounds__(kWg, 4) void logprobs_kernel(const LogprobArgs a) {
     constexpr int VEC = Elem<T>::VEC, NV = kEntries / VEC;
     __shared__ Shared sh;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -131,21 +144,30 @@ __global__ __launch_bounds__(kWg, 6) void logprobs_kernel(const LogprobArgs a) {
     const float c = a.c[b];
     const int chunk0 = (int)((int64_t)a.n_chunks * split / a.splits), chunk1 = (int)((int64_t)a.n_chunks * (split + 1) / a.splits);
 
+    // 16 bytes a lane and piece; pieces past the run's or the row's last: the last one again
     uint4 raw[NV];
+    const uint32_t end = (uint32_t)min(vecs, chunk1 * NV * kWg) - 1;
     auto load = [&](int chunk) {
         #pragma unroll
-        for (int j = 0; j < NV; ++j) raw[j] = base[min((chunk * NV + j) * kWg + tid, vecs - 1)];
+        for (int j = 0; j < NV; ++j) {
+            const uint32_t at = min((uint32_t)((chunk * NV + j) * kWg + tid), end) * 16u;
+            raw[j] = *reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(base) + at);
+        }
     };
     load(chunk0);
     const int tok = a.tok ? a.tok[row] : -1;
     const bool has = tok >= 0 && tok < V;
     const float xt = has ? Elem<T>::load1(x0 + tok) : INFINITY;
+    const float below = next_below(xt);
 
     Stats st = {0.0, 0.0, -INFINITY};
     int above = 0, inf = 0;      // (of the wave)
     uint64_t key = 0;            // lane i: the wave's i-th largest
     uint64_t bound = 0;          // only keys above it count
-    if (TOP && tid == 0) sh.bound = 0;
+    if (TOP && tid == 0) {
+        sh.bound = 0;
+        sh.count = 0;
+    }
 
     for (int chunk = chunk0; chunk < chunk1; ++chunk) {
         float x[kEntries];
@@ -156,64 +178,87 @@ __global__ __launch_bounds__(kWg, 6) void logprobs_kernel(const LogprobArgs a) {
             #pragma unroll
             for (int e = 0; e < VEC; ++e) x[j * VEC + e] = f[e];
         }
-        if (chunk + 1 < chunk1) load(chunk + 1);
+        load(chunk + 1);
         const int first = chunk * kLogprobChunk - skew;   // the chunk's first entry
         const bool edge = first < 0 || first + kLogprobChunk > V;
         auto index = [&](int i) { return first + ((i / VEC) * kWg + tid) * VEC + i % VEC; };
-        auto inside = [&](int i) { return !edge || (uint32_t)index(i) < (uint32_t)V; };
-        if (edge) {
+        if (edge) {   // what is not the row's: -inf
             #pragma unroll
-            for (int i = 0; i < kEntries; ++i) x[i] = inside(i) ? x[i] : -INFINITY;
+            for (int i = 0; i < kEntries; ++i) x[i] = (uint32_t)index(i) < (uint32_t)V ? x[i] : -INFINITY;
         }
-        float m = x[0];
+        float mj[NV], m = -INFINITY;   // the pieces' largest
         #pragma unroll
-        for (int i = 1; i < kEntries; ++i) m = fmaxf(m, x[i]);
-
-        const float mn = fmaxf(st.m, m), M = mn * c;
-        float s = 0.f, u = 0.f;
-        if (fabsf(M) < kNear) {
+        for (int j = 0; j < NV; ++j) {
+            mj[j] = x[j * VEC];
             #pragma unroll
-            for (int i = 0; i < kEntries; ++i) {
+            for (int e = 1; e < VEC; ++e) mj[j] = fmaxf(mj[j], x[j * VEC + e]);
+            m = fmaxf(m, mj[j]);
+        }
+
+        if (__any(!((m - st.m) * c <= kLag))) {   // (nothing yet: inf or NaN)
+            const float mn = (m - st.m) * c > kLag && m < INFINITY ? m : st.m;
+            if (st.m < mn) {
+                const float d = fmaxf(lower(st.m, mn, c), -3000.f), f = __builtin_amdgcn_exp2f(d);
+                st.u = (double)f * (st.u + (double)d * st.s);
+                st.s *= (double)f;
+                st.m = mn;
+            }
+        }
+        const float M = st.m * c;
+        float s = 0.f, u = 0.f;
+        if (fabsf(M) < kNear && m < INFINITY) {
+            float s1 = 0.f, u1 = 0.f;   // every other entry's
+            #pragma unroll
+            for (int i = 0; i < kEntries; i += 2) {
                 const float d = fmaf(x[i], c, -M), e = __builtin_amdgcn_exp2f(d);
+                const float d1 = fmaf(x[i + 1], c, -M), e1 = __builtin_amdgcn_exp2f(d1);
                 s += e;
                 u = fmaf(e, d, u);
+                s1 += e1;
+                u1 = fmaf(e1, d1, u1);
             }
+            s += s1;
+            u += u1;
             if (!(u == u)) {   // an e of 0 with a d of -inf, or a NaN (which s has too)
                 u = 0.f;
+                const float again = __int_as_float(here(__float_as_int(M)));   // (no registers held for this)
                 #pragma unroll
                 for (int i = 0; i < kEntries; ++i) {
-                    const float d = fmaf(x[i], c, -M);
-                    u = fmaf(__builtin_amdgcn_exp2f(d), fmaxf(d, -200.f), u);
+                    const float d = fmaf(x[i], c, -again), e = __builtin_amdgcn_exp2f(d);
+                    u = fmaf(e, fmaxf(d, -200.f), u);
                 }
             }
-        } else if (fabsf(mn) < INFINITY) {
+        } else if (fabsf(st.m) < INFINITY && m < INFINITY) {
             #pragma unroll
             for (int i = 0; i < kEntries; ++i) {
-                const float d = (x[i] - mn) * c, e = __builtin_amdgcn_exp2f(d);
+                const float d = (x[i] - st.m) * c, e = __builtin_amdgcn_exp2f(d);
                 s += e;
                 u = fmaf(e, fmaxf(d, -200.f), u);
             }
         }
-        if (__any(!(fabsf(mn) < INFINITY))) {   // nothing but -inf, a +inf, or NaN alone
+        st.s += (double)s;
+        st.u += (double)u;
+        if (__any(!(fabsf(m) < INFINITY))) {   // a +inf, nothing but -inf, or NaN alone
             #pragma unroll
             for (int i = 0; i < kEntries; ++i) {
                 inf += __popcll(__ballot(x[i] == INFINITY));
-                s = x[i] != x[i] ? __builtin_nanf("") : s;
+                if (x[i] != x[i]) st.s = __builtin_nan("");
             }
         }
-        if (st.m < mn && mn < INFINITY) {
-            const float d = fmaxf(lower(st.m, mn, c), -3000.f), f = __builtin_amdgcn_exp2f(d);
-            st.u = (double)f * (st.u + (double)d * st.s);
-            st.s *= (double)f;
-            st.m = mn;
-        }
-        st.s += (double)s;
-        st.u += (double)u;
 
         if (has && __any(m >= xt)) {
+            // above the token's logit; in pieces before the token's, equal to it too: above the next number below
             #pragma unroll
-            for (int i = 0; i < kEntries; ++i)
-                above += __popcll(__ballot(x[i] > xt || (x[i] == xt && index(i) < tok && inside(i))));
+            for (int j = 0; j < NV; ++j) {
+                const float y = index(j * VEC) + VEC <= tok ? below : xt;
+                #pragma unroll
+                for (int e = 0; e < VEC; ++e) above += __popcll(__ballot(x[j * VEC + e] > y));
+            }
+            if (xt == -INFINITY) {   // (nothing is below)
+                #pragma unroll
+                for (int i = 0; i < kEntries; ++i)
+                    above += __popcll(__ballot(x[i] == xt && index(i) >= 0 && index((i / VEC) * VEC) + VEC <= tok));
+            }
         }
         if constexpr (TOP) {
             if (chunk == chunk0) {
@@ -221,34 +266,36 @@ __global__ __launch_bounds__(kWg, 6) void logprobs_kernel(const LogprobArgs a) {
                 __syncthreads();
                 uint32_t g = 0;
                 #pragma unroll
-                for (int k = 0; k < 8; ++k) g = max(g, sh.group[k][lane]);
-                bound = ((uint64_t)nth_of_lanes(g, n) << 32) - 1;   // (no order is 0)
+                for (int k = 0; k < kWaves; ++k) g = max(g, sh.group[k][lane]);
+                bound = ((uint64_t)reached_by(g, n) << 32) - 1;   // (no order is 0)
             } else {
                 bound = max_u64(bound, *reinterpret_cast<volatile uint64_t *>(&sh.bound));
             }
             // entries of the bound's value and above (some of that value are not above it); a bound among the NaNs' keys: all
             float xb = value_of(bound);
             if (__any(!(m < xb))) {
-                int many = 0;
-                #pragma unroll
-                for (int i = 0; i < kEntries; ++i) many += __popcll(__ballot(!(x[i] < xb)));
-                if (many > kMany && chunk > chunk0) {
-                    const uint32_t o = nth_of_lanes(order_of(m), n);
-                    bound = max_u64(bound, ((uint64_t)o << 32) - 1);
+                if (chunk > chunk0 && __popcll(__ballot(!(m < xb))) > kMany) {
+                    bound = max_u64(bound, ((uint64_t)reached_by(order_of(m), n) << 32) - 1);
                     xb = value_of(bound);
                 }
                 const int at0 = here(tid);   // (the keys are made where they are needed)
                 #pragma unroll
-                for (int i = 0; i < kEntries; ++i) {
-                    if (!__any(!(x[i] < xb))) continue;
-                    const int at_i = first + ((i / VEC) * kWg + at0) * VEC + i % VEC;
-                    const uint64_t mine = !edge || (uint32_t)at_i < (uint32_t)V ? argmax_key(x[i], at_i) : 0;
-                    for (uint64_t left = __ballot(mine > bound); left; left = __ballot(mine > bound) & left & (left - 1)) {
-                        const uint64_t y = read_lane_u64(mine, __builtin_ctzll(left));
-                        const int at = __popcll(__ballot(key > y));
-                        const uint64_t before = dpp_u64<0x138>(key);   // the lane below's (wave_shr 1)
-                        key = lane < at ? key : lane == at ? y : before;
-                        bound = max_u64(bound, read_lane_u64(key, n - 1));
+                for (int j = 0; j < NV; ++j) {
+                    if (!__any(!(mj[j] < xb))) continue;
+                    #pragma unroll
+                    for (int e = 0; e < VEC; ++e) {
+                        const float v = x[j * VEC + e];
+                        if (!__any(!(v < xb))) continue;
+                        const int at_i = first + (j * kWg + at0) * VEC + e;
+                        const uint64_t mine = (uint32_t)at_i < (uint32_t)V ? argmax_key(v, at_i) : 0;
+                        for (uint64_t left = __ballot(mine > bound); left; left = __ballot(mine > bound) & left & (left - 1)) {
+                            const uint64_t y = read_lane_u64(mine, __builtin_ctzll(left));
+                            const int at = __popcll(__ballot(key > y));
+                            const uint64_t before = dpp_u64<0x138>(key);   // the lane below's (wave_shr 1)
+                            key = lane < at ? key : lane == at ? y : before;
+                            bound = max_u64(bound, read_lane_u64(key, n - 1));
+                        }
+                        xb = value_of(bound);
                     }
                 }
                 if (lane == 0 && chunk + 1 < chunk1) atomicMax((unsigned long long *)&sh.bound, (unsigned long long)bound);
@@ -257,8 +304,8 @@ __global__ __launch_bounds__(kWg, 6) void logprobs_kernel(const LogprobArgs a) {
     }
 
     // ---- the workgroup's waves together ----
+    if (TOP && lane == 0) atomicMax((unsigned long long *)&sh.bound, (unsigned long long)bound);
     st = wave_join(st, c);
-    if (TOP) sh.list[wave][lane] = key;
     if (lane == 0) {
         sh.s[wave] = st.s;
         sh.u[wave] = st.u;
@@ -268,17 +315,18 @@ __global__ __launch_bounds__(kWg, 6) void logprobs_kernel(const LogprobArgs a) {
     }
     __syncthreads();
     if (TOP) {
+        to_list(sh, key, key != 0 && key >= sh.bound);   // (a wave's top_n-th, if that is the bound, among them)
         if (tid < n) sh.best[tid] = 0;
         __syncthreads();
-        join_lists(sh, 8, n);
+        first_of_list(sh, sh.count, n);
         __syncthreads();
     }
     const LogprobRecord *rec = a.records + (size_t)row * a.splits;
     if (wave == 0) {
-        st = lane < 8 ? Stats{sh.s[lane & 7], sh.u[lane & 7], sh.m[lane & 7]} : Stats{0.0, 0.0, -INFINITY};
+        st = lane < kWaves ? Stats{sh.s[lane & (kWaves - 1)], sh.u[lane & (kWaves - 1)], sh.m[lane & (kWaves - 1)]} : Stats{0.0, 0.0, -INFINITY};
         st = wave_join(st, c);
         above = inf = 0;
-        for (int k = 0; k < 8; ++k) {
+        for (int k = 0; k < kWaves; ++k) {
             above += sh.above[k];
             inf += sh.inf[k];
         }
@@ -306,10 +354,18 @@ __global__ __launch_bounds__(kWg, 6) void logprobs_kernel(const LogprobArgs a) {
         __syncthreads();
         if (!sh.last) return;
         if (TOP) {
+            // what any workgroup has as its top_n-th is a bound for all
+            uint64_t least = lane < a.splits ? load_agent64(&rec[lane].best[n - 1]) : 0;
+            if (tid == 0) sh.count = 0;
             if (tid < n) sh.best[tid] = 0;
-            for (int i = tid; i < a.splits * n; i += kWg) sh.list[i / n][i % n] = load_agent64(&rec[i / n].best[i % n]);
+            least = wave_fold_u64(least, max_u64);
             __syncthreads();
-            join_lists(sh, a.splits, n);
+            for (int k = wave; k < a.splits; k += kWaves) {
+                const uint64_t x = lane < n ? load_agent64(&rec[k].best[lane]) : 0;
+                to_list(sh, x, x != 0 && x >= least);
+            }
+            __syncthreads();
+            first_of_list(sh, sh.count, n);
             __syncthreads();
         }
         if (wave == 0) {
@@ -337,6 +393,11 @@ __global__ __launch_bounds__(kWg, 6) void logprobs_kernel(const LogprobArgs a) {
         const double d = near ? (double)v * (double)c - (double)(st.m * c) : ((double)v - (double)st.m) * (double)c;
         return (float)(d * ln2 - ls);
     };
+    // equal entries before the token in its own 16-byte piece
+    if (has) {
+        const int piece = (tok + skew) & ~(VEC - 1), i = piece - skew + lane;
+        above += __popcll(__ballot(lane < VEC && i >= 0 && i < tok && Elem<T>::load1(x0 + max(i, 0)) == xt));
+    }
     if (lane == 0) {
         if (a.logp) a.logp[row] = none ? (float)nan : has ? log_p(xt) : -INFINITY;
         if (a.rank) a.rank[row] = none ? -1 : has ? above : V;
