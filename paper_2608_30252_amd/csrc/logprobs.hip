@@ -11,14 +11,14 @@
 // units: few steps do), and sums within a step in fp32, over steps and threads in
 // fp64.
 //
-// The first top_n of the order: each wave keeps its largest 64 keys (value, then
-// index) sorted, one to a lane.  An entry above the wave's top_n-th, and above what
-// any wave of the workgroup has as its top_n-th, is put in by a ballot (its place)
-// and a shift by one lane; few entries of a row come that far.  Before there are
-// top_n: the top_n-th largest of 64 maxima of disjoint groups (lane l of every
-// wave), which top_n entries at least reach.  The same bound, of the lanes' maxima,
-// thins a step in which many entries are above the list (a rising row).  At the end the places
-// of what the waves have above the bound are counted.
+// The first top_n of the order: entries (keys of value, then index) above a bound go
+// into their wave's list in LDS.  The first bound is a value that top_n entries of the
+// workgroup's first chunk reach: the top_n-th largest of 64 maxima of disjoint
+// groups.  A list that grows beyond about 1.5 top_n is cut to its first top_n by
+// counting what is above each key; the last that stays is a bound for every wave of
+// the workgroup.  A step in which many lanes have entries above the bound (a rising
+// row) is thinned first by the bound of its lanes' maxima.  At the end what the lists
+// hold above the largest bound is put in order, again by counting.
 //
 // Work: a workgroup takes a run of a row's chunks of 8192, its waves 2048 of each
 // and no barrier between the first chunk and the last; with few rows, more
@@ -30,10 +30,12 @@ namespace mad {
 
 namespace {
 
-constexpr int kWg = 256, kEntries = 32;   // threads, entries of a thread and step
-constexpr int kWaves = kWg / 64;
-static_assert(kWg * kEntries == kLogprobChunk, "");
-constexpr int kMany = 24;                 // lanes with entries above the list from which on a step is thinned first
+constexpr int kWg = 256, kWaves = kWg / 64;
+constexpr int kMany = 24;                 // lanes with entries above the bound from which on a step is thinned first
+constexpr int kOwn = 128;                 // a wave's list while it grows
+static_assert(MAD_MAX_TOP + 64 <= kOwn, "what a cut leaves, and an entry of each lane");
+constexpr int kRecs = (kLogprobSplits + kWaves - 1) / kWaves;   // records that a wave joins
+constexpr int kList = kRecs * MAD_MAX_TOP > kOwn ? kRecs * MAD_MAX_TOP : kOwn;
 constexpr float kLag = 8.f;               // M is raised where a step's largest x c is above it by more (log2 units)
 constexpr float kNear = 0x1p26f;          // |m| c below which M is m c as rounded
 
@@ -67,22 +69,21 @@ __device__ __forceinline__ uint64_t read_lane_u64(uint64_t v, int l) {
 }
 __device__ __forceinline__ uint64_t max_u64(uint64_t a, uint64_t b) { return a > b ? a : b; }
 
-// A value that n of the lanes' values reach: the n-th largest of the maxima of 16, 32 or 64 groups of lanes, at least
-// four for each that is looked for where there are so many (fewer groups are a shorter chain, and a looser bound).
+// A value that n of the lanes' values reach, n of them at least: the n-th largest but for its low 16 bits (for bf16 entries
+// it is that one), bit by bit over the lanes that still share its upper bits.
 __device__ __forceinline__ uint32_t reached_by(uint32_t g, int n) {
-    if (n <= 16) g = max(g, (uint32_t)__shfl_xor((int)g, 32));
-    if (n <= 4) g = max(g, (uint32_t)__shfl_xor((int)g, 16));
-    const int groups = n <= 4 ? 16 : n <= 16 ? 32 : 64;
-    int above = 0;
-    for (int l = 0; l < groups; l += 16)
-        #pragma unroll
-        for (int k = 0; k < 16; ++k) above += (uint32_t)__builtin_amdgcn_readlane((int)g, l + k) > g ? 1 : 0;
-    // the least value with fewer than n above it
-    uint32_t least = above < n ? g : 0xffffffffu;
+    uint64_t in = ~0ull;
+    uint32_t value = 0;
     #pragma unroll
-    for (int k = 1; k < 16; k <<= 1) least = min(least, (uint32_t)__shfl_xor((int)least, k));
-    least = min(least, (uint32_t)__shfl_xor((int)least, 16));
-    return min(least, (uint32_t)__shfl_xor((int)least, 32));
+    for (int bit = 31; bit >= 16; --bit) {
+        const uint64_t up = __ballot(g >> bit & 1) & in;
+        const int k = __popcll(up);
+        const bool has = k >= n;
+        value |= has ? 1u << bit : 0u;
+        in = has ? up : in ^ up;
+        n -= has ? 0 : k;
+    }
+    return value;
 }
 
 // the lanes' sums together, in every lane
@@ -97,42 +98,58 @@ __device__ __forceinline__ Stats wave_join(Stats a, float c) {
 }
 
 struct Shared {
-    uint64_t list[kLogprobSplits * MAD_MAX_TOP], best[MAD_MAX_TOP];
+    uint64_t own[kWaves][kList], best[MAD_MAX_TOP];
     uint64_t bound;
-    int count;
+    int place[kWaves * kList];
+    float entries[kWaves][64];
     uint32_t group[kWaves][64];
     double s[kWaves], u[kWaves];
     float m[kWaves];
-    int above[kWaves], inf[kWaves];
+    int above[kWaves], inf[kWaves], held[kWaves];
     int last;
 };
-static_assert(kLogprobSplits >= kWaves, "a list for each wave");
 
-// The first n of the order among list[0 .. count) into best (behind a barrier).  An entry's place is the number of keys
-// above it (keys differ: their index is in them).
-__device__ __forceinline__ void first_of_list(Shared &sh, int count, int n) {
-    for (int i = threadIdx.x; i < count; i += kWg) {
-        const uint64_t x = sh.list[i];
-        int at = 0;
+// The first n of the order among the waves' lists (held[w] keys each) into best: a key's place is the number of keys above
+// it (keys differ: their index is in them), each wave counting in its own list.  Begins and ends at a barrier.
+__device__ __forceinline__ void join_lists(Shared &sh, int wave, int lane, int held, int n) {
+    for (int i = threadIdx.x; i < kWaves * kList; i += kWg) sh.place[i] = 0;
+    if (lane == 0) sh.held[wave] = held;
+    if ((int)threadIdx.x < n) sh.best[threadIdx.x] = 0;
+    __syncthreads();
+    int from[kWaves + 1] = {0};
+    #pragma unroll
+    for (int w = 0; w < kWaves; ++w) from[w + 1] = from[w] + sh.held[w];
+    auto key_of = [&](int i) {
+        int w = 0;
+        #pragma unroll
+        for (int k = 1; k < kWaves; ++k) w += i >= from[k] ? 1 : 0;
+        int start = 0;
+        #pragma unroll
+        for (int k = 1; k < kWaves; ++k) start = w == k ? from[k] : start;
+        return sh.own[w][i - start];
+    };
+    const uint64_t *own = sh.own[wave];
+    for (int i = lane; i < from[kWaves]; i += 64) {
+        const uint64_t x = key_of(i);
+        int above = 0;
         #pragma unroll 4
-        for (int k = 0; k < count; ++k) at += sh.list[k] > x ? 1 : 0;
-        if (at < n) sh.best[at] = x;
+        for (int k = 0; k < held; ++k) above += own[k] > x ? 1 : 0;
+        if (above > 0) atomicAdd(&sh.place[i], above);
     }
-}
-// a lane's key goes into the list if `in`
-__device__ __forceinline__ void to_list(Shared &sh, uint64_t key, bool in) {
-    const uint64_t lanes = __ballot(in);
-    int at = 0;
-    if ((threadIdx.x & 63) == 0) at = atomicAdd(&sh.count, __popcll(lanes));
-    at = __builtin_amdgcn_readfirstlane(at) + __popcll(lanes & ((1ull << (threadIdx.x & 63)) - 1));
-    if (in) sh.list[at] = key;
+    __syncthreads();
+    for (int i = threadIdx.x; i < from[kWaves]; i += kWg) {
+        const int at = sh.place[i];
+        if (at < n) sh.best[at] = key_of(i);
+    }
+    __syncthreads();
 }
 
 }  // namespace
 
-template <typename T, bool TOP>
+// E: entries of a thread and step
+template <typename T, int E, bool TOP>
 __global__ __launch_bounds__(kWg, 4) void logprobs_kernel(const LogprobArgs a) {
-    constexpr int VEC = Elem<T>::VEC, NV = kEntries / VEC;
+    constexpr int VEC = Elem<T>::VEC, NV = E / VEC, CHUNK = kWg * E;
     __shared__ Shared sh;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int row = blockIdx.x / a.splits, split = blockIdx.x - row * a.splits;
@@ -162,15 +179,28 @@ __global__ __launch_bounds__(kWg, 4) void logprobs_kernel(const LogprobArgs a) {
 
     Stats st = {0.0, 0.0, -INFINITY};
     int above = 0, inf = 0;      // (of the wave)
-    uint64_t key = 0;            // lane i: the wave's i-th largest
+    uint64_t *own = sh.own[wave];
+    int held = 0;                // keys in it
     uint64_t bound = 0;          // only keys above it count
-    if (TOP && tid == 0) {
-        sh.bound = 0;
-        sh.count = 0;
-    }
+    // the wave's list to its first n, the last of which is a bound
+    auto cut = [&]() {
+        const uint64_t k0 = lane < held ? own[lane] : 0, k1 = 64 + lane < held ? own[64 + lane] : 0;
+        int a0 = 0, a1 = 0;
+        #pragma unroll 4
+        for (int i = 0; i < held; ++i) {
+            const uint64_t x = own[i];
+            a0 += x > k0 ? 1 : 0;
+            a1 += x > k1 ? 1 : 0;
+        }
+        if (k0 != 0 && a0 < n) own[a0] = k0;
+        if (k1 != 0 && a1 < n) own[a1] = k1;
+        if (held >= n) bound = max_u64(bound, own[n - 1]);
+        held = min(held, n);
+    };
+    if (TOP && tid == 0) sh.bound = 0;
 
     for (int chunk = chunk0; chunk < chunk1; ++chunk) {
-        float x[kEntries];
+        float x[E];
         #pragma unroll
         for (int j = 0; j < NV; ++j) {
             float f[VEC];
@@ -179,12 +209,12 @@ __global__ __launch_bounds__(kWg, 4) void logprobs_kernel(const LogprobArgs a) {
             for (int e = 0; e < VEC; ++e) x[j * VEC + e] = f[e];
         }
         load(chunk + 1);
-        const int first = chunk * kLogprobChunk - skew;   // the chunk's first entry
-        const bool edge = first < 0 || first + kLogprobChunk > V;
+        const int first = chunk * CHUNK - skew;   // the chunk's first entry
+        const bool edge = first < 0 || first + CHUNK > V;
         auto index = [&](int i) { return first + ((i / VEC) * kWg + tid) * VEC + i % VEC; };
         if (edge) {   // what is not the row's: -inf
             #pragma unroll
-            for (int i = 0; i < kEntries; ++i) x[i] = (uint32_t)index(i) < (uint32_t)V ? x[i] : -INFINITY;
+            for (int i = 0; i < E; ++i) x[i] = (uint32_t)index(i) < (uint32_t)V ? x[i] : -INFINITY;
         }
         float mj[NV], m = -INFINITY;   // the pieces' largest
         #pragma unroll
@@ -209,7 +239,7 @@ __global__ __launch_bounds__(kWg, 4) void logprobs_kernel(const LogprobArgs a) {
         if (fabsf(M) < kNear && m < INFINITY) {
             float s1 = 0.f, u1 = 0.f;   // every other entry's
             #pragma unroll
-            for (int i = 0; i < kEntries; i += 2) {
+            for (int i = 0; i < E; i += 2) {
                 const float d = fmaf(x[i], c, -M), e = __builtin_amdgcn_exp2f(d);
                 const float d1 = fmaf(x[i + 1], c, -M), e1 = __builtin_amdgcn_exp2f(d1);
                 s += e;
@@ -223,14 +253,14 @@ __global__ __launch_bounds__(kWg, 4) void logprobs_kernel(const LogprobArgs a) {
                 u = 0.f;
                 const float again = __int_as_float(here(__float_as_int(M)));   // (no registers held for this)
                 #pragma unroll
-                for (int i = 0; i < kEntries; ++i) {
+                for (int i = 0; i < E; ++i) {
                     const float d = fmaf(x[i], c, -again), e = __builtin_amdgcn_exp2f(d);
                     u = fmaf(e, fmaxf(d, -200.f), u);
                 }
             }
         } else if (fabsf(st.m) < INFINITY && m < INFINITY) {
             #pragma unroll
-            for (int i = 0; i < kEntries; ++i) {
+            for (int i = 0; i < E; ++i) {
                 const float d = (x[i] - st.m) * c, e = __builtin_amdgcn_exp2f(d);
                 s += e;
                 u = fmaf(e, fmaxf(d, -200.f), u);
@@ -240,7 +270,7 @@ __global__ __launch_bounds__(kWg, 4) void logprobs_kernel(const LogprobArgs a) {
         st.u += (double)u;
         if (__any(!(fabsf(m) < INFINITY))) {   // a +inf, nothing but -inf, or NaN alone
             #pragma unroll
-            for (int i = 0; i < kEntries; ++i) {
+            for (int i = 0; i < E; ++i) {
                 inf += __popcll(__ballot(x[i] == INFINITY));
                 if (x[i] != x[i]) st.s = __builtin_nan("");
             }
@@ -256,7 +286,7 @@ __global__ __launch_bounds__(kWg, 4) void logprobs_kernel(const LogprobArgs a) {
             }
             if (xt == -INFINITY) {   // (nothing is below)
                 #pragma unroll
-                for (int i = 0; i < kEntries; ++i)
+                for (int i = 0; i < E; ++i)
                     above += __popcll(__ballot(x[i] == xt && index(i) >= 0 && index((i / VEC) * VEC) + VEC <= tok));
             }
         }
@@ -267,44 +297,54 @@ __global__ __launch_bounds__(kWg, 4) void logprobs_kernel(const LogprobArgs a) {
                 uint32_t g = 0;
                 #pragma unroll
                 for (int k = 0; k < kWaves; ++k) g = max(g, sh.group[k][lane]);
-                bound = ((uint64_t)reached_by(g, n) << 32) - 1;   // (no order is 0)
+                bound = ((uint64_t)reached_by(g, n) << 32) - 1;   // (an order's upper half is not 0 but for NaN's)
             } else {
                 bound = max_u64(bound, *reinterpret_cast<volatile uint64_t *>(&sh.bound));
             }
-            // entries of the bound's value and above (some of that value are not above it); a bound among the NaNs' keys: all
-            float xb = value_of(bound);
-            if (__any(!(m < xb))) {
-                if (chunk > chunk0 && __popcll(__ballot(!(m < xb))) > kMany) {
+            // lanes with entries of the bound's value and above (some of that value are not above it)
+            auto lanes_above = [&]() { return __ballot(!(m < value_of(bound))); };
+            uint64_t lanes = lanes_above();
+            if (lanes) {
+                if (chunk > chunk0 && __popcll(lanes) > kMany) {
                     bound = max_u64(bound, ((uint64_t)reached_by(order_of(m), n) << 32) - 1);
-                    xb = value_of(bound);
+                    lanes = lanes_above();
                 }
-                const int at0 = here(tid);   // (the keys are made where they are needed)
-                #pragma unroll
-                for (int j = 0; j < NV; ++j) {
-                    if (!__any(!(mj[j] < xb))) continue;
+                while (lanes) {
+                    // 64 / E of these lanes spread their entries over the wave
+                    int from = -1, slot = -1;   // whose entry this lane takes, where this lane's go
                     #pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        const float v = x[j * VEC + e];
-                        if (!__any(!(v < xb))) continue;
-                        const int at_i = first + (j * kWg + at0) * VEC + e;
-                        const uint64_t mine = (uint32_t)at_i < (uint32_t)V ? argmax_key(v, at_i) : 0;
-                        for (uint64_t left = __ballot(mine > bound); left; left = __ballot(mine > bound) & left & (left - 1)) {
-                            const uint64_t y = read_lane_u64(mine, __builtin_ctzll(left));
-                            const int at = __popcll(__ballot(key > y));
-                            const uint64_t before = dpp_u64<0x138>(key);   // the lane below's (wave_shr 1)
-                            key = lane < at ? key : lane == at ? y : before;
-                            bound = max_u64(bound, read_lane_u64(key, n - 1));
-                        }
-                        xb = value_of(bound);
+                    for (int k = 0; k < 64 / E; ++k) {
+                        const int l = lanes ? __builtin_ctzll(lanes) : -1;
+                        lanes &= lanes - 1;
+                        from = lane / E == k ? l : from;
+                        slot = lane == l ? k : slot;
                     }
+                    if (slot >= 0) {
+                        #pragma unroll
+                        for (int q = 0; q < E / 4; ++q)
+                            reinterpret_cast<float4 *>(sh.entries[wave])[slot * (E / 4) + q] = make_float4(x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]);
+                    }
+                    const float v = sh.entries[wave][lane];
+                    const int e = lane % E, i = first + ((e / VEC) * kWg + wave * 64 + from) * VEC + e % VEC;
+                    const uint64_t mine = from >= 0 && (uint32_t)i < (uint32_t)V ? argmax_key(v, i) : 0;
+                    uint64_t in = __ballot(mine > bound);
+                    if (held + __popcll(in) > kOwn) {
+                        cut();
+                        in = __ballot(mine > bound);
+                        lanes &= lanes_above();
+                    }
+                    if (mine > bound) own[held + __popcll(in & ((1ull << lane) - 1))] = mine;
+                    held += __popcll(in);
                 }
-                if (lane == 0 && chunk + 1 < chunk1) atomicMax((unsigned long long *)&sh.bound, (unsigned long long)bound);
+                if (chunk + 1 < chunk1 && held > n + max(n >> 1, 4)) {
+                    cut();
+                    if (lane == 0) atomicMax((unsigned long long *)&sh.bound, (unsigned long long)bound);
+                }
             }
         }
     }
 
     // ---- the workgroup's waves together ----
-    if (TOP && lane == 0) atomicMax((unsigned long long *)&sh.bound, (unsigned long long)bound);
     st = wave_join(st, c);
     if (lane == 0) {
         sh.s[wave] = st.s;
@@ -313,15 +353,8 @@ __global__ __launch_bounds__(kWg, 4) void logprobs_kernel(const LogprobArgs a) {
         sh.above[wave] = above;
         sh.inf[wave] = inf;
     }
-    __syncthreads();
-    if (TOP) {
-        to_list(sh, key, key != 0 && key >= sh.bound);   // (a wave's top_n-th, if that is the bound, among them)
-        if (tid < n) sh.best[tid] = 0;
-        __syncthreads();
-        first_of_list(sh, sh.count, n);
-        __syncthreads();
-    }
-    const LogprobRecord *rec = a.records + (size_t)row * a.splits;
+    if (TOP) join_lists(sh, wave, lane, held, n);
+    else __syncthreads();
     if (wave == 0) {
         st = lane < kWaves ? Stats{sh.s[lane & (kWaves - 1)], sh.u[lane & (kWaves - 1)], sh.m[lane & (kWaves - 1)]} : Stats{0.0, 0.0, -INFINITY};
         st = wave_join(st, c);
@@ -334,8 +367,9 @@ __global__ __launch_bounds__(kWg, 4) void logprobs_kernel(const LogprobArgs a) {
 
     if (a.splits > 1) {
         // a record for each workgroup of the row; the last to arrive joins them
+        LogprobRecord *rec = a.records + (size_t)row * a.splits;
         if (wave == 0) {
-            LogprobRecord *mine = const_cast<LogprobRecord *>(rec + split);
+            LogprobRecord *mine = rec + split;
             if (TOP && lane < n) __hip_atomic_store(&mine->best[lane], sh.best[lane], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             if (lane == 0) {
                 const uint64_t w[4] = {(uint64_t)__double_as_longlong(st.s), (uint64_t)__double_as_longlong(st.u),
@@ -353,25 +387,29 @@ __global__ __launch_bounds__(kWg, 4) void logprobs_kernel(const LogprobArgs a) {
         }
         __syncthreads();
         if (!sh.last) return;
+        // everything that is read of the records, at once
+        uint64_t w[4] = {0, 0, 0xff800000u, 0}, part[kRecs], least = 0;
+        if (lane < a.splits) {
+            #pragma unroll
+            for (int k = 0; k < 4; ++k) w[k] = load_agent64(reinterpret_cast<const uint64_t *>(rec + lane) + k);
+            if (TOP) least = load_agent64(&rec[lane].best[n - 1]);
+        }
         if (TOP) {
-            // what any workgroup has as its top_n-th is a bound for all
-            uint64_t least = lane < a.splits ? load_agent64(&rec[lane].best[n - 1]) : 0;
-            if (tid == 0) sh.count = 0;
-            if (tid < n) sh.best[tid] = 0;
-            least = wave_fold_u64(least, max_u64);
-            __syncthreads();
-            for (int k = wave; k < a.splits; k += kWaves) {
-                const uint64_t x = lane < n ? load_agent64(&rec[k].best[lane]) : 0;
-                to_list(sh, x, x != 0 && x >= least);
+            #pragma unroll
+            for (int k = 0; k < kRecs; ++k)
+                part[k] = k * kWaves + wave < a.splits && lane < n ? load_agent64(&rec[k * kWaves + wave].best[lane]) : 0;
+            least = wave_fold_u64(least, max_u64);   // what any workgroup has as its top_n-th is a bound for all
+            held = 0;
+            #pragma unroll
+            for (int k = 0; k < kRecs; ++k) {
+                const bool in = part[k] != 0 && part[k] >= least;
+                const uint64_t all = __ballot(in);
+                if (in) own[held + __popcll(all & ((1ull << lane) - 1))] = part[k];
+                held += __popcll(all);
             }
-            __syncthreads();
-            first_of_list(sh, sh.count, n);
-            __syncthreads();
+            join_lists(sh, wave, lane, held, n);
         }
         if (wave == 0) {
-            uint64_t w[4] = {0, 0, 0xff800000u, 0};
-            if (lane < a.splits)
-                for (int k = 0; k < 4; ++k) w[k] = load_agent64(reinterpret_cast<const uint64_t *>(rec + lane) + k);
             st = wave_join(Stats{__longlong_as_double((long long)w[0]), __longlong_as_double((long long)w[1]), __uint_as_float((uint32_t)w[2])}, c);
             above = inf = 0;
             for (int k = 0; k < a.splits; ++k) {
@@ -410,16 +448,33 @@ __global__ __launch_bounds__(kWg, 4) void logprobs_kernel(const LogprobArgs a) {
     }
 }
 
+// Few rows: 16 entries to a thread and step, and as many workgroups to a row as the CUs hold at once, so that a call is
+// one round of short steps.  Else 32, a workgroup to a row.
+LogprobPlan plan_logprobs(int rows, int V) {
+    LogprobPlan p;
+    p.entries = (int64_t)rows * V <= kLogprobShort ? 16 : 32;
+    p.n_chunks = (V + 7 + kWg * p.entries - 1) / (kWg * p.entries);   // (a row may begin up to 7 entries into its first 16 bytes)
+    const int want = rows > kCounterLines / 4 ? 1 : kLogprobWgs / rows < kLogprobSplits ? kLogprobWgs / rows : kLogprobSplits;
+    const int each = want < 1 ? p.n_chunks : (p.n_chunks + want - 1) / want;
+    p.splits = (p.n_chunks + each - 1) / each;
+    return p;
+}
+
 size_t logprobs_ws_bytes(int rows, int V) {
-    const int splits = logprob_splits(rows, V);
-    return kCounterRegionBytes + (splits > 1 ? align256((size_t)rows * splits * sizeof(LogprobRecord)) : 0);
+    const LogprobPlan p = plan_logprobs(rows, V);
+    return kCounterRegionBytes + (p.splits > 1 ? align256((size_t)rows * p.splits * sizeof(LogprobRecord)) : 0);
 }
 
 template <typename T>
 static hipError_t launch_t(const LogprobArgs &a, hipStream_t st) {
     const dim3 grid((unsigned)(a.rows * a.splits)), wg(kWg);
-    if (a.top_n > 0) hipLaunchKernelGGL((logprobs_kernel<T, true>), grid, wg, 0, st, a);
-    else hipLaunchKernelGGL((logprobs_kernel<T, false>), grid, wg, 0, st, a);
+    if (a.entries == 16) {
+        if (a.top_n > 0) hipLaunchKernelGGL((logprobs_kernel<T, 16, true>), grid, wg, 0, st, a);
+        else hipLaunchKernelGGL((logprobs_kernel<T, 16, false>), grid, wg, 0, st, a);
+    } else {
+        if (a.top_n > 0) hipLaunchKernelGGL((logprobs_kernel<T, 32, true>), grid, wg, 0, st, a);
+        else hipLaunchKernelGGL((logprobs_kernel<T, 32, false>), grid, wg, 0, st, a);
+    }
     return hipGetLastError();
 }
 

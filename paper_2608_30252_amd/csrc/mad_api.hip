@@ -1049,8 +1049,10 @@ int mad_token_logprobs(const void *logits, int dtype, int64_t seq_stride, int64_
     a.T = T;
     a.V = V;
     a.top_n = top_n;
-    a.n_chunks = mad::logprob_chunks(V);
-    a.splits = mad::logprob_splits(a.rows, V);
+    const mad::LogprobPlan p = mad::plan_logprobs(a.rows, V);
+    a.n_chunks = p.n_chunks;
+    a.splits = p.splits;
+    a.entries = p.entries;
     return hip_status(mad::launch_logprobs(a, dtype, (hipStream_t)stream), "logprobs launch");
 }
 

@@ -291,10 +291,10 @@ size_t sample_ws_bytes(int B, int T, int V);
 hipError_t launch_sample(const SampleArgs &a, int dtype, hipStream_t st);
 
 // -------------------------------------------------------------- logprobs ----
-constexpr int kLogprobChunk = 8192;                            // entries of a workgroup's step
 constexpr int kLogprobSplits = 16;                             // workgroups to a row, at most
 constexpr int kLogprobMaxV = 1 << 20, kLogprobMaxRows = 1 << 22;
-constexpr int kLogprobWgs = 2048;                              // workgroups that a call of few rows is split into, about
+constexpr int kLogprobWgs = 1024;                              // workgroups that the CUs hold at once
+constexpr int64_t kLogprobShort = 1 << 21;                     // entries up to which a call is split finely
 struct LogprobRecord {   // one workgroup's part of a row
     double s, u;
     float m;
@@ -310,16 +310,14 @@ struct LogprobArgs {
     int32_t *rank, *top_tok;
     LogprobRecord *records;  // [rows][splits]
     unsigned *counters;      // line r: arrivals of row r's workgroups
-    int rows, T, V, top_n, n_chunks, splits;
+    int rows, T, V, top_n;
+    int n_chunks, splits, entries;   // plan_logprobs
     float c[kMaxB];          // log2 e / temperature
 };
-// chunks of a row (a row may begin up to 7 entries into its first 16 bytes)
-inline int logprob_chunks(int V) { return (V + 7 + kLogprobChunk - 1) / kLogprobChunk; }
-inline int logprob_splits(int rows, int V) {
-    if (rows > kCounterLines / 4) return 1;
-    const int want = kLogprobWgs / rows, most = logprob_chunks(V) < kLogprobSplits ? logprob_chunks(V) : kLogprobSplits;
-    return want < 1 ? 1 : want < most ? want : most;
-}
+struct LogprobPlan {
+    int n_chunks, splits, entries;   // chunks of a row, workgroups to a row, entries of a thread and chunk
+};
+LogprobPlan plan_logprobs(int rows, int V);
 size_t logprobs_ws_bytes(int rows, int V);
 hipError_t launch_logprobs(const LogprobArgs &a, int dtype, hipStream_t st);
 
