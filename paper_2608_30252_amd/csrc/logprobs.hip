@@ -32,6 +32,7 @@ namespace {
 
 constexpr int kWg = 256, kWaves = kWg / 64;
 constexpr int kMany = 24;                 // lanes with entries above the bound from which on a step is thinned first
+constexpr int kFewGroups = 32;            // top_n up to which 64 groups give the first bound, else 256 (fewer entries pass, longer to find)
 constexpr int kOwn = 128;                 // a wave's list while it grows
 static_assert(MAD_MAX_TOP + 64 <= kOwn, "what a cut leaves, and an entry of each lane");
 constexpr int kRecs = (kLogprobSplits + kWaves - 1) / kWaves;   // records that a wave joins
@@ -69,22 +70,32 @@ __device__ __forceinline__ uint64_t read_lane_u64(uint64_t v, int l) {
 }
 __device__ __forceinline__ uint64_t max_u64(uint64_t a, uint64_t b) { return a > b ? a : b; }
 
-// A value that n of the lanes' values reach, n of them at least: the n-th largest but for its low 16 bits (for bf16 entries
-// it is that one), bit by bit over the lanes that still share its upper bits.
-__device__ __forceinline__ uint32_t reached_by(uint32_t g, int n) {
-    uint64_t in = ~0ull;
+// A value that n of the lanes' values g (G to a lane) reach, n of them at least: the n-th largest but for its low 16 bits
+// (for bf16 entries it is that one), bit by bit over the values that still share its upper bits.
+template <int G>
+__device__ __forceinline__ uint32_t reached_by(const uint32_t (&g)[G], int n) {
+    uint64_t in[G];
+    #pragma unroll
+    for (int k = 0; k < G; ++k) in[k] = ~0ull;
     uint32_t value = 0;
     #pragma unroll
     for (int bit = 31; bit >= 16; --bit) {
-        const uint64_t up = __ballot(g >> bit & 1) & in;
-        const int k = __popcll(up);
-        const bool has = k >= n;
+        uint64_t up[G];
+        int many = 0;
+        #pragma unroll
+        for (int k = 0; k < G; ++k) {
+            up[k] = __ballot(g[k] >> bit & 1) & in[k];
+            many += __popcll(up[k]);
+        }
+        const bool has = many >= n;
         value |= has ? 1u << bit : 0u;
-        in = has ? up : in ^ up;
-        n -= has ? 0 : k;
+        #pragma unroll
+        for (int k = 0; k < G; ++k) in[k] = has ? up[k] : in[k] ^ up[k];
+        n -= has ? 0 : many;
     }
     return value;
 }
+__device__ __forceinline__ uint64_t below_order(uint32_t order) { return order == 0 ? 0 : ((uint64_t)order << 32) - 1; }
 
 // the lanes' sums together, in every lane
 __device__ __forceinline__ Stats wave_join(Stats a, float c) {
@@ -98,7 +109,7 @@ __device__ __forceinline__ Stats wave_join(Stats a, float c) {
 }
 
 struct Shared {
-    uint64_t own[kWaves][kList], best[MAD_MAX_TOP];
+    uint64_t own[kWaves][kList + 8], best[MAD_MAX_TOP];
     uint64_t bound;
     int place[kWaves * kList];
     float entries[kWaves][64];
@@ -113,6 +124,7 @@ struct Shared {
 // it (keys differ: their index is in them), each wave counting in its own list.  Begins and ends at a barrier.
 __device__ __forceinline__ void join_lists(Shared &sh, int wave, int lane, int held, int n) {
     for (int i = threadIdx.x; i < kWaves * kList; i += kWg) sh.place[i] = 0;
+    if (lane < 8) sh.own[wave][held + lane] = 0;   // (read, and above nothing)
     if (lane == 0) sh.held[wave] = held;
     if ((int)threadIdx.x < n) sh.best[threadIdx.x] = 0;
     __syncthreads();
@@ -132,8 +144,13 @@ __device__ __forceinline__ void join_lists(Shared &sh, int wave, int lane, int h
     for (int i = lane; i < from[kWaves]; i += 64) {
         const uint64_t x = key_of(i);
         int above = 0;
-        #pragma unroll 4
-        for (int k = 0; k < held; ++k) above += own[k] > x ? 1 : 0;
+        for (int k = 0; k < held; k += 8) {
+            ulonglong2 y[4];
+            #pragma unroll
+            for (int q = 0; q < 4; ++q) y[q] = reinterpret_cast<const ulonglong2 *>(own + k)[q];
+            #pragma unroll
+            for (int q = 0; q < 4; ++q) above += (y[q].x > x ? 1 : 0) + (y[q].y > x ? 1 : 0);
+        }
         if (above > 0) atomicAdd(&sh.place[i], above);
     }
     __syncthreads();
@@ -294,10 +311,13 @@ __global__ __launch_bounds__(kWg, 4) void logprobs_kernel(const LogprobArgs a) {
             if (chunk == chunk0) {
                 sh.group[wave][lane] = order_of(m);
                 __syncthreads();
-                uint32_t g = 0;
+                uint32_t g[kWaves], all[1] = {0};
                 #pragma unroll
-                for (int k = 0; k < kWaves; ++k) g = max(g, sh.group[k][lane]);
-                bound = ((uint64_t)reached_by(g, n) << 32) - 1;   // (an order's upper half is not 0 but for NaN's)
+                for (int k = 0; k < kWaves; ++k) {
+                    g[k] = sh.group[k][lane];
+                    all[0] = max(all[0], g[k]);
+                }
+                bound = below_order(n > kFewGroups ? reached_by(g, n) : reached_by(all, n));
             } else {
                 bound = max_u64(bound, *reinterpret_cast<volatile uint64_t *>(&sh.bound));
             }
@@ -306,7 +326,8 @@ __global__ __launch_bounds__(kWg, 4) void logprobs_kernel(const LogprobArgs a) {
             uint64_t lanes = lanes_above();
             if (lanes) {
                 if (chunk > chunk0 && __popcll(lanes) > kMany) {
-                    bound = max_u64(bound, ((uint64_t)reached_by(order_of(m), n) << 32) - 1);
+                    const uint32_t g[1] = {order_of(m)};
+                    bound = max_u64(bound, below_order(reached_by(g, n)));
                     lanes = lanes_above();
                 }
                 while (lanes) {
@@ -388,21 +409,23 @@ __global__ __launch_bounds__(kWg, 4) void logprobs_kernel(const LogprobArgs a) {
         __syncthreads();
         if (!sh.last) return;
         // everything that is read of the records, at once
-        uint64_t w[4] = {0, 0, 0xff800000u, 0}, part[kRecs], least = 0;
+        uint64_t w[4] = {0, 0, 0xff800000u, 0}, part[kRecs];
+        uint32_t nth[1] = {0};
+        const int half = (a.splits + 1) / 2, deep = (n + half - 1) / half;   // some half of the lists, this deep, hold top_n
         if (lane < a.splits) {
             #pragma unroll
             for (int k = 0; k < 4; ++k) w[k] = load_agent64(reinterpret_cast<const uint64_t *>(rec + lane) + k);
-            if (TOP) least = load_agent64(&rec[lane].best[n - 1]);
+            if (TOP) nth[0] = (uint32_t)(load_agent64(&rec[lane].best[deep - 1]) >> 32);
         }
         if (TOP) {
             #pragma unroll
             for (int k = 0; k < kRecs; ++k)
                 part[k] = k * kWaves + wave < a.splits && lane < n ? load_agent64(&rec[k * kWaves + wave].best[lane]) : 0;
-            least = wave_fold_u64(least, max_u64);   // what any workgroup has as its top_n-th is a bound for all
+            const uint64_t least = below_order(reached_by(nth, (n + deep - 1) / deep));
             held = 0;
             #pragma unroll
             for (int k = 0; k < kRecs; ++k) {
-                const bool in = part[k] != 0 && part[k] >= least;
+                const bool in = part[k] > least;
                 const uint64_t all = __ballot(in);
                 if (in) own[held + __popcll(all & ((1ull << lane) - 1))] = part[k];
                 held += __popcll(all);
