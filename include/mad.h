@@ -68,6 +68,7 @@ extern "C" {
 #define MAD_OP_DECODE_LEAST 5
 #define MAD_OP_SAMPLE 6
 #define MAD_OP_LOGPROBS 7
+#define MAD_OP_VERIFY_KV4 8
 
 /*
  * A per-sequence, per-KV-head run of key/value rows in device memory.
@@ -399,7 +400,7 @@ int mad_kv4_append(const mad_rows *k_new, const mad_rows *v_new, const mad_rows 
  * |value| below 2^124.  T * G <= MAD_MAX_VERIFY_ROWS; d in {64, 128}; dtype BF16
  * or F32, both on the matrix cores (a cached value is exact in bf16; F32: q and
  * the probabilities as three bf16 terms each, so that products keep fp32's
- * precision).  Workspace MAD_OP_VERIFY.
+ * precision).  Workspace MAD_OP_VERIFY_KV4.
  */
 int mad_verify_attn_kv4(const void *q, int B, int T, int Hq, int Hkv, int d, int dtype, float scale,
                         const mad_kv4_view *kv, void *out, float *lse, void *ws, size_t ws_bytes, void *stream);
@@ -618,7 +619,7 @@ int mad_probe_handoff_latency(void *buf, size_t buf_bytes, unsigned long long *c
 /*
  * Workspace bytes needed by op (MAD_OP_*) for calls with at most these sizes:
  *   DECODE: B, Hq, Hkv, d                       (T, max_keys ignored)
- *   VERIFY: B, Hq, Hkv, d, T                    (max_keys ignored)
+ *   VERIFY, VERIFY_KV4: B, Hq, Hkv, d, T        (max_keys ignored)
  *   ACCEPT: B, T, max_keys = V                  (Hq, Hkv, d ignored)
  *   ACCEPT_STOCH: B, max_keys = V               (Hq, Hkv, d, T ignored)
  *   DECODE_LEAST: B, Hq, Hkv, d

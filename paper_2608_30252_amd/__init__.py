@@ -38,7 +38,7 @@ LIB_PATH = os.path.join(_HERE, "libmad.so")
 MAD_OK, MAD_EINVAL, MAD_ENOTSUP, MAD_EHIP, MAD_EWS = 0, -1, -2, -3, -4
 MAD_F32, MAD_BF16 = 0, 1
 MAD_OP_DECODE, MAD_OP_UPDATE, MAD_OP_VERIFY, MAD_OP_ACCEPT, MAD_OP_ACCEPT_STOCH, MAD_OP_DECODE_LEAST = 0, 1, 2, 3, 4, 5
-MAD_OP_SAMPLE, MAD_OP_LOGPROBS = 6, 7
+MAD_OP_SAMPLE, MAD_OP_LOGPROBS, MAD_OP_VERIFY_KV4 = 6, 7, 8
 MAX_BATCH = 64
 MAX_TOP = 64
 
@@ -741,7 +741,7 @@ def verify_attn_kv4(q: torch.Tensor, kv: KV4, out=None, lse=None, scale: Optiona
     Hkv = kv.k.shape[1]
     _need(Hkv >= 1 and Hq % Hkv == 0, f"Hq={Hq} must be a multiple of the KV heads {Hkv}")
     view = kv.view(B, Hkv, d, q.device, "kv")
-    nbytes = workspace_bytes(MAD_OP_VERIFY, B, Hq, Hkv, d, T)
+    nbytes = workspace_bytes(MAD_OP_VERIFY_KV4, B, Hq, Hkv, d, T)
     w = _ws_for(q.device, nbytes, ws)
     rc = _On(q.device).mad_verify_attn_kv4(_ptr(q), B, T, Hq, Hkv, d, _dtype_code(q), float(scale), ctypes.byref(view),
                                            _ptr(out), _ptr(lse), _ptr(w), w.numel(), _stream(q.device))

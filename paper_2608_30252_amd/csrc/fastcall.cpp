@@ -687,7 +687,7 @@ PyObject *verify4(PyObject *, PyObject *const *a, Py_ssize_t n) {
         need(shape(lse, {B, T, Hq}) && lse.scalar_type() == at::kFloat);
         const float scale = scale_of(a[4], d);
         void *st = stream_of(dev);
-        const Scratch ws(a[5], dev, st, g.ws_bytes(MAD_OP_VERIFY, B, Hq, (int)Hkv, d, T, 0));
+        const Scratch ws(a[5], dev, st, g.ws_bytes(MAD_OP_VERIFY_KV4, B, Hq, (int)Hkv, d, T, 0));
         const int dt = dtype_code(q);
         void *qp = q.data_ptr(), *op = out.data_ptr();
         float *lp = (float *)lse.data_ptr();

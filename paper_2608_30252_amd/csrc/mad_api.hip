@@ -174,6 +174,9 @@ size_t mad_workspace_bytes(int op, int B, int Hq, int Hkv, int d, int T, int max
         case MAD_OP_VERIFY:
             if (B < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv || (d != 64 && d != 128) || T < 1) return 0;
             return mad::verify_ws_bytes(B, Hq, Hkv, d, T);
+        case MAD_OP_VERIFY_KV4:
+            if (B < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv || (d != 64 && d != 128) || T < 1) return 0;
+            return mad::verify4_ws_bytes(B, Hq, Hkv, d, T);
         case MAD_OP_ACCEPT_STOCH:   // B, max_keys = V
             if (B < 1 || B > MAD_MAX_BATCH || max_keys < 1) return 0;
             return mad::stoch_ws_bytes(B, max_keys);
@@ -748,7 +751,7 @@ int mad_verify_attn_kv4(const void *q, int B, int T, int Hq, int Hkv, int d, int
     if ((uintptr_t)lse & 3) return fail(MAD_EINVAL, "lse not 4-byte aligned");
     if (!(scale > 0.f) || isinf(scale)) return fail(MAD_EINVAL, "scale must be positive and finite");
     if ((rc = check_view4(kv, B, Hkv, d))) return rc;
-    const size_t need = mad::verify_ws_bytes(B, Hq, Hkv, d, T);
+    const size_t need = mad::verify4_ws_bytes(B, Hq, Hkv, d, T);
     if (!ws) return fail(MAD_EWS, "workspace required (%zu bytes)", need);
     if (ws_bytes < need) return fail(MAD_EWS, "workspace %zu bytes < %zu", ws_bytes, need);
     if (!aligned16(ws)) return fail(MAD_EINVAL, "workspace not 16-byte aligned");
@@ -759,7 +762,6 @@ int mad_verify_attn_kv4(const void *q, int B, int T, int Hq, int Hkv, int d, int
     a.v = kv->v;
     a.k_scale = kv->k_scale;
     a.v_scale = kv->v_scale;
-    a.kind = mad::kStream4;
     a.out = out;
     a.lse = lse;
     a.seq = kv->seq_stride;
@@ -773,7 +775,7 @@ int mad_verify_attn_kv4(const void *q, int B, int T, int Hq, int Hkv, int d, int
     a.Hq = Hq;
     a.G = G;
     a.T = T;
-    mad::plan_stream(a, B, Hkv, d, kv->len);
+    mad::plan_stream4(a, B, Hkv, d, dtype, kv->len);
     return hip_status(mad::launch_stream4(a, dtype, d, (hipStream_t)stream), "4-bit verify launch");
 }
 

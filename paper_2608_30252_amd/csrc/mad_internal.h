@@ -86,8 +86,8 @@ constexpr int kMergeBytes = 128 << 10;      // LDS for the pieces of a unit that
 constexpr int kMergeInLaunch = 48 << 10;    // such pieces where the units are few (plan_stream)
 
 // verify over a cache of K and V rows; over K rows and V^T (one run of cap keys per feature);
-// the draft's decode: memory rows, window ring, new token (T = 1); verify over an 8-bit cache, a 4-bit one
-enum { kStreamRows = 0, kStreamVT = 1, kStreamDraft = 2, kStream8 = 3, kStream4 = 4 };
+// the draft's decode: memory rows, window ring, new token (T = 1); verify over an 8-bit cache
+enum { kStreamRows = 0, kStreamVT = 1, kStreamDraft = 2, kStream8 = 3 };
 
 struct StreamArgs {
     const void *q, *k, *v;    // draft: k and v are the memory rows
@@ -185,7 +185,10 @@ hipError_t launch_kv4_append(const Kv4AppendArgs &a, int dtype, int d, hipStream
 struct Stream4Args : StreamArgs {
     const void *k_scale, *v_scale;
     int64_t s_seq, s_head;
+    int waves;               // of a workgroup: plan_stream4
 };
+void plan_stream4(Stream4Args &a, int B, int Hkv, int d, int dtype, const int *n_keys);
+size_t verify4_ws_bytes(int B, int Hq, int Hkv, int d, int T);
 hipError_t launch_stream4(const Stream4Args &a, int dtype, int d, hipStream_t st);
 
 // ----------------------------------------------------------------- layer ----

@@ -584,10 +584,9 @@ __global__ __launch_bounds__(512, 1) void stream_kernel(const StreamArgs args) {
 // splits of one length).  By unit also serves launches with more units than workgroups can
 // count (a unit each: no pieces, no counters).
 void plan_stream(StreamArgs &a, int B, int Hkv, int d, const int *n_keys) {
-    const bool coded = a.kind == kStream8 || a.kind == kStream4;
-    const int slab = coded ? stream8_slab(d) : stream_slab(d);
-    // slabs that a workgroup takes at least (8 and 4 bits: two chunks each, for its eight waves four slabs)
-    const int least = coded ? 4 : 1;
+    const int slab = a.kind == kStream8 ? stream8_slab(d) : stream_slab(d);
+    // slabs that a workgroup takes at least (8 bits: two chunks of 8 KB each, for its eight waves four slabs)
+    const int least = a.kind == kStream8 ? 4 : 1;
     int64_t rows = 0;
     int nt[kMaxB], nt_max = 1;
     for (int b = 0; b < B; ++b) {
@@ -613,7 +612,7 @@ void plan_stream(StreamArgs &a, int B, int Hkv, int d, const int *n_keys) {
     // Pieces of one unit each (none crosses into the next unit) where that costs a workgroup at most `slack` slabs over
     // the mean.  Over 8 bits a unit's end costs about 5 slabs' time (a slab has twice the keys, the exchange as many bytes):
     // 16 sequences of 600 .. 12000 keys, 48 rows, 67.8 us with runs that cross -> 60.1.
-    const int slack = coded ? 12 + even / 8 : 2 + even / 16;
+    const int slack = a.kind == kStream8 ? 12 + even / 8 : 2 + even / 16;
     for (int share = whole ? nt_max : even; whole || share <= even + slack; share += 1 + even / 64) {
         int wgs = 0;
         np_max = 1;

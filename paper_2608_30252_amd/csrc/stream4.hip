@@ -10,7 +10,7 @@
 // scale from an fp32's exponent field, which the scale's byte is, shifted.
 //   S^T = K Q^T   bf16 x bf16; an fp32 query is split into three bf16 terms
 //                 (24 bits), three products to the same accumulator.
-//   O^T = V^T P^T bf16 x bf16: a probability is rounded to bf16 (2^-8 relative,
+//   O = P V       bf16 x bf16: a probability is rounded to bf16 (2^-8 relative,
 //                 the output's own rounding); V's values keep bf16's range, so keys
 //                 of any size meet in one sum.  fp32: three bf16 terms.
 // m is raised, and the sums scaled, only where a score exceeds it by more than 4
@@ -18,19 +18,41 @@
 // little.
 //
 // Operands without a transposition.  A matrix step takes 32 keys in any order that
-// both operands share; here key 4 e + lg of the step is element e of lane group
-// lg (lane = 16 lg + lr).
-//   K: lane (lr, lg) reads a quarter of one key's row (features D/4 * lg ..),
-//      which one scale covers, and the queries' fragments hold the same features.
+// both operands share.
+//   K: lane (lr, lg) (lane = 16 lg + lr) reads a quarter of one key's row (features
+//      D/4 * lg ..), which one scale covers, and the queries' fragments hold the
+//      same features.
 //   V: lane (lr, lg) reads, for its eight keys, the D/16 features that start at
-//      D/16 * lr: a matrix row is a lane's j-th feature.  The conversion gives
-//      pairs of features of a key; a byte permute of two keys' pairs gives two
-//      features' pairs of keys.
+//      D/16 * lr.  The conversion gives pairs of features of a key, where a product
+//      over keys wants pairs of keys of a feature.  The sparse product (A has two of
+//      every four entries of a row) takes them as they are: its 64 entries are (key,
+//      feature of the pair), and A's index keeps the even or the odd ones, so that
+//      the probabilities meet one feature of each pair.  Two of them cost what two
+//      dense ones do, and the byte permutes that would form pairs of keys are not
+//      there (16 sequences, 48 rows: 47 us with them, 44).
+// The order of the keys follows from the sparse operand's: accumulator element i of
+// the scores' block blk in lane group lg is key 16 (lg / 2) + 4 i + (lg ^ 2 blk), and
+// that is how the K rows are laid out and the V rows are read.
 //
-// Work decomposition: stream8.hip's.  Units (sequence, KV head) are cut into slabs
-// that are dealt to one workgroup per CU (plan_stream); inside it the eight waves
-// take chunks of 4 KB (32 keys at d 128, 64 at d 64) in turn, each through its
-// own ring of LDS stages, for every query row, and merge at a unit's end.
+// Work decomposition.  Units (sequence, KV head) are cut into pieces, one to a
+// workgroup (plan_stream4); inside it the eight waves (or four: two workgroups to a
+// CU) take chunks of 4 KB (32 keys at d 128, 64 at d 64) in turn, each through its
+// own ring of LDS stages, for every query row, and add up at the end.  No run of
+// slabs crosses from one unit to the next (plan_stream's do where that balances
+// better): the code for it took registers from the loop and the runs themselves cost
+// more than they balanced (16 sequences of 600 .. 12000 keys: 60 us, 44 by unit; 40
+// such, 32 rows: 83, 44).  The unit's pieces are merged by its last workgroup, or by
+// a second launch.
+//
+// What bounds it: instructions.  A chunk of 32 keys by 48 rows takes a wave about
+// 64 conversions, 24 dense and 24 sparse products, 24 exponentials and some 150
+// others; without its loads the kernel takes nearly as long, without its arithmetic
+// three quarters.  Waves with more chunks ahead of them go first (s_setprio), so that
+// the workgroup's waves end together: 2 - 6 us of 47.
+// Measured (us, d 128 unless given): 16 sequences of 600 .. 12000 keys, 64/8 heads,
+// 6 queries, 104 MB: 42 (2.5 TB/s), 1 query 26 (4.0 TB/s); one of 32773 keys, 5
+// queries, 23; one of 131072 keys, 1 query 31 (4.6 TB/s); 64 of 2000, 1 query 29
+// (4.8 TB/s); one of 317 keys, d 64, 6.1.
 //
 // What a row does not see is left out whatever it holds: scores by selection, rows
 // past the length are never read, and where a step with hidden keys has a NaN
@@ -43,13 +65,16 @@ namespace mad {
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_v;
 typedef __attribute__((ext_vector_type(2))) unsigned int u32x2_v;
 
+constexpr int kLeast4 = 4;             // slabs of a piece, at least (of eight waves each takes a chunk)
+constexpr int kMergeFew4 = 64 << 10;   // pieces of a unit that are merged in the launch where the units are few
 constexpr float kLazy4 = 4.f;      // the maximum is raised where a score exceeds it by more (log2 units)
 
-// T: bf16_t or float (queries and output)
-template <int D, int NB, typename T>
+// T: bf16_t or float (queries and output); W: waves of a workgroup, 8 or 4 (two workgroups to a CU)
+template <int D, int NB, typename T, int W>
 struct Stream4Cfg {
     static constexpr bool F32 = std::is_same<T, float>::value;
-    static constexpr int NWV = 8;                          // waves
+    static constexpr int NWV = W, NT = 64 * W;
+    static constexpr int LDS = (160 * 1024) * W / 8;       // a workgroup's share
     static constexpr int RB = D / 2;                       // bytes per K (and V) row
     static constexpr int CPR = D / 32;                     // 16-byte pieces, and scales, per row
     static constexpr int CHUNK = 4096;                     // K, then V
@@ -60,21 +85,20 @@ struct Stream4Cfg {
     static constexpr int RP = NB * 16;                     // padded query rows
     // query fragments (1 KB each), in registers where they and the accumulators leave room for the rest
     static constexpr int QBYTES = NB * KST * NQ * 1024;
-    static constexpr bool QREG = NB * (KST * NQ + DB) * 4 < 120;
+    static constexpr bool QREG = NB * (KST * NQ + DB) * 4 <= 72;
     static constexpr int REST = NWV * RP * 8 + QBYTES, STAGES = NWV * (CHUNK + SCALES);
-    static constexpr int NST = 4 * STAGES + REST + 1536 <= 160 * 1024 ? 4 : 3;   // stages per wave
-    static constexpr int PRE = NST - 2;                    // ... that the waves' exchange leaves alone
+    static constexpr int NST = 4 * STAGES + REST + 1024 <= LDS ? 4 : 3;   // stages per wave
     static constexpr int RING = NST * NWV * CHUNK;         // stage 0 of every wave, then stage 1, ..
     static constexpr int OFF_S = RING;                     // scales, likewise
     static constexpr int OFF_ML = OFF_S + NST * NWV * SCALES;   // the waves' (maximum, sum) per row
     static constexpr int OFF_Q = OFF_ML + NWV * RP * 8;
     static constexpr int USED = OFF_Q + QBYTES;
-    static constexpr int SMEM = USED > kMergeBytes ? USED : kMergeBytes;
-    // the waves' exchange goes through the last two stages of all of them, XD feature blocks at a time
-    static constexpr int OFF_X = PRE * NWV * CHUNK;
-    static constexpr int XD = NB * DB <= 8 ? DB : NB == 2 ? 4 : NB == 1 ? 8 : 2;
-    static_assert(SMEM + 2 * MAD_MAX_VERIFY_ROWS * 4 + 64 <= 160 * 1024, "LDS, with the kernel's static arrays");
-    static_assert(NWV * NB * XD * 1024 <= 2 * NWV * CHUNK && NB * XD <= NWV && DB % XD == 0, "exchange");
+    static constexpr int MERGE = kMergeBytes * W / 8;      // pieces that are merged in the launch
+    static constexpr int SMEM = USED > MERGE ? USED : MERGE;
+    // the waves' exchange goes through the stages, XD feature quads of a lane at a time
+    static constexpr int XD = NB * DB <= 4 * NST ? DB : NB * 4 <= 4 * NST ? 4 : 2;
+    static_assert(SMEM + MAD_MAX_VERIFY_ROWS * 4 + 64 <= LDS, "LDS, with the kernel's static arrays");
+    static_assert(NB * XD <= 4 * NST && DB % XD == 0, "exchange");
 };
 
 // A direct load of one dword, one half-word (zero-extended) per lane; lanes of a wave: consecutive dwords at lds.
@@ -89,6 +113,21 @@ __device__ __forceinline__ void lds_stream2(const void *src, uint32_t lds) {
     uint32_t saved;
     asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_ushort %1, off\n\ts_mov_b32 m0, %0"
                  : "=&s"(saved) : "v"(src), "s"(m) : "memory");
+}
+
+// P V for one feature of every pair: A is the 16 rows' probabilities of 32 keys, taken as the two kept of every four entries
+// (2:4 sparse) of 64 that are (key, feature of a pair): the even or the odd ones; B the keys' pairs as the conversion makes
+// them.  Element t of A's lane group g meets pair t of B's group 2 (g % 2) + t / 4 (t < 4 and up alike), its second four
+// pairs for g >= 2.
+typedef __attribute__((ext_vector_type(8))) unsigned int u32x8_v;
+typedef __attribute__((ext_vector_type(16))) __bf16 bf16x16_v;
+constexpr int kEven = 0x8888, kOdd = 0xdddd;
+template <int FEATURE> __device__ __forceinline__ f32x4_v smfma(bf16x8_v p, u32x8_v v, f32x4_v c) {
+    return __builtin_amdgcn_smfmac_f32_16x16x64_bf16(p, __builtin_bit_cast(bf16x16_v, v), c, FEATURE, 0, 0);
+}
+
+template <typename V> __device__ __forceinline__ V lds_at(uint32_t at) {
+    return *(const __attribute__((address_space(3))) V *)(uintptr_t)at;
 }
 
 // 16-byte piece c of K row k sits at piece c ^ k4_swz(k), so that a pass of the operand reads finds its 16 rows (every
@@ -109,12 +148,12 @@ struct Kv4Scales {
     int64_t seq, head;
 };
 
-template <int D, int NB, typename T>
-__global__ __launch_bounds__(512, 1) void stream4_kernel(const Stream4Args args) {
-    using C = Stream4Cfg<D, NB, T>;
+template <int D, int NB, typename T, int W>
+__global__ __launch_bounds__(64 * W, 2) void stream4_kernel(const Stream4Args args) {
+    using C = Stream4Cfg<D, NB, T, W>;
     constexpr int KST = C::KST, DB = C::DB, NQ = C::NQ, SLAB = stream8_slab(D);
     extern __shared__ __align__(16) unsigned char smem[];
-    __shared__ int s_last[2];
+    __shared__ int s_last;
     const StreamCtx a = load_ctx(args);
     Kv4Scales sc = {ptr_bits(args.k_scale), ptr_bits(args.v_scale), args.s_seq, args.s_head};
     asm volatile("" : "+s"(sc.k), "+s"(sc.v), "+s"(sc.seq), "+s"(sc.head));
@@ -124,27 +163,19 @@ __global__ __launch_bounds__(512, 1) void stream4_kernel(const Stream4Args args)
     const int w = blockIdx.x;
     const int TT = a.T, G = a.G, R = TT * G, Hkv = a.Hkv;
 
-    // ---- this workgroup's run of slabs: the first one's unit (b, c) and slab t, and their number ----
-    int b, c, t, left, piece = w;   // piece: this run's number within its unit's pieces, less the unit's
-    if (a.by_unit) {
-        b = __popcll(__ballot(Hkv * a.rec.z <= w)) - 1;   // records past the last row hold the end
-        const int k = a.splits(b), rel = w - Hkv * a.wg0(b), n0 = a.slabs(b);
-        const bool turn = a.by_unit == 1;   // neighbouring workgroups take the row's units in turn
-        const int m = turn ? Hkv : k, x0 = rel / m, x1 = rel - x0 * m;
-        c = turn ? x1 : x0;
-        const int part = turn ? x0 : x1;
-        piece = w - rel + c * k + part;
-        const int lo = n0 / k, hi = n0 - lo * k;   // hi pieces of lo + 1 slabs, then of lo
-        t = part * lo + min(part, hi);
-        left = lo + (part < hi ? 1 : 0);
-    } else {
-        const int g0 = stream_first(w, a.base, a.rem);
-        left = stream_first(w + 1, a.base, a.rem) - g0;
-        b = __popcll(__ballot(Hkv * a.rec.w <= g0)) - 1;
-        const int n0 = a.slabs(b), rel = g0 - Hkv * a.tile0(b);
-        c = rel / n0;
-        t = rel - c * n0;
-    }
+    // ---- this workgroup's piece: slabs t .. t1 - 1 of the unit u = (b, c), keys [key0, key1) ----
+    const int b = __popcll(__ballot(Hkv * a.rec.z <= w)) - 1;   // records past the last row hold the end
+    const int len = a.len(b), nt = len > 0 ? (len - 1) / SLAB + 1 : 1;
+    const int np = a.splits(b), rel = w - Hkv * a.wg0(b);
+    const bool turn = a.by_unit == 1;   // neighbouring workgroups take the row's units in turn
+    const int div = turn ? Hkv : np, x0 = rel / div, x1 = rel - x0 * div;
+    const int c = turn ? x1 : x0, part = turn ? x0 : x1;
+    const int u = b * Hkv + c;
+    const int lo = nt / np, hi = nt - lo * np;   // hi pieces of lo + 1 slabs, then of lo
+    const int t = part * lo + min(part, hi), t1 = t + lo + (part < hi ? 1 : 0);
+    const int64_t key0 = (int64_t)t * SLAB, key1 = min((int64_t)len, (int64_t)t1 * SLAB);
+    const uint8_t *k_base = bits_ptr<const uint8_t>(a.k) + b * a.seq + c * a.head, *v_base = bits_ptr<const uint8_t>(a.v) + b * a.seq + c * a.head;
+    const uint8_t *ks_base = bits_ptr<const uint8_t>(sc.k) + b * sc.seq + c * sc.head, *vs_base = bits_ptr<const uint8_t>(sc.v) + b * sc.seq + c * sc.head;
 
     // ---- loads: lane l of load j (j = 0, 1 for K, and for V) fetches LDS slot cidx % CPR of the chunk's row cidx / CPR
     // (cidx = 64 j + l): for K the row's piece slot ^ swizzle(row).  The second load of a pair adds 1024 to both of its
@@ -160,41 +191,23 @@ __global__ __launch_bounds__(512, 1) void stream4_kernel(const Stream4Args args)
     unsigned char *ring = smem + wave * C::CHUNK;
     unsigned char *ring_s = smem + C::OFF_S + wave * C::SCALES;
     const uint32_t lds_k = lds_addr(ring), lds_s = lds_addr(ring_s);
+    // V operand: keys 4 e + v_row (e < 4), 4 e + (v_row ^ 2) of a step
+    const int v_row = (lg >> 1) | ((lg & 1) << 1);
+    const uint32_t v_at = lds_k + 2048 + v_row * C::RB + lr * (D / 32), vs_at = lds_s + C::KPC * 4 + v_row * 4 + lr * C::CPR / 16;
+    const uint32_t v_at2 = lds_k + 2048 + (v_row ^ 2) * C::RB + lr * (D / 32), vs_at2 = lds_s + C::KPC * 4 + (v_row ^ 2) * 4 + lr * C::CPR / 16;
     const float cs = a.cs;
     float *lse = bits_ptr<float>(a.lse);
-    int pu0 = -1, pu1 = -1;   // units of which this run holds a piece: begun by an earlier workgroup, begun here
-
-    // ---- a segment of the run: slabs t .. t1 - 1 of unit (b, c), keys [key0, key1) ----
-    struct Segment {
-        int b, c, t, t1, nt, len;
-        int64_t key0, key1;
-        const uint8_t *k, *v, *ks, *vs;
-    };
-    auto segment = [&](int b, int c, int t, int left) {
-        Segment x;
-        x.b = b; x.c = c; x.t = t;
-        x.nt = a.slabs(b);
-        x.len = a.len(b);
-        x.t1 = min(x.nt, t + left);
-        x.key0 = (int64_t)t * SLAB;
-        x.key1 = min((int64_t)x.len, (int64_t)x.t1 * SLAB);
-        x.k = bits_ptr<const uint8_t>(a.k) + b * a.seq + c * a.head;
-        x.v = bits_ptr<const uint8_t>(a.v) + b * a.seq + c * a.head;
-        x.ks = bits_ptr<const uint8_t>(sc.k) + b * sc.seq + c * sc.head;
-        x.vs = bits_ptr<const uint8_t>(sc.v) + b * sc.seq + c * sc.head;
-        return x;
-    };
-    auto issue = [&](const Segment &g, int64_t key, int stage) {
+    auto issue = [&](int64_t key, int stage) {
         const uint32_t at = lds_k + stage * STAGE, at_s = lds_s + stage * SSTAGE;
-        const uint8_t *k0 = g.k + key * C::RB, *v0 = g.v + key * C::RB;
-        const int last = (int)min(g.key1 - key, (int64_t)C::KPC) - 1;   // the chunk's last key
+        const uint8_t *k0 = k_base + key * C::RB, *v0 = v_base + key * C::RB;
+        const int last = (int)min(key1 - key, (int64_t)C::KPC) - 1;   // the chunk's last key
         if constexpr (D == 128) {
             const int ln = here(lane), row = min(ln & 31, last);
-            lds_stream4((ln < 32 ? g.ks : g.vs) + (key + row) * 4, at_s);
+            lds_stream4((ln < 32 ? ks_base : vs_base) + (key + row) * 4, at_s);
         } else {
             const int row = min(here(lane), last);
-            lds_stream2(g.ks + (key + row) * 2, at_s);
-            lds_stream2(g.vs + (key + row) * 2, at_s + 256);
+            lds_stream2(ks_base + (key + row) * 2, at_s);
+            lds_stream2(vs_base + (key + row) * 2, at_s + 256);
         }
         if (last == C::KPC - 1) {
             lds_stream16_x2<true>(k0, koff[0], koff[1], at);
@@ -210,14 +223,14 @@ __global__ __launch_bounds__(512, 1) void stream4_kernel(const Stream4Args args)
             }
         }
     };
-    // ---- a unit's queries: fragment (nb, ks) holds feature D/4 * lg + 8 ks + e of row 16 nb + lr; rows past R repeat
-    // the last.  Wave w loads fragments w, w + 8, .. into LDS, 1 KB each as they are used (bf16); fp32 ones as 2 KB that
+    // ---- the unit's queries: fragment (nb, ks) holds feature D/4 * lg + 8 ks + e of row 16 nb + lr; rows past R repeat
+    // the last.  Wave w loads fragments w, w + W, .. into LDS, 1 KB each as they are used (bf16); fp32 ones as 2 KB that
     // split_q turns into their three bf16 terms, each what the ones before leave. ----
-    auto fetch_q = [&](const Segment &g) {
+    auto fetch_q = [&]() {
         const int ln = here(lane), q_lr = ln & 15, q_lg = ln >> 4;
         for (int f = wave; f < KST * NB; f += C::NWV) {
             const int ks = f % KST, row = min(f / KST * 16 + q_lr, R - 1), rt = row / G;
-            const T *src = bits_ptr<const T>(a.q) + (((size_t)g.b * TT + rt) * a.Hq + (size_t)g.c * G + (row - rt * G)) * D +
+            const T *src = bits_ptr<const T>(a.q) + (((size_t)b * TT + rt) * a.Hq + (size_t)c * G + (row - rt * G)) * D +
                            D / 4 * q_lg + 8 * ks;
             unsigned char *dst = smem + C::OFF_Q + f * NQ * 1024;
             lds_stream16(src, dst);
@@ -245,16 +258,18 @@ __global__ __launch_bounds__(512, 1) void stream4_kernel(const Stream4Args args)
     };
 
     constexpr int STEP = C::NWV * C::KPC;
-    Segment g = segment(b, c, t, left);
-    int64_t key = g.key0 + wave * C::KPC;   // this wave's next chunk
-    fetch_q(g);
+    int64_t key = key0 + wave * C::KPC;   // this wave's next chunk
+    fetch_q();
     #pragma unroll
-    for (int s = 0; s < C::PRE; ++s)
-        if (key + s * STEP < g.key1) issue(g, key + s * STEP, s);
+    for (int s = 0; s < C::NST; ++s)
+        if (key + s * STEP < key1) issue(key + s * STEP, s);
     // the wave's oldest chunk (and queries) have landed; the loads of up to `ahead` later chunks may be on their way
     auto landed = [&](int ahead) {
         static_assert(C::LOADS == 5 || C::LOADS == 6, "");
-        if (ahead >= 3) {
+        if (ahead >= 4) {
+            if constexpr (C::LOADS == 5) asm volatile("s_waitcnt vmcnt(20)" : : : "memory");
+            else asm volatile("s_waitcnt vmcnt(24)" : : : "memory");
+        } else if (ahead == 3) {
             if constexpr (C::LOADS == 5) asm volatile("s_waitcnt vmcnt(15)" : : : "memory");
             else asm volatile("s_waitcnt vmcnt(18)" : : : "memory");
         } else if (ahead == 2) {
@@ -268,350 +283,332 @@ __global__ __launch_bounds__(512, 1) void stream4_kernel(const Stream4Args args)
         }
     };
     // this wave's chunks from `key` on: behind the first, at most `most`
-    auto later = [&](int64_t key, int most) { return key < g.key1 ? (int)min((g.key1 - 1 - key) / STEP, (int64_t)most) : 0; };
-    for (bool first = true;; first = false) {
-        const int u = g.b * Hkv + g.c;
-        // the stages that the exchange held; the queries are older than these loads
+    auto later = [&](int64_t key, int most) { return key < key1 ? (int)min((key1 - 1 - key) / STEP, (int64_t)most) : 0; };
+    // (the queries are older than the chunks)
+    landed(key < key1 ? later(key, C::NST - 1) + 1 : 0);
+if constexpr (C::F32) split_q();
+    __syncthreads();
+    bf16x8_v qf[C::QREG ? NB : 1][KST][NQ];
+    if constexpr (C::QREG) {
         #pragma unroll
-        for (int s = C::PRE; s < C::NST; ++s)
-            if (key + s * STEP < g.key1) issue(g, key + s * STEP, s);
-        landed(max(later(key, C::NST - 1) - (C::PRE - 1), 0));
-        if constexpr (C::F32) split_q();
-        __syncthreads();
-        bf16x8_v qf[C::QREG ? NB : 1][KST][NQ];
-        if constexpr (C::QREG) {
+        for (int nb = 0; nb < NB; ++nb)
             #pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
+            for (int ks = 0; ks < KST; ++ks)
                 #pragma unroll
-                for (int ks = 0; ks < KST; ++ks)
+                for (int i = 0; i < NQ; ++i) qf[nb][ks][i] = q_frag(nb, ks, i);
+    }
+
+    f32x4_v o[NB][DB];   // o[nb][j][i]: feature D/16 * lr + j of row 16 nb + 4 lg + i
+    float m_run[NB], l_run[NB];   // m in log2 units; sum of p
+    // the last key that row 16 nb + lr sees (G is a power of two)
+    auto lim = [&](int nb, int lr) { return len - TT + (min(16 * nb + lr, R - 1) >> __builtin_ctz(G)); };
+    #pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+        m_run[nb] = -INFINITY;
+        l_run[nb] = 0.f;
+        #pragma unroll
+        for (int db = 0; db < DB; ++db) o[nb][db] = f32x4_v{0.f, 0.f, 0.f, 0.f};
+    }
+    const int open_to = len - TT;   // keys up to here are seen by every row
+
+    for (int stage = 0; key < key1; key += STEP, stage = stage == C::NST - 1 ? 0 : stage + 1) {
+        const int rest = later(key, 6);
+        if (rest >= 6) __builtin_amdgcn_s_setprio(3);
+        else if (rest >= 4) __builtin_amdgcn_s_setprio(2);
+        else if (rest >= 2) __builtin_amdgcn_s_setprio(1);
+        else __builtin_amdgcn_s_setprio(0);
+        landed(min(rest, C::NST - 1));
+        const unsigned char *st = ring + stage * STAGE, *ss = ring_s + stage * SSTAGE;
+        #pragma unroll
+        for (int kh = 0; kh < C::KPC / 32; ++kh) {
+            // accumulator element i of block blk is key 32 kh + 16 (lg / 2) + 4 i + (lg ^ 2 blk): A row 4 lg' + i of it is that key
+            uint32_t kc[2][KST], vc[8];
+            float ksc[2], vsc[8];
+            #pragma unroll
+            for (int blk = 0; blk < 2; ++blk) {
+                const int kr = 32 * kh + 16 * (lr >> 3) + 4 * (lr & 3) + ((lr >> 2) ^ (2 * blk));
+                if constexpr (D == 128) {
+                    const u32x4_v x = *reinterpret_cast<const u32x4_v *>(st + kr * C::RB + ((lg ^ k4_swz<D>(kr)) << 4));
                     #pragma unroll
-                    for (int i = 0; i < NQ; ++i) qf[nb][ks][i] = q_frag(nb, ks, i);
-        }
-
-        f32x4_v o[NB][DB];   // o[nb][j][i]: feature D/16 * (4 lg + i) + j of row 16 nb + lr
-        float m_run[NB], l_run[NB];   // m in log2 units; sum of p
-        int lim[NB];                          // the last key that row 16 nb + lr sees
-        #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-            m_run[nb] = -INFINITY;
-            l_run[nb] = 0.f;
-            lim[nb] = g.len - TT + min(16 * nb + lr, R - 1) / G;
+                    for (int ks = 0; ks < KST; ++ks) kc[blk][ks] = x[ks];
+                    ksc[blk] = scale_of(ss[kr * 4 + lg]);
+                } else {
+                    const u32x2_v x = *reinterpret_cast<const u32x2_v *>(st + kr * C::RB + (((lg >> 1) ^ k4_swz<D>(kr)) << 4) + 8 * (lg & 1));
+                    #pragma unroll
+                    for (int ks = 0; ks < KST; ++ks) kc[blk][ks] = x[ks];
+                    ksc[blk] = scale_of(ss[kr * 4 + (lg >> 1)]);
+                }
+            }
+            uint32_t at_v[2] = {v_at + stage * STAGE, v_at2 + stage * STAGE}, at_s[2] = {vs_at + stage * SSTAGE, vs_at2 + stage * SSTAGE};
+            asm volatile("" : "+v"(at_v[0]), "+v"(at_v[1]), "+v"(at_s[0]), "+v"(at_s[1]));   // (the rest of an address in its instruction)
             #pragma unroll
-            for (int db = 0; db < DB; ++db) o[nb][db] = f32x4_v{0.f, 0.f, 0.f, 0.f};
-        }
-        const int open_to = g.len - TT;   // keys up to here are seen by every row
-
-        for (int stage = 0; key < g.key1; key += STEP, stage = stage == C::NST - 1 ? 0 : stage + 1) {
-            landed(later(key, C::NST - 1));
-            const unsigned char *st = ring + stage * STAGE, *ss = ring_s + stage * SSTAGE;
-            #pragma unroll
-            for (int kh = 0; kh < C::KPC / 32; ++kh) {
-                // accumulator element i of block blk is key 32 kh + 4 (4 blk + i) + lg: A row 4 lg' + i of it is that key
-                uint32_t kc[2][KST], vc[8];
-                float ksc[2], vsc[8];
+            for (int e = 0; e < 8; ++e) {
+                if constexpr (D == 128) vc[e] = lds_at<uint32_t>(at_v[e >> 2] + (32 * kh + 4 * e) * C::RB);
+                else vc[e] = lds_at<uint16_t>(at_v[e >> 2] + (32 * kh + 4 * e) * C::RB);
+                vsc[e] = scale_of(lds_at<uint8_t>(at_s[e >> 2] + (32 * kh + 4 * e) * 4));
+            }
+            bf16x8_v qc[NB];
+            if constexpr (!C::QREG) {
                 #pragma unroll
-                for (int blk = 0; blk < 2; ++blk) {
-                    const int kr = 32 * kh + 16 * blk + 4 * (lr & 3) + (lr >> 2);
-                    if constexpr (D == 128) {
-                        const u32x4_v x = *reinterpret_cast<const u32x4_v *>(st + kr * C::RB + ((lg ^ k4_swz<D>(kr)) << 4));
+                for (int nb = 0; nb < NB; ++nb) qc[nb] = q_frag(nb, 0, 0);
+            }
+            if (kh == C::KPC / 32 - 1) {
+                asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");   // the stage is read
+                if (key + C::NST * STEP < key1) issue(key + C::NST * STEP, stage);
+            }
+
+            f32x4_v sacc[NB][2];
+            bf16x8_v kf[2];
+            #pragma unroll
+            for (int n = 0; n < KST * NQ; ++n) {   // step ks = n / NQ, query term n % NQ
+                const int ks = n / NQ;
+                bf16x8_v qn[NB];   // the next term's, on their way from LDS
+                if constexpr (!C::QREG) {
+                    if (n + 1 < KST * NQ) {
                         #pragma unroll
-                        for (int ks = 0; ks < KST; ++ks) kc[blk][ks] = x[ks];
-                        ksc[blk] = scale_of(ss[kr * 4 + lg]);
-                    } else {
-                        const u32x2_v x = *reinterpret_cast<const u32x2_v *>(st + kr * C::RB + (((lg >> 1) ^ k4_swz<D>(kr)) << 4) + 8 * (lg & 1));
-                        #pragma unroll
-                        for (int ks = 0; ks < KST; ++ks) kc[blk][ks] = x[ks];
-                        ksc[blk] = scale_of(ss[kr * 4 + (lg >> 1)]);
+                        for (int nb = 0; nb < NB; ++nb) qn[nb] = q_frag(nb, (n + 1) / NQ, (n + 1) % NQ);
                     }
                 }
-                #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int vr = 32 * kh + 4 * e + lg;
-                    const unsigned char *p = st + 2048 + vr * C::RB + lr * (D / 32);
-                    if constexpr (D == 128) vc[e] = *reinterpret_cast<const uint32_t *>(p);
-                    else vc[e] = *reinterpret_cast<const uint16_t *>(p);
-                    vsc[e] = scale_of(ss[C::KPC * 4 + vr * 4 + lr * C::CPR / 16]);
+                if (n % NQ == 0) {
+                    #pragma unroll
+                    for (int blk = 0; blk < 2; ++blk) kf[blk] = codes_bf16(kc[blk][ks], ksc[blk]);
                 }
-                bf16x8_v qc[NB];
+                #pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+                    #pragma unroll
+                    for (int blk = 0; blk < 2; ++blk) {
+                        const f32x4_v acc = n == 0 ? f32x4_v{0.f, 0.f, 0.f, 0.f} : sacc[nb][blk];
+                        if constexpr (C::QREG) sacc[nb][blk] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[blk], qf[nb][ks][n % NQ], acc, 0, 0, 0);
+                        else sacc[nb][blk] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[blk], qc[nb], acc, 0, 0, 0);
+                    }
                 if constexpr (!C::QREG) {
                     #pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) qc[nb] = q_frag(nb, 0, 0);
+                    for (int nb = 0; nb < NB; ++nb) qc[nb] = qn[nb];
                 }
-                if (kh == C::KPC / 32 - 1) {
-                    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");   // the stage is read
-                    if (key + C::NST * STEP < g.key1) issue(g, key + C::NST * STEP, stage);
-                }
-
-                f32x4_v sacc[NB][2];
-                bf16x8_v kf[2];
-                #pragma unroll
-                for (int n = 0; n < KST * NQ; ++n) {   // step ks = n / NQ, query term n % NQ
-                    const int ks = n / NQ;
-                    bf16x8_v qn[NB];   // the next term's, on their way from LDS
-                    if constexpr (!C::QREG) {
-                        if (n + 1 < KST * NQ) {
-                            #pragma unroll
-                            for (int nb = 0; nb < NB; ++nb) qn[nb] = q_frag(nb, (n + 1) / NQ, (n + 1) % NQ);
-                        }
-                    }
-                    if (n % NQ == 0) {
-                        #pragma unroll
-                        for (int blk = 0; blk < 2; ++blk) kf[blk] = codes_bf16(kc[blk][ks], ksc[blk]);
-                    }
-                    #pragma unroll
-                    for (int nb = 0; nb < NB; ++nb)
-                        #pragma unroll
-                        for (int blk = 0; blk < 2; ++blk) {
-                            const f32x4_v acc = n == 0 ? f32x4_v{0.f, 0.f, 0.f, 0.f} : sacc[nb][blk];
-                            if constexpr (C::QREG) sacc[nb][blk] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[blk], qf[nb][ks][n % NQ], acc, 0, 0, 0);
-                            else sacc[nb][blk] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[blk], qc[nb], acc, 0, 0, 0);
-                        }
-                    if constexpr (!C::QREG) {
-                        #pragma unroll
-                        for (int nb = 0; nb < NB; ++nb) qc[nb] = qn[nb];
-                    }
-                    if (n % 2 == 1 || !C::QREG) __builtin_amdgcn_sched_barrier(0);
-                }
-                __builtin_amdgcn_sched_barrier(0);
-                const bool open = key + C::KPC - 1 <= open_to;   // every row sees the whole chunk
-                u32x4_v pk[NB][NQ];   // the probabilities' bf16 terms
+            }
+            const bool open = key + C::KPC - 1 <= open_to;   // every row sees the whole chunk
+            if (!open) {   // hidden scores are -inf from here on
+                const int ln = here(lane), lr = ln & 15, lg = ln >> 4;
                 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
-                    // the lane's largest score (hidden ones -inf from here on)
-                    if (!open) {
-                        const int seen = lim[nb] - (int)key - 32 * kh - lg;   // element e is key 4 e + lg
-                        #pragma unroll
-                        for (int e = 0; e < 8; ++e) sacc[nb][e >> 2][e & 3] = 4 * e <= seen ? sacc[nb][e >> 2][e & 3] : -INFINITY;
-                    }
-                    float mt = sacc[nb][0][0];
                     #pragma unroll
-                    for (int e = 1; e < 8; ++e) mt = fmaxf(mt, sacc[nb][e >> 2][e & 3]);
-                    mt *= cs;
-                    if (__any(mt > m_run[nb] + kLazy4)) {
-                        // the four lanes of a row agree on its maximum; rows that stay have a factor of 1
-                        mt = max_over_row_lanes(mt);
-                        const float mn = mt > m_run[nb] + kLazy4 ? mt : m_run[nb];
-                        const float alpha = mn == m_run[nb] ? 1.f : __builtin_amdgcn_exp2f(m_run[nb] - mn);
-                        l_run[nb] *= alpha;
-                        m_run[nb] = mn;
+                    for (int blk = 0; blk < 2; ++blk) {
+                        const int seen = lim(nb, lr) - (int)key - 32 * kh - 16 * (lg >> 1) - (lg ^ 2 * blk);
                         #pragma unroll
-                        for (int db = 0; db < DB; ++db) o[nb][db] *= alpha;
+                        for (int i = 0; i < 4; ++i) sacc[nb][blk][i] = 4 * i <= seen ? sacc[nb][blk][i] : -INFINITY;
                     }
-                    const float ms = m_run[nb] == -INFINITY ? 0.f : m_run[nb];
-                    float ps = 0.f;
-                    #pragma unroll
-                    for (int h = 0; h < 4; ++h) {
-                        float p0 = __builtin_amdgcn_exp2f(fmaf(sacc[nb][h >> 1][2 * (h & 1)], cs, -ms));
-                        float p1 = __builtin_amdgcn_exp2f(fmaf(sacc[nb][h >> 1][2 * (h & 1) + 1], cs, -ms));
-                        ps += p0 + p1;
-                        #pragma unroll
-                        for (int n = 0; n < NQ; ++n) {
-                            const uint32_t r = cvt_pk_bf16(p0, p1);
-                            pk[nb][n][h] = r;
-                            if (n + 1 < NQ) {
-                                p0 -= bf16_lo(r);
-                                p1 -= bf16_hi(r);
-                            }
-                        }
-                    }
-                    l_run[nb] += ps;
-                    __builtin_amdgcn_sched_barrier(0);
                 }
-                if (!open) {
-                    // NaN scales in V at keys that some row does not see: out of the product, and into the rows that see them
-                    uint32_t any = 0;
+            }
+            float mt[NB];   // the lane's largest score
+            bool grows = false;
+            #pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                mt[nb] = sacc[nb][0][0];
+                #pragma unroll
+                for (int e = 1; e < 8; ++e) mt[nb] = fmaxf(mt[nb], sacc[nb][e >> 2][e & 3]);
+                mt[nb] *= cs;
+                grows |= mt[nb] > m_run[nb] + kLazy4;
+            }
+            if (__any(grows)) {
+                const int lg = here(lane) >> 4;
+                #pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    // the four lanes of a row agree on its maximum; rows that stay have a factor of 1
+                    const float m4 = max_over_row_lanes(mt[nb]);
+                    const float mn = m4 > m_run[nb] + kLazy4 ? m4 : m_run[nb];
+                    const float alpha = mn == m_run[nb] ? 1.f : __builtin_amdgcn_exp2f(m_run[nb] - mn);
+                    l_run[nb] *= alpha;
+                    m_run[nb] = mn;
+                    f32x4_v ar;   // of the rows that this lane accumulates
                     #pragma unroll
-                    for (int e = 0; e < 8; ++e) any |= __float_as_uint(vsc[e]) == 0x7f800000u ? 1u : 0u;
-                    if (__any(any != 0)) {
-                        bf16x8_v is_nan;
-                        #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const bool nan = __float_as_uint(vsc[e]) == 0x7f800000u;
-                            is_nan[e] = nan ? (__bf16)1.f : (__bf16)0.f;
-                            vsc[e] = nan ? 1.f : vsc[e];
-                            vc[e] = nan ? 0u : vc[e];
+                    for (int i = 0; i < 4; ++i) ar[i] = __shfl(alpha, 4 * lg + i);
+                    #pragma unroll
+                    for (int db = 0; db < DB; ++db) o[nb][db] *= ar;
+                }
+            }
+            u32x4_v pk[NB][NQ];   // the probabilities' bf16 terms
+            #pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                const float ms = m_run[nb] == -INFINITY ? 0.f : m_run[nb];
+                float ps[4];
+                #pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    float p0 = __builtin_amdgcn_exp2f(fmaf(sacc[nb][h >> 1][2 * (h & 1)], cs, -ms));
+                    float p1 = __builtin_amdgcn_exp2f(fmaf(sacc[nb][h >> 1][2 * (h & 1) + 1], cs, -ms));
+                    ps[h] = p0 + p1;
+                    #pragma unroll
+                    for (int n = 0; n < NQ; ++n) {
+                        const uint32_t r = cvt_pk_bf16(p0, p1);
+                        pk[nb][n][h] = r;
+                        if (n + 1 < NQ) {
+                            p0 -= bf16_lo(r);
+                            p1 -= bf16_hi(r);
                         }
+                    }
+                }
+                l_run[nb] += (ps[0] + ps[1]) + (ps[2] + ps[3]);
+            }
+            if (!open) {
+                // NaN scales in V at keys that some row does not see: out of the product, and into the rows that see them
+                uint32_t any = 0;
+                #pragma unroll
+                for (int e = 0; e < 8; ++e) any |= __float_as_uint(vsc[e]) == 0x7f800000u ? 1u : 0u;
+                if (__any(any != 0)) {
+                    const int ln = here(lane), lr = ln & 15, lg = ln >> 4;
+                    u32x8_v is_nan;
+                    #pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const bool nan = __float_as_uint(vsc[e]) == 0x7f800000u;
+                        is_nan[e] = nan ? 0x3f803f80u : 0u;   // 1.0 for both features of a pair
+                        vsc[e] = nan ? 1.f : vsc[e];
+                        vc[e] = nan ? 0u : vc[e];
+                    }
+                    #pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) {
+                        bf16x8_v seen;
                         #pragma unroll
-                        for (int nb = 0; nb < NB; ++nb) {
-                            bf16x8_v seen;
+                        for (int e = 0; e < 8; ++e)
+                            seen[e] = 32 * kh + 16 * (lg >> 1) + 4 * (e & 3) + (lg ^ 2 * (e >> 2)) <= lim(nb, lr) - (int)key ? (__bf16)1.f : (__bf16)0.f;
+                        const f32x4_v hit = smfma<kEven>(seen, is_nan, f32x4_v{0.f, 0.f, 0.f, 0.f});
+                        #pragma unroll
+                        for (int db = 0; db < DB; ++db)
                             #pragma unroll
-                            for (int e = 0; e < 8; ++e) seen[e] = 32 * kh + 4 * e + lg <= lim[nb] - (int)key ? (__bf16)1.f : (__bf16)0.f;
-                            const f32x4_v hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(is_nan, seen, f32x4_v{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-                            #pragma unroll
-                            for (int db = 0; db < DB; ++db)
-                                #pragma unroll
-                                for (int i = 0; i < 4; ++i) o[nb][db][i] = hit[i] > 0.f ? __builtin_nanf("") : o[nb][db][i];
-                        }
+                            for (int i = 0; i < 4; ++i) o[nb][db][i] = hit[i] > 0.f ? __builtin_nanf("") : o[nb][db][i];
                     }
                 }
+            }
+            #pragma unroll
+            for (int h = 0; h < DB / 2; ++h) {   // the lane's features 2 h, 2 h + 1
+                u32x8_v v2;
                 #pragma unroll
-                for (int h = 0; h < DB / 2; ++h) {   // the lane's features 2 h, 2 h + 1
-                    u32x4_v f0, f1;
+                for (int e = 0; e < 8; ++e) {
+                    if (h == 0) v2[e] = pair_bf16<0>(vc[e], vsc[e]);
+                    else if (h == 1) v2[e] = pair_bf16<1>(vc[e], vsc[e]);
+                    else if (h == 2) v2[e] = pair_bf16<2>(vc[e], vsc[e]);
+                    else v2[e] = pair_bf16<3>(vc[e], vsc[e]);
+                }
+                #pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
                     #pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        uint32_t y0, y1;
-                        if (h == 0) { y0 = pair_bf16<0>(vc[2 * x], vsc[2 * x]); y1 = pair_bf16<0>(vc[2 * x + 1], vsc[2 * x + 1]); }
-                        else if (h == 1) { y0 = pair_bf16<1>(vc[2 * x], vsc[2 * x]); y1 = pair_bf16<1>(vc[2 * x + 1], vsc[2 * x + 1]); }
-                        else if (h == 2) { y0 = pair_bf16<2>(vc[2 * x], vsc[2 * x]); y1 = pair_bf16<2>(vc[2 * x + 1], vsc[2 * x + 1]); }
-                        else { y0 = pair_bf16<3>(vc[2 * x], vsc[2 * x]); y1 = pair_bf16<3>(vc[2 * x + 1], vsc[2 * x + 1]); }
-                        f0[x] = __builtin_amdgcn_perm(y1, y0, 0x05040100u);
-                        f1[x] = __builtin_amdgcn_perm(y1, y0, 0x07060302u);
+                    for (int n = 0; n < NQ; ++n) {
+                        const bf16x8_v p = __builtin_bit_cast(bf16x8_v, pk[nb][n]);
+                        o[nb][2 * h] = smfma<kEven>(p, v2, o[nb][2 * h]);
+                        o[nb][2 * h + 1] = smfma<kOdd>(p, v2, o[nb][2 * h + 1]);
                     }
-                    #pragma unroll
-                    for (int nb = 0; nb < NB; ++nb)
-                        #pragma unroll
-                        for (int n = 0; n < NQ; ++n) {
-                            const bf16x8_v p = __builtin_bit_cast(bf16x8_v, pk[nb][n]);
-                            o[nb][2 * h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_v, f0), p, o[nb][2 * h], 0, 0, 0);
-                            o[nb][2 * h + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_v, f1), p, o[nb][2 * h + 1], 0, 0, 0);
-                        }
-                    __builtin_amdgcn_sched_barrier(0);
-                }
             }
         }
-
-        // ---- the segment's end.  The next one's first chunks (into the stages that the exchange leaves) and queries
-        // are on their way while the waves' results are added up ----
-        left -= g.t1 - g.t;
-        const bool whole = g.t == 0 && g.t1 == g.nt;   // every slab of the unit ran here
-        if (!whole) {
-            if (first) pu0 = u;   // the run's first unit; another one that does not end here is its last
-            else pu1 = u;
-        }
-        const bool more = left > 0;
-        if (more) {
-            const bool wrap = g.c + 1 == Hkv;
-            g = segment(wrap ? g.b + 1 : g.b, wrap ? 0 : g.c + 1, 0, left);
-            key = g.key0 + wave * C::KPC;
-            #pragma unroll
-            for (int s = 0; s < C::PRE; ++s)
-                if (key + s * STEP < g.key1) issue(g, key + s * STEP, s);
-        }
-        // each wave's (max, sum of p) per row, in log2 units, and from all of them its factor
-        const int x_lane = here(lane), x_lr = x_lane & 15, x_lg = x_lane >> 4;
-        float2 *xml = reinterpret_cast<float2 *>(smem + C::OFF_ML);   // [8][RP]
-        #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-            const float lt = sum_over_row_lanes(l_run[nb]);
-            if (x_lg == 0) xml[wave * C::RP + 16 * nb + x_lr] = make_float2(m_run[nb], lt);
-        }
-        __syncthreads();   // (also: every wave is done with its stages and the queries)
-        if (more) fetch_q(g);
-        float M[NB], L[NB];
-        #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-            float2 ml[C::NWV];
-            M[nb] = -INFINITY;
-            L[nb] = 0.f;
-            #pragma unroll
-            for (int k = 0; k < C::NWV; ++k) {
-                ml[k] = xml[k * C::RP + 16 * nb + x_lr];
-                M[nb] = fmaxf(M[nb], ml[k].x);
-            }
-            const float mr = M[nb] == -INFINITY ? 0.f : M[nb];
-            #pragma unroll
-            for (int k = 0; k < C::NWV; ++k) L[nb] = fmaf(__builtin_amdgcn_exp2f(ml[k].x - mr), ml[k].y, L[nb]);
-            const float wt = __builtin_amdgcn_exp2f(m_run[nb] - mr);
-            #pragma unroll
-            for (int db = 0; db < DB; ++db) o[nb][db] *= wt;
-        }
-        // the sums, XD feature quads at a time: every wave's fragments to LDS as they are (1 KB each), wave w adds up
-        // the w-th of them.  Quad q is features D/4 * lg + 4 q .. + 3: o[nb][4 q % DB + e][4 q / DB].
-        f32x4_v *xo = reinterpret_cast<f32x4_v *>(smem + C::OFF_X) + x_lane;
-        #pragma unroll
-        for (int d0 = 0; d0 < DB; d0 += C::XD) {
-            if (d0 > 0) __syncthreads();
-            #pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
-                #pragma unroll
-                for (int db = 0; db < C::XD; ++db) {
-                    const int j = 4 * (d0 + db) % DB, i = 4 * (d0 + db) / DB;
-                    xo[((nb * C::XD + db) * C::NWV + wave) * 64] = f32x4_v{o[nb][j][i], o[nb][j + 1][i], o[nb][j + 2][i], o[nb][j + 3][i]};
-                }
-            __syncthreads();
-            if (wave < NB * C::XD) {
-                const int nb = wave / C::XD, db = d0 + wave % C::XD, r = 16 * nb + x_lr;
-                f32x4_v y = xo[wave * C::NWV * 64];
-                #pragma unroll
-                for (int k = 1; k < C::NWV; ++k) y += xo[(wave * C::NWV + k) * 64];
-                float mr = M[0], lr_ = L[0];
-                #pragma unroll
-                for (int n = 1; n < NB; ++n) {
-                    mr = nb == n ? M[n] : mr;
-                    lr_ = nb == n ? L[n] : lr_;
-                }
-                const int f = D / 4 * x_lg + 4 * db;   // this lane's four features
-                if (r < R) {
-                    if (whole) {
-                        const size_t head = out_head(a, u, r);
-                        const float inv = lr_ == 0.f ? 0.f : 1.f / lr_;
-                        store_quad(bits_ptr<T>(a.out) + head * D + f, y * inv);
-                        if (lse && f == 0) lse[head] = lr_ == 0.f ? -INFINITY : (mr + log2f(lr_)) * kLn2;
-                    } else {
-                        // runs and units both advance in slab order, so piece + u numbers the pieces one after the other
-                        float *pp = bits_ptr<float>(a.part) + (size_t)(piece + u) * piece_floats(R, D);
-                        store_agent4(pp + r * D + f, y);
-                        if (f == 0) store_agent2(pp + R * D + 2 * r, mr, lr_);
-                    }
-                }
-            }
-        }
-        if (!more) break;
-        __syncthreads();   // the exchange area is the last two stages
     }
-    if ((pu0 < 0 && pu1 < 0) || a.merge2) return;
 
-    // ---- arrivals; the last workgroup at a unit merges its pieces (stream.hip) ----
-    const UnitPieces up0 = unit_pieces(a, max(pu0, 0)), up1 = unit_pieces(a, max(pu1, 0));
+    // each wave's (max, sum of p) per row, in log2 units, and from all of them its factor
+    const int x_lane = here(lane), x_lr = x_lane & 15, x_lg = x_lane >> 4;
+    float2 *xml = reinterpret_cast<float2 *>(smem + C::OFF_ML);   // [W][RP]
+    #pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+        const float lt = sum_over_row_lanes(l_run[nb]);
+        if (x_lg == 0) xml[wave * C::RP + 16 * nb + x_lr] = make_float2(m_run[nb], lt);
+    }
+    __syncthreads();   // (also: every wave is done with its stages)
+    float M[NB], L[NB];
+    #pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+        float2 ml[C::NWV];
+        M[nb] = -INFINITY;
+        L[nb] = 0.f;
+        #pragma unroll
+        for (int k = 0; k < C::NWV; ++k) {
+            ml[k] = xml[k * C::RP + 16 * nb + x_lr];
+            M[nb] = fmaxf(M[nb], ml[k].x);
+        }
+        const float mr = M[nb] == -INFINITY ? 0.f : M[nb];
+        #pragma unroll
+        for (int k = 0; k < C::NWV; ++k) L[nb] = fmaf(__builtin_amdgcn_exp2f(ml[k].x - mr), ml[k].y, L[nb]);
+        const float wt = __builtin_amdgcn_exp2f(m_run[nb] - mr);
+        f32x4_v wr;
+        #pragma unroll
+        for (int i = 0; i < 4; ++i) wr[i] = __shfl(wt, 4 * x_lg + i);
+        #pragma unroll
+        for (int db = 0; db < DB; ++db) o[nb][db] *= wr;
+    }
+    // the sums, some feature quads at a time: every wave's fragments to LDS as they are (1 KB each), wave w adds up every
+    // W-th of them.  Quad q is features D/16 * lr + 4 (q % (D/64)) .. + 3 of row 4 lg + q / (D/64) of a block.
+    const UnitPieces up = unit_pieces(a, u);
+    f32x4_v *xo = reinterpret_cast<f32x4_v *>(smem) + x_lane;
+    #pragma unroll
+    for (int d0 = 0; d0 < DB; d0 += C::XD) {
+        if (d0 > 0) __syncthreads();
+        #pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+            #pragma unroll
+            for (int db = 0; db < C::XD; ++db) {
+                const int j = 4 * ((d0 + db) % (D / 64)), i = (d0 + db) / (D / 64);
+                xo[((nb * C::XD + db) * C::NWV + wave) * 64] = f32x4_v{o[nb][j][i], o[nb][j + 1][i], o[nb][j + 2][i], o[nb][j + 3][i]};
+            }
+        __syncthreads();
+        for (int x = wave; x < NB * C::XD; x += C::NWV) {
+            const int nb = x / C::XD, db = d0 + x % C::XD, row = 4 * x_lg + db / (D / 64), r = 16 * nb + row;
+            f32x4_v y = xo[x * C::NWV * 64];
+            #pragma unroll
+            for (int k = 1; k < C::NWV; ++k) y += xo[(x * C::NWV + k) * 64];
+            float mr = M[0], lr_ = L[0];
+            #pragma unroll
+            for (int n = 1; n < NB; ++n) {
+                mr = nb == n ? M[n] : mr;
+                lr_ = nb == n ? L[n] : lr_;
+            }
+            mr = __shfl(mr, row);
+            lr_ = __shfl(lr_, row);
+            const int f = D / 16 * x_lr + 4 * (db % (D / 64));   // this lane's four features
+            if (r < R) {
+                if (np == 1) {
+                    const size_t head = out_head(a, u, r);
+                    const float inv = lr_ == 0.f ? 0.f : 1.f / lr_;
+                    store_quad(bits_ptr<T>(a.out) + head * D + f, y * inv);
+                    if (lse && f == 0) lse[head] = lr_ == 0.f ? -INFINITY : (mr + log2f(lr_)) * kLn2;
+                } else {
+                    float *pp = bits_ptr<float>(a.part) + (size_t)(up.p0 + part) * piece_floats(R, D);
+                    store_agent4(pp + r * D + f, y);
+                    if (f == 0) store_agent2(pp + R * D + 2 * r, mr, lr_);
+                }
+            }
+        }
+    }
+    if (np == 1 || a.merge2) return;
+
+    // ---- arrivals; the last workgroup at a unit merges its pieces ----
     wait_vm_stores();
     __syncthreads();
-    if (tid == 0 || tid == 64) {
-        const int u = tid == 0 ? pu0 : pu1;
-        int last = 0;
-        if (u >= 0) {
-            unsigned *cnt = bits_ptr<unsigned>(a.counters) + (size_t)u * kCounterStride;
-            last = arrive(cnt) == (unsigned)((tid == 0 ? up0.np : up1.np) - 1);
-            if (last) reset_counter(cnt);
-        }
-        s_last[tid >> 6] = last;
+    if (tid == 0) {
+        unsigned *cnt = bits_ptr<unsigned>(a.counters) + (size_t)u * kCounterStride;
+        s_last = arrive(cnt) == (unsigned)(np - 1);
+        if (s_last) reset_counter(cnt);
     }
     __syncthreads();
+    if (!s_last) return;
     const int pf = piece_floats(R, D);
-    const float *part = bits_ptr<const float>(a.part);
-    const int last = (s_last[0] ? 1 : 0) + (s_last[1] ? 2 : 0);
-    if (last == 0) return;
-    const int bytes0 = (last & 1) ? up0.np * pf * 4 : 0, bytes1 = (last & 2) ? up1.np * pf * 4 : 0;
-    const int at1 = (bytes0 + 1023) & ~1023;
-    __shared__ float sinv[2 * MAD_MAX_VERIFY_ROWS];
-    auto merge = [&](bool first_unit, bool second_unit, int at) {
-        if (first_unit) load_pieces(part + (size_t)up0.p0 * pf, bytes0, smem);
-        if (second_unit) load_pieces(part + (size_t)up1.p0 * pf, bytes1, smem + at);
-        const MergeJob<D, T, true> j0 = {pu0, up0.np, R, smem, smem + R * D * 4, pf * 4, sinv};
-        const MergeJob<D, T, true> j1 = {pu1, up1.np, R, smem + at, smem + at + R * D * 4, pf * 4, sinv + R};
-        wait_vm(0);
-        __syncthreads();
-        if (first_unit) j0.weights(a);
-        if (second_unit) j1.weights(a);
-        __syncthreads();
-        if (first_unit) j0.sums(a);
-        if (second_unit) j1.sums(a);
-    };
-    if (at1 + bytes1 <= kMergeBytes) {
-        merge(last & 1, last & 2, at1);
-    } else {   // one after the other (each fits: plan_stream)
-        merge(true, false, 0);
-        __syncthreads();
-        merge(false, true, 0);
-    }
+    __shared__ float sinv[MAD_MAX_VERIFY_ROWS];
+    load_pieces<C::NT>(bits_ptr<const float>(a.part) + (size_t)up.p0 * pf, np * pf * 4, smem);   // (they fit: plan_stream4)
+    const MergeJob<D, T, true, C::NT> job = {u, np, R, smem, smem + R * D * 4, pf * 4, sinv};
+    wait_vm(0);
+    __syncthreads();
+    job.weights(a);
+    __syncthreads();
+    job.sums(a);
 }
 
 // ------------------------------------------------------------------ host ----
 
+template <int D, int NB, typename T, int W>
+static hipError_t launch_w(const Stream4Args &a, hipStream_t st) {
+    using C = Stream4Cfg<D, NB, T, W>;
+    hipLaunchKernelGGL((stream4_kernel<D, NB, T, W>), dim3((unsigned)a.n_wg), dim3(C::NT), C::SMEM, st, a);
+    return hipGetLastError();
+}
 template <int D, int NB, typename T>
 static hipError_t launch_nb(const Stream4Args &a, hipStream_t st) {
-    using C = Stream4Cfg<D, NB, T>;
-    hipLaunchKernelGGL((stream4_kernel<D, NB, T>), dim3((unsigned)a.n_wg), dim3(64 * C::NWV), C::SMEM, st, a);
-    return hipGetLastError();
+    if constexpr (!std::is_same<T, float>::value) {
+        if (a.waves == 4) return launch_w<D, NB, T, 4>(a, st);
+    }
+    return launch_w<D, NB, T, 8>(a, st);
 }
 
 template <int D, typename T>
@@ -626,6 +623,62 @@ static hipError_t launch_d(const Stream4Args &a, hipStream_t st) {
     if (e != hipSuccess || a.merge2 == 0) return e;
     hipLaunchKernelGGL((stream_merge_kernel<D, T, true>), dim3((unsigned)(a.B * a.Hkv), (unsigned)(a.T * a.G)), dim3(256), 0, st, a);
     return hipGetLastError();
+}
+
+// The pieces: every workgroup one of at most `share` slabs, the smallest share whose pieces find a workgroup's place each
+// (a second round of workgroups costs its start and its end again: 16 sequences of 600 .. 12000 keys, 48 rows, 43 us in 512
+// places, 54 with pieces for 768).
+//
+// Eight waves, one workgroup to a CU, while every unit has a CU; above, four waves and two workgroups to a CU (bf16; in fp32
+// the queries' three terms leave no room for a second one).  Eight -> four, us, d 128: up to 256 units, 20 sequences of 2000
+// keys, 8 KV heads, 15.8 -> 17.5; 32 of 300 .. 6000, 64 rows, 57 -> 62; one of 32773, 40 rows, 23.2 -> 24.1; more units: 40
+// sequences of 1000 keys, 20.4 -> 15.5; 40 of 300 .. 6000, 32 rows, 57 -> 44; 64 of 2000, 33 -> 29.
+void plan_stream4(Stream4Args &a, int B, int Hkv, int d, int dtype, const int *n_keys) {
+    const int slab = stream8_slab(d);
+    const int64_t units = (int64_t)B * Hkv;
+    int64_t total = 0;
+    int nt[kMaxB], nt_max = 1;
+    for (int b = 0; b < B; ++b) {
+        nt[b] = n_keys[b] > 0 ? (n_keys[b] - 1) / slab + 1 : 1;
+        a.row[b].x = n_keys[b];
+        total += (int64_t)nt[b] * Hkv;
+        nt_max = nt[b] > nt_max ? nt[b] : nt_max;
+    }
+    a.B = B;
+    a.Hkv = Hkv;
+    a.waves = units > kStreamWGs && dtype == MAD_BF16 ? 4 : 8;
+    const int64_t places = kStreamWGs * 8 / a.waves;
+    int np_max;
+    auto deal = [&](int64_t share) {   // -> workgroups
+        a.wgs = 0;
+        np_max = 1;
+        for (int b = 0; b < B; ++b) {
+            const int k = (int)((nt[b] - 1) / share + 1);
+            a.row[b].z = a.wgs;
+            a.wgs += k;
+            np_max = k > np_max ? k : np_max;
+        }
+        for (int b = B; b < kMaxB; ++b) a.row[b].z = a.wgs;
+        return (int64_t)a.wgs * Hkv;
+    };
+    int64_t share = units >= places ? nt_max : (total + places - 1) / places;   // (no more places than units: whole ones)
+    if (share < kLeast4) share = kLeast4;
+    while (deal(share) > places && share < nt_max) share += 1 + share / 64;
+    a.n_wg = a.wgs * Hkv;
+    // neighbouring workgroups take the row's units in turn, each XCD its own (plan_stream), where the pieces are short
+    a.by_unit = Hkv % 8 == 0 && share <= (a.T * a.G >= 32 ? 16 : a.T * a.G > 16 ? 3 : 0) ? 1 : 2;
+    // merged by a unit's last workgroup or by a second launch: plan_stream's rule, of what LDS there is
+    const int64_t bytes = (int64_t)np_max * piece_floats(a.T * a.G, d) * 4;
+    const bool in_launch = bytes <= kMergeInLaunch || (units >= 64 && bytes <= kMergeBytes * a.waves / 8) ||
+                           (units >= 32 && np_max <= 4 && bytes <= kMergeFew4);
+    a.merge2 = np_max > 1 && !in_launch ? 1 : 0;
+}
+
+// the counters, and the pieces of units that are not whole (a piece's number is its workgroup's and its unit's)
+size_t verify4_ws_bytes(int B, int Hq, int Hkv, int d, int T) {
+    constexpr size_t places = 2 * kStreamWGs;
+    const size_t units = (size_t)B * Hkv, most = units < places ? units + places : 0;
+    return kCounterRegionBytes + align256(most * piece_floats(T * (Hq / Hkv), d) * 4);
 }
 
 hipError_t launch_stream4(const Stream4Args &a, int dtype, int d, hipStream_t st) {

@@ -81,10 +81,10 @@ __device__ __forceinline__ void store_quad(float *p, f32x4_v y) { *reinterpret_c
 
 // NAN_LSE: a row that saw NaN has an lse of NaN (else -inf).
 // Log-sum-exp merge of the nr rows of unit u from its np pieces as they lie in
-// LDS, by a workgroup of 512 threads: eight lanes per row turn the pieces'
+// LDS, by a workgroup of NT threads: eight lanes per row turn the pieces'
 // (max, sum) into weights, then (behind a barrier) one thread per feature quad.
 // Piece p's o rows are at so + p * po bytes, its (max, sum) pairs at sm + p * po.
-template <int D, typename T, bool NAN_LSE = false>
+template <int D, typename T, bool NAN_LSE = false, int NT = 512>
 struct MergeJob {
     int u, np, nr;
     unsigned char *so, *sm;
@@ -92,7 +92,7 @@ struct MergeJob {
     float *sinv;   // [nr]
 
     __device__ __forceinline__ void weights(const StreamCtx &a) const {
-        for (int r = threadIdx.x >> 3; r < nr; r += 64) {
+        for (int r = threadIdx.x >> 3; r < nr; r += NT / 8) {
             const int l8 = threadIdx.x & 7;
             float M = -INFINITY, L = 0.f;
             for (int p = l8; p < np; p += 8) M = fmaxf(M, reinterpret_cast<const float2 *>(sm + p * po)[r].x);
@@ -113,7 +113,7 @@ struct MergeJob {
         }
     }
     __device__ __forceinline__ void sums(const StreamCtx &a) const {
-        for (int x = threadIdx.x; x < nr * (D / 4); x += 512) {   // feature quad x % (D / 4) of row x / (D / 4)
+        for (int x = threadIdx.x; x < nr * (D / 4); x += NT) {   // feature quad x % (D / 4) of row x / (D / 4)
             const int r = x / (D / 4);
             f32x4_v y = f32x4_v{0.f, 0.f, 0.f, 0.f};
             #pragma unroll 8
@@ -131,8 +131,9 @@ struct MergeJob {
 
 // `bytes` (a multiple of 16) of pieces straight into LDS, whole; lanes past the end read its last 16 bytes
 // again.  The LDS behind is padded to 1 KB.
+template <int NT = 512>
 __device__ __forceinline__ void load_pieces(const float *src, int bytes, unsigned char *lds) {
-    for (int x = (threadIdx.x >> 6) * 1024; x < bytes; x += 8192)
+    for (int x = (threadIdx.x >> 6) * 1024; x < bytes; x += 16 * NT)
         lds_stream16_coherent(reinterpret_cast<const unsigned char *>(src) + min(x + (int)(threadIdx.x & 63) * 16, bytes - 16), lds + x);
 }
 

@@ -184,11 +184,16 @@ def test_attention_pieces(B, Hkv, lens, T, G, d, dtype):
     _attend(_q(B, T, Hkv * G, d, dtype, 3), _bytes(B, Hkv, max(lens) + 3, d, seed=len(lens)), lens, dtype)
 
 
-@pytest.mark.parametrize("T,G", [(1, 4), (5, 8)])
-def test_attention_runs_that_cross_units(T, G):
-    # more units than workgroups: a run begins inside one unit and ends inside another
-    lens = [64 * 5 + 64 * (b % 7) + b for b in range(48)]
-    _attend(_q(48, T, 8 * G, 64, "bf16", 3), _bytes(48, 8, max(lens), 64, seed=1), lens, "bf16")
+@pytest.mark.parametrize("B,Hkv,T,G,d,dtype", [
+    (33, 8, 1, 4, 64, "bf16"), (33, 8, 1, 4, 128, "bf16"), (40, 8, 4, 8, 128, "bf16"), (40, 8, 6, 8, 64, "bf16"),
+    (33, 8, 8, 8, 128, "bf16"), (33, 8, 8, 8, 64, "bf16"), (33, 8, 8, 8, 128, "f32"),
+    (64, 9, 2, 1, 64, "bf16"), (48, 11, 5, 2, 128, "bf16"), (64, 5, 1, 1, 64, "f32")])
+def test_attention_more_units_than_cus(B, Hkv, T, G, d, dtype):
+    # some sequences cut into pieces, the others whole; (64, 9) and (48, 11): more units than places, all whole
+    lens = [b * 13 % 90 if b % 3 else 640 + 11 * b for b in range(B)]
+    lens[5] = 4 * 640
+    lens = [max(n, T) for n in lens]
+    _attend(_q(B, T, Hkv * G, d, dtype, 3), _bytes(B, Hkv, max(lens) + 1, d, seed=1), lens, dtype)
 
 
 @pytest.mark.parametrize("d", [64, 128])

@@ -137,7 +137,7 @@ def test_verify_refuses(mad):
     assert _verify(mad, v, d=96) == mad.MAD_ENOTSUP and _verify(mad, v, dtype=3) == mad.MAD_ENOTSUP
     assert _verify(mad, v, Hq=6) == mad.MAD_ENOTSUP              # group 3
     assert _verify(mad, v, ws=0) == mad.MAD_EWS
-    need = mad.workspace_bytes(mad.MAD_OP_VERIFY, 2, 8, 2, 64, 2)
+    need = mad.workspace_bytes(mad.MAD_OP_VERIFY_KV4, 2, 8, 2, 64, 2)
     assert _verify(mad, v, ws_bytes=need - 1) == mad.MAD_EWS
 
 
