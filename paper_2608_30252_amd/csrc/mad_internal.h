@@ -153,7 +153,7 @@ struct RowsArg {
     int64_t seq, row;    // element strides
 };
 // queries' and keys' norms and rotation (rope.hip)
-constexpr int kRopeWholeTokens = 2048;   // calls of this many tokens: a wave takes all heads of its token
+constexpr int kRopeWaves = 8192;   // waves that the CUs hold: calls of more rounds of heads take two to a wave
 struct NormRopeArgs {
     RowsArg q, k, q_out, k_out;
     const void *q_gamma, *k_gamma;
@@ -169,7 +169,9 @@ hipError_t launch_norm_rope(NormRopeArgs &a, int dtype, int d, hipStream_t st);
 
 // ------------------------------------------------------------------- kv4 ----
 // new rows into the 4-bit cache (kv4.hip)
-constexpr int kKv4WideTiles = 1024;   // calls of this many workgroups with four pieces to a thread take them
+// calls of this many workgroups with four pieces to a thread take them (8 KV heads of d 128, bf16, one piece -> four: 2048 rows
+// 4.5 us -> 4.6, 8192 10.1 -> 9.4, 16384 17.5 -> 16.2)
+constexpr int kKv4WideTiles = 1024;
 __host__ __device__ constexpr int kv4_tile(int d, int pieces) { return 2048 / d * pieces; }   // rows of a workgroup
 struct Kv4AppendArgs {
     RowsArg k_new, v_new, k_held, v_held;

@@ -8,14 +8,18 @@
 // The angle is formed and reduced modulo 2 pi in double precision (mad_device.h),
 // everything else is fp32, rounded to the output's type once.
 //
-// Bound: bytes (every element read and written once).  A wave takes one token: a
-// lane makes one angle's cosine and sine (d / 2 of them serve every head of the
-// token, and are the only transcendental work), the wave exchanges them through
-// LDS, and then 8 (d 128) or 16 (d 64) heads at a time pass through it, a lane
-// with 8 elements of a head's first half and the 8 that they pair with, so the
-// norm's sum is an exchange among 8 or 4 lanes and the rotation is within a lane.
-// Few tokens: a wave takes one such round of heads only, and makes the angles
-// again, so that a call's latency is one round's.
+// Bound: bytes (every element read and written once).  A wave takes 8 (d 128) or 16
+// (d 64) heads of a token at a time: a lane makes one angle's cosine and sine (d / 2
+// of them serve every head of the token, and are the only transcendental work), the
+// wave exchanges them through LDS, and a lane holds 8 elements of a head's first half
+// and the 8 that they pair with, so the norm's sum is an exchange among 8 or 4 lanes
+// and the rotation is within a lane.  A wave takes two such rounds of its token where
+// the call has more waves than the chip holds, else one: making the angles again
+// costs less than waiting for them in longer waves does (64 + 8 heads of d 128, one
+// round -> two -> all nine: 64 tokens 4.8 us -> 5 -> 9.2; 2048 tokens 15.6 -> 14.2 ->
+// 16.8; 14000 tokens 105 -> 99 -> 111).
+// Measured: 14000 tokens, 64 + 8 heads of d 128, bf16, 99 us (5.2 TB/s, a copy's
+// rate); 80 tokens 4.7 us, one token of 32 + 8 heads of d 64 4.6 (a launch).
 #include "mad_device.h"
 #include "mad_internal.h"
 
@@ -115,7 +119,8 @@ static hipError_t launch_t(const NormRopeArgs &a, int d, hipStream_t st) {
 // a.row and a.tokens are set; the waves' shares here
 hipError_t launch_norm_rope(NormRopeArgs &a, int dtype, int d, hipStream_t st) {
     const int per = 64 / (d / 16), rounds = (a.Hq + a.Hkv + per - 1) / per;
-    a.rounds = a.tokens >= kRopeWholeTokens ? rounds : 1;
+    a.rounds = (int64_t)a.tokens * rounds > kRopeWaves ? 2 : 1;
+    while ((int64_t)a.tokens * ((rounds + a.rounds - 1) / a.rounds) > 1 << 25) a.rounds *= 2;   // (a launch has fewer than 2^32 threads)
     a.groups = (rounds + a.rounds - 1) / a.rounds;
     a.items = a.tokens * a.groups;
     return dtype == MAD_BF16 ? launch_t<bf16_t>(a, d, st) : launch_t<float>(a, d, st);
