@@ -9,6 +9,9 @@
  *   - the memory adaptor's update: mirrored K/V projection of new slot
  *     hidden states, RoPE at the slot's position id, append-only write Sec. 3.2
  *   - the target's (gamma+1)-query verify attention over its full KV  Sec. 2.1, 3.3
+ *   - the same over 8-bit and 4-bit caches, with their appends       Sec. 2.1, 3.3
+ *   - norms and position rotation of the target's queries and keys   Sec. 2.1
+ *   - sampling; log probabilities, ranks, entropies of tokens        Sec. 2.1
  *   - the greedy and the stochastic accept/reject rules              Sec. 2.1, 4.1
  *   - the draft's memory-prefill attention                          Sec. 3.3, App.
  *   - the linear maps of a draft decoder layer around the attention  Sec. 2.3, 3.2

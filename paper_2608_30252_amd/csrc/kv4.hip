@@ -13,7 +13,12 @@
 // held are asked for).  A thread takes 8 features (a 16-byte load and one dword of
 // codes), four lanes a group, 8 or 16 a row.  A wave holds consecutive rows of one
 // head, whose codes and scales lie side by side; the heads are neighbours in the
-// grid, since a token's heads lie side by side in the rows that are read.
+// grid, since a token's heads lie side by side in the rows that are read (dealt so
+// that an XCD takes neighbours: 7 % slower).  Large calls: four pieces to a thread
+// (kKv4WideTiles).
+// Measured: 18000 rows of 8 heads of d 128, bf16, K and V, with the values held, 39 us
+// (4.6 TB/s read and written; a copy reaches 5.1), without them 21 (4.5 TB/s); 80 rows
+// 4.4 us (a launch).
 #include "mad_device.h"
 #include "mad_internal.h"
 

@@ -23,6 +23,13 @@
 // Work: a workgroup takes a run of a row's chunks of 8192, its waves 2048 of each
 // and no barrier between the first chunk and the last; with few rows, more
 // workgroups to a row, whose results the last of them to arrive joins.
+//
+// What bounds it: many rows, the vector ALU (85 % busy; an entry takes about 7
+// instructions, one of them an exponential at half rate, and 3 more where it may be
+// above the token's logit); few rows, the chain load - first bound - sums - lists -
+// arrival - join, 0.4 to 3.6 us each.
+// Measured: 2048 rows of 128256, bf16, top 1: 103 - 109 us (5.0 TB/s); 80 rows of
+// 128256, fp32, top 5: 20 us; one row of 50257, top 20: 12.6 us.
 #include "mad_device.h"
 #include "mad_internal.h"
 

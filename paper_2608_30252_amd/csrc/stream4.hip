@@ -40,19 +40,22 @@
 // own ring of LDS stages, for every query row, and add up at the end.  No run of
 // slabs crosses from one unit to the next (plan_stream's do where that balances
 // better): the code for it took registers from the loop and the runs themselves cost
-// more than they balanced (16 sequences of 600 .. 12000 keys: 60 us, 44 by unit; 40
-// such, 32 rows: 83, 44).  The unit's pieces are merged by its last workgroup, or by
+// more than they balanced (16 sequences of 600 .. 12000 keys: 60 us against 47 by
+// unit; 40 such, 32 rows: 83 against 45).  The unit's pieces are merged by its last workgroup, or by
 // a second launch.
 //
 // What bounds it: instructions.  A chunk of 32 keys by 48 rows takes a wave about
-// 64 conversions, 24 dense and 24 sparse products, 24 exponentials and some 150
-// others; without its loads the kernel takes nearly as long, without its arithmetic
-// three quarters.  Waves with more chunks ahead of them go first (s_setprio), so that
-// the workgroup's waves end together: 2 - 6 us of 47.
+// 64 conversions, 24 dense and 24 sparse products, 24 exponentials and some 190
+// others (vector ALU 58 % busy, the matrix cores 24 %, with two waves to a SIMD whose
+// steps depend on each other); without its loads the kernel takes nearly as long.
+// Beside that a start of 5 us, 3.5 for the waves' exchange at 48 rows, and, with
+// ragged lengths, pieces up to a third longer than the mean.  Waves with more chunks
+// ahead of them go first (s_setprio), so that the workgroup's waves end together:
+// 2 - 6 us of 47.
 // Measured (us, d 128 unless given): 16 sequences of 600 .. 12000 keys, 64/8 heads,
-// 6 queries, 104 MB: 42 (2.5 TB/s), 1 query 26 (4.0 TB/s); one of 32773 keys, 5
-// queries, 23; one of 131072 keys, 1 query 31 (4.6 TB/s); 64 of 2000, 1 query 29
-// (4.8 TB/s); one of 317 keys, d 64, 6.1.
+// 6 queries, 104 MB: 40 (2.6 TB/s), 1 query 25 (4.1 TB/s); one of 32773 keys, 5
+// queries, 22; one of 131072 keys, 1 query 30.5 (4.7 TB/s); 64 of 2000, 1 query 29
+// (4.8 TB/s); one of 317 keys, d 64, 6.0.
 //
 // What a row does not see is left out whatever it holds: scores by selection, rows
 // past the length are never read, and where a step with hidden keys has a NaN
@@ -83,10 +86,10 @@ struct Stream4Cfg {
     static constexpr int LOADS = 4 + SCALES / 256;         // direct loads per chunk: 2 + 2 of 1 KB, and the scales
     static constexpr int KST = D / 32, DB = D / 16, NQ = F32 ? 3 : 1;
     static constexpr int RP = NB * 16;                     // padded query rows
-    // query fragments (1 KB each), in registers where they and the accumulators leave room for the rest (two waves to a
-    // SIMD have 256 each): 16 sequences, 48 rows, 43.8 us from LDS, 41.4
+    // query fragments (1 KB each), in registers where those, the accumulators, scores and probabilities leave room for the
+    // rest (two waves to a SIMD have 256 each): 16 sequences, 48 rows, 43.8 us from LDS, 41.4
     static constexpr int QBYTES = NB * KST * NQ * 1024;
-    static constexpr bool QREG = NB * (KST * NQ + DB) * 4 <= 160;
+    static constexpr bool QREG = NB * (KST * NQ + DB + 2 + NQ) * 4 <= 200;
     static constexpr int REST = NWV * RP * 8 + QBYTES, STAGES = NWV * (CHUNK + SCALES);
     static constexpr int NST = 4 * STAGES + REST + 1024 <= LDS ? 4 : 3;   // stages per wave
     static constexpr int RING = NST * NWV * CHUNK;         // stage 0 of every wave, then stage 1, ..
