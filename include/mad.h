@@ -327,7 +327,8 @@ typedef struct mad_rows {
  *   z = RoPE(y, pos)                            (rope_base > 0; else z = y), as
  *       mad_memory_update rotates: pairs (j, j+d/2), angle pos * base^(-2j/d), fp64
  *   q, q_out   Hq heads a row, or both NULL;   k, k_out   Hkv heads, or both NULL.
- *              An output is its input (in place) or shares no element with an input.
+ *              An output is its input (in place) or shares no element with an input
+ *              or the other output.
  *   q_gamma, k_gamma  device [d], dtype, or NULL: no norm
  *   start   HOST int32[B]: row i is at position start[b] + i
  *   pos     device int32 [B][n_cap], any values: the rows' positions.  With a
@@ -380,8 +381,8 @@ typedef struct mad_kv4_view {
  *   an x that is not finite makes its 32 features NaN: scale byte 255, codes 0
  * Other rows and their scales are left as they are.
  *   k_new, v_new    Hkv heads a row, n_cap rows; rows from n[b] on are not read
- *   k_held, v_held  both NULL, or rows like k_new (k_new and v_new themselves
- *                   too) that receive the values that the cache now holds, exact
+ *   k_held, v_held  both NULL, or rows like k_new (k_new itself for k_held, v_new
+ *                   for v_held, too; else sharing no element with them) that receive the values that the cache now holds, exact
  *                   in either type: what the rows' own attention in higher
  *                   precision has to read to see what later steps see
  *   n               HOST int32[B], 0 <= n[b] <= n_cap, len[b] + n[b] <= cap;
@@ -400,7 +401,7 @@ int mad_kv4_append(const mad_rows *k_new, const mad_rows *v_new, const mad_rows 
  *   q    device [B][T][Hq][d], dtype     out  device [B][T][Hq][d], dtype
  *   lse  device fp32 [B][T][Hq] or NULL
  * Sums over a row's keys are formed in fp32: the number of keys times the largest
- * |value| below 2^124.  T * G <= MAD_MAX_VERIFY_ROWS; d in {64, 128}; dtype BF16
+ * |value| below 2^124.  T * G <= MAD_MAX_VERIFY_ROWS; B * Hkv <= 2^20; d in {64, 128}; dtype BF16
  * or F32, both on the matrix cores (a cached value is exact in bf16; F32: q and
  * the probabilities as three bf16 terms each, so that products keep fp32's
  * precision).  Workspace MAD_OP_VERIFY_KV4.

@@ -658,6 +658,8 @@ int mad_qk_norm_rope(const mad_rows *q, const mad_rows *k, const mad_rows *q_out
         return rc;
     if (k && ((rc = check_rows(k, "k", B, n_cap, Hkv, d, dtype, false, &a.k)) || (rc = check_rows(k_out, "k_out", B, n_cap, Hkv, d, dtype, true, &a.k_out))))
         return rc;
+    if (q && k && (q_out->p == k_out->p || q_out->p == k->p || k_out->p == q->p))
+        return fail(MAD_EINVAL, "q_out and k_out: one tensor, or the other's input");
     int64_t tokens = 0;
     for (int b = 0; b < B; ++b) {
         const int nb = n ? n[b] : n_cap;
@@ -704,6 +706,9 @@ int mad_kv4_append(const mad_rows *k_new, const mad_rows *v_new, const mad_rows 
     if ((rc = check_view4(kv, B, Hkv, d))) return rc;
     if (B > 1 && (kv->seq_stride == 0 || kv->scale_seq_stride == 0))
         return fail(MAD_EINVAL, "kv: sequences that share one buffer cannot all append to it");
+    if (kv->k == kv->v || kv->k_scale == kv->v_scale) return fail(MAD_EINVAL, "kv: K and V cannot append to one buffer");
+    if (k_held && (k_held->p == v_held->p || k_held->p == v_new->p || v_held->p == k_new->p))
+        return fail(MAD_EINVAL, "k_held and v_held: one tensor, or the other's new rows");
     // a thread takes four pieces where that leaves enough workgroups
     int64_t rows = 0;
     for (int b = 0; b < B; ++b) {
@@ -749,7 +754,8 @@ int mad_verify_attn_kv4(const void *q, int B, int T, int Hq, int Hkv, int d, int
     if (!q || !out) return fail(MAD_EINVAL, "null q or out");
     if (!aligned16(q) || !aligned16(out)) return fail(MAD_EINVAL, "q/out not 16-byte aligned");
     if ((uintptr_t)lse & 3) return fail(MAD_EINVAL, "lse not 4-byte aligned");
-    if (!(scale > 0.f) || isinf(scale)) return fail(MAD_EINVAL, "scale must be positive and finite");
+    if (!(scale > 0.f) || isinf(scale * 1.4426950408889634f)) return fail(MAD_EINVAL, "scale must be positive and below 2^127");
+    if ((int64_t)B * Hkv > 1 << 20) return fail(MAD_EINVAL, "B*Hkv=%lld: more than a call takes", (long long)B * Hkv);
     if ((rc = check_view4(kv, B, Hkv, d))) return rc;
     const size_t need = mad::verify4_ws_bytes(B, Hq, Hkv, d, T);
     if (!ws) return fail(MAD_EWS, "workspace required (%zu bytes)", need);

@@ -317,3 +317,34 @@ def test_calls_repeat_bit_for_bit_on_streams_and_in_graphs(dtype):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip((out, lse, hk, hv), eager))
+
+
+def test_four_wave_calls_repeat_bit_for_bit_on_streams_and_in_graphs():
+    import bench
+    mad = _mad()
+    B, T = 33, 6
+    lens = [T + 97 * b % 700 for b in range(B)]
+    lens[3] = 3000                                                                  # cut into pieces
+    kv = mad.KV4(*[t.cuda() for t in _bytes(B, 8, 3001, 128, seed=16)], lens)
+    q = [_q(B, T, 64, 128, "bf16", s).cuda() for s in (4, 5)]
+    want = [mad.verify_attn_kv4(x, kv) for x in q]
+    for x, w in zip(q, want):
+        _attend(x.cpu(), [t.cpu() for t in (kv.k, kv.v, kv.k_scale, kv.v_scale)], lens, "bf16", got=w)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    nbytes = mad.workspace_bytes(mad.MAD_OP_VERIFY_KV4, B, 64, 8, 128, T)
+    ws = [torch.zeros(nbytes, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(3):                                                              # two calls at once, a workspace each
+        with torch.cuda.stream(side):
+            a = mad.verify_attn_kv4(q[0], kv, ws=ws[0])
+        b = mad.verify_attn_kv4(q[1], kv, ws=ws[1])
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip((*a, *b), (*want[0], *want[1])))
+    out, lse = torch.empty_like(q[0]), torch.empty(q[0].shape[:3], device="cuda")
+    graphs = [bench.graph_of(torch, lambda x=x: mad.verify_attn_kv4(x, kv, out=out, lse=lse, ws=ws[0])) for x in q]   # one workspace
+    for i in (0, 1, 1, 0):
+        out.fill_(float("nan"))
+        graphs[i].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[i][0]) and torch.equal(lse, want[i][1])

@@ -91,8 +91,9 @@ def test_layouts_and_uneven_rows(out, layout):
 
 @pytest.mark.parametrize("d,dtype", [(64, "bf16"), (128, "f32")])
 def test_many_tokens(d, dtype):
-    # a wave takes all heads of its token; sequences that end anywhere
+    # sequences that end anywhere; one round of heads to a wave, two (the last wave of a token one)
     _check(3, 1500, 8, 2, d, dtype, n=[1500, 37, 1111], out="in place", layout="fused", seed=7)
+    _check(3, 1500, 64, 3, d, dtype, n=[1500, 37, 1111], out="in place", layout="fused", seed=8)
 
 
 @pytest.mark.parametrize("parts", ["q", "k"])

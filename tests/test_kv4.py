@@ -123,8 +123,15 @@ def test_append_refuses(mad):
     assert "more than a call takes" in mad._load_library().mad_last_error().decode()
     shared = _view(mad, seq_stride=0, scale_seq_stride=0)
     assert _append(mad, shared) == mad.MAD_EINVAL                # two sequences write one buffer
-    for held in (_rows(mad), _rows(mad, seq=128, row=256)):      # sequence by sequence, row by row
-        assert _append(mad, v, i32(0, 0), kh=held, vh=held) == mad.MAD_OK   # nothing to do: nothing is launched
+    for lay in (dict(), dict(seq=128, row=256)):                 # sequence by sequence, row by row
+        kh, vh = _rows(mad, **lay), _rows(mad, 1 << 25, **lay)
+        assert _append(mad, v, i32(0, 0), kh=kh, vh=vh) == mad.MAD_OK       # nothing to do: nothing is launched
+    # what would be written twice, or written while it is read
+    a, b, c = _rows(mad), _rows(mad, 1 << 25), _rows(mad, 1 << 26)
+    for kh, vh in ((c, c), (b, c), (c, a)):
+        assert _append(mad, v, i32(0, 0), kh=kh, vh=vh) == mad.MAD_EINVAL
+    for one in (dict(v=1 << 20), dict(v_scale=1 << 22)):
+        assert _append(mad, _view(mad, **one), i32(0, 0)) == mad.MAD_EINVAL
 
 
 def test_verify_refuses(mad):
@@ -136,6 +143,10 @@ def test_verify_refuses(mad):
         assert _verify(mad, v, **kw) == mad.MAD_EINVAL, kw
     assert _verify(mad, v, d=96) == mad.MAD_ENOTSUP and _verify(mad, v, dtype=3) == mad.MAD_ENOTSUP
     assert _verify(mad, v, Hq=6) == mad.MAD_ENOTSUP              # group 3
+    assert _verify(mad, v, scale=2.0 ** 127 * 1.9) == mad.MAD_EINVAL           # times log2 e beyond fp32
+    many = _view(mad, seq_stride=64 * 32 << 20, scale_seq_stride=128 << 20)
+    assert _verify(mad, many, Hq=1 << 20, Hkv=1 << 20) == mad.MAD_EINVAL
+    assert "more than a call takes" in mad._load_library().mad_last_error().decode()
     assert _verify(mad, v, ws=0) == mad.MAD_EWS
     need = mad.workspace_bytes(mad.MAD_OP_VERIFY_KV4, 2, 8, 2, 64, 2)
     assert _verify(mad, v, ws_bytes=need - 1) == mad.MAD_EWS

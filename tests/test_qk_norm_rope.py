@@ -37,6 +37,8 @@ def test_refusals(mad):
         assert _call(mad, **kw) == mad.MAD_EINVAL, kw
     assert _call(mad, d=96) == mad.MAD_ENOTSUP and _call(mad, dtype=3) == mad.MAD_ENOTSUP
     none = i32(0, 0)
+    for kw in (dict(ko=R(1 << 26, seq, row)), dict(qo=R(1 << 25, seq, row)), dict(ko=R(1 << 24, seq, row))):   # written twice, or while it is read
+        assert _call(mad, n=none, **kw) == mad.MAD_EINVAL, kw
     assert _call(mad, n=none) == mad.MAD_OK                                    # nothing to do: nothing is launched
     assert _call(mad, n=none, qo=R(1 << 26, 256, 512)) == mad.MAD_OK           # rows first, the sequences inside a row
     assert _call(mad, n=none, q=R(1 << 24, 0, row)) == mad.MAD_OK              # read only: sequences may share rows
