@@ -65,7 +65,6 @@
 
 namespace mad {
 
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_v;
 typedef __attribute__((ext_vector_type(2))) unsigned int u32x2_v;
 
 constexpr int kLeast4 = 4;             // slabs of a piece, at least (of eight waves each takes a chunk)
