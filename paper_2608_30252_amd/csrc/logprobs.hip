@@ -7,7 +7,7 @@
 //   rank = entries above the token's logit, and equal ones before it.
 // M is some entry times c as fp32 rounds it, so that d is one fused operation with
 // one rounding whatever the logits' offset.  A thread keeps M, s and u of what it
-// has seen, raises M where a step of 32 entries exceeds it by more than 8 (log2
+// has seen, raises M where a step of 16 (32) entries exceeds it by more than 8 (log2
 // units: few steps do), and sums within a step in fp32, over steps and threads in
 // fp64.
 //
@@ -20,16 +20,17 @@
 // row) is thinned first by the bound of its lanes' maxima.  At the end what the lists
 // hold above the largest bound is put in order, again by counting.
 //
-// Work: a workgroup takes a run of a row's chunks of 8192, its waves 2048 of each
-// and no barrier between the first chunk and the last; with few rows, more
+// Work: a workgroup takes a run of a row's chunks of 4096 (8192), its waves a quarter
+// of each and no barrier between the first chunk and the last; with few rows, more
 // workgroups to a row, whose results the last of them to arrive joins.
 //
 // What bounds it: many rows, the vector ALU (85 % busy; an entry takes about 7
 // instructions, one of them an exponential at half rate, and 3 more where it may be
 // above the token's logit); few rows, the chain load - first bound - sums - lists -
 // arrival - join, 0.4 to 3.6 us each.
-// Measured: 2048 rows of 128256, bf16, top 1: 103 - 109 us (5.0 TB/s); 80 rows of
-// 128256, fp32, top 5: 20 us; one row of 50257, top 20: 12.6 us.
+// Measured: 2048 rows of 128256, bf16, top 1: 103 - 112 us (5.0 TB/s); 4096 rows of
+// 2000, top 5: 29 us; 80 rows of 128256, fp32, top 5: 19.8 us; one row of 50257, top
+// 20: 12.4 us.
 #include "mad_device.h"
 #include "mad_internal.h"
 
@@ -478,12 +479,12 @@ __global__ __launch_bounds__(kWg, 4) void logprobs_kernel(const LogprobArgs a) {
     }
 }
 
-// Few rows: 16 entries to a thread and step, and as many workgroups to a row as the CUs hold at once, so that a call is
-// one round of short steps.  Else 32, a workgroup to a row.
+// Few rows: as many workgroups to a row as the CUs hold at once, so that a call is one round (80 rows of 128256, fp32: 20.3 us;
+// in 1280 places 24.2, in 512 20.1).  Else a workgroup to a row.
 LogprobPlan plan_logprobs(int rows, int V) {
     LogprobPlan p;
-    p.entries = (int64_t)rows * V <= kLogprobShort ? 16 : 32;
-    p.n_chunks = (V + 7 + kWg * p.entries - 1) / (kWg * p.entries);   // (a row may begin up to 7 entries into its first 16 bytes)
+    constexpr int chunk = kWg * 16;
+    p.n_chunks = (V + 7 + chunk - 1) / chunk;   // (a row may begin up to 7 entries into its first 16 bytes)
     const int want = rows > kCounterLines / 4 ? 1 : kLogprobWgs / rows < kLogprobSplits ? kLogprobWgs / rows : kLogprobSplits;
     const int each = want < 1 ? p.n_chunks : (p.n_chunks + want - 1) / want;
     p.splits = (p.n_chunks + each - 1) / each;
@@ -495,21 +496,20 @@ size_t logprobs_ws_bytes(int rows, int V) {
     return kCounterRegionBytes + (p.splits > 1 ? align256((size_t)rows * p.splits * sizeof(LogprobRecord)) : 0);
 }
 
-template <typename T>
+template <typename T, int E>
 static hipError_t launch_t(const LogprobArgs &a, hipStream_t st) {
     const dim3 grid((unsigned)(a.rows * a.splits)), wg(kWg);
-    if (a.entries == 16) {
-        if (a.top_n > 0) hipLaunchKernelGGL((logprobs_kernel<T, 16, true>), grid, wg, 0, st, a);
-        else hipLaunchKernelGGL((logprobs_kernel<T, 16, false>), grid, wg, 0, st, a);
-    } else {
-        if (a.top_n > 0) hipLaunchKernelGGL((logprobs_kernel<T, 32, true>), grid, wg, 0, st, a);
-        else hipLaunchKernelGGL((logprobs_kernel<T, 32, false>), grid, wg, 0, st, a);
-    }
+    if (a.top_n > 0) hipLaunchKernelGGL((logprobs_kernel<T, E, true>), grid, wg, 0, st, a);
+    else hipLaunchKernelGGL((logprobs_kernel<T, E, false>), grid, wg, 0, st, a);
     return hipGetLastError();
 }
 
 hipError_t launch_logprobs(const LogprobArgs &a, int dtype, hipStream_t st) {
-    return dtype == MAD_BF16 ? launch_t<bf16_t>(a, st) : launch_t<float>(a, st);
+    if (dtype != MAD_BF16) return launch_t<float, 16>(a, st);
+    if (a.splits > 1 || a.V < kLogprobLong) return launch_t<bf16_t, 16>(a, st);
+    LogprobArgs x = a;
+    x.n_chunks = (a.V + 7 + kWg * 32 - 1) / (kWg * 32);
+    return launch_t<bf16_t, 32>(x, st);
 }
 
 }  // namespace mad

@@ -1060,7 +1060,6 @@ int mad_token_logprobs(const void *logits, int dtype, int64_t seq_stride, int64_
     const mad::LogprobPlan p = mad::plan_logprobs(a.rows, V);
     a.n_chunks = p.n_chunks;
     a.splits = p.splits;
-    a.entries = p.entries;
     return hip_status(mad::launch_logprobs(a, dtype, (hipStream_t)stream), "logprobs launch");
 }
 

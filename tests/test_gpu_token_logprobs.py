@@ -71,6 +71,27 @@ def test_the_largest_vocabulary_and_one_workgroup_rows():
     _check(x, _tok(2, 1500, 700), 3, rows=range(0, 1500, 37))
 
 
+@pytest.mark.parametrize("top_n", [0, 1, 33])
+def test_many_long_rows(top_n):
+    # a workgroup to a row, steps of 32 entries; an odd vocabulary puts the rows at every alignment
+    B, T, V = 9, 65, 65539
+    g = torch.Generator(device="cuda").manual_seed(top_n)
+    x = (2.2 * torch.randn((B, T, V), generator=g, device="cuda")).to(torch.bfloat16)
+    x[0, 0] = torch.arange(V, device="cuda").div(256).floor()                    # rises, in equal values
+    x[0, 1] = -x[0, 0]
+    x[0, 2, ::3] = -float("inf")
+    x[0, 3, 65000] = float("nan")
+    x[0, 4, [7, 65538]] = float("inf")
+    x[1, 0] = torch.finfo(torch.bfloat16).min
+    x[1, 1], x[1, 1, 40000] = -float("inf"), 3.0
+    x[1, 2] = 0.0
+    x[1, 3] = 1e30 * torch.sign(x[1, 3].float())
+    x[1, 4] = -float("inf")
+    tok = _tok(B, T, V, 5)
+    tok[0, 0], tok[0, 1], tok[1, 1], tok[1, 2] = 30000, 30000, 40000, 65538
+    _check(x, tok, top_n, [0.5 + 0.2 * b for b in range(B)], rows=[0, 1, 2, 3, 4, 31, 64])
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_rows_of_few_different_values(dtype):
     """More equal values than the list of candidates holds: in one chunk, in a later one, everywhere."""
