@@ -54,12 +54,14 @@ struct Stats {
     double s, u;
     float m;        // -inf: nothing yet
 };
-// M of a less M of b (a <= b)
+// M of a less M of b (a <= b), one of them rounded where only it is near: logits next to each other lie on both sides of
+// the border
 __device__ __forceinline__ float lower(float a, float b, float c) {
     #pragma clang fp contract(off)   // each M as it was rounded
     const float ma = a * c, mb = b * c;
-    if (!(fabsf(ma) < kNear)) return (a - b) * c;   // (far below any near b)
-    return fabsf(mb) < kNear ? ma - mb : fmaf(-b, c, ma);
+    const bool near_a = fabsf(ma) < kNear, near_b = fabsf(mb) < kNear;
+    if (near_a) return near_b ? ma - mb : fmaf(-b, c, ma);
+    return near_b ? fmaf(a, c, -mb) : (a - b) * c;
 }
 
 // the next number below (-inf: itself)
