@@ -51,6 +51,13 @@ int check_heads(int B, int Hq, int Hkv, int d, int dtype) {
     return MAD_OK;
 }
 
+// T queries of G heads to a KV head are within what a verify call takes (G is checked; T is any number).
+int check_query_rows(int T, int G) {
+    if (T < 1 || T > MAD_MAX_VERIFY_ROWS / G)
+        return fail(MAD_EINVAL, "T=%d: T*G=%lld must be in [1, %d]", T, (long long)T * G, MAD_MAX_VERIFY_ROWS);
+    return MAD_OK;
+}
+
 // Validate a kv view for B sequences; `ring` enables the start array check;
 // rows with append[b] != 0 need room for one more row.
 int check_view(const mad_kv_view *v, const char *name, int B, int Hkv, int d, int dtype, bool ring,
@@ -458,8 +465,7 @@ int verify_impl(const void *q, int B, int T, int Hq, int Hkv, int d, int dtype, 
     if (dtype != MAD_BF16 && !(dtype == MAD_F32 && vnat))
         return fail(MAD_ENOTSUP, "the transposed-V verify runs in bf16 only (matrix cores)");
     const int G = Hq / Hkv;
-    if (T < 1 || T * G > MAD_MAX_VERIFY_ROWS)
-        return fail(MAD_EINVAL, "T=%d: T*G=%d must be in [1, %d]", T, T * G, MAD_MAX_VERIFY_ROWS);
+    if ((rc = check_query_rows(T, G))) return rc;
     if (!q || !k || !v || !out || !len) return fail(MAD_EINVAL, "null q, k, v, out or len");
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out))
         return fail(MAD_EINVAL, "q/k/v/out not 16-byte aligned");
@@ -599,8 +605,7 @@ int mad_verify_attn_kv8(const void *q, int B, int T, int Hq, int Hkv, int d, int
     int rc = check_heads(B, Hq, Hkv, d, dtype);
     if (rc) return rc;
     const int G = Hq / Hkv;
-    if (T < 1 || T * G > MAD_MAX_VERIFY_ROWS)
-        return fail(MAD_EINVAL, "T=%d: T*G=%d must be in [1, %d]", T, T * G, MAD_MAX_VERIFY_ROWS);
+    if ((rc = check_query_rows(T, G))) return rc;
     if (!q || !out) return fail(MAD_EINVAL, "null q or out");
     if (!aligned16(q) || !aligned16(out)) return fail(MAD_EINVAL, "q/out not 16-byte aligned");
     if (!(scale > 0.f) || scale != scale) return fail(MAD_EINVAL, "scale must be positive");
@@ -749,8 +754,7 @@ int mad_verify_attn_kv4(const void *q, int B, int T, int Hq, int Hkv, int d, int
     int rc = check_heads(B, Hq, Hkv, d, dtype);
     if (rc) return rc;
     const int G = Hq / Hkv;
-    if (T < 1 || T * G > MAD_MAX_VERIFY_ROWS)
-        return fail(MAD_EINVAL, "T=%d: T*G=%d must be in [1, %d]", T, T * G, MAD_MAX_VERIFY_ROWS);
+    if ((rc = check_query_rows(T, G))) return rc;
     if (!q || !out) return fail(MAD_EINVAL, "null q or out");
     if (!aligned16(q) || !aligned16(out)) return fail(MAD_EINVAL, "q/out not 16-byte aligned");
     if ((uintptr_t)lse & 3) return fail(MAD_EINVAL, "lse not 4-byte aligned");

@@ -122,6 +122,8 @@ __host__ __device__ inline int stream_owner(int x, int base, int rem) {
 }
 void plan_stream(StreamArgs &a, int B, int Hkv, int d, const int *n_keys);
 hipError_t launch_stream(const StreamArgs &a, int d, hipStream_t st);
+// query rows of a unit; more than a call takes count as the most that one does
+inline int query_rows(int T, int G) { return (int64_t)T * G < MAD_MAX_VERIFY_ROWS ? T * G : MAD_MAX_VERIFY_ROWS; }
 size_t verify_ws_bytes(int B, int Hq, int Hkv, int d, int T);
 size_t stream_part_bytes(int units, int rows, int d);
 

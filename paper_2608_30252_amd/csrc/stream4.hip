@@ -685,7 +685,7 @@ void plan_stream4(Stream4Args &a, int B, int Hkv, int d, int dtype, const int *n
 size_t verify4_ws_bytes(int B, int Hq, int Hkv, int d, int T) {
     constexpr size_t places = 2 * kStreamWGs;
     const size_t units = (size_t)B * Hkv, most = units < places ? units + places : 0;
-    return kCounterRegionBytes + align256(most * piece_floats(T * (Hq / Hkv), d) * 4);
+    return kCounterRegionBytes + align256(most * piece_floats(query_rows(T, Hq / Hkv), d) * 4);
 }
 
 hipError_t launch_stream4(const Stream4Args &a, int dtype, int d, hipStream_t st) {
