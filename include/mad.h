@@ -327,8 +327,8 @@ typedef struct mad_rows {
  *   z = RoPE(y, pos)                            (rope_base > 0; else z = y), as
  *       mad_memory_update rotates: pairs (j, j+d/2), angle pos * base^(-2j/d), fp64
  *   q, q_out   Hq heads a row, or both NULL;   k, k_out   Hkv heads, or both NULL.
- *              An output is its input (in place) or shares no element with an input
- *              or the other output.
+ *              An output is its input (in place, with its strides) or shares no
+ *              element with an input or the other output.
  *   q_gamma, k_gamma  device [d], dtype, or NULL: no norm
  *   start   HOST int32[B]: row i is at position start[b] + i
  *   pos     device int32 [B][n_cap], any values: the rows' positions.  With a
@@ -381,8 +381,9 @@ typedef struct mad_kv4_view {
  *   an x that is not finite makes its 32 features NaN: scale byte 255, codes 0
  * Other rows and their scales are left as they are.
  *   k_new, v_new    Hkv heads a row, n_cap rows; rows from n[b] on are not read
- *   k_held, v_held  both NULL, or rows like k_new (k_new itself for k_held, v_new
- *                   for v_held, too; else sharing no element with them) that receive the values that the cache now holds, exact
+ *   k_held, v_held  both NULL, or rows like k_new (k_new itself, with its strides,
+ *                   for k_held, v_new for v_held, too; else sharing no element with
+ *                   them) that receive the values that the cache now holds, exact
  *                   in either type: what the rows' own attention in higher
  *                   precision has to read to see what later steps see
  *   n               HOST int32[B], 0 <= n[b] <= n_cap, len[b] + n[b] <= cap;

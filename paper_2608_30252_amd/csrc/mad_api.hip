@@ -161,6 +161,19 @@ int check_rows(const mad_rows *r, const char *name, int B, int n_cap, int heads,
     return MAD_OK;
 }
 
+// An output at its input's place has its strides, else a row would be written over another that is still to be read (those
+// that separate rows of this call count).
+int check_in_place(const mad::RowsArg &in, const mad::RowsArg &out, const char *name, const int32_t *n, int B, int n_cap) {
+    if (in.p != out.p) return MAD_OK;
+    for (int b = 0; b < B; ++b) {
+        const int nb = n ? n[b] : n_cap;
+        if ((nb > 1 && in.row != out.row) || (nb > 0 && b > 0 && in.seq != out.seq))
+            return fail(MAD_EINVAL, "%s: its input's place, other strides (seq %lld for %lld, row %lld for %lld)", name,
+                        (long long)out.seq, (long long)in.seq, (long long)out.row, (long long)in.row);
+    }
+    return MAD_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -665,6 +678,7 @@ int mad_qk_norm_rope(const mad_rows *q, const mad_rows *k, const mad_rows *q_out
         return rc;
     if (q && k && (q_out->p == k_out->p || q_out->p == k->p || k_out->p == q->p))
         return fail(MAD_EINVAL, "q_out and k_out: one tensor, or the other's input");
+    if ((q && (rc = check_in_place(a.q, a.q_out, "q_out", n, B, n_cap))) || (k && (rc = check_in_place(a.k, a.k_out, "k_out", n, B, n_cap)))) return rc;
     int64_t tokens = 0;
     for (int b = 0; b < B; ++b) {
         const int nb = n ? n[b] : n_cap;
@@ -714,6 +728,8 @@ int mad_kv4_append(const mad_rows *k_new, const mad_rows *v_new, const mad_rows 
     if (kv->k == kv->v || kv->k_scale == kv->v_scale) return fail(MAD_EINVAL, "kv: K and V cannot append to one buffer");
     if (k_held && (k_held->p == v_held->p || k_held->p == v_new->p || v_held->p == k_new->p))
         return fail(MAD_EINVAL, "k_held and v_held: one tensor, or the other's new rows");
+    if (k_held && ((rc = check_in_place(a.k_new, a.k_held, "k_held", n, B, n_cap)) || (rc = check_in_place(a.v_new, a.v_held, "v_held", n, B, n_cap))))
+        return rc;
     // a thread takes four pieces where that leaves enough workgroups
     int64_t rows = 0;
     for (int b = 0; b < B; ++b) {
