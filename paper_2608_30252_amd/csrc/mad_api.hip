@@ -36,7 +36,7 @@ bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
 
 int elem_size(int dtype) { return dtype == MAD_BF16 ? 2 : 4; }
 
-bool pow2_group(int G) { return G == 1 || G == 2 || G == 4 || G == 8 || G == 16; }
+bool pow2_group(int G) { return G >= 1 && G <= mad::kMaxGroup && (G & (G - 1)) == 0; }
 
 int log2_of(int x) { return 31 - __builtin_clz((unsigned)x); }
 

@@ -10,6 +10,7 @@
 namespace mad {
 
 constexpr int kMaxB = MAD_MAX_BATCH;
+constexpr int kMaxGroup = 16;   // query heads to a KV head
 
 // ---------------------------------------------------------------- decode ----
 // The split count aims at one 4-wave or two 8-wave workgroups per CU; splits

@@ -681,11 +681,14 @@ void plan_stream4(Stream4Args &a, int B, int Hkv, int d, int dtype, const int *n
     a.merge2 = np_max > 1 && !in_launch ? 1 : 0;
 }
 
-// the counters, and the pieces of units that are not whole (a piece's number is its workgroup's and its unit's)
+// The counters, and the pieces of units that are not whole: a piece's number is its workgroup's and its unit's, and from as
+// many units as places on all are whole.  A workspace holds every call of at most these sizes, so that fewer units (B of 64
+// whole ones, then B of 1) and fewer KV heads of larger groups count: never less where a size grows.
 size_t verify4_ws_bytes(int B, int Hq, int Hkv, int d, int T) {
-    constexpr size_t places = 2 * kStreamWGs;
-    const size_t units = (size_t)B * Hkv, most = units < places ? units + places : 0;
-    return kCounterRegionBytes + align256(most * piece_floats(query_rows(T, Hq / Hkv), d) * 4);
+    constexpr int64_t places = 2 * kStreamWGs;
+    const int64_t units = (int64_t)B * Hkv, most = (units < places ? units : places - 1) + places;
+    const int rows = query_rows(T, Hq < kMaxGroup ? Hq : kMaxGroup);
+    return kCounterRegionBytes + align256((size_t)most * piece_floats(rows, d) * 4);
 }
 
 hipError_t launch_stream4(const Stream4Args &a, int dtype, int d, hipStream_t st) {
