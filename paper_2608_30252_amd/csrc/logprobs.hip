@@ -493,9 +493,13 @@ LogprobPlan plan_logprobs(int rows, int V) {
     return p;
 }
 
+// The counters, and a record for each workgroup of a row that has several: at most kLogprobWgs in all, and a chunk each.  A
+// workspace holds every call of at most these sizes, so that fewer rows count, which take more workgroups each, and shorter ones,
+// whose chunks may divide into more: never less where a size grows.
 size_t logprobs_ws_bytes(int rows, int V) {
-    const LogprobPlan p = plan_logprobs(rows, V);
-    return kCounterRegionBytes + (p.splits > 1 ? align256((size_t)rows * p.splits * sizeof(LogprobRecord)) : 0);
+    const int chunks = plan_logprobs(rows, V).n_chunks, most = chunks < kLogprobSplits ? chunks : kLogprobSplits;
+    const int64_t records = (int64_t)rows * most < kLogprobWgs ? (int64_t)rows * most : kLogprobWgs;
+    return kCounterRegionBytes + (most > 1 ? align256((size_t)records * sizeof(LogprobRecord)) : 0);
 }
 
 template <typename T, int E>

@@ -17,3 +17,15 @@ def test_attention_over_4_bits(d):
         q = _q(B, T, Hq, d, "bf16", B).cuda()
         want, got = mad.verify_attn_kv4(q, part), mad.verify_attn_kv4(q, part, ws=ws)
         assert all(torch.equal(a, b) for a, b in zip(want, got)), (B, Hq, Hkv, T)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_log_probabilities(dtype):
+    import paper_2608_30252_amd as mad
+    ws = torch.zeros(mad.workspace_bytes(mad.MAD_OP_LOGPROBS, 64, T=64, max_keys=128256), dtype=torch.uint8, device="cuda")
+    for B, T, V in ((64, 64, 300), (1, 1, 128256), (1, 1, 70000), (1, 1, 65000), (8, 9, 50257), (63, 8, 9001)):
+        g = torch.Generator(device="cuda").manual_seed(V)
+        x = torch.randn(B, T, V, generator=g, device="cuda").to(dtype)
+        tok = torch.randint(0, V, (B, T), generator=g, device="cuda", dtype=torch.int32)
+        want, got = mad.token_logprobs(x, tok, 20), mad.token_logprobs(x, tok, 20, ws=ws)
+        assert all(torch.equal(a, b) for a, b in zip(want, got)), (B, T, V)

@@ -53,3 +53,21 @@ def test_attention_over_4_bits_holds_its_pieces(mad, d):
             units, piece = B * Hkv, (T * G * (d + 2) + 3) // 4 * 16
             need = (1 << 20) + (units < 512) * (units + 512) * piece
             assert mad.workspace_bytes(mad.MAD_OP_VERIFY_KV4, B, Hkv * G, Hkv, d, T) >= need, (B, Hkv, G, T)
+
+
+def test_log_probabilities(mad):
+    size = lambda B, T, V: mad.workspace_bytes(mad.MAD_OP_LOGPROBS, B, T=T, max_keys=V)   # noqa: E731
+    _grows(size, dict(B=BATCHES, T=[1, 2, 3, 5, 8, 9, 15, 16, 17, 33, 64, 65, 1000, 1024, 65536],
+                      V=[1, 7, 4089, 4090, 8185, 8186, 16384, 30000, 50257, 65000, 65535, 70000, 128256, 262144, 1 << 20]))
+
+
+def test_log_probabilities_hold_their_records(mad):
+    """Up to 1024 rows take up to 1024 / rows workgroups of whole chunks each, 16 at most, and a record for each."""
+    record, region = 16 + 8 + 8 + 8 * 64, 1 << 20
+    for rows in list(range(1, 70)) + [100, 255, 256, 257, 341, 342, 511, 512, 513, 1023, 1024, 1025]:
+        for V in (1, 4089, 4090, 30000, 50257, 65000, 70000, 128256, 1 << 20):
+            chunks = -(-(V + 7) // 4096)
+            want = 1 if rows > 1024 else min(1024 // rows, 16)
+            splits = -(-chunks // -(-chunks // want))
+            need = region + (rows * splits * record if splits > 1 else 0)
+            assert mad.workspace_bytes(mad.MAD_OP_LOGPROBS, 1, T=rows, max_keys=V) >= need, (rows, V)
