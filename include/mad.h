@@ -506,7 +506,7 @@ int mad_sample(const void *logits, int dtype, const float *u, const double *temp
  *           a stride counts only where there is more than one).  The aligned
  *           16-byte pieces that hold a row's ends are read whole.
  *   tok     device int32 [B][T], or NULL: then logp and rank are NULL too
- *   temperature   HOST double [B], finite and above 0; NULL: 1
+ *   temperature   HOST double [B], 2^-126 to 2^126; NULL: 1
  *   logp, entropy   device float32 [B][T] or NULL;  rank  device int32 [B][T] or NULL
  *   top_tok, top_logp   device int32, float32 [B][T][top_n]; NULL where top_n is 0
  * 0 <= top_n <= min(V, MAD_MAX_TOP); B <= MAD_MAX_BATCH, B * T <= 2^22,

@@ -1055,8 +1055,9 @@ int mad_token_logprobs(const void *logits, int dtype, int64_t seq_stride, int64_
     memset(&a, 0, sizeof(a));
     for (int b = 0; b < B; ++b) {
         const double t = temperature ? temperature[b] : 1.0;
-        if (!(t > 0.0) || isinf(t)) return fail(MAD_EINVAL, "temperature[%d]=%g must be finite and > 0", b, t);
-        a.c[b] = (float)fmax(fmin(1.4426950408889634 / t, 1e30), 1e-30);   // (0 and inf would make NaN of differences)
+        // (beyond, the factor is no normal fp32 number: 0 and inf make NaN of differences)
+        if (!(t >= 0x1p-126) || t > 0x1p126) return fail(MAD_EINVAL, "temperature[%d]=%g outside [2^-126, 2^126]", b, t);
+        a.c[b] = (float)(1.4426950408889634 / t);
     }
     const size_t need = mad::logprobs_ws_bytes(B * T, V);
     if (!ws) return fail(MAD_EWS, "workspace required (%zu bytes)", need);
