@@ -69,6 +69,8 @@ typedef __attribute__((ext_vector_type(2))) unsigned int u32x2_v;
 
 constexpr int kLeast4 = 4;             // slabs of a piece, at least (of eight waves each takes a chunk)
 constexpr int kMergeFew4 = 64 << 10;   // pieces of a unit that are merged in the launch where the units are few
+constexpr int merge4_bytes(int waves) { return kMergeBytes * waves / 8; }   // ... at most: what a workgroup of that many waves has in LDS
+static_assert(kMergeInLaunch <= merge4_bytes(4) && kMergeFew4 <= merge4_bytes(4), "the pieces that plan_stream4 has merged in the launch fit");
 constexpr float kLazy4 = 4.f;      // the maximum is raised where a score exceeds it by more (log2 units)
 
 // T: bf16_t or float (queries and output); W: waves of a workgroup, 8 or 4 (two workgroups to a CU)
@@ -96,7 +98,7 @@ struct Stream4Cfg {
     static constexpr int OFF_ML = OFF_S + NST * NWV * SCALES;   // the waves' (maximum, sum) per row
     static constexpr int OFF_Q = OFF_ML + NWV * RP * 8;
     static constexpr int USED = OFF_Q + QBYTES;
-    static constexpr int MERGE = kMergeBytes * W / 8;      // pieces that are merged in the launch
+    static constexpr int MERGE = merge4_bytes(W);          // pieces that are merged in the launch
     static constexpr int SMEM = USED > MERGE ? USED : MERGE;
     // the waves' exchange goes through the stages, XD feature quads of a lane at a time
     static constexpr int XD = NB * DB <= 4 * NST ? DB : NB * 4 <= 4 * NST ? 4 : 2;
@@ -676,7 +678,7 @@ void plan_stream4(Stream4Args &a, int B, int Hkv, int d, int dtype, const int *n
     a.by_unit = Hkv % 8 == 0 && share <= (a.T * a.G >= 32 ? 16 : a.T * a.G > 16 ? 3 : 0) ? 1 : 2;
     // merged by a unit's last workgroup or by a second launch: plan_stream's rule, of what LDS there is
     const int64_t bytes = (int64_t)np_max * piece_floats(a.T * a.G, d) * 4;
-    const bool in_launch = bytes <= kMergeInLaunch || (units >= 64 && bytes <= kMergeBytes * a.waves / 8) ||
+    const bool in_launch = bytes <= kMergeInLaunch || (units >= 64 && bytes <= merge4_bytes(a.waves)) ||
                            (units >= 32 && np_max <= 4 && bytes <= kMergeFew4);
     a.merge2 = np_max > 1 && !in_launch ? 1 : 0;
 }
