@@ -26,21 +26,6 @@ namespace mad {
 
 typedef float f32x2_v __attribute__((ext_vector_type(2)));
 
-__device__ __forceinline__ void load8(const bf16_t *p, float (&f)[8]) {
-    unpack16(*reinterpret_cast<const uint4 *>(p), f, bf16_t());
-}
-__device__ __forceinline__ void load8(const float *p, float (&f)[8]) {
-    const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
-    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
-    f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-}
-__device__ __forceinline__ void store8(bf16_t *p, const float (&f)[8]) {   // (values of a code and a scale: exact)
-    *reinterpret_cast<uint4 *>(p) = make_uint4(cvt_pk_bf16(f[0], f[1]), cvt_pk_bf16(f[2], f[3]), cvt_pk_bf16(f[4], f[5]), cvt_pk_bf16(f[6], f[7]));
-}
-__device__ __forceinline__ void store8(float *p, const float (&f)[8]) {
-    reinterpret_cast<float4 *>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
-    reinterpret_cast<float4 *>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
-}
 __device__ __forceinline__ uint32_t or_dpp4(uint32_t v) { return v | (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x141, 0xF, 0xF, true); }
 __device__ __forceinline__ uint32_t or_dpp8(uint32_t v) { return v | (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x140, 0xF, 0xF, true); }
 
@@ -108,7 +93,7 @@ __global__ __launch_bounds__(256) void kv4_append_kernel(const Kv4AppendArgs a) 
                 const f32x2_v p0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 0), p1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 1);
                 const f32x2_v p2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 2), p3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 3);
                 const float y[8] = {p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
-                store8(back + i * held.row, y);
+                store8(back + i * held.row, y);   // (exact: values of a code and a scale)
             }
         }
     }

@@ -45,16 +45,6 @@ __device__ __forceinline__ float scale_for(float m) {
     return __uint_as_float((uint32_t)(max(k, -100) + 127) << 23);
 }
 
-// 8 consecutive elements of a row as fp32
-__device__ __forceinline__ void load8(const bf16_t *p, float (&f)[8]) {
-    unpack16(*reinterpret_cast<const uint4 *>(p), f, bf16_t());
-}
-__device__ __forceinline__ void load8(const float *p, float (&f)[8]) {
-    const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
-    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
-    f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-}
-
 // NC: 8-element pieces per thread, NC * 256 * 8 >= block * d
 template <typename T, int NC>
 __global__ __launch_bounds__(256) void kv8_append_kernel(const Kv8AppendArgs a) {

@@ -74,10 +74,6 @@ __device__ __forceinline__ float value_of(uint64_t key) {
     const uint32_t o = (uint32_t)(key >> 32);
     return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o);
 }
-__device__ __forceinline__ uint64_t read_lane_u64(uint64_t v, int l) {
-    return ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(v >> 32), l) << 32) |
-           (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, l);
-}
 __device__ __forceinline__ uint64_t max_u64(uint64_t a, uint64_t b) { return a > b ? a : b; }
 
 // A value that n of the lanes' values g (G to a lane) reach, n of them at least: the n-th largest but for its low 16 bits

@@ -60,6 +60,23 @@ __device__ __forceinline__ void unpack16(const uint4 &u, float (&f)[8], bf16_t) 
     f[4] = bf16_lo(u.z); f[5] = bf16_hi(u.z); f[6] = bf16_lo(u.w); f[7] = bf16_hi(u.w);
 }
 
+// eight consecutive elements (16-byte aligned) as fp32, and back, each rounded once
+__device__ __forceinline__ void load8(const bf16_t *p, float (&f)[8]) {
+    unpack16(*reinterpret_cast<const uint4 *>(p), f, bf16_t());
+}
+__device__ __forceinline__ void load8(const float *p, float (&f)[8]) {
+    const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
+    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
+    f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+}
+__device__ __forceinline__ void store8(bf16_t *p, const float (&f)[8]) {
+    *reinterpret_cast<uint4 *>(p) = make_uint4(cvt_pk_bf16(f[0], f[1]), cvt_pk_bf16(f[2], f[3]), cvt_pk_bf16(f[4], f[5]), cvt_pk_bf16(f[6], f[7]));
+}
+__device__ __forceinline__ void store8(float *p, const float (&f)[8]) {
+    reinterpret_cast<float4 *>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
+    reinterpret_cast<float4 *>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
+}
+
 // Cross-lane exchange inside a wave64, all on the vector ALU (no LDS
 // crossbar).  Patterns 1 and 2 use DPP quad permutes, 4 and 8 use DPP row
 // mirrors (valid for sum/max reductions over aligned groups); across 16 and

@@ -25,22 +25,6 @@
 
 namespace mad {
 
-__device__ __forceinline__ void load8f(const bf16_t *p, float (&f)[8]) {
-    unpack16(*reinterpret_cast<const uint4 *>(p), f, bf16_t());
-}
-__device__ __forceinline__ void load8f(const float *p, float (&f)[8]) {
-    const float4 a = reinterpret_cast<const float4 *>(p)[0], b = reinterpret_cast<const float4 *>(p)[1];
-    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
-    f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-}
-__device__ __forceinline__ void store8f(bf16_t *p, const float (&f)[8]) {
-    *reinterpret_cast<uint4 *>(p) = make_uint4(cvt_pk_bf16(f[0], f[1]), cvt_pk_bf16(f[2], f[3]), cvt_pk_bf16(f[4], f[5]), cvt_pk_bf16(f[6], f[7]));
-}
-__device__ __forceinline__ void store8f(float *p, const float (&f)[8]) {
-    reinterpret_cast<float4 *>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
-    reinterpret_cast<float4 *>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
-}
-
 template <typename T, int D>
 __global__ __launch_bounds__(256) void norm_rope_kernel(const NormRopeArgs a) {
     constexpr int H = D / 2, LPH = D / 16, HPW = 64 / LPH;   // lanes per head, heads per wave and round
@@ -83,12 +67,12 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(const NormRopeArgs a) {
         T *dst = reinterpret_cast<T *>(out.p) + b * out.seq + i * out.row + h * D + 8 * sub;
         const T *gamma = reinterpret_cast<const T *>(is_k ? a.k_gamma : a.q_gamma);
         float x[8], y[8];
-        load8f(src, x);
-        load8f(src + H, y);
+        load8(src, x);
+        load8(src + H, y);
         if (gamma) {
             float g0[8], g1[8], ss = 0.f;
-            load8f(gamma + 8 * sub, g0);
-            load8f(gamma + 8 * sub + H, g1);
+            load8(gamma + 8 * sub, g0);
+            load8(gamma + 8 * sub + H, g1);
             #pragma unroll
             for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], fmaf(y[e], y[e], ss));
             ss = group_sum<LPH>(ss);
@@ -103,8 +87,8 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(const NormRopeArgs a) {
             #pragma unroll
             for (int e = 0; e < 8; ++e) rope_apply(x[e], y[e], c[e], s[e], &x[e], &y[e]);
         }
-        store8f(dst, x);
-        store8f(dst + H, y);
+        store8(dst, x);
+        store8(dst + H, y);
     }
 }
 
