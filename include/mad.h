@@ -335,8 +335,10 @@ typedef struct mad_rows {
  *           rotation one of start and pos is given, the other NULL.
  *   n       HOST int32[B], 0 <= n[b] <= n_cap (NULL: n_cap); rows from n[b] on
  *           are neither read nor written
- * dtype F32 or BF16; d in {64, 128}.  The squares' sum is formed in fp32: |x| below 2^60.
- * rope_base 0 (no rotation) or finite and above 1.  No workspace.
+ * dtype F32 or BF16; d in {64, 128}; Hq, Hkv <= 4096; at most 2^24 rows in all.
+ * The squares' sum is formed in fp32: |x| below 2^60, and with eps below 2^-100 a
+ * head's largest |x| above 2^-50.  rope_base 0 (no rotation) or finite and above
+ * 1.  No workspace.
  */
 int mad_qk_norm_rope(const mad_rows *q, const mad_rows *k, const mad_rows *q_out, const mad_rows *k_out, const void *q_gamma,
                      const void *k_gamma, float eps, double rope_base, const int32_t *start, const int32_t *pos,
@@ -388,7 +390,8 @@ typedef struct mad_kv4_view {
  *                   precision has to read to see what later steps see
  *   n               HOST int32[B], 0 <= n[b] <= n_cap, len[b] + n[b] <= cap;
  *                   NULL = n_cap for every sequence
- * dtype F32 or BF16; d in {64, 128}.  No workspace.
+ * dtype F32 or BF16; d in {64, 128}; Hkv <= 4096; new rows of all sequences times
+ * Hkv up to 2^28.  No workspace.
  */
 int mad_kv4_append(const mad_rows *k_new, const mad_rows *v_new, const mad_rows *k_held, const mad_rows *v_held,
                    const int32_t *n, int B, int n_cap, int Hkv, int d, int dtype, const mad_kv4_view *kv, void *stream);
@@ -497,6 +500,7 @@ int mad_sample(const void *logits, int dtype, const float *u, const double *temp
  *              values by the lower index first (0: the most probable)
  *   entropy  = - sum p log p
  *   top_tok, top_logp   the first top_n entries of that order and their log p
+ * (log p below what fp32 holds: -inf.)
  * A v outside [0, V) is no token: logp -inf, rank V.  -inf is an entry of
  * probability 0 (log p = -inf); +inf takes the whole mass, shared by equal ones.
  * A row with a NaN, or with nothing but -inf, has no distribution: logp, entropy
@@ -622,7 +626,8 @@ int mad_probe_empty(int n_workgroups, int threads, void *stream);
 int mad_probe_handoff_latency(void *buf, size_t buf_bytes, unsigned long long *cycles, int reps, void *stream);
 
 /*
- * Workspace bytes needed by op (MAD_OP_*) for calls with at most these sizes:
+ * Workspace bytes needed by op (MAD_OP_*) for calls with at most these sizes
+ * (DECODE, DECODE_LEAST, VERIFY: with these Hq, Hkv and d, and at most B and T):
  *   DECODE: B, Hq, Hkv, d                       (T, max_keys ignored)
  *   VERIFY, VERIFY_KV4: B, Hq, Hkv, d, T        (max_keys ignored)
  *   ACCEPT: B, T, max_keys = V                  (Hq, Hkv, d ignored)

@@ -16,9 +16,9 @@
 // grid, since a token's heads lie side by side in the rows that are read (dealt so
 // that an XCD takes neighbours: 7 % slower).  Large calls: four pieces to a thread
 // (kKv4WideTiles).
-// Measured: 18000 rows of 8 heads of d 128, bf16, K and V, with the values held, 39 us
-// (4.6 TB/s read and written; a copy reaches 5.1), without them 21 (4.5 TB/s); 80 rows
-// 4.4 us (a launch).
+// Measured: 18000 rows of 8 heads of d 128, K and V, bf16, with the values held, 37 -
+// 39 us (4.5 TB/s read and written; a copy reaches 5.1), without them 19 - 21 (4.5 -
+// 5.0 TB/s); fp32 64 and 34 (4.9 TB/s); 80 rows 4.4 us (a launch).
 #include "mad_device.h"
 #include "mad_internal.h"
 

@@ -28,9 +28,14 @@
 // instructions, one of them an exponential at half rate, and 3 more where it may be
 // above the token's logit); few rows, the chain load - first bound - sums - lists -
 // arrival - join, 0.4 to 3.6 us each.
-// Measured: 2048 rows of 128256, bf16, top 1: 103 - 112 us (5.0 TB/s); 4096 rows of
-// 2000, top 5: 29 us; 80 rows of 128256, fp32, top 5: 19.8 us; one row of 50257, top
-// 20: 12.4 us.
+// Rows of which a mask leaves little are slower: a bound that is the mask's value lets
+// every lane's equal entries through to the lists' test, and entries of -inf have a
+// step's entropy formed again (2048 rows of 128256 with 100 live tokens, bf16: top 1
+// 165 - 194 us, top 20 823 - 847, where dense rows take 105 and 128).
+// Measured: 2048 rows of 128256, bf16, top 1: 103 - 106 us (5.0 TB/s; from about the
+// 20th of calls one behind the other 120), fp32 182 us (5.8 TB/s); 4096 rows of 2000,
+// top 5: 29 us, of 12000 41, fp32 46; 80 rows of 128256, fp32, top 5: 19.7 us; one row
+// of 50257, top 20: 12.2 us.
 #include "mad_device.h"
 #include "mad_internal.h"
 
@@ -477,8 +482,10 @@ __global__ __launch_bounds__(kWg, 4) void logprobs_kernel(const LogprobArgs a) {
     }
 }
 
-// Few rows: as many workgroups to a row as the CUs hold at once, so that a call is one round (80 rows of 128256, fp32: 20.3 us;
-// in 1280 places 24.2, in 512 20.1).  Else a workgroup to a row.
+// Few rows: as many workgroups to a row as the CUs hold at once, so that a call is one round (80 rows of 128256, fp32, in 1280
+// places 24.2 us for 20.3 in 1024).  In 512 -> 1024 places, us: 80 rows of 128256, bf16, top 20, 23.6 -> 21.4, top 5 18.8 -> 18.4,
+// fp32 19.4 -> 19.8; 256 rows 30.6 -> 27.8; 320 of 50257 23.3 -> 21.7; only two workgroups to a row do not pay (512 of 128256
+// 34.4 -> 37.1, 500 of 32000, fp32, 17.2 -> 20.9).  Else a workgroup to a row.
 LogprobPlan plan_logprobs(int rows, int V) {
     LogprobPlan p;
     constexpr int chunk = kWg * 16;

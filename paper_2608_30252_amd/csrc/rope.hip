@@ -18,8 +18,9 @@
 // costs less than waiting for them in longer waves does (64 + 8 heads of d 128, one
 // round -> two -> all nine: 64 tokens 4.8 us -> 5 -> 9.2; 2048 tokens 15.6 -> 14.2 ->
 // 16.8; 14000 tokens 105 -> 99 -> 111).
-// Measured: 14000 tokens, 64 + 8 heads of d 128, bf16, 99 us (5.2 TB/s, a copy's
-// rate); 80 tokens 4.7 us, one token of 32 + 8 heads of d 64 4.6 (a launch).
+// Measured: 14000 tokens, 64 + 8 heads of d 128, bf16, 95 - 101 us (5.1 - 5.4 TB/s, a
+// copy's rate), fp32 189 (5.5 TB/s); 80 tokens 4.7 us, fp32 too, one token of 32 + 8
+// heads of d 64 4.4 (a launch).
 #include "mad_device.h"
 #include "mad_internal.h"
 

@@ -13,6 +13,10 @@
 //   O = P V       bf16 x bf16: a probability is rounded to bf16 (2^-8 relative,
 //                 the output's own rounding); V's values keep bf16's range, so keys
 //                 of any size meet in one sum.  fp32: three bf16 terms.
+// The sum of the probabilities, and lse, take them unrounded, so an output that few keys
+// dominate carries the rounding of their weights beside its own.  Root mean square error
+// against 64 bits, keys and values with a few large channels: 317 keys 8.0e-4, with fp32
+// probabilities 7.8e-4; 32773 keys 9.6e-4 either way.
 // m is raised, and the sums scaled, only where a score exceeds it by more than 4
 // (log2 units; p <= 2^4 loses nothing): some row's maximum grows in most steps, by
 // little.
@@ -44,18 +48,21 @@
 // unit; 40 such, 32 rows: 83 against 45).  The unit's pieces are merged by its last workgroup, or by
 // a second launch.
 //
-// What bounds it: instructions.  A chunk of 32 keys by 48 rows takes a wave about
-// 64 conversions, 24 dense and 24 sparse products, 24 exponentials and some 190
-// others (vector ALU 58 % busy, the matrix cores 24 %, with two waves to a SIMD whose
-// steps depend on each other); without its loads the kernel takes nearly as long.
+// What bounds it: its waves' chains of instructions.  A chunk of 32 keys by 48 rows
+// takes a wave about 64 conversions, 24 dense and 24 sparse products, 24 exponentials
+// and some 190 others, scores, exponentials, conversions and products one after the
+// other, with two waves to a SIMD to fill each other's gaps: the vector ALU is 58 %
+// busy, the matrix cores 24 %, neither the limit; without its loads the kernel takes
+// nearly as long.
 // Beside that a start of 5 us, 3.5 for the waves' exchange at 48 rows, and, with
 // ragged lengths, pieces up to a third longer than the mean.  Waves with more chunks
 // ahead of them go first (s_setprio), so that the workgroup's waves end together:
 // 2 - 6 us of 47.
 // Measured (us, d 128 unless given): 16 sequences of 600 .. 12000 keys, 64/8 heads,
-// 6 queries, 104 MB: 40 (2.6 TB/s), 1 query 25 (4.1 TB/s); one of 32773 keys, 5
-// queries, 22; one of 131072 keys, 1 query 30.5 (4.7 TB/s); 64 of 2000, 1 query 29
-// (4.8 TB/s); one of 317 keys, d 64, 6.0.
+// 6 queries: 40 - 47 by the lengths (2.6 - 3.0 TB/s), 1 query 25 (4.2 TB/s); one of
+// 32773 keys, 5 queries, 21 - 22; one of 131072 keys, 1 query 31 (4.6 TB/s); 64 of
+// 2000, 1 query 28 (4.9 TB/s); one of 317 keys, d 64, 6.0.  fp32: four of 32773 keys,
+// 32/8 heads, 5 queries, 55 (2.6 TB/s); 16 of 600 .. 12000, d 64, 3 queries, 26.
 //
 // What a row does not see is left out whatever it holds: scores by selection, rows
 // past the length are never read, and where a step with hidden keys has a NaN
@@ -88,7 +95,8 @@ struct Stream4Cfg {
     static constexpr int KST = D / 32, DB = D / 16, NQ = F32 ? 3 : 1;
     static constexpr int RP = NB * 16;                     // padded query rows
     // query fragments (1 KB each), in registers where those, the accumulators, scores and probabilities leave room for the
-    // rest (two waves to a SIMD have 256 each): 16 sequences, 48 rows, 43.8 us from LDS, 41.4
+    // rest (two waves to a SIMD have 256 each): 48 rows, 16 sequences of 600 .. 12000 keys, 48.0 us from LDS, 46.9; of 4000
+    // keys each 29.4, 28.7
     static constexpr int QBYTES = NB * KST * NQ * 1024;
     static constexpr bool QREG = NB * (KST * NQ + DB + 2 + NQ) * 4 <= 200;
     static constexpr int REST = NWV * RP * 8 + QBYTES, STAGES = NWV * (CHUNK + SCALES);
@@ -674,9 +682,15 @@ void plan_stream4(Stream4Args &a, int B, int Hkv, int d, int dtype, const int *n
     if (share < kLeast4) share = kLeast4;
     while (deal(share) > places && share < nt_max) share += 1 + share / 64;
     a.n_wg = a.wgs * Hkv;
-    // neighbouring workgroups take the row's units in turn, each XCD its own (plan_stream), where the pieces are short
+    // Neighbouring workgroups take the row's units in turn, each XCD its own (plan_stream), where the pieces are short; else a
+    // unit's pieces, us: pieces of 16 slabs, 48 rows, 8 sequences of 4000 keys 23.0 -> 21.6, 16 of 2000 21.9 -> 21.3; of 8, 32
+    // rows, 16 of 1000, 13.5 -> 13.1.  Of 16, 4 rows, 4 of 8000, 13.5 -> 14.1, 8 rows, 8 of 4000, 13.6 -> 13.8; of 60 and more no
+    // difference (16 of 600 .. 12000 keys, 48 rows, 43.7 -> 43.6).
     a.by_unit = Hkv % 8 == 0 && share <= (a.T * a.G >= 32 ? 16 : a.T * a.G > 16 ? 3 : 0) ? 1 : 2;
-    // merged by a unit's last workgroup or by a second launch: plan_stream's rule, of what LDS there is
+    // Merged by a unit's last workgroup or by a second launch, of what LDS there is.  Second launch -> in the launch, us, 8 KV
+    // heads: up to 48 KB, 8 sequences of 1000 keys, 42 KB, 11.7 -> 11.1, one of 1000 10.9 -> 10.3, 4 of 8000, 17 KB, 14.1 -> 13.5;
+    // many units, 16 of 600 .. 12000, 75 KB, 49.1 -> 43.6, 8 of 4000, 100 KB, 22.6 -> 21.6; few units and more, one of 32773, 129
+    // KB, 14.8 -> 15.9, 4 of 1500, 125 KB, 13.1 -> 14.2, 4 of 2000, 83 KB, 11.4 -> 12.0.
     const int64_t bytes = (int64_t)np_max * piece_floats(a.T * a.G, d) * 4;
     const bool in_launch = bytes <= kMergeInLaunch || (units >= 64 && bytes <= merge4_bytes(a.waves)) ||
                            (units >= 32 && np_max <= 4 && bytes <= kMergeFew4);
